@@ -30,7 +30,7 @@ def sources():
 
 def _deps():
     return sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + \
-        [os.path.join(os.path.dirname(HERE), "include", "wici.h")]
+        glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h"))
 
 
 def up_to_date() -> bool:

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "../../include/wici.h"
+#include "../../include/wici_ops.h"
 #include "common.cuh"
 #include "kernels.h"
 
@@ -816,6 +817,21 @@ int wici_check_bounded_wait(void *cuda_stream, int64_t limit_ns) {
     }
     if (e != cudaSuccess) return fail(nullptr, WICI_E_CUDA, "bounded-wait probe: %s", cudaGetErrorString(e));
     if (h_err != 0) return fail(nullptr, WICI_E_TIMEOUT, "wait gave up as designed (site %d)", h_err);
+    return WICI_OK;
+}
+
+int wici_kv_view(const wici_ctx *c, int32_t layer, wici_kv_cache *cache, const int32_t **pages, int32_t *n_logical) {
+    if (!c || !cache || !pages || !n_logical) return fail(nullptr, WICI_E_ARG, "kv view: null argument");
+    const Plan &p = c->plan;
+    if (layer < 0 || layer >= p.L) return fail(nullptr, WICI_E_ARG, "kv view: layer %d of %d", layer, p.L);
+    cache->data = c->bufs.KV + (size_t)layer * p.kv_layer_elems;
+    cache->page_stride = (int64_t)p.kv_page_elems * 2;
+    cache->n_pages = p.max_pages;
+    cache->n_kv_heads = p.nkv;
+    cache->head_dim = p.d;
+    cache->format = WICI_KV_BF16;
+    *pages = c->bufs.pages;
+    *n_logical = p.max_pages;
     return WICI_OK;
 }
 

@@ -333,6 +333,36 @@ class WiciModel:
         wici_decode(self.ctx, n_steps, token_in, out)
         return out
 
+    def kv_cache(self, layer: int):
+        """(PagedKV, page table int32 [pages]) of a layer: views of the context's own cache, whose first kv_len
+        positions hold tokens, for calls on the context's stream or after it."""
+        import torch
+
+        from . import ops
+        cache, pages, n = ops.wici_kv_view(self.ctx, layer)
+        first = cache.data - self._kv.data_ptr()
+        data = self._kv[first:first + cache.n_pages * cache.page_stride]
+        at = pages - self._ws.data_ptr()
+        return (ops.PagedKV(cache.n_kv_heads, cache.head_dim, "bf16", data=data),
+                self._ws[at:at + 4 * n].view(torch.int32))
+
+    def read_kv(self, layer: int, first: int = 0, count: int | None = None, dtype=None):
+        """(k, v) [count, kv heads, head_dim] of the cached positions first.. (k after RoPE), on the device; the
+        stream has been synchronised."""
+        import torch
+
+        from . import ops
+        count = self.kv_len - first if count is None else count
+        if first < 0 or count < 0 or first + count > self.kv_len:
+            raise ValueError(f"positions {first}..{first + count - 1} of {self.kv_len} cached ones")
+        with torch.cuda.stream(self.stream):
+            cache, table = self.kv_cache(layer)
+            pos = torch.arange(first, first + count, device=table.device, dtype=torch.int32)
+            slots = table[pos // ops.PAGE_TOKENS] * ops.PAGE_TOKENS + pos % ops.PAGE_TOKENS
+            out = cache.read(slots, dtype or torch.bfloat16)
+            cache.check()
+        return out
+
     def reset(self):
         wici_reset(self.ctx)
 

@@ -1,0 +1,646 @@
+"""The operators of a batched decode step (include/wici_ops.h) through their binding against
+the fp64 oracle (oracle/paged.py).
+
+Tolerances, from the arithmetic:
+* storing to a type: half a step, eps / 2 of the value (plus half the smallest fp16 step).
+* a rotation in fp32: the angle's rest of at most pi / 4 is off by 2^-24 of itself (a conversion) and 2^-30 turns,
+  sincospif by two units in the last place, the gain's product and each product and sum by half one: below
+  2^-21 (|x_a| + |x_b|) g.
+* a code: x / scale has to round as in 64 bits unless it lies within `near` of a border: 127 * 2^-22 for given
+  values (quotient and scale rounded to fp32), and for rotated ones, off by 2^-21 (|x_a| + |x_b|) <= 2^-20 * 1.42 amax
+  in x as well as in the scale: 127 * 2^-18.  e4m3 borders are relative: the same with 1 in place of 127.
+* attention: a product q.k is off by 2 d 2^-23 of the sum of its |products| (tensor cores may truncate each
+  add) and by 2^-16 of it where q has more bits than two 16-bit terms hold; probabilities carry at least 16 bits and
+  the exponential is good to 2^-21; sums over n keys add n 2^-23.  All act on sum p |v|.
+"""
+import numpy as np
+import pytest
+
+from oracle import paged
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a CUDA GPU", allow_module_level=True)
+
+import gen  # noqa: E402
+import oracle  # noqa: E402
+from paper_2608_24204_gb300 import PagedKV, Rope, WiciModel, ops, wici  # noqa: E402
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def ints(a):
+    return torch.tensor(np.asarray(a, np.int32), device="cuda")
+
+
+def half_step(v, dtype):
+    return np.abs(v) * (torch.finfo(DT[dtype]).eps / 2) * (1 + 2.0 ** -10) + (2.0 ** -25 if dtype == "f16" else 0)
+
+
+def within(got, want, tol, what):
+    got, want = np.asarray(got), np.asarray(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), f"{what}: NaNs"
+    with np.errstate(invalid="ignore"):
+        bad = ~((np.abs(got - want) <= tol) | (got == want) | np.isnan(want))
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, worst {np.nanmax((np.abs(got - want) / tol)[bad]):.2f} x the tolerance"
+
+
+def randn(rng, *shape, dtype="f32", scale=1.0):
+    return torch.tensor(rng.normal(size=shape) * scale, device="cuda").to(DT[dtype])
+
+
+SCALED = {"none": {}, "linear": {"factor": 4.0}, "bands": {"factor": 8.0, "original_len": 512, "low": 1.0, "high": 4.0},
+          "yarn": {"factor": 16.0, "original_len": 512, "low": 1.0, "high": 32.0}}
+
+
+# ------------------------------------------------------------------- rotary --
+def check_rope(x, y, pos, rot, theta, interleaved, scaling, inverse, dtype):
+    f, g = paged.rope_frequencies(rot, theta, scaling, **SCALED[scaling])
+    want = paged.rope(f64(x), pos, rot, f, g, interleaved, inverse)
+    ax = np.abs(f64(x))
+    mix = np.zeros_like(ax)
+    a, b = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    mix[..., a] = mix[..., b] = ax[..., a] + ax[..., b]
+    within(f64(y), want, 2.0 ** -21 * g * mix + half_step(want, dtype), "rope")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tokens,heads,d,rot,interleaved,scaling,inverse", [
+    (1, 1, 128, 128, False, "none", False),
+    (1, 40, 128, 128, False, "bands", False),
+    (7, 3, 64, 64, True, "linear", False),
+    (33, 5, 128, 64, False, "yarn", True),
+    (19, 2, 80, 20, True, "yarn", False),       # odd sizes: element-wise accesses
+    (5, 9, 2, 2, False, "none", False),
+    (4, 3, 256, 250, False, "bands", True),
+    (300, 33, 96, 96, False, "none", False),
+    (2000, 8, 32, 16, True, "none", True),
+])
+def test_rope(dtype, tokens, heads, d, rot, interleaved, scaling, inverse):
+    rng = np.random.default_rng(tokens * 1000 + d)
+    pos = rng.integers(-3, 1 << 20, tokens)
+    x = randn(rng, tokens, heads, d, dtype=dtype)
+    kept = x.clone()
+    r = Rope(d, 5e5, rot_dim=rot, interleaved=interleaved, scaling=scaling, **SCALED[scaling])
+    y = r.apply(x, ints(pos), inverse=inverse)
+    assert torch.equal(x, kept)
+    check_rope(x, y, pos, rot, 5e5, interleaved, scaling, inverse, dtype)
+    z = r.apply(x, ints(pos), out=x, inverse=inverse)        # in place
+    assert z is x and torch.equal(x, y)
+
+
+@pytest.mark.parametrize("layout", ["packed", "heads first", "unaligned", "broadcast tokens"])
+def test_rope_strides(layout):
+    rng = np.random.default_rng(3)
+    T, H, d = 37, 4, 64
+    if layout == "packed":
+        x = randn(rng, T, H + 3, d, dtype="bf16")[:, 1:1 + H]
+        y = torch.full((T, H + 2, d), 7.0, dtype=torch.bfloat16, device="cuda")
+        out = y[:, 2:]
+    elif layout == "heads first":
+        x = randn(rng, H, T, d, dtype="bf16").transpose(0, 1)
+        y = torch.full((H, T + 5, d), 7.0, dtype=torch.bfloat16, device="cuda")
+        out = y[:, :T].transpose(0, 1)
+    elif layout == "unaligned":
+        x = randn(rng, T * H * d + 1, dtype="bf16")[1:].view(T, H, d)
+        y = torch.full((T * H * d + 3,), 7.0, dtype=torch.bfloat16, device="cuda")
+        out = y[3:].view(T, H, d)
+    else:
+        x = randn(rng, 1, H, d, dtype="bf16").expand(T, H, d)
+        y = out = torch.full((T, H, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    pos = rng.integers(0, 5000, T)
+    Rope(d, 1e4).apply(x, ints(pos), out=out)
+    check_rope(x, out, pos, d, 1e4, False, "none", False, "bf16")
+    assert int((y == 7.0).sum()) >= y.numel() - out.numel()  # nothing beside the output was written
+    out.fill_(7.0)
+    assert bool((y == 7.0).all())
+
+
+def test_rope_of_extreme_positions_and_values():
+    rng = np.random.default_rng(4)
+    pos = np.array([-2 ** 31, 2 ** 31 - 1, 2 ** 24 + 1, 123456789, 0, -1])
+    x = randn(rng, 6, 2, 128)
+    check_rope(x, Rope(128, 5e5).apply(x, ints(pos)), pos, 128, 5e5, False, "none", False, "f32")
+    x[1, 0, 3], x[2, 1, 70] = float("inf"), float("nan")
+    y = Rope(128, 5e5).apply(x, ints(pos))
+    touched = torch.zeros(6, 2, 128, dtype=torch.bool, device="cuda")
+    touched[1, 0, [3, 67]] = touched[2, 1, [70, 6]] = True
+    assert bool(torch.isfinite(y[~touched]).all()) and not bool(torch.isfinite(y[touched]).any())
+
+
+def test_rope_inverse_is_the_gradient_by_differences():
+    # L = sum(w * rope(x)): dL/dx by central differences in x of the fp64 oracle, at step 1 (the map is linear)
+    rng = np.random.default_rng(5)
+    T, d, rot = 3, 32, 24
+    r = Rope(d, 1e4, rot_dim=rot, interleaved=True, scaling="yarn", **SCALED["yarn"])
+    f, g = paged.rope_frequencies(rot, 1e4, "yarn", **SCALED["yarn"])
+    pos = np.array([2, 900, 77])
+    x, w = rng.normal(size=(T, 1, d)), rng.normal(size=(T, 1, d))
+    got = f64(r.apply(torch.tensor(w, device="cuda").float(), ints(pos), inverse=True))
+    for i in range(d):
+        e = np.zeros((1, 1, d))
+        e[..., i] = 1.0
+        up, down = (paged.rope(x + s * e, pos, rot, f, g, True) for s in (0.5, -0.5))
+        want = (w * (up - down)).sum((1, 2))
+        assert np.all(np.abs(got[:, 0, i] - want) <= 2.0 ** -20 * g * np.abs(w).max())
+
+
+# ------------------------------------------------------------- append, read --
+def near_border(x, scale, fmt, near):
+    """Where x / scale lies within `near` of a value that rounds either way."""
+    with np.errstate(divide="ignore", invalid="ignore"):
+        q = np.nan_to_num(np.abs(x) / scale[..., None])
+    if fmt == "int8":
+        return np.abs(q - np.floor(q) - 0.5) <= 127 * near
+    grid = paged.E4M3[:127]
+    mid = (grid[1:] + grid[:-1]) / 2
+    j = np.clip(np.searchsorted(mid, q), 1, 125)
+    return np.minimum(np.abs(q - mid[j]), np.abs(q - mid[j - 1])) <= near * np.maximum(q, 2.0 ** -9) * 2
+
+
+def check_written(data, slots, k, v, fmt, d, kv, before, rotated, g=1.0):
+    """The cache bytes after an append of k, v (fp64 [tokens, kv, d], rotated in 64 bits) at slots."""
+    codes, scales = paged.unpack(data.cpu().numpy(), kv, d, fmt)
+    old_codes, old_scales = paged.unpack(before.cpu().numpy(), kv, d, fmt)
+    live = slots >= 0
+    others = np.ones(codes.shape[0], bool)
+    others[slots[live]] = False
+    np.testing.assert_array_equal(codes[others], old_codes[others])
+    if scales is not None:
+        np.testing.assert_array_equal(scales[others].view(np.uint32), old_scales[others].view(np.uint32))
+    for which, x in ((0, k), (1, v)):
+        x, got = x[live], codes[slots[live], which]
+        turned = rotated and which == 0
+        slack = 2.0 ** -20 * 1.42 * g * np.abs(x).max(-1, keepdims=True) if turned else 0
+        if fmt == "bf16":
+            val = (got.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+            within(val, x, half_step(x, "bf16") + slack, "bf16 cache")
+            continue
+        s = scales[slots[live], which]
+        want_codes, want_s = paged.quantise(x, fmt)
+        within(s, want_s, want_s * (2.0 ** -18 if turned else 2.0 ** -23), "scale")
+        gv, wv = paged.code_values(got, fmt), paged.code_values(want_codes, fmt)
+        near = near_border(x, want_s, fmt, 2.0 ** -18 if turned else 2.0 ** -22)
+        same = gv == wv
+        assert np.all(same | near), f"{fmt}: {(~(same | near)).sum()} codes differ away from a border"
+        step = 1.0 if fmt == "int8" else 2.0 ** -3 * np.maximum(np.abs(wv), 2.0 ** -6) * 2
+        assert np.all(np.abs(gv - wv) <= step)
+
+
+def slots_for(rng, tokens, pages):
+    s = rng.permutation(pages * 16)[:tokens]
+    return s.astype(np.int64)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("dtype,tokens,kv,d,q_heads,rot,scaling,interleaved", [
+    ("bf16", 1, 8, 128, 32, 128, "bands", False),
+    ("f32", 1, 1, 64, 0, 0, "none", False),
+    ("f16", 17, 2, 64, 6, 64, "none", True),
+    ("bf16", 100, 3, 128, 15, 64, "yarn", False),
+    ("f32", 333, 8, 128, 8, 128, "linear", False),
+    ("f16", 50, 5, 128, 0, 0, "none", False),
+    ("bf16", 1000, 4, 64, 0, 32, "none", True),      # k rotated without a q
+])
+def test_append_and_read(fmt, dtype, tokens, kv, d, q_heads, rot, scaling, interleaved):
+    rng = np.random.default_rng(tokens + d)
+    pages = tokens // 16 + 3
+    before = torch.tensor(rng.integers(0, 256, pages * ops.wici_kv_page_bytes(ops.FORMATS[fmt], kv, d)), dtype=torch.uint8,
+                          device="cuda")
+    cache = PagedKV(kv, d, fmt, data=before.clone())
+    k, v = randn(rng, tokens, kv, d, dtype=dtype, scale=3.0), randn(rng, tokens, kv, d, dtype=dtype)
+    if tokens > 3:
+        v[1] = 0                                              # a head of zeros
+        k[2, 0] *= 2.0 ** -10
+    slots = slots_for(rng, tokens, pages)
+    if tokens > 5:
+        slots[[3, tokens - 1]] = [-1, -7]                      # padding
+    pos = rng.integers(0, 100000, tokens)
+    kw, g, k64 = {}, 1.0, f64(k)
+    if rot:
+        r = Rope(d, 5e5, rot_dim=rot, interleaved=interleaved, scaling=scaling, **SCALED[scaling])
+        f, g = paged.rope_frequencies(rot, 5e5, scaling, **SCALED[scaling])
+        kw = {"rope": r, "positions": ints(pos)}
+        k64 = paged.rope(k64, pos, rot, f, g, interleaved)
+        if q_heads:
+            kw["q"] = randn(rng, tokens, q_heads, d, dtype=dtype)
+    q_out = cache.append(k, v, ints(slots), **kw)
+    cache.check()
+    check_written(cache.data, slots, k64, f64(v), fmt, d, kv, before, bool(rot), g)
+    if q_heads:
+        check_rope(kw["q"], q_out, pos, rot, 5e5, interleaved, scaling, False, dtype)
+    codes, scales = paged.unpack(cache.data.cpu().numpy(), kv, d, fmt)
+    back = np.concatenate([slots[::-1], slots[:2], [-3]])     # any order, repeats, padding
+    for out_dtype in DT:
+        got = cache.read(ints(back), dtype=DT[out_dtype])
+        for which in (0, 1):
+            c = codes[back, which]
+            if fmt == "bf16":
+                want = (c.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+            else:
+                want = paged.code_values(c, fmt) * scales[back, which][..., None].astype(np.float64)
+            want[back < 0] = 0
+            if out_dtype == "f16":
+                want = np.where(np.abs(want) >= 65520, np.sign(want) * np.inf, want)
+            within(f64(got[which]), want, half_step(want, out_dtype) + 2.0 ** -24 * np.abs(want), f"read {out_dtype}")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_append_of_infinities_nans_and_tiny_heads(fmt):
+    k = torch.ones(5, 1, 64, device="cuda")
+    k[0, 0, 5], k[1, 0, 63], k[2] = float("inf"), float("nan"), 1e-40
+    k[3] = 1e-30
+    cache = PagedKV(1, 64, fmt, n_pages=1)
+    cache.append(k, -k, ints(range(5)))
+    kk, vv = (f64(t)[:, 0] for t in cache.read(ints(range(5)), dtype=torch.float32))
+    assert np.isnan(kk[:2]).all() and np.isnan(vv[:2]).all()
+    assert np.all((kk[2] >= 0) & (kk[2] <= 2e-40))            # below the normal range: codes are coarse, not wild
+    np.testing.assert_allclose(kk[3], 1e-30, rtol=2.0 ** -21)  # the largest magnitude takes the largest code
+    np.testing.assert_allclose(kk[4], 1.0, rtol=2.0 ** -22)
+    np.testing.assert_array_equal(vv[2:], -kk[2:])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+def test_bad_slots_write_nothing_read_nan_and_are_reported(fmt):
+    cache = PagedKV(2, 64, fmt, n_pages=2)
+    k = torch.ones(4, 2, 64, device="cuda")
+    slots = ints([0, 32, 2 ** 31 - 1, 31])
+    cache.append(k, k, slots)
+    with pytest.raises(wici.WiciError, match="slot"):
+        cache.check()
+    cache.check()                                             # cleared
+    codes, _ = paged.unpack(cache.data.cpu().numpy(), 2, 64, fmt)
+    assert [int(s) for s in np.nonzero(codes.reshape(32, -1).any(-1))[0]] == [0, 31]
+    got, _ = cache.read(slots, dtype=torch.float32)
+    with pytest.raises(wici.WiciError, match="slot"):
+        cache.check()
+    assert bool(torch.isnan(got[1:3]).all()) and bool(((got[[0, 3]] - 1).abs() < 2.0 ** -20).all())
+
+
+def test_read_of_one_side_into_strided_outputs():
+    rng = np.random.default_rng(6)
+    cache = PagedKV(3, 64, "e4m3", n_pages=4)
+    x = randn(rng, 60, 3, 64)
+    cache.append(x, 2 * x, ints(range(60)))
+    both = cache.read(ints(range(60)), dtype=torch.float32)
+    wide = torch.full((3, 61, 65), 7.0, device="cuda")
+    out = wide[:, :60, :64].transpose(0, 1)                   # heads first, unaligned rows
+    st = torch.cuda.current_stream().cuda_stream
+    slots = ints(range(60))
+    for which in (0, 1):
+        hs = ops.heads_of(out, 64, out.device, "out")
+        ops.wici_kv_read(st, cache.cache, slots.data_ptr(), 60, *((hs, None) if which == 0 else (None, hs)))
+        assert torch.equal(out, both[which])
+    assert bool((wide[:, 60] == 7.0).all()) and bool((wide[:, :, 64] == 7.0).all())
+
+
+# ---------------------------------------------------------------- attention --
+def attention_case(rng, B, kv, group, d, fmt, dtype, lengths, max_pages=None, spread=1.0, poison=True):
+    """A cache whose used slots hold values and whose every other byte is set (NaN in each format), q, pages."""
+    lengths = np.asarray(lengths)
+    need = [(max(int(n), 0) + 15) // 16 for n in lengths]
+    total = sum(need) + 2
+    slots = total * 16
+    values = rng.normal(size=(slots, 2, kv, d)) * np.exp(0.5 * rng.normal(size=(2, kv, d)))
+    values[:, 1] += 0.2
+    if fmt == "bf16":
+        codes = f64(torch.tensor(values).to(torch.bfloat16))
+        codes = torch.tensor(codes).to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+        scales, vals = None, (codes.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+    else:
+        codes, scales = paged.quantise(values, fmt)
+        scales = scales.astype(np.float32)
+        vals = paged.code_values(codes, fmt) * scales[..., None].astype(np.float64)
+    order = rng.permutation(total)
+    pages = np.full((len(lengths), max_pages or max(max(need), 1)), -1)
+    used = np.zeros(slots, bool)
+    at = 0
+    for b, n in enumerate(need):
+        pages[b, :n] = order[at:at + n]
+        for t in range(max(int(lengths[b]), 0)):
+            used[pages[b, t // 16] * 16 + t % 16] = True
+        at += n
+    if poison:
+        codes = codes.copy()
+        codes[~used] = np.array(0xFFFF if fmt == "bf16" else 0xFF, np.uint16 if fmt == "bf16" else np.uint8).astype(codes.dtype)
+        if scales is not None:
+            scales[~used] = np.nan
+    data = torch.tensor(paged.pack(codes, scales, fmt), device="cuda")
+    q = randn(rng, len(lengths), kv * group, d, dtype=dtype, scale=spread)
+    return PagedKV(kv, d, fmt, data=data), q, pages, vals
+
+
+def check_attention(cache, q, pages, lengths, vals, scale, window, out, lse, dtype, out_dtype=None):
+    d = q.shape[-1]
+    q64 = f64(q)
+    want, want_lse, weight = paged.paged_attention(q64, vals[:, 0], vals[:, 1], pages, lengths, scale, window)
+    for b in range(q.shape[0]):
+        n = max(int(lengths[b]), 0)
+        if n == 0:
+            assert bool((out[b] == 0).all()) and (lse is None or bool((lse[b] == -np.inf).all()))
+            continue
+        keys = range(max(0, n - window) if window else 0, n)
+        slots = [int(pages[b][t // 16]) * 16 + t % 16 for t in keys]
+        for h in range(q.shape[1]):
+            kk = vals[slots, 0, h // (q.shape[1] // vals.shape[2])]
+            size = float(np.max(np.abs(kk) @ np.abs(q64[b, h])) * abs(scale))
+            ds = size * (2 * d * 2.0 ** -23 + (2.0 ** -16 if dtype == "f32" else 0.0))
+            rel = 2 * ds + 2.0 ** -16 + 2.0 ** -21 + len(slots) * 2.0 ** -23
+            within(f64(out[b, h]), want[b, h], rel * weight[b, h] + half_step(want[b, h], out_dtype or dtype) + 1e-30,
+                   f"attention of sequence {b}, head {h}")
+            if lse is not None:
+                within(float(lse[b, h]), want_lse[b, h], ds + 2.0 ** -20 + len(slots) * 2.0 ** -23 + 2.0 ** -23 * abs(want_lse[b, h]),
+                       f"lse of sequence {b}, head {h}")
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("dtype,kv,group,d,lengths,window", [
+    ("bf16", 1, 1, 128, [1], 0),
+    ("f32", 2, 4, 64, [0, 1, 2, 15, 16, 17, 31, 33], 0),
+    ("bf16", 8, 4, 128, [300, 0, 129, 1, 128, 127], 0),
+    ("f16", 3, 5, 128, [70, 257, 16], 0),
+    ("f32", 1, 8, 128, [1000, 3], 0),
+    ("bf16", 2, 16, 64, [200, 90], 0),
+    ("bf16", 1, 71, 64, [40, 150, 0], 0),
+    ("f32", 2, 7, 128, [500, 64, 20, 0, 1], 33),
+    ("bf16", 4, 2, 64, [400, 399, 385, 384], 16),
+    ("f16", 1, 9, 128, [333, 18], 1),
+])
+def test_attention(fmt, dtype, kv, group, d, lengths, window):
+    rng = np.random.default_rng(len(lengths) * 100 + group)
+    cache, q, pages, vals = attention_case(rng, len(lengths), kv, group, d, fmt, dtype, lengths)
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    for out_dtype in {dtype, "f32"}:
+        out = torch.full(q.shape, 7.0, dtype=DT[out_dtype], device="cuda")
+        cache.attend(q, ints(pages), ints(lengths), window=window, out=out, lse=lse)
+        cache.check()
+        check_attention(cache, q, pages, lengths, vals, d ** -0.5, window, out, lse, dtype, out_dtype)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+def test_attention_over_a_long_cache_of_few_sequences(fmt):
+    # one KV head: the length is what the work is split over
+    rng = np.random.default_rng(11)
+    lengths = [9001, 5]
+    cache, q, pages, vals = attention_case(rng, 2, 1, 2, 128, fmt, "bf16", lengths, max_pages=700)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    out = cache.attend(q, ints(pages), ints(lengths), lse=lse)
+    check_attention(cache, q, pages, lengths, vals, 128 ** -0.5, 0, out, lse, "bf16")
+    for window in (8999, 4000, 100):
+        out = cache.attend(q, ints(pages), ints(lengths), window=window, lse=lse)
+        check_attention(cache, q, pages, lengths, vals, 128 ** -0.5, window, out, lse, "bf16")
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+def test_attention_of_many_ragged_sequences(fmt):
+    rng = np.random.default_rng(12)
+    lengths = rng.integers(0, 120, 300)
+    lengths[[5, 299]] = 0
+    cache, q, pages, vals = attention_case(rng, 300, 1, 2, 64, fmt, "bf16", lengths)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    out = cache.attend(q, ints(pages), ints(lengths), lse=lse)
+    check_attention(cache, q, pages, lengths, vals, 0.125, 0, out, lse, "bf16")
+
+
+def test_attention_scores_far_apart_and_scale():
+    # one key takes everything, its score hundreds above the others; then a scale of zero and a negative one
+    rng = np.random.default_rng(13)
+    cache, q, pages, vals = attention_case(rng, 2, 2, 4, 64, "bf16", "f32", [100, 37], spread=40.0)
+    for scale in (1.0, 0.0, -0.5):
+        lse = torch.empty(q.shape[:2], device="cuda")
+        out = cache.attend(q, ints(pages), ints([100, 37]), scale=scale, lse=lse)
+        check_attention(cache, q, pages, [100, 37], vals, scale, 0, out, lse, "f32")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_attention_with_scales_of_very_different_sizes(fmt):
+    # V scales of a sequence differ by 2^40 and some heads are zero: small ones must not vanish beside each other's
+    rng = np.random.default_rng(14)
+    n = 90
+    cache = PagedKV(1, 64, fmt, n_pages=6)
+    mag = 2.0 ** rng.integers(-30, 10, n)
+    mag[[3, 50]] = 0
+    k, v = randn(rng, n, 1, 64), randn(rng, n, 1, 64) * torch.tensor(mag, device="cuda").float()[:, None, None]
+    cache.append(k, v, ints(range(n)))
+    kk, vv = (f64(t) for t in cache.read(ints(range(n)), dtype=torch.float32))
+    q = randn(rng, 1, 3, 64)
+    pages = np.arange(6)[None]
+    out = cache.attend(q, ints(pages), ints([n]))
+    vals = np.zeros((96, 2, 1, 64))
+    vals[:n, 0], vals[:n, 1] = kk, vv
+    check_attention(cache, q, pages, [n], vals, 0.125, 0, out, None, "f32")
+
+
+def test_attention_of_a_nan_or_infinite_key_stays_in_its_sequence():
+    rng = np.random.default_rng(15)
+    lengths = [20, 20, 20]
+    cache, q, pages, vals = attention_case(rng, 3, 1, 2, 64, "bf16", "f32", lengths)
+    blocks = cache.data.view(torch.bfloat16).view(-1, 2, 1, 16, 64)
+    blocks[int(pages[1][0]), 0, 0, 3, 10] = float("nan")
+    blocks[int(pages[2][1]), 1, 0, 2, 10] = float("inf")
+    out = cache.attend(q, ints(pages), ints(lengths))
+    assert bool(torch.isnan(out[1]).all())
+    assert not bool(torch.isfinite(out[2, :, 10]).any()) and bool(torch.isfinite(out[2, :, :10]).all())
+    check_attention(cache, q[:1], pages[:1], lengths[:1], vals, 0.125, 0, out[:1], None, "f32")
+
+
+def test_attention_strides_shared_pages_and_rows_past_the_batch():
+    rng = np.random.default_rng(16)
+    cache, _, pages, vals = attention_case(rng, 3, 2, 3, 64, "bf16", "bf16", [50, 64, 10])
+    pages[2] = pages[0]                                        # a shared prefix
+    big = randn(rng, 6, 7, 128, dtype="bf16")
+    q = big[:6, :, :64].transpose(0, 1)[:3]                    # heads-first, strided rows
+    out = torch.full((8, 9, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = cache.attend(q, ints(pages), ints([50, 64, 10]), out=out[:, 1:7])
+    check_attention(cache, q, pages, [50, 64, 10], vals, 0.125, 0, got, None, "bf16")
+    assert bool((out[3:] == 7.0).all()) and bool((out[:, 0] == 7.0).all()) and bool((out[:, 7:] == 7.0).all())
+    odd = torch.full((3 * 6 * 64 + 1,), 7.0, dtype=torch.bfloat16, device="cuda")[1:].view(3, 6, 64)
+    qo = torch.empty(3 * 6 * 64 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(3, 6, 64)
+    qo.copy_(q)                                                # 2-byte aligned
+    cache.attend(qo, ints(pages), ints([50, 64, 10]), out=odd)
+    assert torch.equal(odd, out[:3, 1:7])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+def test_bad_pages_and_lengths_give_nan_and_are_reported(fmt):
+    rng = np.random.default_rng(17)
+    lengths = [40, 40, 40, 40, 40]
+    cache, q, pages, vals = attention_case(rng, 5, 2, 2, 64, fmt, "f32", lengths)
+    pages[1, 2], pages[2, 0] = -1, cache.n_pages
+    lse = torch.empty(q.shape[:2], device="cuda")
+    out = cache.attend(q, ints(pages), ints(lengths), lse=lse)
+    with pytest.raises(wici.WiciError, match="page"):
+        cache.check()
+    assert bool(torch.isnan(out[1:3]).all()) and bool(torch.isnan(lse[1:3]).all())
+    for b in (0, 3, 4):
+        check_attention(cache, q[b:b + 1], pages[b:b + 1], [40], vals, 0.125, 0, out[b:b + 1], lse[b:b + 1], "f32")
+    out = cache.attend(q, ints(pages), ints([40, -5, -2 ** 31, 49, 2 ** 31 - 1]), lse=lse)
+    with pytest.raises(wici.WiciError, match="length"):
+        cache.check()
+    assert bool((out[1:3] == 0).all()) and bool((lse[1:3] == -np.inf).all())
+    assert bool(torch.isnan(out[3:]).all()) and bool(torch.isnan(lse[3:]).all())
+    check_attention(cache, q[:1], pages[:1], [40], vals, 0.125, 0, out[:1], lse[:1], "f32")
+    # a bad page before the window is not needed
+    out = cache.attend(q, ints(pages), ints(lengths), window=9)
+    with pytest.raises(wici.WiciError, match="page"):
+        cache.check()
+    assert bool(torch.isnan(out[1]).all()) and bool(torch.isfinite(out[2]).all())
+
+
+def test_attention_repeats_itself_and_workspaces_serve_any_order_of_calls():
+    rng = np.random.default_rng(18)
+    big, small = [3000, 10, 700], [30, 500, 0]
+    cache, q, pages, _ = attention_case(rng, 3, 2, 4, 128, "int8", "bf16", [3000, 500, 700])
+    ws = cache.workspace(8, 3)
+    first = {}
+    for i in range(6):
+        for name, lengths in (("big", big), ("small", small)):
+            out = cache.attend(q, ints(pages), ints(lengths), workspace=ws)
+            assert torch.equal(out, first.setdefault(name, out)), (name, i)
+    assert torch.equal(cache.attend(q, ints(pages), ints(big)), first["big"])
+    with pytest.raises(ValueError, match="workspace"):
+        cache.attend(q, ints(pages), ints(big), workspace=ws[:16])
+
+
+def test_two_streams_at_once():
+    rng = np.random.default_rng(19)
+    lengths = [4000] * 4
+    cache, q, pages, _ = attention_case(rng, 4, 2, 4, 64, "bf16", "bf16", lengths)
+    p, n = ints(pages), ints(lengths)
+    want = [cache.attend(q * (i + 1), p, n) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(cache.attend(q * (i + 1), p, n))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+# ----------------------------------------------------------------- together --
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+def test_a_decode_loop_of_a_batch_captured_and_replayed(fmt):
+    """Prompts of several sequences appended at once, then decode steps (append + attend) as a captured graph whose
+    inputs change between replays; every step against the oracle on what the cache then holds."""
+    rng = np.random.default_rng(20)
+    B, kv, group, d = 3, 2, 4, 64
+    H = kv * group
+    prompt, steps = [21, 0, 40], 12
+    r = Rope(d, 1e4, scaling="bands", **SCALED["bands"])
+    f, g = paged.rope_frequencies(d, 1e4, "bands", **SCALED["bands"])
+    cache = PagedKV(kv, d, fmt, data=torch.full((12 * ops.wici_kv_page_bytes(ops.FORMATS[fmt], kv, d),), 255,
+                                                dtype=torch.uint8, device="cuda"))
+    pages = rng.permutation(12).reshape(B, 4)
+    lengths = np.array(prompt)
+    rows = randn(rng, sum(prompt), H + 2 * kv, d, dtype="bf16")
+    pos = np.concatenate([np.arange(n) for n in prompt])
+    seq = np.concatenate([np.full(n, b) for b, n in enumerate(prompt)])
+    slots = pages[seq, pos // 16] * 16 + pos % 16
+    cache.append(rows[:, H:H + kv], rows[:, H + kv:], ints(slots), rope=r, positions=ints(pos))
+
+    step = torch.zeros(B, H + 2 * kv, d, dtype=torch.bfloat16, device="cuda")
+    q_out, out = torch.empty(B, H, d, dtype=torch.bfloat16, device="cuda"), torch.empty(B, H, d, dtype=torch.bfloat16, device="cuda")
+    d_pos, d_slots, d_len, d_pages = ints([0] * B), ints([-1] * B), ints([0] * B), ints(pages)
+
+    def one():
+        cache.append(step[:, H:H + kv], step[:, H + kv:], d_slots, rope=r, positions=d_pos, q=step[:, :H], q_out=q_out)
+        cache.attend(q_out, d_pages, d_len, out=out)
+
+    before = cache.data.clone()
+    one()                                                     # slots -1: nothing is written
+    assert torch.equal(cache.data, before) and bool((out == 0).all())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one()
+    for s in range(steps):
+        live = np.array([True, True, s % 3 != 0])              # a client that pauses: padding
+        step.copy_(randn(rng, B, H + 2 * kv, d, dtype="bf16"))
+        slot = np.where(live, pages[np.arange(B), lengths // 16] * 16 + lengths % 16, -1)
+        d_pos.copy_(ints(lengths))
+        d_slots.copy_(ints(slot))
+        now = lengths
+        lengths = lengths + live
+        d_len.copy_(ints(np.where(live, lengths, 0)))
+        graph.replay()
+        torch.cuda.synchronize()
+        q64 = paged.rope(f64(step[:, :H]), now, d, f, g)
+        mix = np.abs(f64(step[:, :H]))
+        mix = np.tile(mix[..., :d // 2] + mix[..., d // 2:], 2)
+        within(f64(q_out), q64, 2.0 ** -21 * g * mix + half_step(q64, "bf16"), "q")
+        used = np.concatenate([pages[b, t // 16] * 16 + t % 16 for b in range(B) for t in [np.arange(lengths[b])]])
+        vals = np.zeros((192, 2, kv, d))
+        kk, vv = cache.read(ints(used), dtype=torch.float32)
+        vals[used, 0], vals[used, 1] = f64(kk), f64(vv)
+        check_attention(cache, q_out, pages, np.where(live, lengths, 0), vals, d ** -0.5, 0, out, None, "bf16")
+    cache.check()
+
+
+def test_two_captured_graphs_replayed_on_two_streams():
+    rng = np.random.default_rng(21)
+    lengths = [2500, 100, 1]
+    cache, q, pages, _ = attention_case(rng, 3, 2, 4, 64, "e4m3", "f32", lengths)
+    p, n = ints(pages), ints(lengths)
+    want = cache.attend(q, p, n)
+    outs, graphs = [torch.empty_like(q) for _ in range(2)], [torch.cuda.CUDAGraph() for _ in range(2)]
+    for g, o in zip(graphs, outs):
+        with torch.cuda.graph(g):
+            cache.attend(q, p, n, out=o)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        cache.attend(q, p, n)                                  # an eager call beside them
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
+def test_a_contexts_cache_read_attended_and_quantised():
+    """A model's own cache through wici_kv_view: K and V of its prompt against the model oracle's, attention over it,
+    and a batch of clients continuing from that prompt in an 8-bit cache."""
+    cfg = gen.TINY
+    w = gen.make_weights(cfg)
+    prompt = gen.make_prompt(cfg, 45, seed=3)
+    model = WiciModel(cfg, max_tokens=64).load(w)
+    perm = np.random.default_rng(22).permutation(4)
+    wici.wici_set_page_table(model.ctx, perm)
+    model.prefill(prompt)
+    ref = oracle.OracleModel(cfg, w, max_tokens=64)
+    ref.prefill(prompt)
+    kv, d = cfg.n_kv_heads, cfg.head_dim
+    for layer in range(cfg.n_layers):
+        k, v = model.read_kv(layer)
+        assert k.shape == (45, kv, d)
+        for got, want in ((k, ref.K[layer][:, :45]), (v, ref.V[layer][:, :45])):
+            want = np.asarray(want, np.float64).transpose(1, 0, 2)
+            err = np.linalg.norm(f64(got) - want) / np.linalg.norm(want)
+            assert err <= 1e-2                                 # the model's own tolerance (bf16 storage is 1.7e-3 of it)
+        part, _ = model.read_kv(layer, first=17, count=20)
+        assert torch.equal(part, k[17:37])
+        cache, table = model.kv_cache(layer)
+        assert table.tolist() == perm.tolist()
+        q = randn(np.random.default_rng(23), 1, cfg.n_q_heads, d)
+        out = cache.attend(q, table[None], ints([45]))
+        vals = np.zeros((64, 2, kv, d))
+        order = perm[np.arange(45) // 16] * 16 + np.arange(45) % 16
+        vals[order, 0], vals[order, 1] = f64(k), f64(v)
+        check_attention(cache, q, perm[None], [45], vals, d ** -0.5, 0, out, None, "f32")
+        small = PagedKV(kv, d, "int8", n_pages=3)
+        small.append(k, v, ints(range(45)))
+        k8, v8 = small.read(ints(range(45)), dtype=torch.float32)
+        top = k.float().abs().amax(-1, keepdim=True)
+        assert bool(((k8 - k.float()).abs() <= top * (0.5 / 127 + 2.0 ** -16)).all())
+    with pytest.raises(wici.WiciError):
+        model.kv_cache(cfg.n_layers)
+    with pytest.raises(ValueError):
+        model.read_kv(0, first=40, count=6)
+    model.close()
