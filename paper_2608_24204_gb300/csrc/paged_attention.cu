@@ -1,10 +1,12 @@
-// Attention of one new token per sequence over a paged key-value cache (include/wici_ops.h).
+// Attention of one new token per sequence over a paged key-value cache (include/wici_ops.h):
+// argument checks and launches.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 
+#include "device_table.h"
 #include "kernels.h"
-#include "ops.cuh"
+#include "paged_attention.cuh"
 
 using namespace wici;
 
@@ -20,112 +22,25 @@ int fail(int code, const char *fmt, ...) {
     return code;
 }
 
-constexpr int kAttnWarps = 4;
+DeviceTable<int> g_sms;
 
-struct AttnArg {
-    HeadsArg q, out;
-    CacheArg cache;
-    const int32_t *pages, *lengths;
-    float *lse;
-    int32_t *status;
-    int q_heads, group, max_pages, window;
-    int q_dtype, out_dtype;
-    float scale;
-};
-
-__device__ __forceinline__ float load_any(const HeadsArg &t, int dtype, int64_t token, int head, int i) {
-    switch (dtype) {
-        case WICI_BF16: return to_f32(t.row<__nv_bfloat16>(token, head)[i]);
-        case WICI_F16: return to_f32(t.row<__half>(token, head)[i]);
-        default: return t.row<float>(token, head)[i];
-    }
+int sm_count(int *n) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = g_sms.get(dev, n, [dev](int *d) {
+        cudaError_t e1 = setup_attention_bf16();
+        if (e1 == cudaSuccess) e1 = setup_attention_int8();
+        if (e1 == cudaSuccess) e1 = setup_attention_e4m3();
+        if (e1 != cudaSuccess) return e1;
+        return cudaDeviceGetAttribute(d, cudaDevAttrMultiProcessorCount, dev);
+    });
+    return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "attention setup: %s", cudaGetErrorString(e));
 }
 
-__device__ __forceinline__ void store_any(const HeadsArg &t, int dtype, int64_t token, int head, int i, float v) {
-    switch (dtype) {
-        case WICI_BF16: from_f32(v, t.row<__nv_bfloat16>(token, head)[i]); break;
-        case WICI_F16: from_f32(v, t.row<__half>(token, head)[i]); break;
-        default: t.row<float>(token, head)[i] = v; break;
-    }
-}
+constexpr int kTicketBytes = 16384;   // arrivals of every block
+constexpr int kMaxBlocks = kTicketBytes / (int)sizeof(int);
 
-// One block per sequence and query head; a warp takes every fourth key and keeps the running
-// maximum and sum of the softmax (s - max in fp32), a lane D / 32 adjacent elements of the head.
-template <int FMT, int D>
-__global__ void __launch_bounds__(32 * kAttnWarps) attention_kernel(const __grid_constant__ AttnArg a) {
-    constexpr int E = D / 32;
-    __shared__ float sm[kAttnWarps], sl[kAttnWarps], so[kAttnWarps][D];
-    griddep_wait();
-    const int h = blockIdx.x, b = blockIdx.y, kvh = h / a.group;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    const int n = a.lengths[b];
-    const int lo = a.window && n > a.window ? n - a.window : 0;
-    bool bad = n > a.max_pages * (int64_t)kKvPage;
-    int bits = bad ? WICI_BAD_LENGTH : 0;
-    float q[E], o[E] = {}, m = -INFINITY, l = 0.f;
-    for (int e = 0; e < E; ++e) q[e] = load_any(a.q, a.q_dtype, b, h, lane * E + e) * a.scale;
-    for (int t = lo + warp; t < n && !bad; t += kAttnWarps) {
-        const int page = a.pages[(int64_t)b * a.max_pages + t / kKvPage], place = t % kKvPage;
-        if (page < 0 || page >= a.cache.n_pages) {
-            bad = true;
-            bits |= WICI_BAD_PAGE;
-            break;
-        }
-        constexpr int64_t kBlock = FMT == WICI_KV_BF16 ? kKvPage * D * 2 : kKvPage * (D + 4);
-        const uint8_t *kb = a.cache.data + page * a.cache.page_stride + kvh * kBlock;
-        const uint8_t *vb = kb + a.cache.kv_heads * kBlock;
-        float k[E], v[E];
-        if (FMT == WICI_KV_BF16) {
-            for (int e = 0; e < E; ++e) {
-                k[e] = to_f32(((const __nv_bfloat16 *)kb)[place * D + lane * E + e]);
-                v[e] = to_f32(((const __nv_bfloat16 *)vb)[place * D + lane * E + e]);
-            }
-        } else {
-            const float ks = ((const float *)(kb + kKvPage * D))[place], vs = ((const float *)(vb + kKvPage * D))[place];
-            for (int e = 0; e < E; e += 2) {
-                const float2 k2 = __half22float2(decode2<FMT>(*(const uint16_t *)(kb + place * D + lane * E + e)));
-                const float2 v2 = __half22float2(decode2<FMT>(*(const uint16_t *)(vb + place * D + lane * E + e)));
-                k[e] = k2.x * ks;
-                k[e + 1] = k2.y * ks;
-                v[e] = v2.x * vs;
-                v[e + 1] = v2.y * vs;
-            }
-        }
-        float s = 0.f;
-        for (int e = 0; e < E; ++e) s += q[e] * k[e];
-        s = warp_sum(s);
-        const float m2 = fmaxf(m, s), c = m2 == -INFINITY ? 1.f : expf(m - m2), p = s == -INFINITY ? 0.f : expf(s - m2);
-        l = l * c + p;
-        for (int e = 0; e < E; ++e) o[e] = o[e] * c + p * v[e];
-        m = m2;
-    }
-    if (lane == 0) {
-        sm[warp] = m;
-        sl[warp] = l;
-        if (bits && a.status) atomicOr(a.status, bits);
-    }
-    for (int e = 0; e < E; ++e) so[warp][lane * E + e] = o[e];
-    bad = __syncthreads_or(bad);
-    if (threadIdx.x < D) {
-        float top = -INFINITY, sum = 0.f, acc = 0.f;
-        for (int w = 0; w < kAttnWarps; ++w) top = fmaxf(top, sm[w]);
-        for (int w = 0; w < kAttnWarps; ++w) {
-            const float c = sm[w] == -INFINITY ? 0.f : expf(sm[w] - top);
-            sum += sl[w] * c;
-            acc += so[w][threadIdx.x] * c;
-        }
-        const float nan = __uint_as_float(0x7FC00000u);
-        store_any(a.out, a.out_dtype, b, h, threadIdx.x, bad ? nan : sum > 0.f ? acc / sum : acc);
-        if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)b * a.q_heads + h] = bad ? nan : top + logf(sum);
-    }
-}
-
-template <int FMT>
-cudaError_t launch(int d, const AttnArg &a, int batch, cudaStream_t st) {
-    const dim3 grid(a.q_heads, batch);
-    return d == 64 ? launch_kernel(attention_kernel<FMT, 64>, grid, 32 * kAttnWarps, 0, st, 1, true, a)
-                   : launch_kernel(attention_kernel<FMT, 128>, grid, 32 * kAttnWarps, 0, st, 1, true, a);
-}
+int grid_of(int sms) { return 2 * sms < kMaxBlocks ? 2 * sms : kMaxBlocks; }
 
 const char *check_query_heads(const wici_kv_cache *c, int n_q_heads) {
     return n_q_heads < 1 || n_q_heads > kMaxHeads || n_q_heads % c->n_kv_heads
@@ -142,7 +57,14 @@ int wici_paged_attention_workspace_bytes(const wici_kv_cache *cache, int32_t n_q
     if (const char *m = check_query_heads(cache, n_q_heads)) return fail(WICI_E_ARG, "attention: %s", m);
     if (batch < 0 || batch > 65535) return fail(WICI_E_ARG, "attention: batch must be in [0, 65535]");
     if (!bytes) return fail(WICI_E_ARG, "attention: null output");
-    *bytes = 256;
+    int sms = 152;   // without a device: a GB300's
+    int dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess) {
+        if (int rc = sm_count(&sms)) return rc;
+    } else {
+        cudaGetLastError();
+    }
+    *bytes = kTicketBytes + (size_t)grid_of(sms) * 2 * attn_piece_floats(cache->head_dim) * sizeof(float);
     return WICI_OK;
 }
 
@@ -164,27 +86,44 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     if (shape->batch == 0) return WICI_OK;
     if (!pages || !lengths || !workspace || ((uintptr_t)workspace & 15))
         return fail(WICI_E_ARG, "attention: null pages or lengths, or workspace null or not 16-byte aligned");
+    int sms = 0;
+    if (int rc = sm_count(&sms)) return rc;
     AttnArg a = {};
     a.q = heads_arg(q);
     a.out = heads_arg(out);
     a.cache = cache_arg(cache);
-    a.pages = pages;
-    a.lengths = lengths;
-    a.lse = lse;
     a.status = status;
+    a.tickets = (int *)workspace;
+    a.pieces = (float *)((uint8_t *)workspace + kTicketBytes);
     a.q_heads = q->heads;
     a.group = q->heads / cache->n_kv_heads;
+    const bool stack = a.group <= 8;
+    a.tiles = stack ? 1 : (a.group + 15) / 16;
     a.max_pages = shape->max_pages;
     a.window = shape->window;
     a.q_dtype = q->dtype;
     a.out_dtype = out->dtype;
+    a.q_wide = wide_heads(q);
+    a.out_wide = wide_heads(out);
     a.scale = shape->scale;
+    // three terms where a bf16 cache meets fp32, and where a pass holds one term and q needs two
+    const bool exact = q->dtype == WICI_F32 || out->dtype == WICI_F32 || (!stack && q->dtype == WICI_F16);
+    // a launch's page counts add up in 32 bits
+    const int room = INT32_MAX / shape->max_pages, most = room < kAttnMaxBatch ? room : kAttnMaxBatch;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    cudaError_t e;
-    switch (cache->format) {
-        case WICI_KV_BF16: e = launch<WICI_KV_BF16>(cache->head_dim, a, shape->batch, st); break;
-        case WICI_KV_INT8: e = launch<WICI_KV_INT8>(cache->head_dim, a, shape->batch, st); break;
-        default: e = launch<WICI_KV_E4M3>(cache->head_dim, a, shape->batch, st); break;
+    cudaError_t e = cudaSuccess;
+    for (int b = 0; b < shape->batch && e == cudaSuccess; b += most) {
+        a.batch = shape->batch - b < most ? shape->batch - b : most;
+        a.pages = pages + (int64_t)b * shape->max_pages;
+        a.lengths = lengths + b;
+        a.lse = lse ? lse + (int64_t)b * q->heads : nullptr;
+        a.q.data = (uint8_t *)q->data + (int64_t)b * q->token_stride * dtype_bytes(q->dtype);
+        a.out.data = (uint8_t *)out->data + (int64_t)b * out->token_stride * dtype_bytes(out->dtype);
+        switch (cache->format) {
+            case WICI_KV_BF16: e = launch_attention_bf16(cache->head_dim, a, stack, exact, grid_of(sms), st); break;
+            case WICI_KV_INT8: e = launch_attention_int8(cache->head_dim, a, stack, grid_of(sms), st); break;
+            default: e = launch_attention_e4m3(cache->head_dim, a, stack, grid_of(sms), st); break;
+        }
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "attention: %s", cudaGetErrorString(e));
 }

@@ -1,0 +1,33 @@
+// Paged attention over a bf16 cache.
+#include "paged_attention.cuh"
+
+namespace wici {
+
+template <int D>
+static cudaError_t launch_d(const AttnArg &a, bool stack, bool exact, int grid, cudaStream_t st) {
+    if (stack)
+        return exact ? launch_attention<WICI_KV_BF16, D, true, true>(a, grid, st)
+                     : launch_attention<WICI_KV_BF16, D, true, false>(a, grid, st);
+    return exact ? launch_attention<WICI_KV_BF16, D, false, true>(a, grid, st)
+                 : launch_attention<WICI_KV_BF16, D, false, false>(a, grid, st);
+}
+
+cudaError_t launch_attention_bf16(int d, const AttnArg &a, bool stack, bool exact, int grid, cudaStream_t st) {
+    return d == 64 ? launch_d<64>(a, stack, exact, grid, st) : launch_d<128>(a, stack, exact, grid, st);
+}
+
+template <int D>
+static cudaError_t setup_d() {
+    cudaError_t e = limit_attention<WICI_KV_BF16, D, true, true>();
+    if (e == cudaSuccess) e = limit_attention<WICI_KV_BF16, D, true, false>();
+    if (e == cudaSuccess) e = limit_attention<WICI_KV_BF16, D, false, true>();
+    if (e == cudaSuccess) e = limit_attention<WICI_KV_BF16, D, false, false>();
+    return e;
+}
+
+cudaError_t setup_attention_bf16() {
+    const cudaError_t e = setup_d<64>();
+    return e == cudaSuccess ? setup_d<128>() : e;
+}
+
+}  // namespace wici
