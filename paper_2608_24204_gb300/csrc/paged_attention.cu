@@ -38,9 +38,12 @@ int sm_count(int *n) {
 }
 
 constexpr int kTicketBytes = 16384;   // arrivals of every block
-constexpr int kMaxBlocks = kTicketBytes / (int)sizeof(int);
-
-int grid_of(int sms) { return 2 * sms < kMaxBlocks ? 2 * sms : kMaxBlocks; }
+constexpr int kMaxBlocksPerSm = 3;
+// SMs that a launch uses: tickets are for so many blocks
+int used_sms(int sms) {
+    const int most = kTicketBytes / (int)sizeof(int) / kMaxBlocksPerSm;
+    return sms < most ? sms : most;
+}
 
 const char *check_query_heads(const wici_kv_cache *c, int n_q_heads) {
     return n_q_heads < 1 || n_q_heads > kMaxHeads || n_q_heads % c->n_kv_heads
@@ -64,7 +67,7 @@ int wici_paged_attention_workspace_bytes(const wici_kv_cache *cache, int32_t n_q
     } else {
         cudaGetLastError();
     }
-    *bytes = kTicketBytes + (size_t)grid_of(sms) * 2 * attn_piece_floats(cache->head_dim) * sizeof(float);
+    *bytes = kTicketBytes + (size_t)used_sms(sms) * kMaxBlocksPerSm * 2 * attn_piece_floats(cache->head_dim) * sizeof(float);
     return WICI_OK;
 }
 
@@ -83,6 +86,8 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
         return fail(WICI_E_ARG, "attention out: %s", m);
     if (q->heads != out->heads) return fail(WICI_E_ARG, "attention: q and out differ in heads");
     if (const char *m = check_query_heads(cache, q->heads)) return fail(WICI_E_ARG, "attention: %s", m);
+    if ((int64_t)(shape->max_pages + 2) * q->heads >= (int64_t)1 << 31)
+        return fail(WICI_E_ARG, "attention: (max_pages + 2) * heads must be below 2^31");
     if (shape->batch == 0) return WICI_OK;
     if (!pages || !lengths || !workspace || ((uintptr_t)workspace & 15))
         return fail(WICI_E_ARG, "attention: null pages or lengths, or workspace null or not 16-byte aligned");
@@ -106,10 +111,11 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     a.q_wide = wide_heads(q);
     a.out_wide = wide_heads(out);
     a.scale = shape->scale;
-    // three terms where a bf16 cache meets fp32, and where a pass holds one term and q needs two
-    const bool exact = q->dtype == WICI_F32 || out->dtype == WICI_F32 || (!stack && q->dtype == WICI_F16);
-    // a launch's page counts add up in 32 bits
-    const int room = INT32_MAX / shape->max_pages, most = room < kAttnMaxBatch ? room : kAttnMaxBatch;
+    // more terms where fp32 comes in or, over a bf16 cache, goes out or q is not bf16
+    const bool exact = cache->format == WICI_KV_BF16 ? q->dtype != WICI_BF16 || out->dtype == WICI_F32 : q->dtype == WICI_F32;
+    // the weight of a launch's segments adds up in 31 bits
+    const int64_t each = ((int64_t)shape->max_pages + kAttnSegment) * cache->n_kv_heads * a.tiles, room = INT32_MAX / each;
+    const int most = room < 1 ? 1 : room < kAttnMaxBatch ? (int)room : kAttnMaxBatch;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;
     for (int b = 0; b < shape->batch && e == cudaSuccess; b += most) {
@@ -120,9 +126,9 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
         a.q.data = (uint8_t *)q->data + (int64_t)b * q->token_stride * dtype_bytes(q->dtype);
         a.out.data = (uint8_t *)out->data + (int64_t)b * out->token_stride * dtype_bytes(out->dtype);
         switch (cache->format) {
-            case WICI_KV_BF16: e = launch_attention_bf16(cache->head_dim, a, stack, exact, grid_of(sms), st); break;
-            case WICI_KV_INT8: e = launch_attention_int8(cache->head_dim, a, stack, grid_of(sms), st); break;
-            default: e = launch_attention_e4m3(cache->head_dim, a, stack, grid_of(sms), st); break;
+            case WICI_KV_BF16: e = launch_attention_bf16(cache->head_dim, a, stack, exact, used_sms(sms), st); break;
+            case WICI_KV_INT8: e = launch_attention_int8(cache->head_dim, a, stack, exact, used_sms(sms), st); break;
+            default: e = launch_attention_e4m3(cache->head_dim, a, stack, exact, used_sms(sms), st); break;
         }
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "attention: %s", cudaGetErrorString(e));

@@ -4,30 +4,32 @@
 // once per KV head: 4 n_q d flops per 4 n_kv d bytes (bf16), far below what the tensor cores
 // give per byte.  The kernel is bound by HBM; everything else has to stay out of its way.
 //
-// Work.  A unit is one page (16 keys) of one KV head and head tile.  All units of the batch,
-// sequence after sequence, head after head, are cut into equal runs, one per block, however
-// ragged the lengths are.  The warps of a block take its units in turn, each through a ring of
-// its own in shared memory that cp.async fills ahead, across the ends of segments (a segment:
-// the units of one sequence and head).  At a segment's end the block's warps join their
-// states; a segment that spans blocks is joined by the block that finishes last.
+// Work.  A unit is P pages (16 P keys) of one KV head and head tile.  All units of the batch,
+// sequence after sequence, head after head, are cut into equal runs, one per warp, however
+// ragged the lengths are; a segment (the units of one sequence and head) weighs kAttnSegment
+// units more than it has, for its queries' way in and its result's way out.  A warp streams its
+// run through a ring of its own in shared memory that cp.async fills ahead, across the ends of
+// segments.  A segment inside one run is finished by its warp alone; the parts of others are
+// joined by the block at its end, and by the block that finishes last where blocks share one.
 //
 // Softmax in base 2 with a running maximum m and sum l in fp32; O in fp32 accumulators.
 //
 // Products on mma.m16n8k16: S = Q K^T with 16 rows of queries, 8 keys and 16 elements of the
-// head a step, O += P V with the same rows.  Neither operand of K or V is transposed or shuffled:
+// head a step, O += P V with the same rows.  Neither K nor V is transposed or shuffled:
 // * a lane's 16 bytes of a key row serve as its B fragments of several steps.  The order in
 //   which a step's 16 elements stand for elements of the head is free as long as Q agrees;
-// * the 16 keys of a unit are ordered so that the scores a lane gets are the ones its A
+// * the 16 keys of a page are ordered so that the scores a lane gets are the ones its A
 //   fragment of P needs, and V rows t, t + 4, t + 8, t + 12 give its B fragments by byte permutes.
 //
 // Precision.  K and V enter exactly: bf16 as stored; 8-bit codes as fp16, their scales applied
 // to the scores and to the weights in fp32.  Q and P are carried as sums of 16-bit terms.  With
 // at most 8 queries a group the second term's rows fill the upper half of the 16 (STACK), so two
 // terms cost what one does; larger groups take 16 queries a tile and a pass per term.
-//   bf16 cache: q and p as two terms (16 bits), or three where q or the result is fp32 (EXACT);
-//   a bf16 q is one term exactly.
-//   8-bit cache: two fp16 terms (22 bits).  q is scaled by a power of two per head, p by the
-//   value's scale relative to the largest one so far, so that neither leaves fp16's range.
+//   bf16 cache: q that is not bf16 as three terms; p as two (16 bits), or three where q is not
+//   bf16 or the result is fp32 (EXACT).
+//   8-bit cache: q as one fp16 term (bf16 and fp16 fit exactly) or, from fp32, as two (EXACT),
+//   scaled by a power of two per head; p as two (22 bits), scaled by the value's scale relative
+//   to the largest one so far, so that neither leaves fp16's range.
 #pragma once
 #include "ops.cuh"
 
@@ -35,7 +37,9 @@ namespace wici {
 
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = 32 * kAttnWarps;
-constexpr int kAttnMaxBatch = 1024;   // sequences of a launch: their page counts are in shared memory
+constexpr int kAttnMaxBatch = 256;    // sequences of a launch: their keys are in shared memory
+constexpr uint32_t kAttnSegment = 3;       // units that a segment weighs beside its own
+constexpr uint32_t kAttnMinUnits = 8;      // weight of a warp's run at least: shorter ones would not pay for joining more parts
 constexpr int kAttnPieceRows = 16;    // rows of a piece in the workspace (a head tile has 8 or 16)
 
 struct AttnArg {
@@ -45,7 +49,7 @@ struct AttnArg {
     float *lse;
     int32_t *status;
     int *tickets;                     // [blocks]: arrivals at the segment that starts in a block and leaves it
-    float *pieces;                    // [blocks][2][kAttnPieceRows][D + 2]: O, m, l of a block's part of a segment
+    float *pieces;                    // [blocks][2][kAttnPieceRows][D + 2]: O, then m and l, of a block's part of a segment
     int batch, q_heads, group, tiles; // head tiles of a KV head
     int max_pages, window;
     int q_dtype, out_dtype;
@@ -56,17 +60,22 @@ struct AttnArg {
 constexpr int attn_block(int fmt, int d) { return fmt == WICI_KV_BF16 ? kKvPage * d * 2 : kKvPage * (d + 4); }
 constexpr size_t attn_piece_floats(int d) { return (size_t)kAttnPieceRows * (d + 2); }
 
-template <int FMT, int D>
+template <int FMT, int D, bool STACK>
 struct AttnShape {
+    static constexpr int kRows = STACK ? 8 : 16;                   // queries of a head tile
+    static constexpr int kPages = FMT == WICI_KV_BF16 && D == 128 ? 1 : 2;                // of a unit
+    static constexpr int kBlocks = FMT != WICI_KV_BF16 && D == 64 && STACK ? 3 : 2;   // on an SM
     static constexpr int kBlock = attn_block(FMT, D);
-    // ring slots of K and of V: what fits two blocks on an SM beside the join's buffer
-    static constexpr int kKSlots = FMT == WICI_KV_BF16 && D == 128 ? 3 : 4;
+    static constexpr int kSlot = kPages * kBlock;
+    // ring slots of K and of V: what fits beside the parts to be joined
+    static constexpr int kKSlots = FMT != WICI_KV_BF16 && D == 64 ? 4 : 3;
     static constexpr int kVSlots = kKSlots - 1;
-    static constexpr int kRing = (kKSlots + kVSlots) * kBlock;
-    static constexpr int kJoinRow = D + 8;                         // floats: neighbouring rows in other banks
-    static constexpr int kJoin = kAttnWarps * 8 * kJoinRow * 4;    // O of 8 rows of every warp
-    static constexpr int kState = kAttnWarps * 8 * 2 * 4;          // m and l
-    static constexpr int kSmem = kAttnWarps * kRing + kJoin + kState + (kAttnMaxBatch + 1) * 4 + 64;
+    static constexpr int kRing = (kKSlots + kVSlots) * kSlot;
+    static constexpr int kPartRow = D + 4;                         // floats: neighbouring rows in other banks
+    static constexpr int kPart = kRows * (kPartRow + 2) * 4;       // a part of a segment: O, then m and l of each row
+    static constexpr int kSmem = kAttnWarps * kRing + (kAttnWarps - 1) * kPart + (3 * kAttnMaxBatch + 2) * 4 + 128;
+    static_assert(kPart <= kRing, "a warp's last part lies in its ring");
+    static_assert(kBlocks * (kSmem + 1024) <= 228 * 1024, "blocks of an SM");
 };
 
 // ------------------------------------------------------------------ PTX ----
@@ -161,24 +170,48 @@ __device__ __forceinline__ int chunk_at(int r, int c) {
     return r * ROW + ((c ^ ((r & 3) << 1) ^ ((r >> 2 & 1) * 5)) << 4);
 }
 
-__device__ __forceinline__ float load_any(const HeadsArg &t, int dtype, int64_t token, int head, int i) {
-    switch (dtype) {
-        case WICI_BF16: return to_f32(t.row<__nv_bfloat16>(token, head)[i]);
-        case WICI_F16: return to_f32(t.row<__half>(token, head)[i]);
-        default: return t.row<float>(token, head)[i];
+// 8 elements of q from element i on, as they stand: one 16-byte word of a 16-bit type, two of fp32 (W)
+template <int W>
+__device__ __forceinline__ void load_q8(const AttnArg &a, int64_t token, int head, int i, uint4 *v) {
+    if (W == 2 && a.q_dtype == WICI_F32) {
+        const float *p = a.q.row<float>(token, head) + i;
+        if (a.q_wide) {
+            v[0] = ((const uint4 *)p)[0];
+            v[W - 1] = ((const uint4 *)p)[1];
+        } else {
+            v[0] = make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]));
+            v[W - 1] = make_uint4(__float_as_uint(p[4]), __float_as_uint(p[5]), __float_as_uint(p[6]), __float_as_uint(p[7]));
+        }
+        return;
+    }
+    const uint16_t *p = a.q.row<uint16_t>(token, head) + i;
+    if (a.q_wide) {
+        v[0] = *(const uint4 *)p;
+    } else {
+        v[0] = make_uint4(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16, p[4] | (uint32_t)p[5] << 16,
+                          p[6] | (uint32_t)p[7] << 16);
     }
 }
-// 8 elements of q from element i on
-__device__ __forceinline__ void load_q8(const AttnArg &a, int64_t token, int head, int i, float *v) {
-    if (a.q_wide) {
-        switch (a.q_dtype) {
-            case WICI_BF16: load8<__nv_bfloat16, true>(a.q.row<__nv_bfloat16>(token, head) + i, 8, v); break;
-            case WICI_F16: load8<__half, true>(a.q.row<__half>(token, head) + i, 8, v); break;
-            default: load8<float, true>(a.q.row<float>(token, head) + i, 8, v); break;
-        }
-    } else {
+// those as fp32
+template <int W>
+__device__ __forceinline__ void unpack_q8(int dtype, const uint4 *v, float *x) {
+    if (W == 2 && dtype == WICI_F32) {
+        const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[W - 1].x, v[W - 1].y, v[W - 1].z, v[W - 1].w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = load_any(a.q, a.q_dtype, token, head, i + j);
+        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+        return;
+    }
+    const uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (dtype == WICI_BF16) {
+            x[2 * j] = bf16lo(w[j]);
+            x[2 * j + 1] = bf16hi(w[j]);
+        } else {
+            const float2 f = __half22float2(*(const __half2 *)&w[j]);
+            x[2 * j] = f.x;
+            x[2 * j + 1] = f.y;
+        }
     }
 }
 __device__ __forceinline__ void store_out4(const AttnArg &a, int64_t token, int head, int i, const float *v) {
@@ -219,75 +252,104 @@ __device__ __forceinline__ void store_out4(const AttnArg &a, int64_t token, int 
 // the keys of a sequence: [lo, n), none where the length is bad or not positive
 struct Keys {
     int lo, n;
-    bool bad;
-    __device__ __forceinline__ int first_page() const { return lo / kKvPage; }
-    __device__ __forceinline__ int page_count() const { return n > lo ? (n + kKvPage - 1) / kKvPage - lo / kKvPage : 0; }
 };
-__device__ __forceinline__ Keys keys_of(const AttnArg &a, int b) {
-    Keys k;
-    k.n = a.lengths[b];
-    k.bad = k.n > a.max_pages * (int64_t)kKvPage;
-    if (k.bad || k.n < 0) k.n = 0;
-    k.lo = a.window && k.n > a.window ? k.n - a.window : 0;
-    return k;
+__device__ __forceinline__ Keys keys_of(int length, int window) {
+    return Keys{window && length > window ? length - window : 0, length};
 }
 
 template <int FMT, int D, bool STACK, bool EXACT>
-__global__ void __launch_bounds__(kAttnThreads, 2) paged_attention_kernel(const __grid_constant__ AttnArg a) {
-    using S = AttnShape<FMT, D>;
+__global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlocks) paged_attention_kernel(const __grid_constant__ AttnArg a) {
+    using S = AttnShape<FMT, D, STACK>;
     constexpr bool BF16 = FMT == WICI_KV_BF16;
     constexpr int ROW = BF16 ? 2 * D : D;                 // bytes of a key row
     constexpr int CHUNKS = ROW / 16;
-    constexpr int PER = BF16 ? 8 : 16;                    // elements of a chunk
-    constexpr int HT = STACK ? 8 : 16;                    // queries of a head tile
+    constexpr int P = S::kPages, UNIT = P * kKvPage;      // keys of a unit
+    constexpr int HT = S::kRows;
     constexpr int R = STACK ? 1 : 2;                      // queries whose rows a lane holds
-    constexpr int TQ = BF16 && EXACT ? 3 : STACK || !BF16 ? 2 : 1;
+    constexpr int TQ = !EXACT ? 1 : BF16 ? 3 : 2;
     constexpr int TP = BF16 && EXACT ? 3 : 2;
     constexpr int QPASS = STACK ? (TQ + 1) / 2 : TQ, PPASS = STACK ? (TP + 1) / 2 : TP;
     constexpr int STEPS = D / 16, NT = D / 8;
+    constexpr int SETS = P == 1 ? 2 : 1;                  // accumulators of a score: four chains of products at least
     constexpr int KS = S::kKSlots, VS = S::kVSlots;
+    constexpr int PER = BF16 || D == 64 ? 8 : 16;         // adjacent elements of O that a lane holds per column
     constexpr float kPUnit = BF16 ? 1.f : 4096.f;         // what weights are scaled up by (fp16: far from its smallest)
 
     extern __shared__ __align__(128) uint8_t smem[];
-    float *join = (float *)(smem + kAttnWarps * S::kRing);            // [warp][8][kJoinRow]
-    float2 *state = (float2 *)((uint8_t *)join + S::kJoin);           // [warp][8]: m, l
-    int *prefix = (int *)((uint8_t *)state + S::kState);              // [batch + 1]: pages of the sequences before
-    int *sflag = prefix + kAttnMaxBatch + 1;                          // [8]
+    struct Rec {                          // a segment
+        uint32_t start, end;              // units
+        int b, head;                      // head: of HH
+    };
+    struct Shared {
+        Rec leaving[kAttnWarps];          // the segment that goes on past a warp's run (end = 0: none)
+        Rec side[2];                      // the one that enters the block's run, the one that begins in it and leaves it
+        int first[2], last[2];            // blocks that share it
+        int note[kAttnWarps];
+    };
+    static_assert(sizeof(Shared) <= 128, "counted in kSmem");
+    uint8_t *parts = smem + kAttnWarps * S::kRing;                    // of warps 1.. : the part that ends in its run
+    Shared &sh = *(Shared *)(parts + (kAttnWarps - 1) * S::kPart);
+    int *prefix = (int *)((uint8_t *)&sh + 128);                      // [batch + 1]: units of a head before a sequence
+    int *weight = prefix + kAttnMaxBatch + 1;                         // [batch + 1]: the same with their segments' weights
+    int *length = weight + kAttnMaxBatch + 1;                         // [batch]
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * S::kRing;
+    griddep_launch_dependents();
     griddep_wait();
 
-    // ---- page counts of all sequences, and their sums ----
+    // ---- units of every sequence, and their sums ----
     {
         const int per = (a.batch + kAttnThreads - 1) / kAttnThreads;
         const int b0 = min(a.batch, (int)threadIdx.x * per), b1 = min(a.batch, b0 + per);
-        int sum = 0;
-        for (int b = b0; b < b1; ++b) sum += keys_of(a, b).page_count();
-        int incl = sum;
+        int sum = 0, segments = 0;
+        for (int b = b0; b < b1; ++b) {
+            int n = a.lengths[b];
+            if (n > a.max_pages * (int64_t)kKvPage) n = -1;
+            else if (n < 0) n = 0;
+            length[b] = n;                               // -1: too long for its row of pages
+            const Keys k = keys_of(n, a.window);
+            const int units = k.n > 0 ? ((k.n + kKvPage - 1) / kKvPage - k.lo / kKvPage + P - 1) / P : 0;
+            prefix[b] = units;
+            sum += units;
+            segments += units > 0;
+        }
+        int incl = sum, incl_s = segments;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
+            const int v = __shfl_up_sync(0xffffffffu, incl, o), v_s = __shfl_up_sync(0xffffffffu, incl_s, o);
+            if (lane >= o) incl += v, incl_s += v_s;
         }
-        if (lane == 31) sflag[warp] = incl;
+        if (lane == 31) sh.note[warp] = incl;
+        int *count_s = (int *)sh.leaving;                // free until the runs are known
+        if (lane == 31) count_s[warp] = incl_s;
         __syncthreads();
-        int at = incl - sum;
-        for (int w = 0; w < warp; ++w) at += sflag[w];
+        int at = incl - sum, at_s = incl_s - segments;
+        for (int w = 0; w < warp; ++w) at += sh.note[w], at_s += count_s[w];
         for (int b = b0; b < b1; ++b) {
+            const int units = prefix[b];
             prefix[b] = at;
-            at += keys_of(a, b).page_count();
+            weight[b] = at + kAttnSegment * at_s;
+            at += units;
+            at_s += units > 0;
         }
-        if (b1 == a.batch) prefix[a.batch] = at;
+        if (b1 == a.batch) {
+            prefix[a.batch] = at;
+            weight[a.batch] = at + kAttnSegment * at_s;
+        }
         __syncthreads();
     }
-    const int HH = a.cache.kv_heads * a.tiles;
-    const int64_t U = (int64_t)prefix[a.batch] * HH;
+    const uint32_t HH = a.cache.kv_heads * a.tiles;
+    const uint32_t V = weight[a.batch] * HH;             // weight of all segments: below 2^31
 
-    // sequences without keys: zeros, or NaN where the length is bad
-    for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+    // ---- this block's run of units, and this warp's ----
+    // (a whole number of blocks for each head where there are more: equally long segments then share no block)
+    uint32_t blocks = min(gridDim.x, (V + kAttnWarps * kAttnMinUnits - 1) / (kAttnWarps * kAttnMinUnits));
+    if (blocks > HH) blocks -= blocks % HH;
+    // sequences without keys: zeros, or NaN where the length is bad.  The last blocks begin: with few units they have none.
+    for (int b = gridDim.x - 1 - blockIdx.x; b < a.batch; b += gridDim.x) {
         if (prefix[b + 1] != prefix[b]) continue;
-        const bool bad = keys_of(a, b).bad;
+        const bool bad = length[b] < 0;
         const float fill = bad ? __uint_as_float(0x7FC00000u) : 0.f, f4[4] = {fill, fill, fill, fill};
         for (int i = threadIdx.x; i < a.q_heads * (D / 4); i += kAttnThreads)
             store_out4(a, b, i / (D / 4), i % (D / 4) * 4, f4);
@@ -296,60 +358,104 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attention_kernel(const 
                 a.lse[(int64_t)b * a.q_heads + h] = bad ? fill : -INFINITY;
         if (bad && threadIdx.x == 0 && a.status) atomicOr(a.status, WICI_BAD_LENGTH);
     }
-
-    // ---- this block's run of units ----
-    const int64_t blocks = min((int64_t)gridDim.x, (U + 15) / 16);    // at least 16 units a block
     if (blockIdx.x >= blocks) return;
-    const int64_t u0 = blockIdx.x * U / blocks, u1 = (blockIdx.x + 1) * U / blocks;
-    const int count = (int)(u1 - u0);
-    const int mine = count > warp ? (count - warp + kAttnWarps - 1) / kAttnWarps : 0;   // units of this warp
 
-    auto sequence_of = [&](int q) {       // the last b with prefix[b] <= q: it has pages
-        int lo = 0, hi = a.batch;         // prefix[lo] <= q < prefix[hi]
+    auto last_at = [&](const int *sums, int q) {   // the last b with sums[b] <= q: it has units
+        int lo = 0, hi = a.batch;                  // sums[lo] <= q < sums[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (prefix[mid] <= q) lo = mid; else hi = mid;
+            if (sums[mid] <= q) lo = mid; else hi = mid;
         }
         return lo;
     };
+    auto segment_at = [&](uint32_t u) {            // the one that unit u is of
+        Rec s;
+        s.b = last_at(prefix, u / HH);
+        const uint32_t n_b = prefix[s.b + 1] - prefix[s.b], r = u - prefix[s.b] * HH;
+        s.head = r / n_b;
+        s.start = u - (r - s.head * n_b);
+        s.end = s.start + n_b;
+        return s;
+    };
+    // runs are cut where the weight is: run j of n starts at weight floor(j V / n)
+    const uint32_t runs = kAttnWarps * blocks, whole_w = V / runs, rest_w = V - whole_w * runs;
+    auto run_start = [&](uint32_t j) {
+        const uint32_t x = j * whole_w + j * rest_w / runs;         // j, rest_w < 2^14
+        if (x >= V) return prefix[a.batch] * HH;
+        const int b = last_at(weight, x / HH);
+        const uint32_t r = x - weight[b] * HH, n_b = prefix[b + 1] - prefix[b];
+        const uint32_t head = r / (n_b + kAttnSegment), y = r - head * (n_b + kAttnSegment);
+        return prefix[b] * HH + head * n_b + (y > kAttnSegment ? y - kAttnSegment : 0u);
+    };
+    // the block whose run holds unit s.start + z of a segment: of the last run that starts at its weight or before
+    auto block_of = [&](const Rec &s, uint32_t z) {
+        const uint64_t w = weight[s.b] * HH + s.head * (s.end - s.start + kAttnSegment) + kAttnSegment + z;
+        return (int)(((w + 1) * runs - 1) / V / kAttnWarps);
+    };
+    const uint32_t bound = run_start(blockIdx.x * kAttnWarps + (lane <= kAttnWarps ? lane : 0));
+    auto run_at = [&](int w) { return __shfl_sync(0xffffffffu, bound, w); };   // by whole warps
+    const uint32_t u0 = run_at(0), u1 = run_at(kAttnWarps), r0 = run_at(warp), r1 = run_at(warp + 1);
+    const int mine = (int)(r1 - r0);
 
     // ---- issue side: lane l knows unit 32 k + l of this warp's ----
     struct Desc {
-        int page;      // -1: bad
+        int page[P];   // -1: bad; -2: past the sequence's end
         int info;      // kv head | first valid row << 16 | rows end << 24
     };
     auto describe = [&](int i) {
-        Desc d = {-1, 0};
+        Desc d;
+#pragma unroll
+        for (int p = 0; p < P; ++p) d.page[p] = -2;
+        d.info = 0;
         if (i >= mine) return d;
-        const int64_t u = u0 + warp + (int64_t)kAttnWarps * i;
-        const int b = sequence_of((int)(u / HH));
-        const int n_b = prefix[b + 1] - prefix[b];
-        const int64_t r = u - (int64_t)prefix[b] * HH;
-        const int head = (int)(r / n_b), p = (int)(r - (int64_t)head * n_b);
-        const Keys k = keys_of(a, b);
-        const int at = k.first_page() + p;
-        d.page = a.pages[(int64_t)b * a.max_pages + at];
-        if (d.page < 0 || d.page >= a.cache.n_pages) d.page = -1;
-        const int first = max(0, k.lo - at * kKvPage), end = min(kKvPage, k.n - at * kKvPage);
+        const Rec s = segment_at(r0 + i);
+        const int b = s.b, head = s.head, at = (int)(r0 + i - s.start) * P;
+        const Keys k = keys_of(length[b], a.window);
+        const int first_page = k.lo / kKvPage + at;
+        const int32_t *row = a.pages + (int64_t)b * a.max_pages;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if ((first_page + p) * (int64_t)kKvPage < k.n) {
+                d.page[p] = row[first_page + p];
+                if (d.page[p] < 0 || d.page[p] >= a.cache.n_pages) d.page[p] = -1;
+            }
+        }
+        const int first = max(0, k.lo - first_page * kKvPage), end = min(UNIT, k.n - first_page * kKvPage);
         d.info = head / a.tiles | first << 16 | end << 24;
         return d;
     };
     Desc cur = describe(lane), next = describe(32 + lane);
     int issued = 0;                       // K's of units issued; V's follow one behind
     uint32_t bad_units = 0;               // bit i % 32: unit i has a bad page
-    int last_page = -1, last_info = 0;
+    int last_page[P], last_info = 0;
+    bool last = false;
 
-    auto copy_block = [&](uint32_t dst, int page, int info, bool v) {
-        const int first = info >> 16 & 255, end = info >> 24;
-        const uint8_t *src = a.cache.data + page * a.cache.page_stride +
-                             (int64_t)((info & 0xFFFF) + (v ? a.cache.kv_heads : 0)) * S::kBlock;
+    // one page's block of K or V: rows without a key of the sequence are zeroed, what the cache holds there is anything
+    const uint32_t lane_dst = chunk_at<ROW>(lane / CHUNKS, lane % CHUNKS);
+    auto copy_block = [&](uint32_t dst, int page, int64_t block, int first, int end) {
+        constexpr int N = kKvPage * CHUNKS / 32, ROWS = 32 / CHUNKS;   // rows of one round of the warp
+        const uint8_t *src = a.cache.data + (page < 0 ? 0 : page * a.cache.page_stride + block);
+        if (first <= 0 && end >= kKvPage) {
 #pragma unroll
-        for (int i = 0; i < kKvPage * CHUNKS / 32; ++i) {
-            const int c = i * 32 + lane, r = c / CHUNKS, x = c % CHUNKS;
-            // rows without a key of the sequence are zeroed: what the cache holds there is anything
-            cp_async16(dst + chunk_at<ROW>(r, x), src + c * 16, r >= first && r < end ? 16 : 0);
+            for (int i = 0; i < N; ++i)
+                cp_async16(dst + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src + i * 512 + lane * 16, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int r = i * ROWS + lane / CHUNKS;
+                cp_async16(dst + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src + i * 512 + lane * 16,
+                           r >= first && r < end ? 16 : 0);
+            }
         }
-        if (!BF16 && lane < 4) cp_async16(dst + kKvPage * D + lane * 16, src + kKvPage * D + lane * 16, 16);
+        if (!BF16 && lane < 4)
+            cp_async16(dst + kKvPage * D + lane * 16, src + kKvPage * D + lane * 16, page < 0 ? 0 : 16);
+    };
+    auto copy_unit = [&](uint32_t dst, const int *page, int info, int side) {
+        const int first = info >> 16 & 255, end = info >> 24;
+        const int64_t block = (int64_t)((info & 0xFFFF) + side * a.cache.kv_heads) * S::kBlock;
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            copy_block(dst + p * S::kBlock, page[p], block, first - p * kKvPage, page[p] < 0 ? 0 : end - p * kKvPage);
     };
     // group j: K of unit j and V of the one before it (none past the last unit: the groups still count)
     auto issue = [&]() {
@@ -357,96 +463,111 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attention_kernel(const 
             cur = next;
             next = describe(issued + 32 + lane);
         }
-        const int page = __shfl_sync(0xffffffffu, cur.page, issued & 31);
+        int page[P];
+        bool bad = false;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            page[p] = __shfl_sync(0xffffffffu, cur.page[p], issued & 31);
+            bad |= page[p] == -1;
+        }
         const int info = __shfl_sync(0xffffffffu, cur.info, issued & 31);
         if (issued < mine) {
-            if (page < 0) {
+            copy_unit(ring + issued % KS * S::kSlot, page, info, 0);
+            if (bad) {
                 bad_units |= 1u << (issued & 31);
                 if (lane == 0 && a.status) atomicOr(a.status, WICI_BAD_PAGE);
-            } else {
-                copy_block(ring + issued % KS * S::kBlock, page, info, false);
             }
         }
-        if (last_page >= 0)
-            copy_block(ring + KS * S::kBlock + (issued - 1) % VS * S::kBlock, last_page, last_info, true);
-        last_page = issued < mine ? page : -1;
+        if (last) copy_unit(ring + KS * S::kSlot + (issued - 1) % VS * S::kSlot, last_page, last_info, 1);
+        last = issued < mine;
+#pragma unroll
+        for (int p = 0; p < P; ++p) last_page[p] = page[p];
         last_info = info;
         ++issued;
         cp_commit();
     };
+
+    // ---- segments of this warp's run ----
+    Rec seg = {r0, r0, 0, 0};
+    if (mine > 0) seg = segment_at(r0);
+    constexpr int QW = EXACT ? 2 : 1;     // 16-byte words of 8 elements of q: fp32 comes with EXACT alone
+    uint4 qx[R][STEPS / 2][QW];           // the segment's queries
+    auto load_queries = [&]() {
+        const int row0 = seg.head % a.tiles * HT, head0 = seg.head / a.tiles * a.group + row0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < STEPS / 2; ++i) {
+                // a step takes 4 adjacent elements of a lane's chunk: bf16 of chunk 4 i + t, 8-bit of half i % 2 of 4 (i / 2) + t
+                const int e0 = BF16 ? 8 * (4 * i + t) : 16 * (4 * (i / 2) + t) + 8 * (i % 2);
+#pragma unroll
+                for (int w = 0; w < QW; ++w) qx[r][i][w] = make_uint4(0, 0, 0, 0);
+                if (g + 8 * r < a.group - row0) load_q8<QW>(a, seg.b, head0 + g + 8 * r, e0, qx[r][i]);
+            }
+    };
+    if (mine > 0) load_queries();         // before the ring's copies, which queue up in front of what comes after
+#pragma unroll 1
     for (int i = 0; i < KS; ++i) issue();
-
-    // ---- segments ----
-    int seg_b = sequence_of((int)(u0 / HH));
-    int seg_head;
-    int64_t seg_start;                    // first unit
-    {
-        const int n_b = prefix[seg_b + 1] - prefix[seg_b];
-        const int64_t r = u0 - (int64_t)prefix[seg_b] * HH;
-        seg_head = (int)(r / n_b);
-        seg_start = u0 - (r - (int64_t)seg_head * n_b);
+    // while they are on their way: who shares the segments at the block's ends
+    if (lane == 0) sh.leaving[warp].end = 0;
+    if (warp < 2) {
+        Rec s = {0, 0, 0, 0};
+        if (u0 < u1) s = segment_at(warp ? u1 - 1 : u0);   // a block may have got the weight of a segment and none of its units
+        if (warp ? s.end <= u1 || s.start < u0 : s.start >= u0) s.end = 0;
+        else if (lane == 0) sh.first[warp] = block_of(s, 0), sh.last[warp] = block_of(s, s.end - s.start - 1);
+        if (lane == 0) sh.side[warp] = s;
     }
-    int done = 0;                         // units of this warp computed
-    for (int64_t u = u0; u < u1;) {
-        const int n_b = prefix[seg_b + 1] - prefix[seg_b];
-        const int64_t seg_end = seg_start + n_b, stop = min(seg_end, u1);
-        const Keys keys = keys_of(a, seg_b);
-        const int kvh = seg_head / a.tiles, row0 = seg_head % a.tiles * HT;   // first query of the tile in the group
-        const int rows = min(HT, a.group - row0);
-        const int head0 = kvh * a.group + row0;
 
-        // ---- Q fragments: step s of a chunk takes 4 of its elements ----
+    // a part of a segment: rows of O (kPartRow floats each), then m and l of each row
+    auto part_of = [&](int w, bool last_of_run) {
+        return (float *)(last_of_run ? smem + w * S::kRing : parts + (w - 1) * S::kPart);
+    };
+    int done = 0;                         // units of this warp computed
+    while (done < mine) {
+        const int stop = (int)(min(seg.end, r1) - r0);
+        const Keys keys = keys_of(length[seg.b], a.window);
+        const int row0 = seg.head % a.tiles * HT, rows = min(HT, a.group - row0);   // first query of the tile in the group
+        const int head0 = seg.head / a.tiles * a.group + row0, seg_b = seg.b;
+
+        // ---- Q fragments ----
         uint32_t qf[QPASS][STEPS][4];
-        float cq[R];                      // scores to base-2 logits
-        const bool any = done < mine && u0 + warp + (int64_t)kAttnWarps * done < stop;
+        float cq[R];                      // products to base-2 logits
 #pragma unroll
-        for (int r = 0; r < R; ++r) cq[r] = a.scale * 1.44269504088896340736f;
-        if (any) {
+        for (int r = 0; r < R; ++r) {
+            cq[r] = a.scale * 1.44269504088896340736f;
+            float x[STEPS][4];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int row = g + 8 * r;
-                float x[STEPS][4];
+            for (int i = 0; i < STEPS / 2; ++i) unpack_q8<QW>(a.q_dtype, qx[r][i], x[2 * i]);
+            if (!BF16) {
                 uint32_t top = 0;
 #pragma unroll
-                for (int i = 0; i < STEPS / 2; ++i) {
-                    float v[8];
-                    // bf16: chunk 4 i + t; 8-bit: half i % 2 of chunk 4 (i / 2) + t
-                    const int e0 = BF16 ? 8 * (4 * i + t) : 16 * (4 * (i / 2) + t) + 8 * (i % 2);
+                for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = 0.f;
-                    if (row < rows) load_q8(a, seg_b, head0 + row, e0, v);
+                    for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(x[s][j]) & 0x7FFFFFFFu);
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                // 2^(13 - exponent): the largest magnitude to [2^13, 2^14)
+                int e = (int)(top >> 23) - 127 - 13;
+                e = top >= kInfBits || top == 0 ? 0 : max(-126, min(126, e));
+                const float down = __int_as_float((127 - e) << 23);
+                cq[r] *= __int_as_float((127 + e) << 23);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        x[2 * i + j / 4][j % 4] = v[j];
-                        top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-                    }
-                }
-                if (!BF16) {
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    // 2^(13 - exponent): the largest magnitude to [2^13, 2^14)
-                    int e = (int)(top >> 23) - 127 - 13;
-                    e = top >= kInfBits || top == 0 ? 0 : max(-126, min(126, e));
-                    const float down = __int_as_float((127 - e) << 23);
-                    cq[r] *= __int_as_float((127 + e) << 23);
+                for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                    for (int s = 0; s < STEPS; ++s)
+                    for (int j = 0; j < 4; ++j) x[s][j] *= down;
+            }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) x[s][j] *= down;
-                }
+            for (int s = 0; s < STEPS; ++s) {
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s) {
-#pragma unroll
-                    for (int k = 0; k < QPASS; ++k) {
-                        if (STACK) {
-                            qf[k][s][0] = split2<BF16>(x[s][0], x[s][1]);
-                            qf[k][s][2] = split2<BF16>(x[s][2], x[s][3]);
-                            qf[k][s][1] = 2 * k + 1 < TQ ? split2<BF16>(x[s][0], x[s][1]) : 0u;
-                            qf[k][s][3] = 2 * k + 1 < TQ ? split2<BF16>(x[s][2], x[s][3]) : 0u;
-                        } else {
-                            qf[k][s][r] = split2<BF16>(x[s][0], x[s][1]);
-                            qf[k][s][2 + r] = split2<BF16>(x[s][2], x[s][3]);
-                        }
+                for (int k = 0; k < QPASS; ++k) {
+                    if (STACK) {
+                        qf[k][s][0] = split2<BF16>(x[s][0], x[s][1]);
+                        qf[k][s][2] = split2<BF16>(x[s][2], x[s][3]);
+                        qf[k][s][1] = 2 * k + 1 < TQ ? split2<BF16>(x[s][0], x[s][1]) : 0u;
+                        qf[k][s][3] = 2 * k + 1 < TQ ? split2<BF16>(x[s][2], x[s][3]) : 0u;
+                    } else {
+                        qf[k][s][r] = split2<BF16>(x[s][0], x[s][1]);
+                        qf[k][s][2 + r] = split2<BF16>(x[s][2], x[s][3]);
                     }
                 }
             }
@@ -462,33 +583,31 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attention_kernel(const 
         float vref = 0x1p-125f, vinv = 0x1p125f;      // 8-bit: a power of two, at least a quarter of the largest V scale
 
         // ---- units of this segment ----
-        for (; done < mine; ++done) {
-            const int64_t unit = u0 + warp + (int64_t)kAttnWarps * done;
-            if (unit >= stop) break;
+        int key0 = (keys.lo / kKvPage + (int)(r0 + done - seg.start) * P) * kKvPage;   // first key of the unit
+        for (; done < stop; ++done, key0 += UNIT) {
             // group `done` brings K; the KS - 1 after it may be on their way
             cp_wait<KS - 1>();
             __syncwarp();
-            const int base_key = (keys.first_page() + (int)(unit - seg_start)) * kKvPage;
-            const uint32_t ks = ring + done % KS * S::kBlock, vs = ring + KS * S::kBlock + done % VS * S::kBlock;
+            const uint32_t ks = ring + done % KS * S::kSlot, vs = ring + KS * S::kSlot + done % VS * S::kSlot;
 
-            float c[2][2][4];                                // [8 keys][even, odd steps]
+            float c[2 * P][SETS][4];                         // [8 keys][sets of steps]
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < 2 * P; ++n)
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < SETS; ++e)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) c[n][e][j] = 0.f;
 #pragma unroll
             for (int i = 0; i < CHUNKS / 4; ++i) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const int r = (g >> 1) + (g & 1) * 4 + 8 * n;   // the key of column g
-                    const uint4 w = lds128(ks + chunk_at<ROW>(r, 4 * i + t));
+                for (int n = 0; n < 2 * P; ++n) {
+                    const int r = (g >> 1) + (g & 1) * 4 + 8 * (n & 1);   // the key of column g
+                    const uint4 w = lds128(ks + n / 2 * S::kBlock + chunk_at<ROW>(r, 4 * i + t));
                     if (BF16) {
 #pragma unroll
                         for (int k = 0; k < QPASS; ++k) {
                             mma16816<true>(c[n][0], qf[k][2 * i], w.x, w.y);
-                            mma16816<true>(c[n][1], qf[k][2 * i + 1], w.z, w.w);
+                            mma16816<true>(c[n][SETS - 1], qf[k][2 * i + 1], w.z, w.w);
                         }
                     } else {
                         const uint32_t word[4] = {w.x, w.y, w.z, w.w};
@@ -497,32 +616,45 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attention_kernel(const 
                             uint32_t b0, b1;
                             decode4<FMT>(word[s], b0, b1);
 #pragma unroll
-                            for (int k = 0; k < QPASS; ++k) mma16816<false>(c[n][s & 1], qf[k][4 * i + s], b0, b1);
+                            for (int k = 0; k < QPASS; ++k) mma16816<false>(c[n][0], qf[k][4 * i + s], b0, b1);
                         }
                     }
                 }
             }
-            // x[r][j]: query g + 8 r, key t + 4 j
-            float x[R][4], vscale[4];
-            float vtop = 0.f;
+            // x[r][j]: query g + 8 r, key t + 4 j of the unit
+            constexpr int J = 4 * P;
+            float x[R][J];
+            const bool part = key0 < keys.lo || key0 > keys.n - UNIT;   // not every key of the unit is the sequence's
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = j >> 1, col = j & 1, key = t + 4 * j;
-                const bool valid = base_key + key >= keys.lo && base_key + key < keys.n;
-                float ksc = 1.f;
-                if (!BF16) ksc = lds32(ks + kKvPage * D + key * 4);
+            for (int j = 0; j < J; ++j) {
+                const int n = j >> 1, col = j & 1;
+                const float ksc = BF16 ? 1.f : lds32(ks + j / 4 * S::kBlock + kKvPage * D + (t + 4 * (j & 3)) * 4);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const float a0 = c[n][0][col + 2 * r] + c[n][1][col + 2 * r];
-                    const float dot = STACK ? a0 + (c[n][0][col + 2] + c[n][1][col + 2]) : a0;
-                    x[r][j] = valid ? dot * ksc * cq[r] : -INFINITY;
+                    float dot = c[n][0][col + 2 * r];
+                    if (SETS == 2) dot += c[n][SETS - 1][col + 2 * r];
+                    if (STACK && TQ > 1) {
+                        dot += c[n][0][col + 2];
+                        if (SETS == 2) dot += c[n][SETS - 1][col + 2];
+                    }
+                    x[r][j] = dot * (BF16 ? cq[r] : ksc * cq[r]);
+                }
+            }
+            if (part) {
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int key = key0 + t + 4 * j;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) x[r][j] = key >= keys.lo && key < keys.n ? x[r][j] : -INFINITY;
                 }
             }
             float up[R];
             bool grew = false;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float top = fmaxf(fmaxf(x[r][0], x[r][1]), fmaxf(x[r][2], x[r][3]));
+                float top = x[r][0];
+#pragma unroll
+                for (int j = 1; j < J; ++j) top = fmaxf(top, x[r][j]);
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 up[r] = fmaxf(m[r], top);
@@ -531,22 +663,26 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attention_kernel(const 
             // V of this unit is in the next group
             cp_wait<KS - 2>();
             __syncwarp();
-            float ratio = 1.f;
+            float ratio = 1.f, vscale[J];
             if (!BF16) {
+                float vtop = 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = t + 4 * j;
-                    const bool valid = base_key + key >= keys.lo && base_key + key < keys.n;
-                    vscale[j] = valid ? lds32(vs + kKvPage * D + key * 4) : 0.f;
-                    vtop = fmaxf(vtop, vscale[j]);
+                for (int j = 0; j < J; ++j) vscale[j] = lds32(vs + j / 4 * S::kBlock + kKvPage * D + (t + 4 * (j & 3)) * 4);
+                if (part) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const int key = key0 + t + 4 * j;
+                        if (key < keys.lo || key >= keys.n) vscale[j] = 0.f;
+                    }
                 }
+#pragma unroll
+                for (int j = 0; j < J; ++j) vtop = fmaxf(vtop, vscale[j]);
                 vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, 1));
                 vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, 2));
                 if (vtop > vref) {                           // the same in every lane
                     const uint32_t e = min((__float_as_uint(vtop) + 0x7FFFFFu) & 0x7F800000u, 0x7E800000u);
-                    const float ref = __uint_as_float(e);
                     ratio = vref * __uint_as_float(0x7F000000u - e);
-                    vref = ref;
+                    vref = __uint_as_float(e);
                     vinv = __uint_as_float(0x7F000000u - e);
                     grew = true;
                 }
@@ -568,75 +704,81 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attention_kernel(const 
                     o[n][3] *= f[R - 1];
                 }
             }
-            uint32_t pf[PPASS][4];
+            uint32_t pf[P][PPASS][4];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const float ref = m[r] == -INFINITY ? 0.f : m[r];
-                float p[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    p[j] = ex2(x[r][j] - ref);
-                    l[r] += p[j];
-                    if (!BF16) p[j] *= vscale[j] * vinv * kPUnit;
-                }
+                for (int pg = 0; pg < P; ++pg) {
+                    float p[4];
 #pragma unroll
-                for (int k = 0; k < PPASS; ++k) {
-                    if (STACK) {
-                        pf[k][0] = split2<BF16>(p[0], p[1]);
-                        pf[k][2] = split2<BF16>(p[2], p[3]);
-                        pf[k][1] = 2 * k + 1 < TP ? split2<BF16>(p[0], p[1]) : 0u;
-                        pf[k][3] = 2 * k + 1 < TP ? split2<BF16>(p[2], p[3]) : 0u;
-                    } else {
-                        pf[k][r] = split2<BF16>(p[0], p[1]);
-                        pf[k][2 + r] = split2<BF16>(p[2], p[3]);
+                    for (int j = 0; j < 4; ++j) {
+                        p[j] = ex2(x[r][4 * pg + j] - ref);
+                        l[r] += p[j];
+                        if (!BF16) p[j] *= vscale[4 * pg + j] * (vinv * kPUnit);
+                    }
+#pragma unroll
+                    for (int k = 0; k < PPASS; ++k) {
+                        if (STACK) {
+                            pf[pg][k][0] = split2<BF16>(p[0], p[1]);
+                            pf[pg][k][2] = split2<BF16>(p[2], p[3]);
+                            pf[pg][k][1] = 2 * k + 1 < TP ? split2<BF16>(p[0], p[1]) : 0u;
+                            pf[pg][k][3] = 2 * k + 1 < TP ? split2<BF16>(p[2], p[3]) : 0u;
+                        } else {
+                            pf[pg][k][r] = split2<BF16>(p[0], p[1]);
+                            pf[pg][k][2 + r] = split2<BF16>(p[2], p[3]);
+                        }
                     }
                 }
             }
-            // V: rows t + 4 i; column g of tile n is element PER * (g + 8 jj) + e of the head (n = PER jj + e),
-            // or 8 g + n where a lane takes half a chunk (8-bit, d 64)
-            if (BF16) {
+            // V: rows t + 4 i of a page; column g of tile n is element PER (g + 8 (n / PER)) + n % PER of the head
 #pragma unroll
-                for (int jj = 0; jj < CHUNKS / 8; ++jj) {
-                    uint32_t w[4][4];
+            for (int pg = 0; pg < P; ++pg) {
+                const uint32_t vp = vs + pg * S::kBlock;
+                if (BF16) {
+#pragma unroll
+                    for (int jj = 0; jj < CHUNKS / 8; ++jj) {
+                        uint32_t w[4][4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint4 q = lds128(vp + chunk_at<ROW>(t + 4 * i, g + 8 * jj));
+                            w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const uint32_t sel = e & 1 ? 0x7632 : 0x5410;
+                            const uint32_t b0 = __byte_perm(w[0][e / 2], w[1][e / 2], sel);
+                            const uint32_t b1 = __byte_perm(w[2][e / 2], w[3][e / 2], sel);
+#pragma unroll
+                            for (int k = 0; k < PPASS; ++k) mma16816<true>(o[8 * jj + e], pf[pg][k], b0, b1);
+                        }
+                    }
+                } else {
+                    constexpr int WORDS = D / 32;          // 4-byte words of a row that a lane takes
+                    uint32_t w[4][WORDS];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint4 q = lds128(vs + chunk_at<ROW>(t + 4 * i, g + 8 * jj));
-                        w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
+                        if (D == 128) {
+                            const uint4 q = lds128(vp + chunk_at<ROW>(t + 4 * i, g));
+                            w[i][0] = q.x, w[i][1] = q.y, w[i][WORDS - 2] = q.z, w[i][WORDS - 1] = q.w;
+                        } else {
+                            const uint2 q = lds64(vp + chunk_at<ROW>(t + 4 * i, g >> 1) + (g & 1) * 8);
+                            w[i][0] = q.x, w[i][1] = q.y;
+                        }
                     }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint32_t sel = e & 1 ? 0x7632 : 0x5410;
-                        const uint32_t b0 = __byte_perm(w[0][e / 2], w[1][e / 2], sel);
-                        const uint32_t b1 = __byte_perm(w[2][e / 2], w[3][e / 2], sel);
+                    for (int x4 = 0; x4 < WORDS; ++x4) {
+                        // the bytes of two rows interleaved first: a pair of them is a fragment's half
+                        uint32_t h[2][4];
 #pragma unroll
-                        for (int k = 0; k < PPASS; ++k) mma16816<true>(o[8 * jj + e], pf[k], b0, b1);
-                    }
-                }
-            } else {
-                constexpr int WORDS = D / 32;              // 4-byte words of a row that a lane takes
-                uint32_t w[4][WORDS];
+                        for (int i = 0; i < 2; ++i) {
+                            decode4<FMT>(__byte_perm(w[2 * i][x4], w[2 * i + 1][x4], 0x5140), h[i][0], h[i][1]);
+                            decode4<FMT>(__byte_perm(w[2 * i][x4], w[2 * i + 1][x4], 0x7362), h[i][2], h[i][3]);
+                        }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (D == 128) {
-                        const uint4 q = lds128(vs + chunk_at<ROW>(t + 4 * i, g));
-                        w[i][0] = q.x, w[i][1] = q.y, w[i][WORDS - 2] = q.z, w[i][WORDS - 1] = q.w;
-                    } else {
-                        const uint2 q = lds64(vs + chunk_at<ROW>(t + 4 * i, g >> 1) + (g & 1) * 8);
-                        w[i][0] = q.x, w[i][1] = q.y;
-                    }
-                }
+                        for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int x4 = 0; x4 < WORDS; ++x4) {
-                    uint32_t h[4][2];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) decode4<FMT>(w[i][x4], h[i][0], h[i][1]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t sel = e & 1 ? 0x7632 : 0x5410;
-                        const uint32_t b0 = __byte_perm(h[0][e / 2], h[1][e / 2], sel);
-                        const uint32_t b1 = __byte_perm(h[2][e / 2], h[3][e / 2], sel);
-#pragma unroll
-                        for (int k = 0; k < PPASS; ++k) mma16816<false>(o[4 * x4 + e], pf[k], b0, b1);
+                            for (int k = 0; k < PPASS; ++k) mma16816<false>(o[4 * x4 + e], pf[pg][k], h[0][e], h[1][e]);
                     }
                 }
             }
@@ -649,135 +791,159 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attention_kernel(const 
             issue();
         }
 
-        // ---- join the block's warps, 8 rows at a time ----
+        // ---- the segment's state, or this run's part of it ----
+        const bool entered = seg.start < r0, left = seg.end > r1;
+        if (left) {
+            cp_wait<0>();                                   // the ring is free: no unit follows
+            if (lane == 0) sh.leaving[warp] = seg;
+        }
+        __syncwarp();
+        const float unit_of_o = BF16 ? 1.f : vref / kPUnit;
+        // what ends in the block's first run is the block's whole part of its segment
+        const bool to_piece = !left && r0 == u0;
+        float *part_at = to_piece ? a.pieces + (int64_t)blockIdx.x * 2 * attn_piece_floats(D) : part_of(warp, left);
+        const int part_row = to_piece ? D : S::kPartRow;
+        float2 *part_ml = (float2 *)(part_at + (to_piece ? kAttnPieceRows * D : HT * S::kPartRow));
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
             l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-        }
-        const bool whole = seg_start >= u0 && seg_end <= u1;
-        float *piece = a.pieces + ((int64_t)blockIdx.x * 2 + (seg_start >= u0 ? 1 : 0)) * attn_piece_floats(D);
-        const float unit_of_o = BF16 ? 1.f : vref / kPUnit;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            __syncthreads();                                // the buffer's last readers are done
-            float *mine_o = join + (warp * 8 + g) * S::kJoinRow;
+            const int row = g + 8 * r;
+            const bool alone = !entered && !left;
+            const float f = alone ? unit_of_o / l[r] : unit_of_o;
+            if (row >= rows) continue;
 #pragma unroll
             for (int n = 0; n < NT; n += 4) {
                 // columns 2 t and 2 t + 1 of tiles n .. n + 3: four adjacent elements each
-                constexpr int per = BF16 || D == 64 ? 8 : 16;
                 float v[2][4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        v[c][i] = (STACK ? o[n + i][c] + o[n + i][c + 2] : o[n + i][2 * r + c]) * unit_of_o;
-                float *dst = mine_o + per * (2 * t + 8 * (n / per)) + n % per;
-                *(float4 *)dst = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
-                *(float4 *)(dst + per) = make_float4(v[1][0], v[1][1], v[1][2], v[1][3]);
+                    for (int c = 0; c < 2; ++c) v[c][i] = (STACK ? o[n + i][c] + o[n + i][c + 2] : o[n + i][2 * r + c]) * f;
+                const int d0 = PER * (2 * t + 8 * (n / PER)) + n % PER;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (alone) store_out4(a, seg_b, head0 + row, d0 + PER * c, v[c]);
+                    else *(float4 *)(part_at + row * part_row + d0 + PER * c) = make_float4(v[c][0], v[c][1], v[c][2], v[c][3]);
+                }
             }
-            if (t == 0) state[warp * 8 + g] = make_float2(m[r], l[r]);
-            __syncthreads();
-            for (int i = threadIdx.x; i < 8 * (D / 4); i += kAttnThreads) {
-                const int row = i / (D / 4), d0 = i % (D / 4) * 4;
-                if (row + 8 * r >= rows) continue;
-                float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int w = 0; w < kAttnWarps; ++w) top = fmaxf(top, state[w * 8 + row].x);
-#pragma unroll
-                for (int w = 0; w < kAttnWarps; ++w) {
-                    const float2 s = state[w * 8 + row];
-                    const float f = s.x == -INFINITY ? 0.f : ex2(s.x - top);
-                    sum += s.y * f;
-                    const float4 q = *(const float4 *)(join + (w * 8 + row) * S::kJoinRow + d0);
-                    v[0] += q.x * f, v[1] += q.y * f, v[2] += q.z * f, v[3] += q.w * f;
-                }
-                if (whole) {
-                    const float inv = 1.f / sum;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] *= inv;
-                    store_out4(a, seg_b, head0 + row + 8 * r, d0, v);
-                    if (d0 == 0 && a.lse)
-                        a.lse[(int64_t)seg_b * a.q_heads + head0 + row + 8 * r] =
-                            (top + log2f(sum)) * 0.693147180559945309417f;
-                } else {
-                    float *dst = piece + (row + 8 * r) * D + d0;
-                    *(float4 *)dst = make_float4(v[0], v[1], v[2], v[3]);
-                    if (d0 == 0) {
-                        float2 *ml = (float2 *)(piece + kAttnPieceRows * D) + row + 8 * r;
-                        *ml = make_float2(top, sum);
-                    }
-                }
+            if (t == 0) {
+                if (!alone) part_ml[row] = make_float2(m[r], l[r]);
+                else if (a.lse) a.lse[(int64_t)seg_b * a.q_heads + head0 + row] = (m[r] + log2f(l[r])) * 0.693147180559945309417f;
             }
         }
-        if (!whole) {
-            // blocks i0 .. i1 hold the segment; the one that arrives last joins their pieces in order
-            const int i0 = (int)(((seg_start + 1) * blocks - 1) / U), i1 = (int)((seg_end * blocks - 1) / U);
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                const int n = atomicAdd(a.tickets + i0, 1);
-                sflag[0] = n == i1 - i0;
-                if (n == i1 - i0) a.tickets[i0] = 0;
+        if (seg.end < r1) {
+            seg.start = seg.end;
+            if (++seg.head == (int)HH) {
+                seg.head = 0;
+                do ++seg.b; while (prefix[seg.b + 1] == prefix[seg.b]);
             }
-            __syncthreads();
-            if (sflag[0]) {
-                __threadfence();
-                for (int i = threadIdx.x; i < rows * (D / 4); i += kAttnThreads) {
-                    const int row = i / (D / 4), d0 = i % (D / 4) * 4;
-                    float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-                    for (int p = i0; p <= i1; ++p) {
-                        const float *src = a.pieces + ((int64_t)p * 2 + (p == i0)) * attn_piece_floats(D);
-                        const float2 s = __ldcg((const float2 *)(src + kAttnPieceRows * D) + row);
-                        const float4 q = __ldcg((const float4 *)(src + row * D + d0));
-                        const float up = fmaxf(top, s.x), ref = up == -INFINITY ? 0.f : up;
-                        const float fo = ex2(top - ref), fn = ex2(s.x - ref);
-                        sum = sum * fo + s.y * fn;
-                        v[0] = v[0] * fo + q.x * fn, v[1] = v[1] * fo + q.y * fn;
-                        v[2] = v[2] * fo + q.z * fn, v[3] = v[3] * fo + q.w * fn;
-                        top = up;
-                    }
-                    const float inv = 1.f / sum;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] *= inv;
-                    store_out4(a, seg_b, head0 + row, d0, v);
-                    if (d0 == 0 && a.lse)
-                        a.lse[(int64_t)seg_b * a.q_heads + head0 + row] = (top + log2f(sum)) * 0.693147180559945309417f;
-                }
-            }
-            __syncthreads();                                // sflag is free again
-        }
-
-        // ---- the next segment ----
-        u = stop;
-        if (u < u1) {
-            seg_start = seg_end;
-            if (++seg_head == HH) {
-                seg_head = 0;
-                do ++seg_b; while (prefix[seg_b + 1] == prefix[seg_b]);
-            }
+            seg.end = seg.start + prefix[seg.b + 1] - prefix[seg.b];
+            load_queries();
         }
     }
     cp_wait<0>();
+    __syncthreads();
+
+    // ---- segments that several runs share ----
+    auto rows_of = [&](const Rec &s) { return min(HT, a.group - s.head % a.tiles * HT); };
+    auto finish = [&](const Rec &s, int row, int d0, const float *v, float top, float sum) {
+        const int head = s.head / a.tiles * a.group + s.head % a.tiles * HT + row;
+        const float inv = 1.f / sum, q[4] = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+        store_out4(a, s.b, head, d0, q);
+        if (d0 == 0 && a.lse) a.lse[(int64_t)s.b * a.q_heads + head] = (top + log2f(sum)) * 0.693147180559945309417f;
+    };
+    uint32_t run[kAttnWarps + 1];
+#pragma unroll
+    for (int w = 0; w <= kAttnWarps; ++w) run[w] = run_at(w);
+    uint32_t joined = ~0u;                // start of the segment joined last
+#pragma unroll
+    for (int w = 0; w < kAttnWarps; ++w) {
+        const Rec s = sh.leaving[w];
+        if (s.end == 0 || s.start == joined) continue;
+        joined = s.start;
+        // its parts: of warp w, then of the runs after it up to the one where it ends
+        const bool whole = s.start >= u0 && s.end <= u1;
+        float *piece = a.pieces + ((int64_t)blockIdx.x * 2 + (s.start >= u0 ? 1 : 0)) * attn_piece_floats(D);
+        for (int i = threadIdx.x; i < rows_of(s) * (D / 4); i += kAttnThreads) {
+            const int row = i / (D / 4), d0 = i % (D / 4) * 4;
+            float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = w; x < kAttnWarps; ++x)
+                if (run[x] < run[x + 1] && run[x] < s.end)
+                    top = fmaxf(top, ((const float2 *)(part_of(x, s.end > run[x + 1]) + HT * S::kPartRow))[row].x);
+#pragma unroll
+            for (int x = w; x < kAttnWarps; ++x) {
+                if (run[x] == run[x + 1] || run[x] >= s.end) continue;
+                const float *src = part_of(x, s.end > run[x + 1]);
+                const float2 ml = ((const float2 *)(src + HT * S::kPartRow))[row];
+                const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+                const float4 q = *(const float4 *)(src + row * S::kPartRow + d0);
+                sum += ml.y * f;
+                v[0] += q.x * f, v[1] += q.y * f, v[2] += q.z * f, v[3] += q.w * f;
+            }
+            if (whole) {
+                finish(s, row, d0, v, top, sum);
+            } else {
+                *(float4 *)(piece + row * D + d0) = make_float4(v[0], v[1], v[2], v[3]);
+                if (d0 == 0) ((float2 *)(piece + kAttnPieceRows * D))[row] = make_float2(top, sum);
+            }
+        }
+    }
+    // the one that this block's run starts in the middle of, and the one it ends in the middle of
+    for (int side = 0; side < 2; ++side) {
+        const Rec s = sh.side[side];
+        if (s.end == 0) continue;
+        // blocks i0 .. i1 hold it; the one that arrives last joins their pieces in order
+        const int i0 = sh.first[side], i1 = sh.last[side];
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const int n = atomicAdd(a.tickets + i0, 1);
+            sh.note[0] = n == i1 - i0;
+            if (n == i1 - i0) a.tickets[i0] = 0;
+        }
+        __syncthreads();
+        if (sh.note[0]) {
+            __threadfence();
+            auto piece_of = [&](int p) { return a.pieces + ((int64_t)p * 2 + (p == i0)) * attn_piece_floats(D); };
+            for (int i = threadIdx.x; i < rows_of(s) * (D / 4); i += kAttnThreads) {
+                const int row = i / (D / 4), d0 = i % (D / 4) * 4;
+                float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+                for (int p = i0; p <= i1; ++p) top = fmaxf(top, __ldcg((const float2 *)(piece_of(p) + kAttnPieceRows * D) + row).x);
+#pragma unroll 8
+                for (int p = i0; p <= i1; ++p) {
+                    const float2 ml = __ldcg((const float2 *)(piece_of(p) + kAttnPieceRows * D) + row);
+                    const float4 q = __ldcg((const float4 *)(piece_of(p) + row * D + d0));
+                    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+                    sum += ml.y * f;
+                    v[0] += q.x * f, v[1] += q.y * f, v[2] += q.z * f, v[3] += q.w * f;
+                }
+                finish(s, row, d0, v, top, sum);
+            }
+        }
+        __syncthreads();                                    // note is free again
+    }
 }
 
 // Launches, and kernel limits of the current device; one translation unit per format.
-cudaError_t launch_attention_bf16(int d, const AttnArg &a, bool stack, bool exact, int grid, cudaStream_t st);
-cudaError_t launch_attention_int8(int d, const AttnArg &a, bool stack, int grid, cudaStream_t st);
-cudaError_t launch_attention_e4m3(int d, const AttnArg &a, bool stack, int grid, cudaStream_t st);
+cudaError_t launch_attention_bf16(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st);
+cudaError_t launch_attention_int8(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st);
+cudaError_t launch_attention_e4m3(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st);
 cudaError_t setup_attention_bf16();
 cudaError_t setup_attention_int8();
 cudaError_t setup_attention_e4m3();
 
 template <int FMT, int D, bool STACK, bool EXACT>
-cudaError_t launch_attention(const AttnArg &a, int grid, cudaStream_t st) {
-    return launch_kernel(paged_attention_kernel<FMT, D, STACK, EXACT>, dim3(grid), kAttnThreads,
-                         AttnShape<FMT, D>::kSmem, st, 1, true, a);
+cudaError_t launch_attention(const AttnArg &a, int sms, cudaStream_t st) {
+    return launch_kernel(paged_attention_kernel<FMT, D, STACK, EXACT>, dim3(AttnShape<FMT, D, STACK>::kBlocks * sms), kAttnThreads,
+                         AttnShape<FMT, D, STACK>::kSmem, st, 1, true, a);
 }
 template <int FMT, int D, bool STACK, bool EXACT>
 cudaError_t limit_attention() {
     return cudaFuncSetAttribute(paged_attention_kernel<FMT, D, STACK, EXACT>,
-                                cudaFuncAttributeMaxDynamicSharedMemorySize, AttnShape<FMT, D>::kSmem);
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, AttnShape<FMT, D, STACK>::kSmem);
 }
 
 }  // namespace wici

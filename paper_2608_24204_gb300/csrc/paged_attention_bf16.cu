@@ -4,16 +4,16 @@
 namespace wici {
 
 template <int D>
-static cudaError_t launch_d(const AttnArg &a, bool stack, bool exact, int grid, cudaStream_t st) {
+static cudaError_t launch_d(const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st) {
     if (stack)
-        return exact ? launch_attention<WICI_KV_BF16, D, true, true>(a, grid, st)
-                     : launch_attention<WICI_KV_BF16, D, true, false>(a, grid, st);
-    return exact ? launch_attention<WICI_KV_BF16, D, false, true>(a, grid, st)
-                 : launch_attention<WICI_KV_BF16, D, false, false>(a, grid, st);
+        return exact ? launch_attention<WICI_KV_BF16, D, true, true>(a, sms, st)
+                     : launch_attention<WICI_KV_BF16, D, true, false>(a, sms, st);
+    return exact ? launch_attention<WICI_KV_BF16, D, false, true>(a, sms, st)
+                 : launch_attention<WICI_KV_BF16, D, false, false>(a, sms, st);
 }
 
-cudaError_t launch_attention_bf16(int d, const AttnArg &a, bool stack, bool exact, int grid, cudaStream_t st) {
-    return d == 64 ? launch_d<64>(a, stack, exact, grid, st) : launch_d<128>(a, stack, exact, grid, st);
+cudaError_t launch_attention_bf16(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st) {
+    return d == 64 ? launch_d<64>(a, stack, exact, sms, st) : launch_d<128>(a, stack, exact, sms, st);
 }
 
 template <int D>

@@ -3,20 +3,31 @@
 
 namespace wici {
 
-cudaError_t launch_attention_e4m3(int d, const AttnArg &a, bool stack, int grid, cudaStream_t st) {
-    if (d == 64)
-        return stack ? launch_attention<WICI_KV_E4M3, 64, true, false>(a, grid, st)
-                     : launch_attention<WICI_KV_E4M3, 64, false, false>(a, grid, st);
-    return stack ? launch_attention<WICI_KV_E4M3, 128, true, false>(a, grid, st)
-                 : launch_attention<WICI_KV_E4M3, 128, false, false>(a, grid, st);
+template <int D>
+static cudaError_t launch_d(const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st) {
+    if (stack)
+        return exact ? launch_attention<WICI_KV_E4M3, D, true, true>(a, sms, st)
+                     : launch_attention<WICI_KV_E4M3, D, true, false>(a, sms, st);
+    return exact ? launch_attention<WICI_KV_E4M3, D, false, true>(a, sms, st)
+                 : launch_attention<WICI_KV_E4M3, D, false, false>(a, sms, st);
+}
+
+cudaError_t launch_attention_e4m3(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st) {
+    return d == 64 ? launch_d<64>(a, stack, exact, sms, st) : launch_d<128>(a, stack, exact, sms, st);
+}
+
+template <int D>
+static cudaError_t setup_d() {
+    cudaError_t e = limit_attention<WICI_KV_E4M3, D, true, true>();
+    if (e == cudaSuccess) e = limit_attention<WICI_KV_E4M3, D, true, false>();
+    if (e == cudaSuccess) e = limit_attention<WICI_KV_E4M3, D, false, true>();
+    if (e == cudaSuccess) e = limit_attention<WICI_KV_E4M3, D, false, false>();
+    return e;
 }
 
 cudaError_t setup_attention_e4m3() {
-    cudaError_t e = limit_attention<WICI_KV_E4M3, 64, true, false>();
-    if (e == cudaSuccess) e = limit_attention<WICI_KV_E4M3, 64, false, false>();
-    if (e == cudaSuccess) e = limit_attention<WICI_KV_E4M3, 128, true, false>();
-    if (e == cudaSuccess) e = limit_attention<WICI_KV_E4M3, 128, false, false>();
-    return e;
+    const cudaError_t e = setup_d<64>();
+    return e == cudaSuccess ? setup_d<128>() : e;
 }
 
 }  // namespace wici
