@@ -104,9 +104,10 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
  *   WICI_KV_INT8  int8 [16][head_dim], then fp32 scale[16]
  *   WICI_KV_E4M3  e4m3 [16][head_dim], then fp32 scale[16]
  * A token's head stands for code * scale; it is written with scale = max|x| / 127
- * (int8) or / 448 (e4m3) in fp32 and code = x / scale rounded to nearest even; a
- * head of zeros has scale 0, and one that holds an infinity or NaN has scale NaN
- * (it reads as NaN throughout).  Slot s is place s % 16 of page s / 16.  The paper
+ * (int8) or / 448 (e4m3) in fp32 and code = x / scale (an fp32 product with 1 / scale)
+ * rounded to nearest even; a head whose scale would be below 2^-126, one of zeros
+ * among them, has scale 0, and one that holds an infinity or NaN has scale NaN (it
+ * reads as NaN throughout).  Slot s is place s % 16 of page s / 16.  The paper
  * names no cache precision; 8-bit codes halve the bytes that bound decoding. */
 enum { WICI_KV_BF16 = 0, WICI_KV_INT8 = 1, WICI_KV_E4M3 = 2 };
 
@@ -147,10 +148,12 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
  * lse -infinity.  Several sequences may share pages. */
 typedef struct wici_attn_shape {
     int32_t batch;            /* 0 .. 65535 */
-    int32_t max_pages;        /* columns of `pages`, 1 .. 2^27 - 1 */
+    int32_t max_pages;        /* columns of `pages`, 1 .. 2^27 - 1; (max_pages + 2) * heads < 2^31 */
     int32_t window;           /* >= 0 */
     float scale;              /* finite */
 } wici_attn_shape;
+
+enum { WICI_ATTN_ZEROED = 16384 };
 
 /* Bytes of the workspace on the current device for up to `batch` sequences and
  * n_q_heads query heads. */
@@ -158,8 +161,8 @@ int wici_paged_attention_workspace_bytes(const wici_kv_cache *cache, int32_t n_q
 
 /* q and out: `batch` tokens of n_q_heads heads (a multiple of n_kv_heads), each of
  * its own type; out rows past the batch are left as they are.  lse: device
- * fp32 [batch][n_q_heads], or NULL.  workspace: 16-byte aligned, zeroed once by the
- * caller before its first use; calls that share one must be ordered on one stream
+ * fp32 [batch][n_q_heads], or NULL.  workspace: 16-byte aligned, its first
+ * WICI_ATTN_ZEROED bytes zeroed once by the caller before its first use; calls that share one must be ordered on one stream
  * (a captured graph needs one of its own unless its launches are ordered with every
  * other user's). */
 int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wici_attn_shape *shape,

@@ -26,9 +26,11 @@ int fail(int code, const char *fmt, ...) {
     return code;
 }
 
-constexpr int kRowThreads = 256;
-constexpr int kBlockTokens = 16;      // tokens of a block at most: their angles are in shared memory
+constexpr int kRowThreads = 128;
+constexpr int kRowBlocks = 8;         // blocks on an SM: 64 registers a thread
+constexpr int kBlockTokens = 8;       // tokens of a block at most
 constexpr int kRopeOnly = -1;         // FMT of a launch without a cache
+enum Path { WIDE_HALF, WIDE_PAIRS, NARROW };   // 16-byte accesses of either layout, or element by element
 
 struct RopeArg {
     uint64_t turns[128];
@@ -43,8 +45,8 @@ struct RowsArg {
     const int32_t *positions, *slots;
     int32_t *status;
     int64_t tokens;
+    int block_tokens;                 // a power of two
     int q_heads, heads;               // rows of a token: q heads, then (with a cache) k heads and v heads
-    int block_tokens, block_heads;
     int chunks, rot_chunks;           // lanes of a row, those of them that hold rotated pairs
     bool rotate_k;
 };
@@ -70,146 +72,164 @@ __device__ __forceinline__ float2 turn_of(uint64_t phase) {
     return make_float2(c, s);
 }
 
+// the largest of three, NaN where one is
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // One launch rotates q rows (FMT = kRopeOnly: all rows) and writes k and v rows into the cache.
-// A block takes block_tokens tokens (or block_heads heads of one): it computes their cosines
-// and sines once, one pair a thread, then every row reads them from shared memory.
-template <typename T, int FMT, bool WIDE>
-__global__ void __launch_bounds__(kRowThreads) rows_kernel(const __grid_constant__ RowsArg a) {
+// A block takes block_tokens tokens.  It computes their cosines and sines once, one pair a thread
+// and turn, through shared memory; then a thread keeps its token, with its chunk's cosines and
+// sines in registers, and walks over the token's heads: what is left for a row is its loads (issued
+// before the row ahead of it is worked on), the arithmetic and its stores.  A warp holds the same
+// head of up to four tokens, which lie side by side in a page.
+template <typename T, int FMT, int PATH>
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __grid_constant__ RowsArg a) {
+    constexpr bool WIDE = PATH != NARROW;
+    constexpr int W = sizeof(T) / 2;                             // 16-byte words of 8 elements
     extern __shared__ float4 cs[];    // [token][4][rot_chunks]: (cos, sin) of pairs 8 chunk + 2 j, + 2 j + 1
+    const bool pairs = PATH == NARROW ? a.rope.interleaved : PATH == WIDE_PAIRS;
+    const int c = threadIdx.x, half = a.rope.rot / 2;
+    const int tid = threadIdx.y * blockDim.x + c, nthreads = blockDim.x * blockDim.y;
+    // the chunk's two groups of 8 elements in a rotated row: where they start, how many they hold
+    int o0, o1, n0, n1;
+    const bool turns = c < a.rot_chunks;
+    if (turns) {
+        const int n = half - 8 * c < 8 ? half - 8 * c : 8;
+        o0 = pairs ? 16 * c : 8 * c;
+        o1 = pairs ? o0 + 8 : half + 8 * c;
+        n0 = pairs ? (2 * n < 8 ? 2 * n : 8) : n;
+        n1 = pairs ? 2 * n - n0 : n;
+    } else {
+        o0 = a.rope.rot + 16 * (c - a.rot_chunks);
+        o1 = o0 + 8;
+        const int n = a.rope.head_dim - o0 < 16 ? a.rope.head_dim - o0 : 16;
+        n0 = n < 8 ? n : 8;
+        n1 = n - n0;
+    }
+    griddep_launch_dependents();
     griddep_wait();
     const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
-    const int nt = (int)(a.tokens - t0 < a.block_tokens ? a.tokens - t0 : a.block_tokens);
-    const int h0 = blockIdx.y * a.block_heads;
-    const int nh = a.heads - h0 < a.block_heads ? a.heads - h0 : a.block_heads;
-    const int half = a.rope.rot / 2;
-    const int tid = threadIdx.y * blockDim.x + threadIdx.x, nthreads = blockDim.x * blockDim.y;
+    const int tl = threadIdx.y & (a.block_tokens - 1), step = blockDim.y / a.block_tokens;
+    const int64_t t = t0 + tl < a.tokens ? t0 + tl : a.tokens - 1;   // past the end: the last token's, not stored
+    const bool here = t0 + tl < a.tokens;
+    float2 w[8];                                                 // cosine and sine of the chunk's pairs
     if (a.positions) {
-        const int pairs = 8 * a.rot_chunks;
-        for (int i = tid; i < nt * pairs; i += nthreads) {
-            const int t = i / pairs, p = i - t * pairs;
-            float2 w = make_float2(1.f, 0.f);
+        const int per = 8 * a.rot_chunks;
+        for (int i = tid; i < a.block_tokens * per; i += nthreads) {
+            const int tt = i / per, p = i - tt * per;
+            const int64_t token = t0 + tt < a.tokens ? t0 + tt : a.tokens - 1;
+            float2 v = make_float2(1.f, 0.f);
             if (p < half) {
-                w = turn_of((uint64_t)(int64_t)a.positions[t0 + t] * a.rope.turns[p]);
-                w.x *= a.rope.gain;
-                w.y *= a.rope.gain * a.rope.sign;
+                v = turn_of((uint64_t)(int64_t)a.positions[token] * a.rope.turns[p]);
+                v.x *= a.rope.gain;
+                v.y *= a.rope.gain * a.rope.sign;
             }
-            ((float2 *)cs)[(((t * 4 + (p & 7) / 2) * a.rot_chunks + p / 8) << 1) + (p & 1)] = w;
+            ((float2 *)cs)[(((tt * 4 + (p & 7) / 2) * a.rot_chunks + p / 8) << 1) + (p & 1)] = v;
         }
         __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 v = cs[(tl * 4 + j) * a.rot_chunks + (turns ? c : 0)];
+            w[2 * j] = make_float2(v.x, v.y);
+            w[2 * j + 1] = make_float2(v.z, v.w);
+        }
     }
-    const int c = threadIdx.x;
-    const int rows = nt * nh;
-    for (int base = 0; base < rows; base += blockDim.y) {   // every lane of a warp stays: rows are reduced by shuffles
-        const int idx = base + threadIdx.y;
-        const bool live = idx < rows;
-        const int tl = live ? idx / nh : 0;
-        const int64_t t = t0 + tl;
-        int h = h0 + (live ? idx - tl * nh : 0);
-        const bool is_q = FMT == kRopeOnly || h < a.q_heads;
-        const bool is_v = !is_q && h >= a.q_heads + a.cache.kv_heads;
-        if (!is_q) h -= a.q_heads + (is_v ? a.cache.kv_heads : 0);
-        const bool rotate = is_q || (!is_v && a.rotate_k);
-        // the chunk's two groups of 8: where they start, how many they hold
-        int o0, o1, n0, n1;
-        if (!rotate) {
-            o0 = 16 * c;
-            o1 = o0 + 8;
-            n0 = n1 = 8;              // head_dim is 64 or 128 here
-        } else if (c < a.rot_chunks) {
-            const int n = half - 8 * c < 8 ? half - 8 * c : 8;
-            if (a.rope.interleaved) {
-                o0 = 16 * c;
-                o1 = o0 + 8;
-                n0 = 2 * n < 8 ? 2 * n : 8;
-                n1 = 2 * n - n0;
-            } else {
-                o0 = 8 * c;
-                o1 = half + 8 * c;
-                n0 = n1 = n;
+    int slot = -1;
+    if (FMT != kRopeOnly && here) {
+        slot = a.slots[t];
+        if (slot >= a.cache.n_pages * kKvPage) {
+            if (a.status) atomicOr(a.status, WICI_BAD_SLOT);
+            slot = -1;
+        }
+    }
+    const int d = FMT == kRopeOnly ? 0 : 16 * a.chunks, where = slot & (kKvPage - 1);
+    const int kv_block = FMT == WICI_KV_BF16 ? kKvPage * d * 2 : kKvPage * (d + 4);
+    uint8_t *page = FMT == kRopeOnly || slot < 0 ? nullptr : a.cache.data + (int64_t)(slot / kKvPage) * a.cache.page_stride;
+    const T *const sq = a.q.template row<T>(t, 0), *const sk = a.k.template row<T>(t, 0), *const sv = a.v.template row<T>(t, 0);
+    T *const dq = a.q_out.template row<T>(t, 0);
+    const int k0 = a.q_heads, v0 = FMT == kRopeOnly ? a.heads : a.q_heads + a.cache.kv_heads;   // first k row, first v row
+    // a row's two groups of elements as they stand
+    auto fetch = [&](int h, uint4 *raw) {
+        const bool is_q = FMT == kRopeOnly || h < k0, is_v = !is_q && h >= v0, rotate = is_q || (!is_v && a.rotate_k);
+        const T *src = is_q ? sq + h * a.q.hs : is_v ? sv + (h - v0) * a.v.hs : sk + (h - k0) * a.k.hs;
+        const T *p0 = src + (rotate ? o0 : 16 * c), *p1 = src + (rotate ? o1 : 16 * c + 8);
+        if (WIDE) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) raw[i] = ((const uint4 *)p0)[i];
+            if (FMT != kRopeOnly || n1 > 0) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) raw[W + i] = ((const uint4 *)p1)[i];
             }
         } else {
-            o0 = a.rope.rot + 16 * (c - a.rot_chunks);
-            o1 = o0 + 8;
-            const int n = a.rope.head_dim - o0 < 16 ? a.rope.head_dim - o0 : 16;
-            n0 = n < 8 ? n : 8;
-            n1 = n - n0;
+            float *x = (float *)raw;
+            load8<T, false>(p0, rotate ? n0 : 8, x);
+            load8<T, false>(p1, rotate ? n1 : 8, x + 8);
         }
+    };
+    constexpr int RAW = WIDE ? 2 * W : 4;
+    uint4 raw[RAW] = {};
+    const int h0 = threadIdx.y / a.block_tokens;
+    if (h0 < a.heads) fetch(h0, raw);
+    // every lane of a warp stays: rows are reduced by shuffles
+    for (int base = 0; base < a.heads; base += step) {
+        const int h = base + h0;
+        const bool live = here && h < a.heads;
+        const bool is_q = FMT == kRopeOnly || h < k0, is_v = !is_q && h >= v0, rotate = is_q || (!is_v && a.rotate_k);
         float x[16];
+        if (WIDE) {
+            const T *e = (const T *)raw;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = 0.f;
-        if (live) {
-            const T *src = (is_q ? a.q : is_v ? a.v : a.k).template row<T>(t, h);
-            load8<T, WIDE>(src + o0, n0, x);
-            load8<T, WIDE>(src + o1, n1, x + 8);
+            for (int j = 0; j < 16; ++j) x[j] = to_f32(e[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] = ((const float *)raw)[j];
         }
-        if (rotate && c < a.rot_chunks) {
+        if (h + step < a.heads) fetch(h + step, raw);
+        const int p0 = rotate ? o0 : 16 * c, p1 = rotate ? o1 : 16 * c + 8;
+        if (rotate && turns) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 w = cs[(tl * 4 + j) * a.rot_chunks + c];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int p = 2 * j + u;
-                    const float co = u ? w.z : w.x, si = u ? w.w : w.y;
-                    // both layouts with static register names
-                    const float xa = a.rope.interleaved ? x[2 * p] : x[p];
-                    const float xb = a.rope.interleaved ? x[2 * p + 1] : x[p + 8];
-                    const float ya = xa * co - xb * si, yb = xa * si + xb * co;
-                    if (a.rope.interleaved) {
-                        x[2 * p] = ya;
-                        x[2 * p + 1] = yb;
-                    } else {
-                        x[p] = ya;
-                        x[p + 8] = yb;
-                    }
-                }
+            for (int p = 0; p < 8; ++p) {
+                const float xa = pairs ? x[2 * p] : x[p], xb = pairs ? x[2 * p + 1] : x[p + 8];
+                const float ya = xa * w[p].x - xb * w[p].y, yb = xa * w[p].y + xb * w[p].x;
+                // the pair's own places are read and written by this step alone
+                if (pairs) x[2 * p] = ya, x[2 * p + 1] = yb;
+                else x[p] = ya, x[p + 8] = yb;
             }
         }
         if (is_q) {
             if (live) {
-                T *dst = a.q_out.template row<T>(t, h);
-                store8<T, WIDE>(dst + o0, n0, x);
-                store8<T, WIDE>(dst + o1, n1, x + 8);
+                T *dst = dq + h * a.q_out.hs;
+                store8<T, WIDE>(dst + p0, n0, x);
+                if (n1 > 0) store8<T, WIDE>(dst + p1, n1, x + 8);
             }
+            if (FMT == kRopeOnly || FMT == WICI_KV_BF16) continue;
         }
         if (FMT != kRopeOnly) {
-            int slot = -1;
-            if (live && !is_q) {
-                slot = a.slots[t];
-                if (slot >= a.cache.n_pages * kKvPage) {
-                    if (a.status) atomicOr(a.status, WICI_BAD_SLOT);
-                    slot = -1;
-                }
-            }
-            const int d = 16 * a.chunks;
-            uint8_t *block = a.cache.data + (int64_t)(slot / kKvPage) * a.cache.page_stride +
-                             (int64_t)(is_v ? a.cache.kv_heads + h : h) *
-                                 (FMT == WICI_KV_BF16 ? kKvPage * d * 2 : kKvPage * (d + 4));
-            const int place = slot & (kKvPage - 1);
+            uint8_t *block = page + (int64_t)(h - k0) * kv_block;   // V's blocks follow K's
+            const bool store = live && !is_q && slot >= 0;
             if (FMT == WICI_KV_BF16) {
-                if (slot >= 0) {
-                    __nv_bfloat16 *dst = (__nv_bfloat16 *)block + place * d;
-                    store8<__nv_bfloat16, true>(dst + o0, 8, x);
-                    store8<__nv_bfloat16, true>(dst + o1, 8, x + 8);
+                if (store) {
+                    __nv_bfloat16 *dst = (__nv_bfloat16 *)block + where * d;
+                    store8<__nv_bfloat16, true>(dst + p0, 8, x);
+                    store8<__nv_bfloat16, true>(dst + p1, 8, x + 8);
                 }
-            } else {
-                // the row's largest magnitude, as a bit pattern: infinities and NaNs are the largest
-                uint32_t top = 0;
+            } else if (__any_sync(0xffffffffu, store)) {
+                // the row's largest magnitude
+                float top = fabsf(x[0]);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
-                for (int o = a.chunks / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                if (slot >= 0) {
-                    float scale = __uint_as_float(top) / largest_code<FMT>();
-                    uint32_t code[4] = {0, 0, 0, 0};
-                    if (top >= kInfBits) {
-                        scale = __uint_as_float(0x7FC00000u);
-                    } else if (scale > 0.f) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) code[j] = encode4<FMT>(x + 4 * j, scale);
-                    }
-                    uint8_t *dst = block + place * d;
-                    *(uint2 *)(dst + o0) = make_uint2(code[0], code[1]);
-                    *(uint2 *)(dst + o1) = make_uint2(code[2], code[3]);
-                    if (c == 0) ((float *)(block + kKvPage * d))[place] = scale;
+                for (int j = 1; j < 15; j += 2) top = max3(top, fabsf(x[j]), fabsf(x[j + 1]));
+                top = max3(top, fabsf(x[15]), 0.f);
+                for (int o = a.chunks / 2; o > 0; o >>= 1) top = max3(top, __shfl_xor_sync(0xffffffffu, top, o), 0.f);
+                if (store) {
+                    uint32_t code[4];
+                    const float scale = quantise16<FMT>(x, top, code);
+                    uint8_t *dst = block + where * d;
+                    *(uint2 *)(dst + p0) = make_uint2(code[0], code[1]);
+                    *(uint2 *)(dst + p1) = make_uint2(code[2], code[3]);
+                    if (c == 0) ((float *)(block + kKvPage * d))[where] = scale;
                 }
             }
         }
@@ -222,57 +242,78 @@ struct ReadArg {
     const int32_t *slots;
     int32_t *status;
     int64_t tokens;
+    int block_tokens;                 // a power of two
     int heads;                        // rows of a token: those of k, then those of v
-    int block_tokens, block_heads;
     bool has_k;
 };
 
-// A row of the cache to a row of k or v.
+// Rows of the cache to rows of k and v.  A thread keeps its token and walks over the heads, kReadRows
+// of them under way at a time; a warp reads the same head of up to four tokens: side by side in a page.
+constexpr int kReadRows = 4;
 template <typename T, int FMT, int D, bool WIDE>
-__global__ void __launch_bounds__(kRowThreads) read_kernel(const __grid_constant__ ReadArg a) {
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks) read_kernel(const __grid_constant__ ReadArg a) {
+    constexpr int W = FMT == WICI_KV_BF16 ? 2 : 1;               // 16-byte words of a lane's 16 values
+    constexpr int kBlock = FMT == WICI_KV_BF16 ? kKvPage * D * 2 : kKvPage * (D + 4);
+    griddep_launch_dependents();
     griddep_wait();
-    const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
-    const int nt = (int)(a.tokens - t0 < a.block_tokens ? a.tokens - t0 : a.block_tokens);
-    const int h0 = blockIdx.y * a.block_heads;
-    const int nh = a.heads - h0 < a.block_heads ? a.heads - h0 : a.block_heads;
-    const int c = threadIdx.x;
-    for (int idx = threadIdx.y; idx < nt * nh; idx += blockDim.y) {
-        const int tl = idx / nh;
-        const int64_t t = t0 + tl;
-        int h = h0 + idx - tl * nh;
-        const bool is_v = !a.has_k || h >= a.cache.kv_heads;
-        if (a.has_k && is_v) h -= a.cache.kv_heads;
-        const int slot = a.slots[t];
-        float x[16];
-        if (slot < 0 || slot >= a.cache.n_pages * kKvPage) {
-            const float fill = slot < 0 ? 0.f : __uint_as_float(0x7FC00000u);
-            if (slot >= 0 && a.status) atomicOr(a.status, WICI_BAD_SLOT);
+    const int64_t t = (int64_t)blockIdx.x * a.block_tokens + (threadIdx.y & (a.block_tokens - 1));
+    if (t >= a.tokens) return;
+    const int c = threadIdx.x, step = blockDim.y / a.block_tokens;
+    const int slot = a.slots[t], where = slot & (kKvPage - 1);
+    const bool good = slot >= 0 && slot < a.cache.n_pages * kKvPage;
+    // no slot: zeros; a slot outside the cache: NaN
+    const float fill = slot < 0 ? 0.f : __uint_as_float(0x7FC00000u);
+    if (!good && slot >= 0 && a.status) atomicOr(a.status, WICI_BAD_SLOT);
+    const uint8_t *src = a.cache.data + (int64_t)(good ? slot / kKvPage : 0) * a.cache.page_stride;
+    if (!a.has_k) src += a.cache.kv_heads * (int64_t)kBlock;
+    T *const dk = a.k.template row<T>(t, 0) + 16 * c, *const dv = a.v.template row<T>(t, 0) + 16 * c;
+    for (int h0 = threadIdx.y / a.block_tokens; h0 < a.heads; h0 += kReadRows * step) {
+        uint4 word[kReadRows][W];
+        float scale[kReadRows];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) x[j] = fill;
-        } else {
-            const uint8_t *block = a.cache.data + (int64_t)(slot / kKvPage) * a.cache.page_stride +
-                                   (int64_t)(is_v ? a.cache.kv_heads + h : h) *
-                                       (FMT == WICI_KV_BF16 ? kKvPage * D * 2 : kKvPage * (D + 4));
-            const int place = slot & (kKvPage - 1);
-            if (FMT == WICI_KV_BF16) {
-                const __nv_bfloat16 *src = (const __nv_bfloat16 *)block + place * D + 16 * c;
-                load8<__nv_bfloat16, true>(src, 8, x);
-                load8<__nv_bfloat16, true>(src + 8, 8, x + 8);
-            } else {
-                const uint4 w = *(const uint4 *)(block + place * D + 16 * c);
-                const float scale = ((const float *)(block + kKvPage * D))[place];
-                const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+        for (int i = 0; i < kReadRows; ++i) {
+            const int h = h0 + i * step;
+            scale[i] = fill;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float2 f = __half22float2(decode2<FMT>(word[j / 2] >> (16 * (j & 1))));
-                    x[2 * j] = f.x * scale;
-                    x[2 * j + 1] = f.y * scale;
+            for (int w = 0; w < W; ++w) word[i][w] = make_uint4(0, 0, 0, 0);
+            if (good && h < a.heads) {
+                const uint8_t *block = src + (int64_t)h * kBlock;
+                if (FMT == WICI_KV_BF16) {
+#pragma unroll
+                    for (int w = 0; w < W; ++w) word[i][w] = *(const uint4 *)(block + (where * D + 16 * c) * 2 + 16 * w);
+                } else {
+                    word[i][0] = *(const uint4 *)(block + where * D + 16 * c);
+                    scale[i] = ((const float *)(block + kKvPage * D))[where];
                 }
             }
         }
-        T *dst = (is_v ? a.v : a.k).template row<T>(t, h) + 16 * c;
-        store8<T, WIDE>(dst, 8, x);
-        store8<T, WIDE>(dst + 8, 8, x + 8);
+#pragma unroll
+        for (int i = 0; i < kReadRows; ++i) {
+            const int h = h0 + i * step;
+            if (h >= a.heads) break;
+            float x[16];
+            const uint32_t *w = (const uint32_t *)word[i];
+            if (FMT == WICI_KV_BF16) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x[2 * j] = good ? bf16lo(w[j]) : fill;
+                    x[2 * j + 1] = good ? bf16hi(w[j]) : fill;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t lo, hi;
+                    decode4<FMT>(w[j], lo, hi);
+                    const float2 f = __half22float2(*(const __half2 *)&lo), g = __half22float2(*(const __half2 *)&hi);
+                    x[4 * j] = f.x * scale[i], x[4 * j + 1] = f.y * scale[i];
+                    x[4 * j + 2] = g.x * scale[i], x[4 * j + 3] = g.y * scale[i];
+                }
+            }
+            const bool is_v = !a.has_k || h >= a.cache.kv_heads;
+            T *dst = is_v ? dv + (a.has_k ? h - a.cache.kv_heads : h) * a.v.hs : dk + h * a.k.hs;
+            store8<T, WIDE>(dst, 8, x);
+            store8<T, WIDE>(dst + 8, 8, x + 8);
+        }
     }
 }
 
@@ -286,29 +327,47 @@ int sm_count(int *n) {
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "SM count: %s", cudaGetErrorString(e));
 }
 
-template <typename T, int FMT>
-cudaError_t launch_rows(const RowsArg &a, const RowSplit &s, bool wide, cudaStream_t st) {
-    const dim3 block(a.chunks, kRowThreads / a.chunks);
+// Tokens of a block: as many as leave two waves of blocks and more, and rows for a block's lanes.
+int tokens_of_block(int64_t tokens, int most, int sms) {
+    int n = 1;
+    while (2 * n <= most && tokens / (2 * n) >= 2 * kRowBlocks * sms) n *= 2;
+    return n;
+}
+
+template <typename Kern, typename Arg>
+cudaError_t launch(Kern kern, const Arg &a, int chunks, size_t smem, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)s.token_blocks, s.head_blocks);
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = a.positions ? (size_t)s.tokens * 4 * a.rot_chunks * sizeof(float4) : 0;
+    cfg.gridDim = dim3((unsigned)((a.tokens + a.block_tokens - 1) / a.block_tokens));
+    int rows = kRowThreads / chunks;                 // a multiple of block_tokens
+    rows -= rows % a.block_tokens;
+    // no more lanes than there are rows (whole warps: the shuffles of a row)
+    const int need = (a.heads * a.block_tokens + 31) / 32 * 32;
+    rows = rows < need ? rows : need;
+    cfg.blockDim = dim3(chunks, rows);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return wide ? cudaLaunchKernelEx(&cfg, rows_kernel<T, FMT, true>, a)
-                : cudaLaunchKernelEx(&cfg, rows_kernel<T, FMT, false>, a);
+    return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+template <typename T, int FMT>
+cudaError_t launch_rows(const RowsArg &a, bool wide, cudaStream_t st) {
+    const size_t smem = a.positions ? (size_t)a.block_tokens * 4 * a.rot_chunks * sizeof(float4) : 0;
+    if (!wide) return launch(rows_kernel<T, FMT, NARROW>, a, a.chunks, smem, st);
+    return a.rope.interleaved ? launch(rows_kernel<T, FMT, WIDE_PAIRS>, a, a.chunks, smem, st)
+                              : launch(rows_kernel<T, FMT, WIDE_HALF>, a, a.chunks, smem, st);
 }
 
 template <int FMT>
-cudaError_t launch_rows(int dtype, const RowsArg &a, const RowSplit &s, bool wide, cudaStream_t st) {
+cudaError_t launch_rows(int dtype, const RowsArg &a, bool wide, cudaStream_t st) {
     switch (dtype) {
-        case WICI_BF16: return launch_rows<__nv_bfloat16, FMT>(a, s, wide, st);
-        case WICI_F16: return launch_rows<__half, FMT>(a, s, wide, st);
-        default: return launch_rows<float, FMT>(a, s, wide, st);
+        case WICI_BF16: return launch_rows<__nv_bfloat16, FMT>(a, wide, st);
+        case WICI_F16: return launch_rows<__half, FMT>(a, wide, st);
+        default: return launch_rows<float, FMT>(a, wide, st);
     }
 }
 
@@ -323,34 +382,23 @@ void set_rope(RowsArg *a, const wici_rope_plan *plan, bool inverse) {
     a->chunks = a->rot_chunks + (plan->head_dim - plan->rot_dim + 15) / 16;
 }
 
-constexpr int64_t kMaxTokens = (int64_t)1 << 31;   // exclusive: token blocks fit a grid
-
-template <typename T, int FMT, int D>
-cudaError_t launch_read(const ReadArg &a, const RowSplit &s, bool wide, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)s.token_blocks, s.head_blocks);
-    cfg.blockDim = dim3(D / 16, kRowThreads / (D / 16));
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return wide ? cudaLaunchKernelEx(&cfg, read_kernel<T, FMT, D, true>, a)
-                : cudaLaunchKernelEx(&cfg, read_kernel<T, FMT, D, false>, a);
-}
+constexpr int64_t kMaxTokens = (int64_t)1 << 31;   // exclusive
 
 template <typename T, int FMT>
-cudaError_t launch_read(int d, const ReadArg &a, const RowSplit &s, bool wide, cudaStream_t st) {
-    return d == 64 ? launch_read<T, FMT, 64>(a, s, wide, st) : launch_read<T, FMT, 128>(a, s, wide, st);
+cudaError_t launch_read(int d, const ReadArg &a, bool wide, cudaStream_t st) {
+    if (d == 64)
+        return wide ? launch(read_kernel<T, FMT, 64, true>, a, 4, 0, st)
+                    : launch(read_kernel<T, FMT, 64, false>, a, 4, 0, st);
+    return wide ? launch(read_kernel<T, FMT, 128, true>, a, 8, 0, st)
+                : launch(read_kernel<T, FMT, 128, false>, a, 8, 0, st);
 }
 
 template <typename T>
-cudaError_t launch_read(int fmt, int d, const ReadArg &a, const RowSplit &s, bool wide, cudaStream_t st) {
+cudaError_t launch_read(int fmt, int d, const ReadArg &a, bool wide, cudaStream_t st) {
     switch (fmt) {
-        case WICI_KV_BF16: return launch_read<T, WICI_KV_BF16>(d, a, s, wide, st);
-        case WICI_KV_INT8: return launch_read<T, WICI_KV_INT8>(d, a, s, wide, st);
-        default: return launch_read<T, WICI_KV_E4M3>(d, a, s, wide, st);
+        case WICI_KV_BF16: return launch_read<T, WICI_KV_BF16>(d, a, wide, st);
+        case WICI_KV_INT8: return launch_read<T, WICI_KV_INT8>(d, a, wide, st);
+        default: return launch_read<T, WICI_KV_E4M3>(d, a, wide, st);
     }
 }
 
@@ -426,13 +474,11 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
     a.q = heads_arg(x);
     a.q_out = heads_arg(y);
     a.positions = positions;
-    a.tokens = tokens;
     a.q_heads = a.heads = x->heads;
-    const RowSplit s = split_rows(tokens, a.heads, kRowThreads / a.chunks, kBlockTokens, 8 * sms);
-    a.block_tokens = s.tokens;
-    a.block_heads = s.heads;
+    a.tokens = tokens;
+    a.block_tokens = tokens_of_block(tokens, kBlockTokens, sms);
     const bool wide = wide_heads(x) && wide_heads(y) && plan->rot_dim % 16 == 0 && plan->head_dim % 8 == 0;
-    const cudaError_t e = launch_rows<kRopeOnly>(x->dtype, a, s, wide, (cudaStream_t)cuda_stream);
+    const cudaError_t e = launch_rows<kRopeOnly>(x->dtype, a, wide, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "rope: %s", cudaGetErrorString(e));
 }
 
@@ -484,19 +530,17 @@ int wici_kv_append(void *cuda_stream, const wici_kv_cache *cache, const int32_t 
     a.positions = positions;
     a.slots = slots;
     a.status = status;
-    a.tokens = tokens;
     a.q_heads = q ? q->heads : 0;
     a.heads = a.q_heads + 2 * cache->n_kv_heads;
-    const RowSplit s = split_rows(tokens, a.heads, kRowThreads / a.chunks, kBlockTokens, 8 * sms);
-    a.block_tokens = s.tokens;
-    a.block_heads = s.heads;
+    a.tokens = tokens;
+    a.block_tokens = tokens_of_block(tokens, kBlockTokens, sms);
     const bool wide = wide_heads(k) && wide_heads(v) && (!q || (wide_heads(q) && wide_heads(q_out)));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
     switch (cache->format) {
-        case WICI_KV_BF16: e = launch_rows<WICI_KV_BF16>(k->dtype, a, s, wide, st); break;
-        case WICI_KV_INT8: e = launch_rows<WICI_KV_INT8>(k->dtype, a, s, wide, st); break;
-        default: e = launch_rows<WICI_KV_E4M3>(k->dtype, a, s, wide, st); break;
+        case WICI_KV_BF16: e = launch_rows<WICI_KV_BF16>(k->dtype, a, wide, st); break;
+        case WICI_KV_INT8: e = launch_rows<WICI_KV_INT8>(k->dtype, a, wide, st); break;
+        default: e = launch_rows<WICI_KV_E4M3>(k->dtype, a, wide, st); break;
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "append: %s", cudaGetErrorString(e));
 }
@@ -523,19 +567,17 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
     a.cache = cache_arg(cache);
     a.slots = slots;
     a.status = status;
-    a.tokens = tokens;
     a.heads = cache->n_kv_heads * ((k ? 1 : 0) + (v ? 1 : 0));
+    a.tokens = tokens;
+    a.block_tokens = tokens_of_block(tokens, kBlockTokens, sms);
     a.has_k = k != nullptr;
-    const RowSplit s = split_rows(tokens, a.heads, kRowThreads / (d / 16), 1 << 16, 8 * sms);
-    a.block_tokens = s.tokens;
-    a.block_heads = s.heads;
     const bool wide = (!k || wide_heads(k)) && (!v || wide_heads(v));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
     switch ((k ? k : v)->dtype) {
-        case WICI_BF16: e = launch_read<__nv_bfloat16>(cache->format, d, a, s, wide, st); break;
-        case WICI_F16: e = launch_read<__half>(cache->format, d, a, s, wide, st); break;
-        default: e = launch_read<float>(cache->format, d, a, s, wide, st); break;
+        case WICI_BF16: e = launch_read<__nv_bfloat16>(cache->format, d, a, wide, st); break;
+        case WICI_F16: e = launch_read<__half>(cache->format, d, a, wide, st); break;
+        default: e = launch_read<float>(cache->format, d, a, wide, st); break;
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "read: %s", cudaGetErrorString(e));
 }

@@ -80,40 +80,55 @@ __device__ __forceinline__ void store8(T *p, int n, const float *v) {
 }
 
 // ---------------------------------------------------------- 8-bit cache formats
-template <int FMT>
-__device__ __forceinline__ float largest_code() {
-    return FMT == WICI_KV_INT8 ? 127.f : 448.f;
-}
-
-// four codes of x / scale, rounded to nearest even (scale > 0)
-template <int FMT>
-__device__ __forceinline__ uint32_t encode4(const float *x, float scale) {
-    if (FMT == WICI_KV_INT8) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            // a scale below the normal range is rounded coarsely: the quotient may pass 127
-            const int c = __float2int_rn(fminf(fmaxf(x[j] / scale, -127.f), 127.f));
-            w |= (uint32_t)(c & 255) << (8 * j);
-        }
-        return w;
-    }
-    const __nv_fp8x2_storage_t lo =
-        __nv_cvt_float2_to_fp8x2(make_float2(x[0] / scale, x[1] / scale), __NV_SATFINITE, __NV_E4M3);
-    const __nv_fp8x2_storage_t hi =
-        __nv_cvt_float2_to_fp8x2(make_float2(x[2] / scale, x[3] / scale), __NV_SATFINITE, __NV_E4M3);
-    return (uint32_t)lo | (uint32_t)hi << 16;
-}
-
-// two codes (the low half of w) as fp16, exactly
-template <int FMT>
-__device__ __forceinline__ __half2 decode2(uint32_t w) {
-    if (FMT == WICI_KV_INT8)
-        return __halves2half2(__int2half_rn((int8_t)(w & 255)), __int2half_rn((int8_t)((w >> 8) & 255)));
-    return __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFF), __NV_E4M3));
-}
-
 // the smallest NaN-or-infinity pattern of |x|: larger patterns are larger values or NaNs
 constexpr uint32_t kInfBits = 0x7F800000u;
+
+// The codes of 16 values of a head whose largest magnitude is `top` (NaN where one is); the scale is returned.
+// x times the scale's reciprocal stands for x / scale: off by at most 2^-23 of it, which is a code's choice only
+// where the quotient lies that near to a border (one division a head in place of one an element).  A scale below
+// the normal range, whose reciprocal might overflow, is 0: such a head is below 2^-117.
+template <int FMT>
+__device__ __forceinline__ float quantise16(const float *x, float top, uint32_t *code) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) code[j] = 0;
+    if (!(top < __uint_as_float(kInfBits))) return __uint_as_float(0x7FC00000u);   // an infinity or NaN among them
+    const float scale = top / (FMT == WICI_KV_INT8 ? 127.f : 448.f);
+    if (scale < 0x1p-126f) return 0.f;
+    const float r = 1.f / scale;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float *y = x + 4 * j;
+        if (FMT == WICI_KV_INT8) {
+            // 1.5 * 2^23 + y / scale has the rounded code in its low byte
+            uint32_t b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(fmaf(y[i], r, 12582912.f));
+            code[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+        } else {
+            code[j] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y[0] * r, y[1] * r), __NV_SATFINITE, __NV_E4M3) |
+                      (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y[2] * r, y[3] * r), __NV_SATFINITE, __NV_E4M3) << 16;
+        }
+    }
+    return scale;
+}
+
+// The four codes of w as two fp16 pairs, exactly.  An int8 code c is the fp16 number 1024 + (c + 128) less 1152.
+template <int FMT>
+__device__ __forceinline__ void decode4(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    if (FMT == WICI_KV_INT8) {
+        const uint32_t x = w ^ 0x80808080u;
+        const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
+        const __half2 off = __half2half2(__ushort_as_half((unsigned short)0x6480));   // 1152
+        const __half2 p = __hsub2(*(const __half2 *)&a, off), q = __hsub2(*(const __half2 *)&b, off);
+        lo = *(const uint32_t *)&p;
+        hi = *(const uint32_t *)&q;
+    } else {
+        const __half2 p = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFF), __NV_E4M3));
+        const __half2 q = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3));
+        lo = *(const uint32_t *)&p;
+        hi = *(const uint32_t *)&q;
+    }
+}
+
 
 }  // namespace wici

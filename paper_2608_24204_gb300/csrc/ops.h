@@ -66,30 +66,4 @@ inline const char *check_rope(const wici_rope_plan *p) {
     return nullptr;
 }
 
-// Rows that one block of a row-wise operator takes, as whole tokens or as some heads of one:
-// enough blocks for every SM several times over, unless the call is smaller than that.
-struct RowSplit {
-    int tokens, heads;     // of a block
-    int64_t token_blocks;
-    int head_blocks;
-};
-inline RowSplit split_rows(int64_t tokens, int heads, int least, int most_tokens, int blocks) {
-    int64_t rows = tokens * heads / blocks;
-    rows = rows < least ? least : rows;
-    RowSplit s;
-    if (rows < heads) {
-        s.tokens = 1;
-        s.head_blocks = (int)((heads + rows - 1) / rows);
-        s.heads = (heads + s.head_blocks - 1) / s.head_blocks;
-        s.head_blocks = (heads + s.heads - 1) / s.heads;
-    } else {
-        const int64_t t = rows / heads;
-        s.tokens = (int)(t < most_tokens ? t : most_tokens);
-        s.heads = heads;
-        s.head_blocks = 1;
-    }
-    s.token_blocks = (tokens + s.tokens - 1) / s.tokens;
-    return s;
-}
-
 }  // namespace wici

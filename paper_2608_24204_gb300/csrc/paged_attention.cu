@@ -37,7 +37,7 @@ int sm_count(int *n) {
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "attention setup: %s", cudaGetErrorString(e));
 }
 
-constexpr int kTicketBytes = 16384;   // arrivals of every block
+constexpr int kTicketBytes = WICI_ATTN_ZEROED;   // arrivals of every block: zero before the first launch, and after each
 constexpr int kMaxBlocksPerSm = 3;
 // SMs that a launch uses: tickets are for so many blocks
 int used_sms(int sms) {

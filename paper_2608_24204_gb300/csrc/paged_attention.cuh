@@ -105,13 +105,13 @@ __device__ __forceinline__ float lds32(uint32_t a) {
 template <bool BF16>
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
     if (BF16)
-        asm volatile(
+        asm(
             "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
             "{%0, %1, %2, %3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile(
+        asm(
             "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
             "{%0, %1, %2, %3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -139,23 +139,6 @@ __device__ __forceinline__ uint32_t split2(float &lo, float &hi) {
         hi -= f.y;
     }
     return w;
-}
-
-// The four codes of w as two fp16 pairs, exactly.  An int8 code c is the fp16 number 1024 + (c + 128) less 1152.
-template <int FMT>
-__device__ __forceinline__ void decode4(uint32_t w, uint32_t &lo, uint32_t &hi) {
-    if (FMT == WICI_KV_INT8) {
-        const uint32_t x = w ^ 0x80808080u;
-        const uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
-        const __half2 off = __half2half2(__ushort_as_half((unsigned short)0x6480));   // 1152
-        const __half2 p = __hsub2(*(const __half2 *)&a, off), q = __hsub2(*(const __half2 *)&b, off);
-        lo = *(const uint32_t *)&p;
-        hi = *(const uint32_t *)&q;
-    } else {
-        const __half2 p = decode2<FMT>(w), q = decode2<FMT>(w >> 16);
-        lo = *(const uint32_t *)&p;
-        hi = *(const uint32_t *)&q;
-    }
 }
 
 // Where 16-byte chunk c of key row r stands in a ring slot.  The chunks of a row are permuted so
@@ -582,15 +565,9 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             for (int j = 0; j < 4; ++j) o[n][j] = 0.f;
         float vref = 0x1p-125f, vinv = 0x1p125f;      // 8-bit: a power of two, at least a quarter of the largest V scale
 
-        // ---- units of this segment ----
-        int key0 = (keys.lo / kKvPage + (int)(r0 + done - seg.start) * P) * kKvPage;   // first key of the unit
-        for (; done < stop; ++done, key0 += UNIT) {
-            // group `done` brings K; the KS - 1 after it may be on their way
-            cp_wait<KS - 1>();
-            __syncwarp();
-            const uint32_t ks = ring + done % KS * S::kSlot, vs = ring + KS * S::kSlot + done % VS * S::kSlot;
-
-            float c[2 * P][SETS][4];                         // [8 keys][sets of steps]
+        // ---- scores of one unit (unscaled) ----
+        float c[2 * P][SETS][4];                             // [8 keys][sets of steps]
+        auto scores = [&](uint32_t ks) {
 #pragma unroll
             for (int n = 0; n < 2 * P; ++n)
 #pragma unroll
@@ -621,6 +598,19 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     }
                 }
             }
+        };
+
+        // ---- units of this segment: the scores of the next one run beside the softmax of this one (past the last
+        // one they are not used, whatever the slot holds) ----
+        int key0 = (keys.lo / kKvPage + (int)(r0 + done - seg.start) * P) * kKvPage;   // first key of the unit
+        cp_wait<KS - 1>();                                   // group `done` brings its K
+        __syncwarp();
+        scores(ring + done % KS * S::kSlot);
+        for (; done < stop; ++done, key0 += UNIT) {
+            // group done + 1: K of the next unit and V of this one
+            cp_wait<KS - 2>();
+            __syncwarp();
+            const uint32_t ks = ring + done % KS * S::kSlot, vs = ring + KS * S::kSlot + done % VS * S::kSlot;
             // x[r][j]: query g + 8 r, key t + 4 j of the unit
             constexpr int J = 4 * P;
             float x[R][J];
@@ -660,9 +650,6 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 up[r] = fmaxf(m[r], top);
                 grew |= up[r] > m[r];
             }
-            // V of this unit is in the next group
-            cp_wait<KS - 2>();
-            __syncwarp();
             float ratio = 1.f, vscale[J];
             if (!BF16) {
                 float vtop = 0.f;
@@ -704,6 +691,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     o[n][3] *= f[R - 1];
                 }
             }
+            scores(ring + (done + 1) % KS * S::kSlot);       // c has been read
             uint32_t pf[P][PPASS][4];
 #pragma unroll
             for (int r = 0; r < R; ++r) {

@@ -8,6 +8,7 @@ current stream.  There is no fallback: without libwici.so or a GPU these calls r
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -20,6 +21,7 @@ WICI_ROPE_NONE, WICI_ROPE_LINEAR, WICI_ROPE_BANDS, WICI_ROPE_YARN = 0, 1, 2, 3
 WICI_KV_BF16, WICI_KV_INT8, WICI_KV_E4M3 = 0, 1, 2
 
 PAGE_TOKENS = 16
+WICI_ATTN_ZEROED = 16384     # bytes at the start of an attention workspace that are zero before its first use
 SCALINGS = {"none": WICI_ROPE_NONE, "linear": WICI_ROPE_LINEAR, "bands": WICI_ROPE_BANDS, "yarn": WICI_ROPE_YARN}
 FORMATS = {"bf16": WICI_KV_BF16, "int8": WICI_KV_INT8, "e4m3": WICI_KV_E4M3}
 _DTYPES = {torch.bfloat16: WICI_BF16, torch.float16: WICI_F16, torch.float32: WICI_F32}
@@ -57,6 +59,7 @@ class wici_attn_shape(ctypes.Structure):
 
 
 _lib = None
+_fast = {}                   # the same entry points taking addresses and packed structures, for `Rope` and `PagedKV`
 
 
 def lib():
@@ -77,6 +80,10 @@ def lib():
         for name in EXPORTS:
             getattr(L, name).restype = ctypes.c_int
         L.wici_kv_page_bytes.restype = i64
+        for name, types in (("wici_rope", [vp, vp, i32, vp, i64, vp, vp]), ("wici_kv_append", [vp, vp, vp, i64] + [vp] * 7),
+                            ("wici_kv_read", [vp, vp, vp, i64, vp, vp, vp]), ("wici_paged_attention", [vp] * 10)):
+            _fast[name] = L[name]          # a function object of its own
+            _fast[name].argtypes, _fast[name].restype = types, ctypes.c_int
         _lib = L
     return _lib
 
@@ -128,35 +135,48 @@ def wici_kv_view(ctx, layer: int):
 
 
 # ------------------------------------------------------------- tensors
-def heads_of(t: torch.Tensor, head_dim: int, device: torch.device, what: str) -> wici_heads:
-    """A [tokens][heads][head_dim] tensor as the library takes it."""
+_pack_heads = struct.Struct("@Pqqii").pack       # a wici_heads
+_pack_shape = struct.Struct("@iiif").pack        # a wici_attn_shape
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _bad_heads(t, head_dim, device, what):
     if t.dim() != 3 or t.shape[2] != head_dim:
         raise ValueError(f"{what}: expected [tokens, heads, {head_dim}], got {tuple(t.shape)}")
-    dtype = _DTYPES.get(t.dtype)
-    if dtype is None:
+    if t.dtype not in _DTYPES:
         raise TypeError(f"{what}: expected bfloat16, float16 or float32, got {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{what}: on {t.device}, expected {device}")
-    token, head, one = t.stride()
-    if one != 1 and head_dim > 1:
-        raise ValueError(f"{what}: the elements of a head are not adjacent")
-    return wici_heads(t.data_ptr(), token, head, t.shape[1], dtype)
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on {t.device}, expected cuda:{device}")
+    raise ValueError(f"{what}: the elements of a head are not adjacent")
 
 
-def _ints(t: torch.Tensor, shape: tuple, device: torch.device, what: str) -> int:
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what}: expected contiguous int32 {list(shape)} on {device}, got {t.dtype} "
+def _heads(t: torch.Tensor, head_dim: int, device: int, what: str):
+    """(token stride, head stride, heads, type) of a [tokens][heads][head_dim] tensor on the device."""
+    shape, stride, code = t.shape, t.stride(), _DTYPES.get(t.dtype)
+    if code is None or len(shape) != 3 or shape[2] != head_dim or t.get_device() != device or stride[2] != 1:
+        _bad_heads(t, head_dim, device, what)
+    return _pack_heads(t.data_ptr(), stride[0], stride[1], shape[1], code)
+
+
+def heads_of(t: torch.Tensor, head_dim: int, device: torch.device, what: str) -> wici_heads:
+    """A [tokens][heads][head_dim] tensor as the library takes it."""
+    return wici_heads.from_buffer_copy(_heads(t, head_dim, -1 if device.type == "cpu" else device.index, what))
+
+
+def _ints(t: torch.Tensor, shape: tuple, device: int, what: str) -> int:
+    if t.dtype != torch.int32 or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what}: expected contiguous int32 {list(shape)} on cuda:{device}, got {t.dtype} "
                          f"{list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _stream(device: torch.device) -> int:
+def _stream(device: int) -> int:
     """torch's current stream; the library launches on the current device."""
-    if device.type != "cuda":
-        raise ValueError(f"expected a CUDA tensor, got one on {device}")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {device} but the current device is cuda:{torch.cuda.current_device()}")
-    return torch.cuda.current_stream(device).cuda_stream
+    if device < 0:
+        raise ValueError("expected CUDA tensors")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"tensors are on cuda:{device} but the current device is cuda:{torch.cuda.current_device()}")
+    return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
 
 
 class Rope:
@@ -171,18 +191,22 @@ class Rope:
         self.plan = wici_rope_make_plan(wici_rope_spec(
             theta, factor, low, high, gain, original_len, head_dim, head_dim if rot_dim is None else rot_dim,
             int(interleaved), SCALINGS[scaling]))
+        self._plan = ctypes.addressof(self.plan)
 
     def apply(self, x: torch.Tensor, positions: torch.Tensor, out: torch.Tensor | None = None,
               inverse: bool = False) -> torch.Tensor:
         """x [tokens, heads, head_dim] rotated by `positions` (int32 [tokens]); with `inverse` the gradient of
         that with respect to x, from the gradient of its result.  `out` may be x."""
-        stream = _stream(x.device)
+        device, d = x.get_device(), self.head_dim
+        stream = _stream(device)
+        hx = _heads(x, d, device, "x")
         if out is None:
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if out.shape != x.shape:
+        elif out.shape != x.shape:
             raise ValueError(f"out: expected {list(x.shape)}, got {list(out.shape)}")
-        wici_rope(stream, self.plan, int(inverse), _ints(positions, x.shape[:1], x.device, "positions"), x.shape[0],
-                  heads_of(x, self.head_dim, x.device, "x"), heads_of(out, self.head_dim, x.device, "out"))
+        n = x.shape[0]
+        _check(_fast["wici_rope"](stream, self._plan, 1 if inverse else 0, _ints(positions, (n,), device, "positions"), n,
+                                  hx, _heads(out, d, device, "out")))
         return out
 
 
@@ -204,10 +228,11 @@ class PagedKV:
             data = torch.zeros(n_pages * page, dtype=torch.uint8, device=device or "cuda")
         if data.dtype != torch.uint8 or not data.is_contiguous() or data.numel() % page:
             raise ValueError(f"data: expected contiguous uint8 in whole pages of {page} bytes")
-        self.data, self.device = data, data.device
+        self.data, self.device, self._device = data, data.device, data.get_device()
         self.n_pages = data.numel() // page
         self.cache = wici_kv_cache(data.data_ptr(), page, self.n_pages, n_kv_heads, head_dim, FORMATS[fmt])
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._cache, self._status = ctypes.addressof(self.cache), self.status.data_ptr()
         self._workspaces = {}
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, rope: Rope | None = None,
@@ -216,37 +241,38 @@ class PagedKV:
         """Write k, v [tokens, n_kv_heads, head_dim] at `slots` (int32 [tokens], distinct; negative: skipped).
         With a rope, k is rotated by `positions` on the way, and q into q_out, which is returned (a new tensor
         unless given; it may be q)."""
-        stream, d, dev = _stream(self.device), self.head_dim, self.device
+        dev, d = self._device, self.head_dim
+        stream = _stream(dev)
         n = k.shape[0]
         if v.shape[0] != n:
             raise ValueError(f"v: expected {n} tokens, got {v.shape[0]}")
-        qh = oh = pos = None
+        hq = ho = None
         if q is not None:
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
             if q.shape[0] != n or q_out.shape != q.shape:
                 raise ValueError(f"q, q_out: expected {n} tokens and one shape, got {list(q.shape)}, {list(q_out.shape)}")
-            qh, oh = heads_of(q, d, dev, "q"), heads_of(q_out, d, dev, "q_out")
+            hq, ho = _heads(q, d, dev, "q"), _heads(q_out, d, dev, "q_out")
         elif q_out is not None:
             raise ValueError("q_out without q")
-        if positions is not None:
-            pos = _ints(positions, (n,), dev, "positions")
-        wici_kv_append(stream, self.cache, _ints(slots, (n,), dev, "slots"), n, heads_of(k, d, dev, "k"),
-                       heads_of(v, d, dev, "v"), None if rope is None else rope.plan, pos, qh, oh,
-                       self.status.data_ptr())
+        _check(_fast["wici_kv_append"](
+            stream, self._cache, _ints(slots, (n,), dev, "slots"), n, _heads(k, d, dev, "k"), _heads(v, d, dev, "v"),
+            None if rope is None else rope._plan, None if positions is None else _ints(positions, (n,), dev, "positions"),
+            hq, ho, self._status))
         return q_out
 
     def read(self, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out=None):
         """(k, v) [slots, n_kv_heads, head_dim] at `slots` (int32; negative: zeros), into `out` when given."""
-        stream, d, dev = _stream(self.device), self.head_dim, self.device
+        dev, d = self._device, self.head_dim
+        stream = _stream(dev)
         n = slots.shape[0]
         if out is None:
-            out = tuple(torch.empty((n, self.n_kv_heads, d), dtype=dtype, device=dev) for _ in range(2))
+            out = tuple(torch.empty((n, self.n_kv_heads, d), dtype=dtype, device=self.device) for _ in range(2))
         k, v = out
         if k.shape[0] != n or v.shape[0] != n:
             raise ValueError(f"out: expected {n} tokens, got {k.shape[0]} and {v.shape[0]}")
-        wici_kv_read(stream, self.cache, _ints(slots, (n,), dev, "slots"), n, heads_of(k, d, dev, "k"),
-                     heads_of(v, d, dev, "v"), self.status.data_ptr())
+        _check(_fast["wici_kv_read"](stream, self._cache, _ints(slots, (n,), dev, "slots"), n, _heads(k, d, dev, "k"),
+                                     _heads(v, d, dev, "v"), self._status))
         return k, v
 
     def attend(self, q: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor, scale: float | None = None,
@@ -256,35 +282,39 @@ class PagedKV:
         `window` of them, 0: all) of the pages pages[b] (int32 [batch, max_pages]).  scale: head_dim ** -0.5 unless
         given.  Fills lse (float32 [batch, heads]) when given.  The workspace, unless given (`workspace()`), is one
         per stream, or in a graph capture one of that call's own."""
-        stream, d, dev = _stream(self.device), self.head_dim, self.device
-        batch = q.shape[0]
+        dev, d = self._device, self.head_dim
+        stream = _stream(dev)
+        hq = _heads(q, d, dev, "q")
+        batch, heads, _ = q.shape
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        if out.shape[0] < batch:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        elif out.shape[0] < batch:
             raise ValueError(f"out: {out.shape[0]} rows for a batch of {batch}")
-        if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or
-                                lse.device != dev):
-            raise ValueError(f"lse: expected contiguous float32 {list(q.shape[:2])} on {dev}")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (batch, heads) or not lse.is_contiguous() or
+                                lse.get_device() != dev):
+            raise ValueError(f"lse: expected contiguous float32 {[batch, heads]} on cuda:{dev}")
         if pages.dim() != 2:
             raise ValueError("pages: expected [batch, max_pages]")
-        heads = q.shape[1]
         if workspace is None:
             workspace = self._workspace_for(stream, heads, batch)
-        elif workspace.device != dev or workspace.numel() * workspace.element_size() < self.workspace_bytes(heads, batch):
-            raise ValueError(f"workspace: expected {self.workspace_bytes(heads, batch)} bytes on {dev}")
-        shape = wici_attn_shape(batch, pages.shape[1], window, d ** -0.5 if scale is None else scale)
-        wici_paged_attention(stream, self.cache, shape, _ints(pages, (batch, pages.shape[1]), dev, "pages"),
-                             _ints(lengths, (batch,), dev, "lengths"), heads_of(q, d, dev, "q"),
-                             heads_of(out, d, dev, "out"), None if lse is None else lse.data_ptr(),
-                             workspace.data_ptr(), self.status.data_ptr())
+        elif workspace.get_device() != dev or not workspace.is_contiguous() or \
+                workspace.numel() * workspace.element_size() < self.workspace_bytes(heads, batch):
+            raise ValueError(f"workspace: expected {self.workspace_bytes(heads, batch)} bytes on cuda:{dev}")
+        columns = pages.shape[1]
+        shape = _pack_shape(batch, columns, window, d ** -0.5 if scale is None else scale)
+        _check(_fast["wici_paged_attention"](
+            stream, self._cache, shape, _ints(pages, (batch, columns), dev, "pages"), _ints(lengths, (batch,), dev, "lengths"),
+            hq, _heads(out, d, dev, "out"), None if lse is None else lse.data_ptr(), workspace.data_ptr(), self._status))
         return out
 
     def workspace_bytes(self, n_q_heads: int, batch: int) -> int:
         return wici_paged_attention_workspace_bytes(self.cache, n_q_heads, batch)
 
     def workspace(self, n_q_heads: int, batch: int) -> torch.Tensor:
-        """A zeroed workspace of attend's, for calls that are ordered with each other."""
-        return torch.zeros(self.workspace_bytes(n_q_heads, batch), dtype=torch.uint8, device=self.device)
+        """A workspace of attend's, for calls that are ordered with each other."""
+        ws = torch.empty(self.workspace_bytes(n_q_heads, batch), dtype=torch.uint8, device=self.device)
+        ws[:WICI_ATTN_ZEROED].zero_()
+        return ws
 
     def _workspace_for(self, stream: int, n_q_heads: int, batch: int) -> torch.Tensor:
         if torch.cuda.is_current_stream_capturing():
