@@ -39,7 +39,7 @@ constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = 32 * kAttnWarps;
 constexpr int kAttnMaxBatch = 256;    // sequences of a launch: their keys are in shared memory
 constexpr uint32_t kAttnSegment = 3;       // units that a segment weighs beside its own
-constexpr uint32_t kAttnMinUnits = 8;      // weight of a warp's run at least: shorter ones would not pay for joining more parts
+constexpr uint32_t kAttnMinUnits = 3;      // weight of a warp's run at least: shorter ones would not pay for joining more parts
 constexpr int kAttnPieceRows = 16;    // rows of a piece in the workspace (a head tile has 8 or 16)
 
 struct AttnArg {
@@ -63,12 +63,12 @@ constexpr size_t attn_piece_floats(int d) { return (size_t)kAttnPieceRows * (d +
 template <int FMT, int D, bool STACK>
 struct AttnShape {
     static constexpr int kRows = STACK ? 8 : 16;                   // queries of a head tile
-    static constexpr int kPages = FMT == WICI_KV_BF16 && D == 128 ? 1 : 2;                // of a unit
-    static constexpr int kBlocks = FMT != WICI_KV_BF16 && D == 64 && STACK ? 3 : 2;   // on an SM
+    static constexpr int kPages = FMT == WICI_KV_BF16 ? (D == 128 ? 1 : 2) : (D == 128 ? 2 : 4);                // of a unit
+    static constexpr int kBlocks = 2;   // on an SM
     static constexpr int kBlock = attn_block(FMT, D);
     static constexpr int kSlot = kPages * kBlock;
     // ring slots of K and of V: what fits beside the parts to be joined
-    static constexpr int kKSlots = FMT != WICI_KV_BF16 && D == 64 ? 4 : 3;
+    static constexpr int kKSlots = 3;
     static constexpr int kVSlots = kKSlots - 1;
     static constexpr int kRing = (kKSlots + kVSlots) * kSlot;
     static constexpr int kPartRow = D + 4;                         // floats: neighbouring rows in other banks
@@ -79,8 +79,10 @@ struct AttnShape {
 };
 
 // ------------------------------------------------------------------ PTX ----
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, int bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, int bytes, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(bytes),
+                 "l"(policy)
+                 : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -141,6 +143,13 @@ __device__ __forceinline__ uint32_t split2(float &lo, float &hi) {
     return w;
 }
 
+// int8 codes c as the fp16 numbers (c + 128) 2^-24, exactly: two operations fewer a pair
+__device__ __forceinline__ void decode4_raised(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    const uint32_t x = w ^ 0x80808080u;
+    lo = __byte_perm(x, 0, 0x4140);
+    hi = __byte_perm(x, 0, 0x4342);
+}
+
 // Where 16-byte chunk c of key row r stands in a ring slot.  The chunks of a row are permuted so
 // that the 8 lanes of a shared-memory phase, which take rows i and i + 4 (K), or rows 0..3 and
 // neighbouring chunks (V), meet 8 different bank groups.  Rows of 64 bytes share a line of 128 in pairs.
@@ -197,38 +206,30 @@ __device__ __forceinline__ void unpack_q8(int dtype, const uint4 *v, float *x) {
         }
     }
 }
+// 4 elements of the result, element by element: heads that are not 16-byte aligned
+static __device__ __noinline__ void store_out4_narrow(const HeadsArg &out, int dtype, int64_t token, int head, int i, float4 v) {
+    const float f[4] = {v.x, v.y, v.z, v.w};
+    for (int j = 0; j < 4; ++j) {
+        if (dtype == WICI_F32) out.row<float>(token, head)[i + j] = f[j];
+        else if (dtype == WICI_F16) out.row<__half>(token, head)[i + j] = __float2half_rn(f[j]);
+        else out.row<__nv_bfloat16>(token, head)[i + j] = __float2bfloat16_rn(f[j]);
+    }
+}
 __device__ __forceinline__ void store_out4(const AttnArg &a, int64_t token, int head, int i, const float *v) {
-    switch (a.out_dtype) {
-        case WICI_F32: {
-            float *p = a.out.row<float>(token, head) + i;
-            if (a.out_wide) {
-                *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
-            } else {
-                for (int j = 0; j < 4; ++j) p[j] = v[j];
-            }
-            break;
+    if (!a.out_wide) {
+        store_out4_narrow(a.out, a.out_dtype, token, head, i, make_float4(v[0], v[1], v[2], v[3]));
+    } else if (a.out_dtype == WICI_F32) {
+        *(float4 *)(a.out.row<float>(token, head) + i) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+        uint2 w;
+        if (a.out_dtype == WICI_F16) {
+            const __half2 lo = __floats2half2_rn(v[0], v[1]), hi = __floats2half2_rn(v[2], v[3]);
+            w = make_uint2(*(const uint32_t *)&lo, *(const uint32_t *)&hi);
+        } else {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+            w = make_uint2(*(const uint32_t *)&lo, *(const uint32_t *)&hi);
         }
-        case WICI_F16: {
-            __half *p = a.out.row<__half>(token, head) + i;
-            alignas(8) __half e[4];
-            for (int j = 0; j < 4; ++j) from_f32(v[j], e[j]);
-            if (a.out_wide) {
-                *(uint2 *)p = *(const uint2 *)e;
-            } else {
-                for (int j = 0; j < 4; ++j) p[j] = e[j];
-            }
-            break;
-        }
-        default: {
-            __nv_bfloat16 *p = a.out.row<__nv_bfloat16>(token, head) + i;
-            alignas(8) __nv_bfloat16 e[4];
-            for (int j = 0; j < 4; ++j) from_f32(v[j], e[j]);
-            if (a.out_wide) {
-                *(uint2 *)p = *(const uint2 *)e;
-            } else {
-                for (int j = 0; j < 4; ++j) p[j] = e[j];
-            }
-        }
+        *(uint2 *)(a.out.row<uint16_t>(token, head) + i) = w;
     }
 }
 
@@ -256,6 +257,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     constexpr int SETS = P == 1 ? 2 : 1;                  // accumulators of a score: four chains of products at least
     constexpr int KS = S::kKSlots, VS = S::kVSlots;
     constexpr int PER = BF16 || D == 64 ? 8 : 16;         // adjacent elements of O that a lane holds per column
+    // K's int8 codes raised by 128: q times 128 is taken off the score again, which costs it 2 bits.  fp32 in: not so.
+    constexpr bool RAISED = FMT == WICI_KV_INT8 && !EXACT;
     constexpr float kPUnit = BF16 ? 1.f : 4096.f;         // what weights are scaled up by (fp16: far from its smallest)
 
     extern __shared__ __align__(128) uint8_t smem[];
@@ -382,13 +385,13 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 
     // ---- issue side: lane l knows unit 32 k + l of this warp's ----
     struct Desc {
-        int page[P];   // -1: bad; -2: past the sequence's end
+        int page[P];   // as the table has it; -1 past the sequence's end
         int info;      // kv head | first valid row << 16 | rows end << 24
     };
     auto describe = [&](int i) {
         Desc d;
 #pragma unroll
-        for (int p = 0; p < P; ++p) d.page[p] = -2;
+        for (int p = 0; p < P; ++p) d.page[p] = -1;
         d.info = 0;
         if (i >= mine) return d;
         const Rec s = segment_at(r0 + i);
@@ -398,10 +401,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
         const int32_t *row = a.pages + (int64_t)b * a.max_pages;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            if ((first_page + p) * (int64_t)kKvPage < k.n) {
-                d.page[p] = row[first_page + p];
-                if (d.page[p] < 0 || d.page[p] >= a.cache.n_pages) d.page[p] = -1;
-            }
+            if ((first_page + p) * (int64_t)kKvPage < k.n) d.page[p] = row[first_page + p];
         }
         const int first = max(0, k.lo - first_page * kKvPage), end = min(UNIT, k.n - first_page * kKvPage);
         d.info = head / a.tiles | first << 16 | end << 24;
@@ -414,6 +414,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     bool last = false;
 
     // one page's block of K or V: rows without a key of the sequence are zeroed, what the cache holds there is anything
+    const uint64_t policy = l2_evict_first();   // read once: code, queries and parts stay in L2 instead
     const uint32_t lane_dst = chunk_at<ROW>(lane / CHUNKS, lane % CHUNKS);
     auto copy_block = [&](uint32_t dst, int page, int64_t block, int first, int end) {
         constexpr int N = kKvPage * CHUNKS / 32, ROWS = 32 / CHUNKS;   // rows of one round of the warp
@@ -421,17 +422,17 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
         if (first <= 0 && end >= kKvPage) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                cp_async16(dst + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src + i * 512 + lane * 16, 16);
+                cp_async16(dst + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src + i * 512 + lane * 16, 16, policy);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int r = i * ROWS + lane / CHUNKS;
                 cp_async16(dst + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src + i * 512 + lane * 16,
-                           r >= first && r < end ? 16 : 0);
+                           r >= first && r < end ? 16 : 0, policy);
             }
         }
         if (!BF16 && lane < 4)
-            cp_async16(dst + kKvPage * D + lane * 16, src + kKvPage * D + lane * 16, page < 0 ? 0 : 16);
+            cp_async16(dst + kKvPage * D + lane * 16, src + kKvPage * D + lane * 16, page < 0 ? 0 : 16, policy);
     };
     auto copy_unit = [&](uint32_t dst, const int *page, int info, int side) {
         const int first = info >> 16 & 255, end = info >> 24;
@@ -446,14 +447,17 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             cur = next;
             next = describe(issued + 32 + lane);
         }
+        const int info = __shfl_sync(0xffffffffu, cur.info, issued & 31);
         int page[P];
         bool bad = false;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             page[p] = __shfl_sync(0xffffffffu, cur.page[p], issued & 31);
-            bad |= page[p] == -1;
+            if ((uint32_t)page[p] >= (uint32_t)a.cache.n_pages) {
+                bad |= info >> 24 > p * kKvPage;             // one that the sequence needs
+                page[p] = -1;
+            }
         }
-        const int info = __shfl_sync(0xffffffffu, cur.info, issued & 31);
         if (issued < mine) {
             copy_unit(ring + issued % KS * S::kSlot, page, info, 0);
             if (bad) {
@@ -514,7 +518,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 
         // ---- Q fragments ----
         uint32_t qf[QPASS][STEPS][4];
-        float cq[R];                      // products to base-2 logits
+        float cq[R], q128[R];             // products to base-2 logits; what RAISED takes off them first
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             cq[r] = a.scale * 1.44269504088896340736f;
@@ -538,6 +542,17 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 for (int s = 0; s < STEPS; ++s)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) x[s][j] *= down;
+            }
+            if (RAISED) {
+                float sum = 0.f;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum += x[s][j];
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                q128[r] = sum * (128.f * 0x1p-24f);
+                cq[r] *= 0x1p24f;
             }
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
@@ -591,7 +606,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
                         for (int s = 0; s < 4; ++s) {
                             uint32_t b0, b1;
-                            decode4<FMT>(word[s], b0, b1);
+                            if (RAISED) decode4_raised(word[s], b0, b1);
+                            else decode4<FMT>(word[s], b0, b1);
 #pragma unroll
                             for (int k = 0; k < QPASS; ++k) mma16816<false>(c[n][0], qf[k][4 * i + s], b0, b1);
                         }
@@ -627,6 +643,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                         dot += c[n][0][col + 2];
                         if (SETS == 2) dot += c[n][SETS - 1][col + 2];
                     }
+                    if (RAISED) dot -= q128[r];
                     x[r][j] = dot * (BF16 ? cq[r] : ksc * cq[r]);
                 }
             }
@@ -878,40 +895,51 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             }
         }
     }
-    // the one that this block's run starts in the middle of, and the one it ends in the middle of
+    // the one that this block's run starts in the middle of, and the one it ends in the middle of: the blocks that
+    // hold it count their arrivals, and the last one joins all pieces, in order
+    if (sh.side[0].end == 0 && sh.side[1].end == 0) return;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        const int side = threadIdx.x;
+        bool final_one = false;
+        if (sh.side[side].end != 0) {
+            int *ticket = a.tickets + sh.first[side];
+            final_one = atomicAdd(ticket, 1) == sh.last[side] - sh.first[side];
+            if (final_one) *ticket = 0;
+        }
+        sh.note[side] = final_one;
+    }
+    __syncthreads();
     for (int side = 0; side < 2; ++side) {
-        const Rec s = sh.side[side];
-        if (s.end == 0) continue;
-        // blocks i0 .. i1 hold it; the one that arrives last joins their pieces in order
-        const int i0 = sh.first[side], i1 = sh.last[side];
+        if (!sh.note[side]) continue;
         __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const int n = atomicAdd(a.tickets + i0, 1);
-            sh.note[0] = n == i1 - i0;
-            if (n == i1 - i0) a.tickets[i0] = 0;
-        }
-        __syncthreads();
-        if (sh.note[0]) {
-            __threadfence();
-            auto piece_of = [&](int p) { return a.pieces + ((int64_t)p * 2 + (p == i0)) * attn_piece_floats(D); };
-            for (int i = threadIdx.x; i < rows_of(s) * (D / 4); i += kAttnThreads) {
-                const int row = i / (D / 4), d0 = i % (D / 4) * 4;
-                float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+        const Rec s = sh.side[side];
+        const int i0 = sh.first[side], i1 = sh.last[side];
+        auto piece_of = [&](int p) { return a.pieces + ((int64_t)p * 2 + (p == i0)) * attn_piece_floats(D); };
+        // a warp per row: a lane looks after a piece's weight, then after 4 of the row's elements
+        for (int row = warp; row < rows_of(s); row += kAttnWarps) {
+            float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int from = i0; from <= i1; from += 32) {
+                const int here = min(32, i1 + 1 - from);
+                float2 ml = make_float2(-INFINITY, 0.f);
+                if (lane < here) ml = __ldcg((const float2 *)(piece_of(from + lane) + kAttnPieceRows * D) + row);
+                const float up = fmaxf(top, warp_max(ml.x)), was = top == -INFINITY ? 0.f : ex2(top - up);
+                const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - up);
+                sum = sum * was + warp_sum(ml.y * f);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] *= was;
+                top = up;
 #pragma unroll 8
-                for (int p = i0; p <= i1; ++p) top = fmaxf(top, __ldcg((const float2 *)(piece_of(p) + kAttnPieceRows * D) + row).x);
-#pragma unroll 8
-                for (int p = i0; p <= i1; ++p) {
-                    const float2 ml = __ldcg((const float2 *)(piece_of(p) + kAttnPieceRows * D) + row);
-                    const float4 q = __ldcg((const float4 *)(piece_of(p) + row * D + d0));
-                    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
-                    sum += ml.y * f;
-                    v[0] += q.x * f, v[1] += q.y * f, v[2] += q.z * f, v[3] += q.w * f;
+                for (int p = 0; p < here; ++p) {
+                    const float fp = __shfl_sync(0xffffffffu, f, p);
+                    float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (lane < D / 4) q = __ldcg((const float4 *)(piece_of(from + p) + row * D) + lane);
+                    v[0] += q.x * fp, v[1] += q.y * fp, v[2] += q.z * fp, v[3] += q.w * fp;
                 }
-                finish(s, row, d0, v, top, sum);
             }
+            if (lane < D / 4) finish(s, row, 4 * lane, v, top, sum);
         }
-        __syncthreads();                                    // note is free again
     }
 }
 
