@@ -14,7 +14,8 @@
  *   - Work is enqueued on cuda_stream (a cudaStream_t, NULL for the legacy
  *     stream) of the current device and the call does not synchronise; every
  *     device pointer belongs to that device.  Every launch can be captured into
- *     a CUDA graph.  No call allocates.
+ *     a CUDA graph (make a device's first wici_paged_attention or
+ *     wici_paged_attention_workspace_bytes before the capture).  No call allocates.
  *   - What the host cannot check without a copy (slots, page numbers, lengths)
  *     is checked by the kernels: nothing outside the cache is read or written,
  *     and `status` (device int32, may be NULL) collects WICI_BAD_* bits.  The
@@ -104,11 +105,11 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
  *   WICI_KV_INT8  int8 [16][head_dim], then fp32 scale[16]
  *   WICI_KV_E4M3  e4m3 [16][head_dim], then fp32 scale[16]
  * A token's head stands for code * scale; it is written with scale = max|x| / 127
- * (int8) or / 448 (e4m3) in fp32 and code = x / scale (an fp32 product with 1 / scale)
- * rounded to nearest even; a head whose scale would be below 2^-126, one of zeros
- * among them, has scale 0, and one that holds an infinity or NaN has scale NaN (it
- * reads as NaN throughout).  Slot s is place s % 16 of page s / 16.  The paper
- * names no cache precision; 8-bit codes halve the bytes that bound decoding. */
+ * (int8) or / 448 (e4m3) in fp32 and code = x / scale rounded to nearest even.  A
+ * head whose scale would be below 2^-126, one of zeros among them, has scale 0, and
+ * one that holds an infinity or NaN has scale NaN (it reads as NaN throughout).
+ * Slot s is place s % 16 of page s / 16.  The paper names no cache precision; 8-bit
+ * codes halve the bytes that bound decoding. */
 enum { WICI_KV_BF16 = 0, WICI_KV_INT8 = 1, WICI_KV_E4M3 = 2 };
 
 typedef struct wici_kv_cache {

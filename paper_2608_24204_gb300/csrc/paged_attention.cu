@@ -24,7 +24,8 @@ int fail(int code, const char *fmt, ...) {
 
 DeviceTable<int> g_sms;
 
-int sm_count(int *n) {
+// the current device's SMs, with the kernels' shared-memory limits set there
+int device_sms(int *n) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = g_sms.get(dev, n, [dev](int *d) {
@@ -38,10 +39,10 @@ int sm_count(int *n) {
 }
 
 constexpr int kTicketBytes = WICI_ATTN_ZEROED;   // arrivals of every block: zero before the first launch, and after each
-constexpr int kMaxBlocksPerSm = 3;
+constexpr int kBlocksPerSm = AttnShape<WICI_KV_BF16, 128, true>::kBlocks;   // of every kernel
 // SMs that a launch uses: tickets are for so many blocks
 int used_sms(int sms) {
-    const int most = kTicketBytes / (int)sizeof(int) / kMaxBlocksPerSm;
+    const int most = kTicketBytes / (int)sizeof(int) / kBlocksPerSm;
     return sms < most ? sms : most;
 }
 
@@ -63,11 +64,11 @@ int wici_paged_attention_workspace_bytes(const wici_kv_cache *cache, int32_t n_q
     int sms = 152;   // without a device: a GB300's
     int dev = 0;
     if (cudaGetDevice(&dev) == cudaSuccess) {
-        if (int rc = sm_count(&sms)) return rc;
+        if (int rc = device_sms(&sms)) return rc;
     } else {
         cudaGetLastError();
     }
-    *bytes = kTicketBytes + (size_t)used_sms(sms) * kMaxBlocksPerSm * 2 * attn_piece_floats(cache->head_dim) * sizeof(float);
+    *bytes = kTicketBytes + (size_t)used_sms(sms) * kBlocksPerSm * 2 * attn_piece_floats(cache->head_dim) * sizeof(float);
     return WICI_OK;
 }
 
@@ -92,7 +93,7 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     if (!pages || !lengths || !workspace || ((uintptr_t)workspace & 15))
         return fail(WICI_E_ARG, "attention: null pages or lengths, or workspace null or not 16-byte aligned");
     int sms = 0;
-    if (int rc = sm_count(&sms)) return rc;
+    if (int rc = device_sms(&sms)) return rc;
     AttnArg a = {};
     a.q = heads_arg(q);
     a.out = heads_arg(out);
@@ -102,8 +103,10 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     a.pieces = (float *)((uint8_t *)workspace + kTicketBytes);
     a.q_heads = q->heads;
     a.group = q->heads / cache->n_kv_heads;
-    const bool stack = a.group <= 8;
-    a.tiles = stack ? 1 : (a.group + 15) / 16;
+    // more terms where fp32 comes in or, over a bf16 cache, goes out or q is not bf16
+    const bool exact = cache->format == WICI_KV_BF16 ? q->dtype != WICI_BF16 || out->dtype == WICI_F32 : q->dtype == WICI_F32;
+    const AttnKind kind = attn_kind(a.group, exact);
+    a.tiles = kind == ATTN_PLAIN ? (a.group + 15) / 16 : (a.group + 7) / 8;
     a.max_pages = shape->max_pages;
     a.window = shape->window;
     a.q_dtype = q->dtype;
@@ -111,8 +114,6 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     a.q_wide = wide_heads(q);
     a.out_wide = wide_heads(out);
     a.scale = shape->scale;
-    // more terms where fp32 comes in or, over a bf16 cache, goes out or q is not bf16
-    const bool exact = cache->format == WICI_KV_BF16 ? q->dtype != WICI_BF16 || out->dtype == WICI_F32 : q->dtype == WICI_F32;
     // the weight of a launch's segments adds up in 31 bits
     const int64_t each = ((int64_t)shape->max_pages + kAttnSegment) * cache->n_kv_heads * a.tiles, room = INT32_MAX / each;
     const int most = room < 1 ? 1 : room < kAttnMaxBatch ? (int)room : kAttnMaxBatch;
@@ -126,9 +127,9 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
         a.q.data = (uint8_t *)q->data + (int64_t)b * q->token_stride * dtype_bytes(q->dtype);
         a.out.data = (uint8_t *)out->data + (int64_t)b * out->token_stride * dtype_bytes(out->dtype);
         switch (cache->format) {
-            case WICI_KV_BF16: e = launch_attention_bf16(cache->head_dim, a, stack, exact, used_sms(sms), st); break;
-            case WICI_KV_INT8: e = launch_attention_int8(cache->head_dim, a, stack, exact, used_sms(sms), st); break;
-            default: e = launch_attention_e4m3(cache->head_dim, a, stack, exact, used_sms(sms), st); break;
+            case WICI_KV_BF16: e = launch_attention_bf16(cache->head_dim, a, kind, used_sms(sms), st); break;
+            case WICI_KV_INT8: e = launch_attention_int8(cache->head_dim, a, kind, used_sms(sms), st); break;
+            default: e = launch_attention_e4m3(cache->head_dim, a, kind, used_sms(sms), st); break;
         }
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "attention: %s", cudaGetErrorString(e));

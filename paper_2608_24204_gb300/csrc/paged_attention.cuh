@@ -63,13 +63,14 @@ constexpr size_t attn_piece_floats(int d) { return (size_t)kAttnPieceRows * (d +
 template <int FMT, int D, bool STACK>
 struct AttnShape {
     static constexpr int kRows = STACK ? 8 : 16;                   // queries of a head tile
-    static constexpr int kPages = FMT == WICI_KV_BF16 ? (D == 128 ? 1 : 2) : (D == 128 ? 2 : 4);                // of a unit
-    static constexpr int kBlocks = 2;   // on an SM
+    // Pages of a unit: 4 to 8 KB of K and V for the work that a unit costs beside its products (bf16, 128: one page
+    // already; 8-bit: one page more a unit took the batch of 64 from 136 to 116 us with 128, from 76 to 74 with 64).
+    static constexpr int kPages = FMT == WICI_KV_BF16 ? (D == 128 ? 1 : 2) : (D == 128 ? 2 : 4);
     static constexpr int kBlock = attn_block(FMT, D);
     static constexpr int kSlot = kPages * kBlock;
-    // ring slots of K and of V: what fits beside the parts to be joined
-    static constexpr int kKSlots = 3;
-    static constexpr int kVSlots = kKSlots - 1;
+    // Two blocks on an SM, 8 warps with 250 registers each: three of 168 spill (131 us in place of 116).
+    static constexpr int kBlocks = 2;
+    static constexpr int kKSlots = 3, kVSlots = kKSlots - 1;       // of the ring: about 100 KB on their way per SM
     static constexpr int kRing = (kKSlots + kVSlots) * kSlot;
     static constexpr int kPartRow = D + 4;                         // floats: neighbouring rows in other banks
     static constexpr int kPart = kRows * (kPartRow + 2) * 4;       // a part of a segment: O, then m and l of each row
@@ -943,10 +944,19 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     }
 }
 
+// The kernels of a format.  A group of more than 8 queries takes 16 a tile where its terms are few, and tiles of 8
+// (each with its own pass over the keys) where they are many: with 16 a tile the terms of fp32 do not fit the
+// registers.  16 sequences of 1000 to 4000 tokens, 16 queries a group, head_dim 128, fp32: 51 us in tiles of 8, 64 in
+// tiles of 16; 12 queries, bf16, 32 sequences: 93 and 64.
+enum AttnKind { ATTN_STACK, ATTN_STACK_EXACT, ATTN_PLAIN };
+inline AttnKind attn_kind(int group, bool exact) {
+    return exact ? ATTN_STACK_EXACT : group <= 8 ? ATTN_STACK : ATTN_PLAIN;
+}
+
 // Launches, and kernel limits of the current device; one translation unit per format.
-cudaError_t launch_attention_bf16(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st);
-cudaError_t launch_attention_int8(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st);
-cudaError_t launch_attention_e4m3(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st);
+cudaError_t launch_attention_bf16(int d, const AttnArg &a, AttnKind kind, int sms, cudaStream_t st);
+cudaError_t launch_attention_int8(int d, const AttnArg &a, AttnKind kind, int sms, cudaStream_t st);
+cudaError_t launch_attention_e4m3(int d, const AttnArg &a, AttnKind kind, int sms, cudaStream_t st);
 cudaError_t setup_attention_bf16();
 cudaError_t setup_attention_int8();
 cudaError_t setup_attention_e4m3();

@@ -4,23 +4,22 @@
 namespace wici {
 
 template <int D>
-static cudaError_t launch_d(const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st) {
-    if (stack)
-        return exact ? launch_attention<WICI_KV_INT8, D, true, true>(a, sms, st)
-                     : launch_attention<WICI_KV_INT8, D, true, false>(a, sms, st);
-    return exact ? launch_attention<WICI_KV_INT8, D, false, true>(a, sms, st)
-                 : launch_attention<WICI_KV_INT8, D, false, false>(a, sms, st);
+static cudaError_t launch_d(const AttnArg &a, AttnKind kind, int sms, cudaStream_t st) {
+    switch (kind) {
+        case ATTN_STACK: return launch_attention<WICI_KV_INT8, D, true, false>(a, sms, st);
+        case ATTN_STACK_EXACT: return launch_attention<WICI_KV_INT8, D, true, true>(a, sms, st);
+        default: return launch_attention<WICI_KV_INT8, D, false, false>(a, sms, st);
+    }
 }
 
-cudaError_t launch_attention_int8(int d, const AttnArg &a, bool stack, bool exact, int sms, cudaStream_t st) {
-    return d == 64 ? launch_d<64>(a, stack, exact, sms, st) : launch_d<128>(a, stack, exact, sms, st);
+cudaError_t launch_attention_int8(int d, const AttnArg &a, AttnKind kind, int sms, cudaStream_t st) {
+    return d == 64 ? launch_d<64>(a, kind, sms, st) : launch_d<128>(a, kind, sms, st);
 }
 
 template <int D>
 static cudaError_t setup_d() {
-    cudaError_t e = limit_attention<WICI_KV_INT8, D, true, true>();
-    if (e == cudaSuccess) e = limit_attention<WICI_KV_INT8, D, true, false>();
-    if (e == cudaSuccess) e = limit_attention<WICI_KV_INT8, D, false, true>();
+    cudaError_t e = limit_attention<WICI_KV_INT8, D, true, false>();
+    if (e == cudaSuccess) e = limit_attention<WICI_KV_INT8, D, true, true>();
     if (e == cudaSuccess) e = limit_attention<WICI_KV_INT8, D, false, false>();
     return e;
 }

@@ -234,6 +234,8 @@ class PagedKV:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._cache, self._status = ctypes.addressof(self.cache), self.status.data_ptr()
         self._workspaces = {}
+        if self._device >= 0 and self._device == torch.cuda.current_device():
+            self.workspace_bytes(n_kv_heads, 1)   # sets the attention kernels up, before a capture may need them
 
     def append(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, rope: Rope | None = None,
                positions: torch.Tensor | None = None, q: torch.Tensor | None = None,

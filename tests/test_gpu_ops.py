@@ -644,3 +644,56 @@ def test_a_contexts_cache_read_attended_and_quantised():
     with pytest.raises(ValueError):
         model.read_kv(0, first=40, count=6)
     model.close()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("group,d", [(9, 64), (16, 128), (33, 64)])
+def test_attention_of_large_groups_in_fp32(fmt, group, d):
+    # more than 8 queries to a KV head with more terms than a tile of 16 holds; odd counts leave a ragged last tile
+    rng = np.random.default_rng(group)
+    lengths = [130, 0, 61, 300]
+    cache, q, pages, vals = attention_case(rng, 4, 2, group, d, fmt, "f32", lengths)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    out = cache.attend(q, ints(pages), ints(lengths), lse=lse, window=140)
+    check_attention(cache, q, pages, lengths, vals, d ** -0.5, 140, out, lse, "f32")
+
+
+@pytest.mark.parametrize("fmt,d", [("bf16", 64), ("bf16", 128), ("int8", 64), ("int8", 128), ("e4m3", 64), ("e4m3", 128)])
+def test_attention_at_every_window_around_a_units_ends(fmt, d):
+    # a unit is 1 to 4 pages: windows and lengths that begin and end in each of them
+    rng = np.random.default_rng(24)
+    lengths = list(range(60, 70)) + [128, 129, 1, 2]
+    cache, q, pages, vals = attention_case(rng, len(lengths), 1, 2, d, fmt, "bf16", lengths)
+    for window in (1, 15, 16, 17, 47, 48, 49, 63, 64, 65):
+        out = cache.attend(q, ints(pages), ints(lengths), window=window)
+        check_attention(cache, q, pages, lengths, vals, d ** -0.5, window, out, None, "bf16")
+
+
+def test_equal_sequences_give_equal_results_wherever_their_runs_are_cut():
+    # 40 sequences share one table row: the splits differ, the sums' order with them, the values only by rounding
+    rng = np.random.default_rng(25)
+    cache, q, pages, vals = attention_case(rng, 1, 2, 3, 64, "bf16", "f32", [777])
+    out = cache.attend(q.expand(40, -1, -1).contiguous(), ints(np.repeat(pages, 40, 0)), ints([777] * 40))
+    for b in (0, 1, 13, 39):
+        check_attention(cache, q, pages, [777], vals, 0.125, 0, out[b:b + 1], None, "f32")
+    assert bool(((out - out[:1]).abs() <= 2.0 ** -15).all())
+
+
+def test_keys_whose_codes_are_small_beside_one_outlier():
+    # a head whose scale one element sets: the other codes are 0 or 1, and an int8 score is the difference of larger sums
+    rng = np.random.default_rng(26)
+    n = 200
+    x = rng.normal(size=(n, 1, 128))
+    x[:, :, 5] = 100.0
+    cache = PagedKV(1, 128, "int8", n_pages=13)
+    cache.append(torch.tensor(x, device="cuda").float(), randn(rng, n, 1, 128), ints(range(n)))
+    kk, vv = (f64(t) for t in cache.read(ints(range(n)), dtype=torch.float32))
+    q = randn(rng, 1, 4, 128, dtype="bf16") + 1.0
+    vals = np.zeros((208, 2, 1, 128))
+    vals[:n, 0], vals[:n, 1] = kk, vv
+    pages = np.arange(13)[None]
+    out = cache.attend(q, ints(pages), ints([n]))
+    # raised by 128, a score is off by up to 2 d 2^-23 of 128 sum |q| scale in place of sum |q k|
+    want, _, weight = paged.paged_attention(f64(q), vals[:, 0], vals[:, 1], pages, [n], 128 ** -0.5)
+    ds = 2 * 128 * 2.0 ** -23 * 128 * np.abs(f64(q)).sum(-1).max() * (100.0 / 127) * 128 ** -0.5
+    within(f64(out), want, (2 * ds + 2.0 ** -16 + n * 2.0 ** -23) * weight + half_step(want, "bf16"), "outlier")
