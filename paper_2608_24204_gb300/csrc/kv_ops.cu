@@ -83,8 +83,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // A block takes block_tokens tokens.  It computes their cosines and sines once, one pair a thread
 // and turn, through shared memory; then a thread keeps its token, with its chunk's cosines and
 // sines in registers, and walks over the token's heads: what is left for a row is its loads (issued
-// before the row ahead of it is worked on), the arithmetic and its stores.  A warp holds the same
-// head of up to four tokens, which lie side by side in a page.
+// before the row ahead of it is worked on), the arithmetic and its stores.  Lanes of a warp take
+// neighbouring heads of a token: a packed row's heads lie side by side.
 template <typename T, int FMT, int PATH>
 __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __grid_constant__ RowsArg a) {
     constexpr bool WIDE = PATH != NARROW;
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
     griddep_launch_dependents();
     griddep_wait();
     const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
-    const int tl = threadIdx.y & (a.block_tokens - 1), step = blockDim.y / a.block_tokens;
+    const int step = blockDim.y / a.block_tokens, tl = threadIdx.y / step;
     const int64_t t = t0 + tl < a.tokens ? t0 + tl : a.tokens - 1;   // past the end: the last token's, not stored
     const bool here = t0 + tl < a.tokens;
     float2 w[8];                                                 // cosine and sine of the chunk's pairs
@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
     };
     constexpr int RAW = WIDE ? 2 * W : 4;
     uint4 raw[RAW] = {};
-    const int h0 = threadIdx.y / a.block_tokens;
+    const int h0 = threadIdx.y % step;
     if (h0 < a.heads) fetch(h0, raw);
     // every lane of a warp stays: rows are reduced by shuffles
     for (int base = 0; base < a.heads; base += step) {
