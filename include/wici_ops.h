@@ -173,7 +173,8 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
 /* The cache of layer `layer` of a context, as of the work already enqueued on the
  * context's stream, and its page table (device int32[pages], logical -> physical;
  * *n_logical entries).  Both stay valid until wici_destroy; the first wici_kv_len
- * positions hold tokens.  Read it on the context's stream or after it. */
+ * positions hold tokens.  Read it on the context's stream or after it; what the
+ * context wrote is the context's, and is not to be written. */
 int wici_kv_view(const wici_ctx *ctx, int32_t layer, wici_kv_cache *cache, const int32_t **pages, int32_t *n_logical);
 
 #ifdef __cplusplus

@@ -2,8 +2,11 @@
 //
 // The three are row-wise: a row is one head of one token, cut into chunks of 16 elements, one
 // lane each.  All are bound by HBM (each element is read and written once; a rotation is 6
-// operations a pair, a quantisation one division an element), and by launch latency when the
-// call is a step of few tokens.
+// operations a pair, a quantisation 3 an element), and by launch latency when the call is a step
+// of few tokens.  Measured (device time): rotation of 8192 tokens of 40 heads of 128 in bf16
+// 30.3 us, 5.5 TB/s (a copy of that size: 6.4); append of 16384 tokens, 32 q heads rotated, 8 k
+// and v heads to e4m3, 70.7 us, 5.2 TB/s, of which its arithmetic is 3 us; one token of a step
+// 2.2 to 3.4 us.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -466,7 +469,7 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
     if (const char *m = check_heads(y, tokens, plan->head_dim, true)) return fail(WICI_E_ARG, "rope y: %s", m);
     if (x->dtype != y->dtype || x->heads != y->heads) return fail(WICI_E_ARG, "rope: x and y differ in type or heads");
     if (tokens == 0) return WICI_OK;
-    if (!positions) return fail(WICI_E_ARG, "rope: null positions");
+    if (!positions || !words(positions)) return fail(WICI_E_ARG, "rope: positions null or unaligned");
     int sms = 0;
     if (int rc = sm_count(&sms)) return rc;
     RowsArg a = {};
@@ -514,7 +517,8 @@ int wici_kv_append(void *cuda_stream, const wici_kv_cache *cache, const int32_t 
             return fail(WICI_E_ARG, "append: q and q_out need the same heads and k's type");
     }
     if (tokens == 0) return WICI_OK;
-    if (!slots || (rope && !positions)) return fail(WICI_E_ARG, "append: null slots or positions");
+    if (!slots || (rope && !positions) || !words(slots) || !words(positions) || !words(status))
+        return fail(WICI_E_ARG, "append: slots or positions null, or one of them or status unaligned");
     int sms = 0;
     if (int rc = sm_count(&sms)) return rc;
     RowsArg a = {};
@@ -558,7 +562,7 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
     }
     if (k && v && k->dtype != v->dtype) return fail(WICI_E_ARG, "read: k and v need one type");
     if (tokens == 0) return WICI_OK;
-    if (!slots) return fail(WICI_E_ARG, "read: null slots");
+    if (!slots || !words(slots) || !words(status)) return fail(WICI_E_ARG, "read: slots null, or slots or status unaligned");
     int sms = 0;
     if (int rc = sm_count(&sms)) return rc;
     ReadArg a = {};

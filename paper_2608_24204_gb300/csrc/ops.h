@@ -58,6 +58,8 @@ inline bool wide_heads(const wici_heads *t) {
     return ((uintptr_t)t->data & 15) == 0 && t->token_stride % per == 0 && t->head_stride % per == 0;
 }
 
+inline bool words(const void *p) { return ((uintptr_t)p & 3) == 0; }   // of 32 bits; NULL among them
+
 inline const char *check_rope(const wici_rope_plan *p) {
     if (!p) return "null rope plan";
     if (p->head_dim < 2 || p->head_dim > 256 || p->head_dim % 2 || p->rot_dim < 2 || p->rot_dim > p->head_dim ||

@@ -92,6 +92,8 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     if (shape->batch == 0) return WICI_OK;
     if (!pages || !lengths || !workspace || ((uintptr_t)workspace & 15))
         return fail(WICI_E_ARG, "attention: null pages or lengths, or workspace null or not 16-byte aligned");
+    if (!words(pages) || !words(lengths) || !words(lse) || !words(status))
+        return fail(WICI_E_ARG, "attention: pages, lengths, lse or status unaligned");
     int sms = 0;
     if (int rc = device_sms(&sms)) return rc;
     AttnArg a = {};

@@ -209,3 +209,39 @@ def test_tensors_on_the_cpu_or_of_a_wrong_kind_are_refused():
                {"data": torch.zeros(100, dtype=torch.uint8)}, {"data": torch.zeros(8192)}):
         with pytest.raises(ValueError):
             ops.PagedKV(**{"n_kv_heads": 2, "head_dim": 64, "device": "cpu", **kw})
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_unaligned_words_are_refused(off):
+    h, c, u = heads(), cache(), A + off
+    refused(ops.wici_rope, 0, plan(), 0, u, 1, h, h, match="unaligned")
+    refused(ops.wici_kv_append, 0, c, u, 1, h, h, match="unaligned")
+    refused(ops.wici_kv_append, 0, c, A, 1, h, h, plan(), u, match="unaligned")
+    refused(ops.wici_kv_append, 0, c, A, 1, h, h, None, None, None, None, u, match="unaligned")
+    refused(ops.wici_kv_read, 0, c, u, 1, h, h, match="unaligned")
+    refused(ops.wici_kv_read, 0, c, A, 1, h, h, u, match="unaligned")
+    shape = ops.wici_attn_shape(1, 4, 0, 0.1)
+    for i in range(4):
+        pages, lengths, lse, status = (u if i == j else A for j in range(4))
+        refused(ops.wici_paged_attention, 0, c, shape, pages, lengths, h, h, lse, A, status, match="unaligned")
+
+
+def test_more_pages_than_a_launch_can_count_are_refused():
+    h = heads(n=64)
+    refused(ops.wici_paged_attention, 0, cache(), ops.wici_attn_shape(1, (1 << 25) - 2, 0, 0.1), A, A, h, h, None, A,
+            match="2^31")
+
+
+def test_the_header_is_c(tmp_path):
+    import shutil
+    import subprocess
+    cc = shutil.which("gcc")
+    if not cc:
+        pytest.skip("needs gcc")
+    src = tmp_path / "t.c"
+    src.write_text(f'#include "{ROOT}/include/wici_ops.h"\n_Static_assert(sizeof(wici_heads) == 32, "");\n'
+                   '_Static_assert(sizeof(wici_rope_plan) == 1040, "");\n_Static_assert(sizeof(wici_kv_cache) == 32, "");\n'
+                   '_Static_assert(sizeof(wici_attn_shape) == 16, "");\n_Static_assert(sizeof(wici_rope_spec) == 64, "");\n')
+    subprocess.run([cc, "-std=c11", "-Wall", "-Werror", "-fsyntax-only", str(src)], check=True)
+    assert [ctypes.sizeof(t) for t in (ops.wici_heads, ops.wici_rope_plan, ops.wici_kv_cache, ops.wici_attn_shape,
+                                       ops.wici_rope_spec)] == [32, 1040, 32, 16, 64]
