@@ -925,18 +925,27 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 const int here = min(32, i1 + 1 - from);
                 float2 ml = make_float2(-INFINITY, 0.f);
                 if (lane < here) ml = __ldcg((const float2 *)(piece_of(from + lane) + kAttnPieceRows * D) + row);
+                auto values = [&](int p) {
+                    return lane < D / 4 && p < here ? __ldcg((const float4 *)(piece_of(from + p) + row * D) + lane)
+                                                    : make_float4(0.f, 0.f, 0.f, 0.f);
+                };
+                constexpr int AHEAD = 8;                    // pieces asked for before their weights are known
+                float4 q[AHEAD];
+#pragma unroll
+                for (int p = 0; p < AHEAD; ++p) q[p] = values(p);
                 const float up = fmaxf(top, warp_max(ml.x)), was = top == -INFINITY ? 0.f : ex2(top - up);
                 const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - up);
                 sum = sum * was + warp_sum(ml.y * f);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] *= was;
                 top = up;
-#pragma unroll 8
-                for (int p = 0; p < here; ++p) {
-                    const float fp = __shfl_sync(0xffffffffu, f, p);
-                    float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (lane < D / 4) q = __ldcg((const float4 *)(piece_of(from + p) + row * D) + lane);
-                    v[0] += q.x * fp, v[1] += q.y * fp, v[2] += q.z * fp, v[3] += q.w * fp;
+                for (int p0 = 0; p0 < here; p0 += AHEAD) {
+#pragma unroll
+                    for (int p = 0; p < AHEAD; ++p) {
+                        const float fp = __shfl_sync(0xffffffffu, f, p0 + p);   // 0 past the last piece
+                        if (p0 + p < here) v[0] += q[p].x * fp, v[1] += q[p].y * fp, v[2] += q[p].z * fp, v[3] += q[p].w * fp;
+                        q[p] = values(p0 + AHEAD + p);
+                    }
                 }
             }
             if (lane < D / 4) finish(s, row, 4 * lane, v, top, sum);
