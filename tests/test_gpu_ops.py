@@ -697,3 +697,77 @@ def test_keys_whose_codes_are_small_beside_one_outlier():
     want, _, weight = paged.paged_attention(f64(q), vals[:, 0], vals[:, 1], pages, [n], 128 ** -0.5)
     ds = 2 * 128 * 2.0 ** -23 * 128 * np.abs(f64(q)).sum(-1).max() * (100.0 / 127) * 128 ** -0.5
     within(f64(out), want, (2 * ds + 2.0 ** -16 + n * 2.0 ** -23) * weight + half_step(want, "bf16"), "outlier")
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+def test_a_cache_of_more_than_4_gb(fmt):
+    # byte offsets past 32 bits, in what is written, read and attended over
+    rng = np.random.default_rng(27)
+    kv, d, n = 8, 128, 100
+    page = ops.wici_kv_page_bytes(ops.FORMATS[fmt], kv, d)
+    pages = (1 << 32) // page + 5000
+    cache = PagedKV(kv, d, fmt, data=torch.empty(pages * page, dtype=torch.uint8, device="cuda"))
+    table = np.concatenate([[pages - 1, 3, pages - 2000], rng.permutation(4000)[:4] + pages - 4500])[None]
+    slots = table[0, np.arange(n) // 16] * 16 + np.arange(n) % 16
+    k, v = randn(rng, n, kv, d, dtype="bf16"), randn(rng, n, kv, d, dtype="bf16")
+    cache.append(k, v, ints(slots))
+    kk, vv = cache.read(ints(slots), dtype=torch.float32)
+    top = torch.stack([k, v]).float().abs().amax(-1, keepdim=True)
+    err = (torch.stack([kk, vv]) - torch.stack([k, v]).float()).abs()
+    assert bool((err <= (0 if fmt == "bf16" else (0.5 / 127 + 2.0 ** -16)) * top).all())
+    q = randn(rng, 1, 16, d)
+    out = cache.attend(q, ints(table), ints([n]))
+    cache.check()
+    vals = np.zeros((16 * 7, 2, kv, d))
+    vals[:n, 0], vals[:n, 1] = f64(kk), f64(vv)
+    check_attention(cache, q, np.arange(7)[None], [n], vals, d ** -0.5, 0, out, None, "f32")
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3"])
+def test_pages_of_several_layers_side_by_side(fmt):
+    # page_stride: [page][layer] pools, one layer of which is this cache; the other layers' bytes stay
+    rng = np.random.default_rng(28)
+    kv, d, layers, pages, n = 3, 64, 3, 5, 70
+    page = ops.wici_kv_page_bytes(ops.FORMATS[fmt], kv, d)
+    pool = torch.full((pages, layers, page), 255, dtype=torch.uint8, device="cuda")
+    cache = ops.wici_kv_cache(pool[0, 1].data_ptr(), layers * page, pages, kv, d, ops.FORMATS[fmt])
+    plain = PagedKV(kv, d, fmt, data=torch.full((pages * page,), 255, dtype=torch.uint8, device="cuda"))
+    k, v, q = (randn(rng, n, kv, d), randn(rng, n, kv, d), randn(rng, 1, 6, d))
+    table, st = rng.permutation(pages)[None], torch.cuda.current_stream().cuda_stream
+    slots, dev = ints(table[0, np.arange(n) // 16] * 16 + np.arange(n) % 16), k.device
+    hk, hv = ops.heads_of(k, d, dev, "k"), ops.heads_of(v, d, dev, "v")
+    ops.wici_kv_append(st, cache, slots.data_ptr(), n, hk, hv)
+    plain.append(k, v, slots)
+    assert torch.equal(pool[:, 1].reshape(-1), plain.data)
+    assert bool((pool[:, 0] == 255).all()) and bool((pool[:, 2] == 255).all())
+    back = [torch.empty(n, kv, d, device="cuda") for _ in range(2)]
+    ops.wici_kv_read(st, cache, slots.data_ptr(), n, *(ops.heads_of(b, d, dev, "b") for b in back))
+    assert all(torch.equal(a, b) for a, b in zip(back, plain.read(slots, dtype=torch.float32)))
+    out, ws = torch.empty_like(q), plain.workspace(6, 1)
+    p, length = ints(table), ints([n])
+    ops.wici_paged_attention(st, cache, ops.wici_attn_shape(1, pages, 0, 0.125), p.data_ptr(), length.data_ptr(),
+                             ops.heads_of(q, d, dev, "q"), ops.heads_of(out, d, dev, "o"), None, ws.data_ptr())
+    assert torch.equal(out, plain.attend(q, p, length, scale=0.125))
+
+
+def test_broadcast_keys_and_odd_alignments_take_the_narrow_path_to_the_same_bytes():
+    rng = np.random.default_rng(29)
+    T, kv, d = 21, 4, 64
+    rope = Rope(d, 1e4, rot_dim=32)
+    slots, pos = ints(rng.permutation(32)[:T]), ints(rng.integers(0, 9999, T))
+    base = randn(rng, T, 1, d, dtype="bf16")
+    k, v = base.expand(T, kv, d), randn(rng, T, kv, d, dtype="bf16")
+    q = randn(rng, T, 5, d, dtype="bf16")
+
+    def odd(x):                                                # the same values, 2-byte aligned
+        y = torch.empty(x.numel() + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape)
+        return y.copy_(x)
+
+    for fmt in ("bf16", "int8", "e4m3"):
+        a, b = PagedKV(kv, d, fmt, n_pages=2), PagedKV(kv, d, fmt, n_pages=2)
+        qa = a.append(k.contiguous(), v, slots, rope=rope, positions=pos, q=q)
+        qb = b.append(odd(k), odd(v), slots, rope=rope, positions=pos, q=odd(q), q_out=odd(q))
+        assert torch.equal(a.data, b.data) and torch.equal(qa, qb)
+        b.data.zero_()
+        b.append(k, v, slots, rope=rope, positions=pos)        # heads of stride 0, and no q
+        assert torch.equal(a.data, b.data)
