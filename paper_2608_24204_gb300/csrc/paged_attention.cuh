@@ -904,22 +904,22 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     // the one that this block's run starts in the middle of, and the one it ends in the middle of: the blocks that
     // hold it count their arrivals, and the last one joins all pieces, in order
     if (sh.side[0].end == 0 && sh.side[1].end == 0) return;
-    __threadfence();
     __syncthreads();
     if (threadIdx.x < 2) {
         const int side = threadIdx.x;
         bool final_one = false;
+        __threadfence();                                    // for the block's writes, which the barrier orders before it
         if (sh.side[side].end != 0) {
             int *ticket = a.tickets + sh.first[side];
             final_one = atomicAdd(ticket, 1) == sh.last[side] - sh.first[side];
             if (final_one) *ticket = 0;
         }
+        __threadfence();                                    // and for the reads of the block's threads after the next one
         sh.note[side] = final_one;
     }
     __syncthreads();
     for (int side = 0; side < 2; ++side) {
         if (!sh.note[side]) continue;
-        __threadfence();
         const Rec s = sh.side[side];
         const int i0 = sh.first[side], i1 = sh.last[side];
         auto piece_of = [&](int p) { return a.pieces + ((int64_t)p * 2 + (p == i0)) * attn_piece_floats(D); };
