@@ -118,39 +118,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
     const int step = blockDim.y / a.block_tokens, tl = threadIdx.y / step;
     const int64_t t = t0 + tl < a.tokens ? t0 + tl : a.tokens - 1;   // past the end: the last token's, not stored
     const bool here = t0 + tl < a.tokens;
-    float2 w[8];                                                 // cosine and sine of the chunk's pairs
-    if (a.positions) {
-        const int per = 8 * a.rot_chunks;
-        for (int i = tid; i < a.block_tokens * per; i += nthreads) {
-            const int tt = i / per, p = i - tt * per;
-            const int64_t token = t0 + tt < a.tokens ? t0 + tt : a.tokens - 1;
-            float2 v = make_float2(1.f, 0.f);
-            if (p < half) {
-                v = turn_of((uint64_t)(int64_t)a.positions[token] * a.rope.turns[p]);
-                v.x *= a.rope.gain;
-                v.y *= a.rope.gain * a.rope.sign;
-            }
-            ((float2 *)cs)[(((tt * 4 + (p & 7) / 2) * a.rot_chunks + p / 8) << 1) + (p & 1)] = v;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float4 v = cs[(tl * 4 + j) * a.rot_chunks + (turns ? c : 0)];
-            w[2 * j] = make_float2(v.x, v.y);
-            w[2 * j + 1] = make_float2(v.z, v.w);
-        }
-    }
-    int slot = -1;
-    if (FMT != kRopeOnly && here) {
-        slot = a.slots[t];
-        if (slot >= a.cache.n_pages * kKvPage) {
-            if (a.status) atomicOr(a.status, WICI_BAD_SLOT);
-            slot = -1;
-        }
-    }
-    const int d = FMT == kRopeOnly ? 0 : 16 * a.chunks, where = slot & (kKvPage - 1);
-    const int kv_block = FMT == WICI_KV_BF16 ? kKvPage * d * 2 : kKvPage * (d + 4);
-    uint8_t *page = FMT == kRopeOnly || slot < 0 ? nullptr : a.cache.data + (int64_t)(slot / kKvPage) * a.cache.page_stride;
+    int slot = FMT != kRopeOnly && here ? a.slots[t] : -1;
     const T *const sq = a.q.template row<T>(t, 0), *const sk = a.k.template row<T>(t, 0), *const sv = a.v.template row<T>(t, 0);
     T *const dq = a.q_out.template row<T>(t, 0);
     const int k0 = a.q_heads, v0 = FMT == kRopeOnly ? a.heads : a.q_heads + a.cache.kv_heads;   // first k row, first v row
@@ -175,7 +143,36 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
     constexpr int RAW = WIDE ? 2 * W : 4;
     uint4 raw[RAW] = {};
     const int h0 = threadIdx.y % step;
-    if (h0 < a.heads) fetch(h0, raw);
+    if (h0 < a.heads) fetch(h0, raw);     // on its way while the angles are computed
+    float2 w[8];                                                 // cosine and sine of the chunk's pairs
+    if (a.positions) {
+        const int per = 8 * a.rot_chunks;
+        for (int i = tid; i < a.block_tokens * per; i += nthreads) {
+            const int tt = i / per, p = i - tt * per;
+            const int64_t token = t0 + tt < a.tokens ? t0 + tt : a.tokens - 1;
+            float2 v = make_float2(1.f, 0.f);
+            if (p < half) {
+                v = turn_of((uint64_t)(int64_t)a.positions[token] * a.rope.turns[p]);
+                v.x *= a.rope.gain;
+                v.y *= a.rope.gain * a.rope.sign;
+            }
+            ((float2 *)cs)[(((tt * 4 + (p & 7) / 2) * a.rot_chunks + p / 8) << 1) + (p & 1)] = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 v = cs[(tl * 4 + j) * a.rot_chunks + (turns ? c : 0)];
+            w[2 * j] = make_float2(v.x, v.y);
+            w[2 * j + 1] = make_float2(v.z, v.w);
+        }
+    }
+    if (FMT != kRopeOnly && slot >= a.cache.n_pages * kKvPage) {
+        if (a.status) atomicOr(a.status, WICI_BAD_SLOT);
+        slot = -1;
+    }
+    const int d = FMT == kRopeOnly ? 0 : 16 * a.chunks, where = slot & (kKvPage - 1);
+    const int kv_block = FMT == WICI_KV_BF16 ? kKvPage * d * 2 : kKvPage * (d + 4);
+    uint8_t *page = FMT == kRopeOnly || slot < 0 ? nullptr : a.cache.data + (int64_t)(slot / kKvPage) * a.cache.page_stride;
     // every lane of a warp stays: rows are reduced by shuffles
     for (int base = 0; base < a.heads; base += step) {
         const int h = base + h0;
