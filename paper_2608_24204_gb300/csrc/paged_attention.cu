@@ -118,7 +118,8 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     a.scale = shape->scale;
     // the weight of a launch's segments adds up in 31 bits
     const int64_t each = ((int64_t)shape->max_pages + kAttnSegment) * cache->n_kv_heads * a.tiles, room = INT32_MAX / each;
-    const int most = room < 1 ? 1 : room < kAttnMaxBatch ? (int)room : kAttnMaxBatch;
+    const int fit = kind == ATTN_PLAIN ? AttnShape<WICI_KV_BF16, 128, false>::kMaxBatch : AttnShape<WICI_KV_BF16, 128, true>::kMaxBatch;
+    const int most = room < 1 ? 1 : room < fit ? (int)room : fit;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;
     for (int b = 0; b < shape->batch && e == cudaSuccess; b += most) {

@@ -42,7 +42,6 @@ namespace wici {
 
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = 32 * kAttnWarps;
-constexpr int kAttnMaxBatch = 256;    // sequences of a launch: their keys are in shared memory
 constexpr uint32_t kAttnSegment = 3;       // units that a segment weighs beside its own
 constexpr uint32_t kAttnMinUnits = 3;      // weight of a warp's run at least: shorter ones would not pay for joining more parts
 constexpr int kAttnPieceRows = 16;    // rows of a piece in the workspace (a head tile has 8 or 16)
@@ -68,6 +67,7 @@ constexpr size_t attn_piece_floats(int d) { return (size_t)kAttnPieceRows * (d +
 template <int FMT, int D, bool STACK>
 struct AttnShape {
     static constexpr int kRows = STACK ? 8 : 16;                   // queries of a head tile
+    static constexpr int kMaxBatch = STACK ? 1024 : 256;           // sequences of a launch: their keys are in shared memory
     // Pages of a unit: 4 to 8 KB of K and V for the work that a unit costs beside its products (bf16, 128: one page
     // already; 8-bit: one page more a unit took the batch of 64 from 136 to 116 us with 128, from 76 to 74 with 64).
     static constexpr int kPages = FMT == WICI_KV_BF16 ? (D == 128 ? 1 : 2) : (D == 128 ? 2 : 4);
@@ -79,7 +79,7 @@ struct AttnShape {
     static constexpr int kRing = (kKSlots + kVSlots) * kSlot;
     static constexpr int kPartRow = D + 4;                         // floats: neighbouring rows in other banks
     static constexpr int kPart = kRows * (kPartRow + 2) * 4;       // a part of a segment: O, then m and l of each row
-    static constexpr int kSmem = kAttnWarps * kRing + (kAttnWarps - 1) * kPart + (3 * kAttnMaxBatch + 2) * 4 + 128;
+    static constexpr int kSmem = kAttnWarps * kRing + (kAttnWarps - 1) * kPart + (3 * kMaxBatch + 2) * 4 + 128;
     static_assert(kPart <= kRing, "a warp's last part lies in its ring");
     static_assert(kBlocks * (kSmem + 1024) <= 228 * 1024, "blocks of an SM");
 };
@@ -282,8 +282,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     uint8_t *parts = smem + kAttnWarps * S::kRing;                    // of warps 1.. : the part that ends in its run
     Shared &sh = *(Shared *)(parts + (kAttnWarps - 1) * S::kPart);
     int *prefix = (int *)((uint8_t *)&sh + 128);                      // [batch + 1]: units of a head before a sequence
-    int *weight = prefix + kAttnMaxBatch + 1;                         // [batch + 1]: the same with their segments' weights
-    int *length = weight + kAttnMaxBatch + 1;                         // [batch]
+    int *weight = prefix + S::kMaxBatch + 1;                         // [batch + 1]: the same with their segments' weights
+    int *length = weight + S::kMaxBatch + 1;                         // [batch]
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t ring = smem_u32(smem) + warp * S::kRing;

@@ -771,3 +771,16 @@ def test_broadcast_keys_and_odd_alignments_take_the_narrow_path_to_the_same_byte
         b.data.zero_()
         b.append(k, v, slots, rope=rope, positions=pos)        # heads of stride 0, and no q
         assert torch.equal(a.data, b.data)
+
+
+@pytest.mark.parametrize("fmt,group,batch", [("bf16", 1, 2100), ("int8", 9, 600)])
+def test_batches_of_more_sequences_than_a_launch_takes(fmt, group, batch):
+    rng = np.random.default_rng(30)
+    lengths = rng.integers(-1, 36, batch)
+    lengths[[0, 255, 256, 512, 599, batch - 1]] = [0, 17, 33, 0, 1, 20]
+    cache, q, pages, vals = attention_case(rng, batch, 1, group, 64, fmt, "bf16", lengths)
+    out, lse = torch.full((batch + 2, group, 64), 7.0, dtype=torch.bfloat16, device="cuda"), torch.empty(batch, group, device="cuda")
+    cache.attend(q, ints(pages), ints(lengths), out=out, lse=lse)
+    cache.check()
+    check_attention(cache, q, pages, lengths, vals, 0.125, 0, out, lse, "bf16")
+    assert bool((out[batch:] == 7.0).all())
