@@ -136,8 +136,8 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
             }
         } else {
             float *x = (float *)raw;
-            load8<T, false>(p0, rotate ? n0 : 8, x);
-            load8<T, false>(p1, rotate ? n1 : 8, x + 8);
+            load8(p0, rotate ? n0 : 8, x);
+            load8(p1, rotate ? n1 : 8, x + 8);
         }
     };
     constexpr int RAW = WIDE ? 2 * W : 4;

@@ -40,28 +40,14 @@ __device__ __forceinline__ void from_f32(float f, __nv_bfloat16 &v) { v = __floa
 __device__ __forceinline__ void from_f32(float f, __half &v) { v = __float2half_rn(f); }
 __device__ __forceinline__ void from_f32(float f, float &v) { v = f; }
 
-// 8 elements at p as fp32: 16-byte loads, or (WIDE false) the first n one by one, zeros after them
-template <typename T, bool WIDE>
+// the first n of 8 elements at p as fp32, one by one, zeros after them
+template <typename T>
 __device__ __forceinline__ void load8(const T *p, int n, float *v) {
-    if (WIDE) {
-        if (n > 0) {
-            alignas(16) T e[8];
-            if (sizeof(T) == 4) {
-                *(uint4 *)e = *(const uint4 *)p;
-                *((uint4 *)e + 1) = *((const uint4 *)p + 1);
-            } else {
-                *(uint4 *)e = *(const uint4 *)p;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
-            return;
-        }
-        n = 0;
-    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = j < n ? to_f32(p[j]) : 0.f;
 }
 
+// 8 elements in 16-byte stores (none where n is 0), or (WIDE false) the first n one by one
 template <typename T, bool WIDE>
 __device__ __forceinline__ void store8(T *p, int n, const float *v) {
     alignas(16) T e[8];

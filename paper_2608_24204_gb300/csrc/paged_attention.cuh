@@ -265,7 +265,10 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     constexpr int PER = BF16 || D == 64 ? 8 : 16;         // adjacent elements of O that a lane holds per column
     // K's int8 codes raised by 128: q times 128 is taken off the score again, which costs it 2 bits.  fp32 in: not so.
     constexpr bool RAISED = FMT == WICI_KV_INT8 && !EXACT;
-    constexpr float kPUnit = BF16 ? 1.f : 4096.f;         // what weights are scaled up by (fp16: far from its smallest)
+    // The reference of a row's exponents moves when a score passes it by more than kLag (base 2): a new maximum
+    // moves it in two units of five, one that far above it hardly ever, and moving it rescales all of O.
+    constexpr float kLag = 6.f;
+    constexpr float kPUnit = BF16 ? 1.f : 128.f;          // what weights are scaled up by: fp16 holds 2^kLag 4 of them
 
     extern __shared__ __align__(128) uint8_t smem[];
     struct Rec {                          // a segment
@@ -415,37 +418,41 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     };
     Desc cur = describe(lane), next = describe(32 + lane);
     int issued = 0;                       // K's of units issued; V's follow one behind
+    uint32_t k_to = ring, v_to = ring + KS * S::kSlot;   // their slots
     uint32_t bad_units = 0;               // bit i % 32: unit i has a bad page
-    int last_page[P], last_info = 0;
-    bool last = false;
+    const uint8_t *last_src[P];           // of the unit before: K of its head in each page (null: no page), its rows
+    int last_first = 0, last_end = 0;     // (end 0: no unit)
 
-    // one page's block of K or V: rows without a key of the sequence are zeroed, what the cache holds there is anything
     const uint64_t policy = l2_evict_first();   // read once: code, queries and parts stay in L2 instead
     const uint32_t lane_dst = chunk_at<ROW>(lane / CHUNKS, lane % CHUNKS);
-    auto copy_block = [&](uint32_t dst, int page, int64_t block, int first, int end) {
-        constexpr int N = kKvPage * CHUNKS / 32, ROWS = 32 / CHUNKS;   // rows of one round of the warp
-        const uint8_t *src = a.cache.data + (page < 0 ? 0 : page * a.cache.page_stride + block);
-        if (first <= 0 && end >= kKvPage) {
+    const int64_t lane_v = (int64_t)a.cache.kv_heads * S::kBlock;   // from K to V of a head in a page
+    constexpr int N = kKvPage * CHUNKS / 32, ROWS = 32 / CHUNKS;    // a page's block in N rounds of the warp, rows of a round
+    // a unit's K or V: rows without a key of the sequence are zeroed, what the cache holds there is anything
+    auto copy_unit = [&](uint32_t dst, const uint8_t *const *src, int64_t off, int first, int end) {
+        if (first == 0 && end == UNIT) {                     // every page is there
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                cp_async16(dst + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src + i * 512 + lane * 16, 16, policy);
+            for (int p = 0; p < P; ++p) {
+                const uint8_t *from = src[p] + off + lane * 16;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    cp_async16(dst + p * S::kBlock + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), from + i * 512, 16, policy);
+                if (!BF16 && lane < 4) cp_async16(dst + p * S::kBlock + kKvPage * D + lane * 16, from + kKvPage * D, 16, policy);
+            }
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int r = i * ROWS + lane / CHUNKS;
-                cp_async16(dst + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src + i * 512 + lane * 16,
-                           r >= first && r < end ? 16 : 0, policy);
+            for (int p = 0; p < P; ++p) {
+                const uint8_t *from = src[p] ? src[p] + off + lane * 16 : a.cache.data;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int r = p * kKvPage + i * ROWS + lane / CHUNKS;
+                    cp_async16(dst + p * S::kBlock + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src[p] ? from + i * 512 : from,
+                               src[p] && r >= first && r < end ? 16 : 0, policy);
+                }
+                if (!BF16 && lane < 4)
+                    cp_async16(dst + p * S::kBlock + kKvPage * D + lane * 16, src[p] ? from + kKvPage * D : from,
+                               src[p] ? 16 : 0, policy);
             }
         }
-        if (!BF16 && lane < 4)
-            cp_async16(dst + kKvPage * D + lane * 16, src + kKvPage * D + lane * 16, page < 0 ? 0 : 16, policy);
-    };
-    auto copy_unit = [&](uint32_t dst, const int *page, int info, int side) {
-        const int first = info >> 16 & 255, end = info >> 24;
-        const int64_t block = (int64_t)((info & 0xFFFF) + side * a.cache.kv_heads) * S::kBlock;
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-            copy_block(dst + p * S::kBlock, page[p], block, first - p * kKvPage, page[p] < 0 ? 0 : end - p * kKvPage);
     };
     // group j: K of unit j and V of the one before it (none past the last unit: the groups still count)
     auto issue = [&]() {
@@ -453,29 +460,31 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             cur = next;
             next = describe(issued + 32 + lane);
         }
-        const int info = __shfl_sync(0xffffffffu, cur.info, issued & 31);
-        int page[P];
-        bool bad = false;
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            page[p] = __shfl_sync(0xffffffffu, cur.page[p], issued & 31);
-            if ((uint32_t)page[p] >= (uint32_t)a.cache.n_pages) {
-                bad |= info >> 24 > p * kKvPage;             // one that the sequence needs
-                page[p] = -1;
-            }
-        }
+        if (last_end) copy_unit(v_to, last_src, lane_v, last_first, last_end);
+        if (issued) v_to = v_to == ring + (KS + VS - 1) * S::kSlot ? ring + KS * S::kSlot : v_to + S::kSlot;
+        last_end = 0;
         if (issued < mine) {
-            copy_unit(ring + issued % KS * S::kSlot, page, info, 0);
+            const int info = __shfl_sync(0xffffffffu, cur.info, issued & 31);
+            int first = info >> 16 & 255, end = info >> 24;
+            const uint8_t *head = a.cache.data + (int64_t)((info & 0xFFFF) * S::kBlock);
+            bool bad = false;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int page = __shfl_sync(0xffffffffu, cur.page[p], issued & 31);
+                const bool there = (uint32_t)page < (uint32_t)a.cache.n_pages;
+                bad |= !there && end > p * kKvPage;          // one that the sequence needs
+                last_src[p] = there ? head + page * a.cache.page_stride : nullptr;
+            }
             if (bad) {
                 bad_units |= 1u << (issued & 31);
                 if (lane == 0 && a.status) atomicOr(a.status, WICI_BAD_PAGE);
+                first = -1;                                  // not the way of whole units
             }
+            copy_unit(k_to, last_src, 0, first, end);
+            last_first = first;
+            last_end = end;
         }
-        if (last) copy_unit(ring + KS * S::kSlot + (issued - 1) % VS * S::kSlot, last_page, last_info, 1);
-        last = issued < mine;
-#pragma unroll
-        for (int p = 0; p < P; ++p) last_page[p] = page[p];
-        last_info = info;
+        k_to = k_to == ring + (KS - 1) * S::kSlot ? ring : k_to + S::kSlot;
         ++issued;
         cp_commit();
     };
@@ -516,6 +525,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
         return (float *)(last_of_run ? smem + w * S::kRing : parts + (w - 1) * S::kPart);
     };
     int done = 0;                         // units of this warp computed
+    uint32_t ks = ring, vs = ring + KS * S::kSlot;       // slots of the next one to compute
     while (done < mine) {
         const int stop = (int)(min(seg.end, r1) - r0);
         const Keys keys = keys_of(length[seg.b], a.window);
@@ -627,12 +637,12 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
         int key0 = (keys.lo / kKvPage + (int)(r0 + done - seg.start) * P) * kKvPage;   // first key of the unit
         cp_wait<KS - 1>();                                   // group `done` brings its K
         __syncwarp();
-        scores(ring + done % KS * S::kSlot);
+        scores(ks);
         for (; done < stop; ++done, key0 += UNIT) {
             // group done + 1: K of the next unit and V of this one
             cp_wait<KS - 2>();
             __syncwarp();
-            const uint32_t ks = ring + done % KS * S::kSlot, vs = ring + KS * S::kSlot + done % VS * S::kSlot;
+            const uint32_t ks_next = ks == ring + (KS - 1) * S::kSlot ? ring : ks + S::kSlot;
             // x[r][j]: query g + 8 r, key t + 4 j of the unit
             constexpr int J = 4 * P;
             float x[R][J];
@@ -671,7 +681,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 up[r] = fmaxf(m[r], top);
-                grew |= up[r] > m[r];
+                grew |= up[r] > m[r] + kLag;
             }
             float ratio = 1.f, vscale[J];
             if (!BF16) {
@@ -714,7 +724,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     o[n][3] *= f[R - 1];
                 }
             }
-            scores(ring + (done + 1) % KS * S::kSlot);       // c has been read
+            scores(ks_next);                                 // c has been read
             uint32_t pf[P][PPASS][4];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -800,6 +810,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             }
             __syncwarp();                                   // every lane has read the slots
             issue();
+            ks = ks_next;
+            vs = vs == ring + (KS + VS - 1) * S::kSlot ? ring + KS * S::kSlot : vs + S::kSlot;
         }
 
         // ---- the segment's state, or this run's part of it ----
