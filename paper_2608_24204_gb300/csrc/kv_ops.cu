@@ -96,17 +96,16 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
     const bool pairs = PATH == NARROW ? a.rope.interleaved : PATH == WIDE_PAIRS;
     const int c = threadIdx.x, half = a.rope.rot / 2;
     const int tid = threadIdx.y * blockDim.x + c, nthreads = blockDim.x * blockDim.y;
-    // the chunk's two groups of 8 elements in a rotated row: where they start, how many they hold
+    // The chunk's two groups of 8 elements in a rotated row: where they start, how many they hold.  Interleaved
+    // rows are cut as they lie, so a chunk may hold pairs that are not rotated; halves are cut apart.
     int o0, o1, n0, n1;
     const bool turns = c < a.rot_chunks;
-    if (turns) {
-        const int n = half - 8 * c < 8 ? half - 8 * c : 8;
-        o0 = pairs ? 16 * c : 8 * c;
-        o1 = pairs ? o0 + 8 : half + 8 * c;
-        n0 = pairs ? (2 * n < 8 ? 2 * n : 8) : n;
-        n1 = pairs ? 2 * n - n0 : n;
+    if (turns && !pairs) {
+        o0 = 8 * c;
+        o1 = half + 8 * c;
+        n0 = n1 = half - 8 * c < 8 ? half - 8 * c : 8;
     } else {
-        o0 = a.rope.rot + 16 * (c - a.rot_chunks);
+        o0 = pairs ? 16 * c : a.rope.rot + 16 * (c - a.rot_chunks);
         o1 = o0 + 8;
         const int n = a.rope.head_dim - o0 < 16 ? a.rope.head_dim - o0 : 16;
         n0 = n < 8 ? n : 8;
@@ -195,8 +194,11 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
                 const float xa = pairs ? x[2 * p] : x[p], xb = pairs ? x[2 * p + 1] : x[p + 8];
                 const float ya = xa * w[p].x - xb * w[p].y, yb = xa * w[p].y + xb * w[p].x;
                 // the pair's own places are read and written by this step alone
-                if (pairs) x[2 * p] = ya, x[2 * p + 1] = yb;
-                else x[p] = ya, x[p + 8] = yb;
+                if (pairs) {
+                    if (8 * c + p < half) x[2 * p] = ya, x[2 * p + 1] = yb;
+                } else {
+                    x[p] = ya, x[p + 8] = yb;
+                }
             }
         }
         if (is_q) {
@@ -233,6 +235,106 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
                 }
             }
         }
+    }
+}
+
+// Rotation of halves that do not lie in whole groups of 8 elements (rot_dim no multiple of 16): an element's
+// partner, rot_dim / 2 places on or back, starts anywhere in a 16-byte word.  Element by element that costs as many
+// accesses as elements (8192 tokens of 32 heads of 128, 126 of them rotated, in bf16: 90.7 us); so a lane takes a
+// whole word, the row's words pass through the warp's shared memory, and a lane cuts its word's partners out of the
+// two words that hold them.  A row is read before any of it is written: y may be x.
+constexpr int kRaggedTokens = 4;      // tokens of a block at most: a warp keeps to one
+constexpr int kWarps = kRowThreads / 32;
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads, kRowBlocks) ragged_kernel(const __grid_constant__ RowsArg a) {
+    constexpr int E = 16 / sizeof(T);              // elements of a word
+    constexpr int NW = sizeof(T) / 2;              // words of a lane: rows of up to 32 of them, or 64 in fp32
+    __shared__ uint4 stage[kWarps][32 * NW];
+    __shared__ float2 cs[kRaggedTokens][128];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, half = a.rope.rot / 2;
+    const int words = a.rope.head_dim / E, lanes = words <= 32 ? words : (words + 1) / 2, rows = 32 / lanes;
+    const int sub = lane / lanes, c = lane - sub * lanes;
+    griddep_launch_dependents();
+    griddep_wait();
+    const int per = kWarps / a.block_tokens, tl = warp / per, step = per * rows;
+    const int64_t t0 = (int64_t)blockIdx.x * a.block_tokens;
+    const int64_t t = t0 + tl < a.tokens ? t0 + tl : a.tokens - 1;   // past the end: the last token's, not stored
+    const bool here = t0 + tl < a.tokens && sub < rows;
+    const T *const src = a.q.template row<T>(t, 0);
+    T *const dst = a.q_out.template row<T>(t, 0);
+    uint4 raw[NW] = {};
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+            if (here && h < a.heads && c + i * lanes < words) raw[i] = ((const uint4 *)(src + h * a.q.hs))[c + i * lanes];
+    };
+    const int h0 = (warp - tl * per) * rows + sub;
+    fetch(h0);
+    for (int i = threadIdx.x; i < a.block_tokens * half; i += kRowThreads) {
+        const int tt = i / half, p = i - tt * half;
+        const int64_t token = t0 + tt < a.tokens ? t0 + tt : a.tokens - 1;
+        const float2 v = turn_of((uint64_t)(int64_t)a.positions[token] * a.rope.turns[p]);
+        cs[tt][p] = make_float2(v.x * a.rope.gain, v.y * a.rope.gain * a.rope.sign);
+    }
+    __syncthreads();
+    float2 w[NW * E];                              // an element's cosine, and the sine that its partner takes
+#pragma unroll
+    for (int j = 0; j < NW * E; ++j) {
+        const int e = (c + j / E * lanes) * E + j % E;
+        w[j] = cs[tl][e < half ? e : e < 2 * half ? e - half : 0];
+        if (e < half) w[j].y = -w[j].y;
+    }
+    uint4 *const row = stage[warp] + (sub < rows ? sub * words : 0);
+    // E elements from element q of the row on, those outside the row anything
+    auto cut = [&](int q, T *x) {
+        const int at = q >= 0 ? q / E : (q - E + 1) / E, bytes = (q - at * E) * (int)sizeof(T);
+        alignas(16) uint32_t r[8];
+        *(uint4 *)r = row[at < 0 ? 0 : at < words ? at : words - 1];
+        *(uint4 *)(r + 4) = row[at + 1 < 0 ? 0 : at + 1 < words ? at + 1 : words - 1];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) r[i] = bytes & 8 ? r[i + 2] : r[i];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) r[i] = bytes & 4 ? r[i + 1] : r[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ((uint32_t *)x)[i] = __funnelshift_r(r[i], r[i + 1], bytes & 2 ? 16 : 0);
+    };
+    for (int base = 0; base < a.heads; base += step) {
+        const int h = base + h0;
+        alignas(16) T own[NW * E];
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            ((uint4 *)own)[i] = raw[i];
+            if (sub < rows && c + i * lanes < words) row[c + i * lanes] = raw[i];
+        }
+        __syncwarp();
+        fetch(h + step);
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const int e0 = (c + i * lanes) * E;
+            alignas(16) T other[E];
+            cut(e0 < half ? e0 + half : e0 - half, other);
+            if (e0 < half && e0 + E > half) {      // both halves meet in this word
+                alignas(16) T back[E];
+                cut(e0 - half, back);
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (e0 + j >= half) other[j] = back[j];
+            }
+            float y[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float x = to_f32(own[i * E + j]);
+                y[j] = e0 + j < 2 * half ? x * w[i * E + j].x + to_f32(other[j]) * w[i * E + j].y : x;
+            }
+            if (here && h < a.heads && e0 < a.rope.head_dim) {
+                alignas(16) T out[E];
+#pragma unroll
+                for (int j = 0; j < E; ++j) from_f32(y[j], out[j]);
+                *(uint4 *)(dst + h * a.q_out.hs + e0) = *(const uint4 *)out;
+            }
+        }
+        __syncwarp();                              // the row has been read
     }
 }
 
@@ -335,15 +437,10 @@ int tokens_of_block(int64_t tokens, int most, int sms) {
 }
 
 template <typename Kern, typename Arg>
-cudaError_t launch(Kern kern, const Arg &a, int chunks, size_t smem, cudaStream_t st) {
+cudaError_t launch_blocks(Kern kern, const Arg &a, dim3 block, size_t smem, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((a.tokens + a.block_tokens - 1) / a.block_tokens));
-    int rows = kRowThreads / chunks;                 // a multiple of block_tokens
-    rows -= rows % a.block_tokens;
-    // no more lanes than there are rows (whole warps: the shuffles of a row)
-    const int need = (a.heads * a.block_tokens + 31) / 32 * 32;
-    rows = rows < need ? rows : need;
-    cfg.blockDim = dim3(chunks, rows);
+    cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr;
@@ -352,6 +449,16 @@ cudaError_t launch(Kern kern, const Arg &a, int chunks, size_t smem, cudaStream_
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+template <typename Kern, typename Arg>
+cudaError_t launch(Kern kern, const Arg &a, int chunks, size_t smem, cudaStream_t st) {
+    int rows = kRowThreads / chunks;                 // a multiple of block_tokens
+    rows -= rows % a.block_tokens;
+    // no more lanes than there are rows (whole warps: the shuffles of a row)
+    const int need = (a.heads * a.block_tokens + 31) / 32 * 32;
+    rows = rows < need ? rows : need;
+    return launch_blocks(kern, a, dim3(chunks, rows), smem, st);
 }
 
 template <typename T, int FMT>
@@ -379,7 +486,7 @@ void set_rope(RowsArg *a, const wici_rope_plan *plan, bool inverse) {
     a->rope.rot = plan->rot_dim;
     a->rope.interleaved = plan->interleaved;
     a->rot_chunks = (plan->rot_dim / 2 + 7) / 8;
-    a->chunks = a->rot_chunks + (plan->head_dim - plan->rot_dim + 15) / 16;
+    a->chunks = plan->interleaved ? (plan->head_dim + 15) / 16 : a->rot_chunks + (plan->head_dim - plan->rot_dim + 15) / 16;
 }
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 31;   // exclusive
@@ -476,9 +583,21 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
     a.positions = positions;
     a.q_heads = a.heads = x->heads;
     a.tokens = tokens;
-    a.block_tokens = tokens_of_block(tokens, kBlockTokens, sms);
-    const bool wide = wide_heads(x) && wide_heads(y) && plan->rot_dim % 16 == 0 && plan->head_dim % 8 == 0;
-    const cudaError_t e = launch_rows<kRopeOnly>(x->dtype, a, wide, (cudaStream_t)cuda_stream);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const bool aligned = wide_heads(x) && wide_heads(y);
+    cudaError_t e;
+    if (aligned && !plan->interleaved && plan->rot_dim % 16 && plan->head_dim % (16 / dtype_bytes(x->dtype)) == 0) {
+        a.block_tokens = tokens_of_block(tokens, kRaggedTokens, sms);
+        switch (x->dtype) {
+            case WICI_BF16: e = launch_blocks(ragged_kernel<__nv_bfloat16>, a, dim3(kRowThreads), 0, st); break;
+            case WICI_F16: e = launch_blocks(ragged_kernel<__half>, a, dim3(kRowThreads), 0, st); break;
+            default: e = launch_blocks(ragged_kernel<float>, a, dim3(kRowThreads), 0, st); break;
+        }
+    } else {
+        a.block_tokens = tokens_of_block(tokens, kBlockTokens, sms);
+        const bool wide = aligned && plan->head_dim % 8 == 0 && (plan->interleaved || plan->rot_dim % 16 == 0);
+        e = launch_rows<kRopeOnly>(x->dtype, a, wide, st);
+    }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "rope: %s", cudaGetErrorString(e));
 }
 

@@ -134,6 +134,38 @@ def test_rope_of_extreme_positions_and_values():
     assert bool(torch.isfinite(y[~touched]).all()) and not bool(torch.isfinite(y[touched]).any())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads,d,rot", [
+    (1, 1, 8, 2), (1, 40, 128, 126), (5, 33, 80, 20), (7, 2, 96, 6), (3, 70, 4, 4), (9, 3, 132, 70), (6, 2, 256, 254),
+    (2, 5, 72, 50), (11, 4, 64, 40), (5000, 3, 16, 10), (3001, 7, 40, 36),
+])
+def test_rope_of_ragged_rotations(dtype, interleaved, tokens, heads, d, rot):
+    # rotated parts that end, or meet, anywhere in a 16-byte word; an output row with gaps that have to stay
+    rng = np.random.default_rng(tokens + d + rot)
+    pos = rng.integers(-3, 1 << 20, tokens)
+    x = randn(rng, tokens, heads, d, dtype=dtype)
+    # infinities and NaNs touch their own pair alone, and behind the rotated part themselves
+    wild = torch.zeros(tokens, heads, d, dtype=torch.bool, device="cuda")
+    places = ({0, 1} if interleaved else {0, rot // 2}) | ({rot} if rot < d else set())
+    wild[tokens // 2, heads - 1, sorted(places)] = True
+    x[tokens // 2, heads - 1, 0] = float("inf")
+    if rot < d:
+        x[tokens // 2, heads - 1, rot] = float("nan")
+    y = torch.full((tokens, heads + 1, d + 8), 7.0, dtype=DT[dtype], device="cuda")
+    r = Rope(d, 5e5, rot_dim=rot, interleaved=interleaved)
+    out = y[:, :heads, :d]
+    r.apply(x, ints(pos), out=out)
+    assert bool((y[:, heads] == 7.0).all()) and bool((y[..., d:] == 7.0).all())
+    assert not bool(torch.isfinite(out[wild]).any()) and bool(torch.isfinite(out[~wild]).all())
+    tame = x.masked_fill(wild, 1.0)
+    check_rope(tame, r.apply(tame, ints(pos)), pos, rot, 5e5, interleaved, "none", False, dtype)
+    assert torch.equal(r.apply(tame, ints(pos))[~wild], out[~wild])
+    want = r.apply(tame, ints(pos), inverse=True)
+    assert torch.equal(r.apply(tame, ints(pos), out=tame, inverse=True), want)      # in place
+    check_rope(x.masked_fill(wild, 1.0), want, pos, rot, 5e5, interleaved, "none", True, dtype)
+
+
 def test_rope_inverse_is_the_gradient_by_differences():
     # L = sum(w * rope(x)): dL/dx by central differences in x of the fp64 oracle, at step 1 (the map is linear)
     rng = np.random.default_rng(5)
