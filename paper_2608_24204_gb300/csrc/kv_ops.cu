@@ -4,8 +4,8 @@
 // lane each.  All are bound by HBM (each element is read and written once; a rotation is 6
 // operations a pair, a quantisation 3 an element), and by launch latency when the call is a step
 // of few tokens.  Measured (device time): rotation of 8192 tokens of 40 heads of 128 in bf16
-// 28.4 us, 5.9 TB/s (a copy of that size: 6.4); append of 16384 tokens, 32 q heads rotated, 8 k
-// and v heads to e4m3, 69.2 us, 5.4 TB/s, of which its arithmetic is 3 us; read of 30011 tokens from
+// 28.3 us, 5.9 TB/s (a copy of that size: 6.4); append of 16384 tokens, 32 q heads rotated, 8 k
+// and v heads to e4m3, 69.1 us, 5.4 TB/s, of which its arithmetic is 3 us; read of 30011 tokens from
 // e4m3 to bf16 32.1 us, 5.8 TB/s; one token of a step 2.3 to 3.4 us.
 #include <math.h>
 #include <stdarg.h>
@@ -242,9 +242,9 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
 // partner, rot_dim / 2 places on or back, starts anywhere in a 16-byte word.  Element by element that costs as many
 // accesses as elements; so a lane takes whole words, the row's words pass through the warp's shared memory, and a
 // lane cuts its word's partners out of the two words that hold them.  A row is read before any of it is written:
-// y may be x.  8192 tokens of 32 heads of 128, 126 of them rotated, in bf16: 33.9 us, 4.0 TB/s, bound by the
+// y may be x.  8192 tokens of 32 heads of 128, 126 of them rotated, in bf16: 33.8 us, 4.0 TB/s, bound by the
 // instructions of the cut (90.7 element by element; 23.2 where all 128 turn, in rows_kernel); 100 of them rotated,
-// in fp32: 44.4 us, 6.1 TB/s (with one word a lane 57.5).
+// in fp32: 44.4 to 46.5 us, 6 TB/s (with one word a lane 57.5).
 constexpr int kRaggedTokens = 4;      // tokens of a block at most: a warp keeps to one
 constexpr int kWarps = kRowThreads / 32;
 

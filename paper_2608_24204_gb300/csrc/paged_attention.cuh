@@ -12,12 +12,13 @@
 // segments.  A segment inside one run is finished by its warp alone; the parts of others are
 // joined by the block at its end, and by the block that finishes last where blocks share one.
 // Measured (device time; 8 KV heads of 128): 32 sequences of up to 4000 tokens in bf16 48 us, 5.5 TB/s
-// of keys; two of 100001 to 131072 142 us, 6.6 TB/s; 64 of up to 8192 in int8, five queries a KV head,
-// 113 us, 5.4 TB/s (the copies alone 104); 256 of 20 to 300 37 us; one of 200 tokens 7.9 us.  Of each
+// of keys; two of 100001 to 131072 145 us, 6.5 TB/s; 64 of up to 8192 in int8, five queries a KV head,
+// 110 us, 5.5 TB/s; 256 of 20 to 300 37 us; 1000 short ones 110 us; one of 200 tokens 7.6 us.  Of each
 // about 4 us pass before the first keys are there (lengths, then pages, then keys), and 4 to 8 after the
 // first warp is done.
 //
-// Softmax in base 2 with a running maximum m and sum l in fp32; O in fp32 accumulators.
+// Softmax in base 2 with a running reference m, at most 6 below the running maximum, and a sum l in
+// fp32; O in fp32 accumulators.
 //
 // Products on mma.m16n8k16: S = Q K^T with 16 rows of queries, 8 keys and 16 elements of the
 // head a step, O += P V with the same rows.  Neither K nor V is transposed or shuffled:
@@ -73,7 +74,7 @@ struct AttnShape {
     static constexpr int kPages = FMT == WICI_KV_BF16 ? (D == 128 ? 1 : 2) : (D == 128 ? 2 : 4);
     static constexpr int kBlock = attn_block(FMT, D);
     static constexpr int kSlot = kPages * kBlock;
-    // Two blocks on an SM, 8 warps with 250 registers each: three of 168 spill (131 us in place of 116).
+    // Two blocks on an SM, 8 warps with 250 registers each: three of 168 spill (131 us in place of then 116).
     static constexpr int kBlocks = 2;
     static constexpr int kKSlots = 3, kVSlots = kKSlots - 1;       // of the ring: about 100 KB on their way per SM
     static constexpr int kRing = (kKSlots + kVSlots) * kSlot;
@@ -265,8 +266,9 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     constexpr int PER = BF16 || D == 64 ? 8 : 16;         // adjacent elements of O that a lane holds per column
     // K's int8 codes raised by 128: q times 128 is taken off the score again, which costs it 2 bits.  fp32 in: not so.
     constexpr bool RAISED = FMT == WICI_KV_INT8 && !EXACT;
-    // The reference of a row's exponents moves when a score passes it by more than kLag (base 2): a new maximum
-    // moves it in two units of five, one that far above it hardly ever, and moving it rescales all of O.
+    // The reference of a row's exponents moves when a score passes it by more than kLag (base 2): moving it
+    // rescales all of O, which a new maximum would ask for in about 24 of a run's first 60 units (random scores, 16
+    // rows of which any may rise), one that far above the last hardly ever.
     constexpr float kLag = 6.f;
     constexpr float kPUnit = BF16 ? 1.f : 128.f;          // what weights are scaled up by: fp16 holds 2^kLag 4 of them
 
@@ -973,7 +975,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 // The kernels of a format.  A group of more than 8 queries takes 16 a tile where its terms are few, and tiles of 8
 // (each with its own pass over the keys) where they are many: with 16 a tile the terms of fp32 do not fit the
 // registers.  16 sequences of 1000 to 4000 tokens, 16 queries a group, head_dim 128, fp32: 51 us in tiles of 8, 64 in
-// tiles of 16; 12 queries, bf16, 32 sequences: 93 and 64.
+// tiles of 16; 12 queries, bf16, 32 sequences: 93 and 64 (an earlier form of the loop).
 enum AttnKind { ATTN_STACK, ATTN_STACK_EXACT, ATTN_PLAIN };
 inline AttnKind attn_kind(int group, bool exact) {
     return exact ? ATTN_STACK_EXACT : group <= 8 ? ATTN_STACK : ATTN_PLAIN;
