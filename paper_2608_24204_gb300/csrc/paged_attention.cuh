@@ -44,7 +44,13 @@ namespace wici {
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = 32 * kAttnWarps;
 constexpr uint32_t kAttnSegment = 3;       // units that a segment weighs beside its own
-constexpr uint32_t kAttnMinUnits = 3;      // weight of a warp's run at least: shorter ones would not pay for joining more parts
+constexpr uint32_t kAttnMinUnits = 2;      // weight of a warp's run at least: shorter ones would not pay for joining more parts
+                                           // (8 heads of 1000 tokens 9.7 us, with 3 10.3; of 4000 12.9, with 3 12.3)
+// Weight of a segment at most that blocks do not share.  Block edges moved by up to half of it cost the longest warp 3
+// units, a joining of pieces 3 us and more: 16 sequences of 70 tokens, 4 KV heads of 8 queries, 10.2 us (13.1 where
+// blocks share), 16 queries of an e4m3 cache 11.6 (23.3); 1000 of 20 to 300 tokens 107.6 (112.4).  16 and 40 in its
+// place: 111.5 and 106.9 for the 1000, the same for the others.
+constexpr uint32_t kAttnWhole = 24;
 constexpr int kAttnPieceRows = 16;    // rows of a piece in the workspace (a head tile has 8 or 16)
 
 struct AttnArg {
@@ -357,8 +363,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     }
     if (blockIdx.x >= blocks) return;
 
-    auto last_at = [&](const int *sums, int q) {   // the last b with sums[b] <= q: it has units
-        int lo = 0, hi = a.batch;                  // sums[lo] <= q < sums[hi]
+    // the last b with sums[b] <= q: it has units (sums[lo] <= q < sums[hi])
+    auto last_at = [&](const int *sums, int q, int lo, int hi) {
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (sums[mid] <= q) lo = mid; else hi = mid;
@@ -367,29 +373,47 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     };
     auto segment_at = [&](uint32_t u) {            // the one that unit u is of
         Rec s;
-        s.b = last_at(prefix, u / HH);
+        s.b = last_at(prefix, u / HH, 0, a.batch);
         const uint32_t n_b = prefix[s.b + 1] - prefix[s.b], r = u - prefix[s.b] * HH;
         s.head = r / n_b;
         s.start = u - (r - s.head * n_b);
         s.end = s.start + n_b;
         return s;
     };
-    // runs are cut where the weight is: run j of n starts at weight floor(j V / n)
+    // Blocks' runs are cut where the weight is: block j of n begins at weight floor(j V / n), or, in a segment of
+    // little weight, at the nearer end of it: such a segment then needs no other block's piece.
     const uint32_t runs = kAttnWarps * blocks, whole_w = V / runs, rest_w = V - whole_w * runs;
-    auto run_start = [&](uint32_t j) {
+    int edge_b = a.batch;                          // the sequence that it lies in
+    uint32_t edge = V;
+    {
+        const uint32_t j = kAttnWarps * (blockIdx.x + (lane >= kAttnWarps));
         const uint32_t x = j * whole_w + j * rest_w / runs;         // j, rest_w < 2^14
+        if (x < V) {
+            edge = x;
+            edge_b = last_at(weight, x / HH, 0, a.batch);
+            const uint32_t n = prefix[edge_b + 1] - prefix[edge_b] + kAttnSegment, y = (x - weight[edge_b] * HH) % n;
+            if (n <= kAttnWhole) edge += 2 * y < n ? -y : n - y;
+        }
+    }
+    // a warp's run is a quarter of its block's, in weight
+    auto unit_at = [&](uint32_t x, int lo, int hi) {
         if (x >= V) return prefix[a.batch] * HH;
-        const int b = last_at(weight, x / HH);
+        const int b = last_at(weight, x / HH, lo, hi);
         const uint32_t r = x - weight[b] * HH, n_b = prefix[b + 1] - prefix[b];
         const uint32_t head = r / (n_b + kAttnSegment), y = r - head * (n_b + kAttnSegment);
         return prefix[b] * HH + head * n_b + (y > kAttnSegment ? y - kAttnSegment : 0u);
     };
-    // the block whose run holds unit s.start + z of a segment: of the last run that starts at its weight or before
+    // the block whose run holds unit s.start + z of a segment that several share: of the last run that starts at its
+    // weight or before (edges that were moved stay on their side of it)
     auto block_of = [&](const Rec &s, uint32_t z) {
         const uint64_t w = weight[s.b] * HH + s.head * (s.end - s.start + kAttnSegment) + kAttnSegment + z;
         return (int)(((w + 1) * runs - 1) / V / kAttnWarps);
     };
-    const uint32_t bound = run_start(blockIdx.x * kAttnWarps + (lane <= kAttnWarps ? lane : 0));
+    const uint32_t w0 = __shfl_sync(0xffffffffu, edge, 0), w_run = __shfl_sync(0xffffffffu, edge, kAttnWarps) - w0;
+    const int b_first = __shfl_sync(0xffffffffu, edge_b, 0), b_last = __shfl_sync(0xffffffffu, edge_b, kAttnWarps);
+    const int part = min(lane, kAttnWarps);
+    const uint32_t bound = unit_at(w0 + w_run / kAttnWarps * part + w_run % kAttnWarps * part / kAttnWarps, b_first,
+                                   min(a.batch, b_last + 2));
     auto run_at = [&](int w) { return __shfl_sync(0xffffffffu, bound, w); };   // by whole warps
     const uint32_t u0 = run_at(0), u1 = run_at(kAttnWarps), r0 = run_at(warp), r1 = run_at(warp + 1);
     const int mine = (int)(r1 - r0);
