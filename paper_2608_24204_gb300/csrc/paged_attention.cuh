@@ -10,10 +10,11 @@
 // units more than it has, for its queries' way in and its result's way out.  A warp streams its
 // run through a ring of its own in shared memory that cp.async fills ahead, across the ends of
 // segments.  A segment inside one run is finished by its warp alone; the parts of others are
-// joined by the block at its end, and by the block that finishes last where blocks share one.
-// Measured (device time; 8 KV heads of 128): 32 sequences of up to 4000 tokens in bf16 48 us, 5.5 TB/s
+// joined by the block at its end, and by the block that finishes last where blocks share one:
+// short segments (kAttnWhole) they never share.
+// Measured (device time; 8 KV heads of 128): 32 sequences of up to 4000 tokens in bf16 47 us, 5.6 TB/s
 // of keys; two of 100001 to 131072 145 us, 6.5 TB/s; 64 of up to 8192 in int8, five queries a KV head,
-// 110 us, 5.5 TB/s; 256 of 20 to 300 37 us; 1000 short ones 110 us; one of 200 tokens 7.6 us.  Of each
+// 109 us, 5.6 TB/s; 256 of 20 to 300 35 us, 1000 of them 107 us; one of 200 tokens 7.9 us.  Of each
 // about 4 us pass before the first keys are there (lengths, then pages, then keys), and 4 to 8 after the
 // first warp is done.
 //
