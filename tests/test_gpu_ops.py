@@ -440,6 +440,23 @@ def test_attention_of_many_ragged_sequences(fmt):
     check_attention(cache, q, pages, lengths, vals, 0.125, 0, out, lse, "bf16")
 
 
+@pytest.mark.parametrize("fmt,d,unit", [("bf16", 128, 16), ("int8", 64, 64), ("e4m3", 128, 32)])
+@pytest.mark.parametrize("kv,group,tail", [(1, 1, 0), (3, 2, 900), (4, 16, 0)])
+def test_attention_of_short_sequences_beside_long_ones(fmt, d, unit, kv, group, tail):
+    # 20 to 22 units: on both sides of the longest segment that blocks do not share; empty sequences between them
+    rng = np.random.default_rng(kv * 10 + group)
+    lengths = [20 * unit, 0, 21 * unit, 21 * unit + 1, 1, 0, 0, 22 * unit, 40 * unit, 3, 21 * unit - 1, 70, 0, tail]
+    cache, q, pages, vals = attention_case(rng, len(lengths), kv, group, d, fmt, "bf16", lengths)
+    lse = torch.empty(len(lengths), kv * group, dtype=torch.float32, device="cuda")
+    out = cache.attend(q, ints(pages), ints(lengths), lse=lse)
+    check_attention(cache, q, pages, lengths, vals, d ** -0.5, 0, out, lse, "bf16")
+    again = cache.attend(q, ints(pages), ints(lengths))
+    assert torch.equal(out, again)
+    for b in range(len(lengths)):                # alone: other blocks, the same sums to rounding
+        one = cache.attend(q[b:b + 1], ints(pages[b:b + 1]), ints(lengths[b:b + 1]))
+        check_attention(cache, q[b:b + 1], pages[b:b + 1], lengths[b:b + 1], vals, d ** -0.5, 0, one, None, "bf16")
+
+
 def test_attention_scores_far_apart_and_scale():
     # one key takes everything, its score hundreds above the others; then a scale of zero and a negative one
     rng = np.random.default_rng(13)
