@@ -29,9 +29,6 @@ int fail(int code, const char *fmt, ...) {
     return code;
 }
 
-constexpr int kRowThreads = 128;
-constexpr int kRowBlocks = 8;         // blocks on an SM: 64 registers a thread
-constexpr int kBlockTokens = 8;       // tokens of a block at most
 constexpr int kRopeOnly = -1;         // FMT of a launch without a cache
 enum Path { WIDE_HALF, WIDE_PAIRS, NARROW };   // 16-byte accesses of either layout, or element by element
 
@@ -431,13 +428,6 @@ int sm_count(int *n) {
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "SM count: %s", cudaGetErrorString(e));
 }
 
-// Tokens of a block: as many as leave two waves of blocks and more, and rows for a block's lanes.
-int tokens_of_block(int64_t tokens, int most, int sms) {
-    int n = 1;
-    while (2 * n <= most && tokens / (2 * n) >= 2 * kRowBlocks * sms) n *= 2;
-    return n;
-}
-
 template <typename Kern, typename Arg>
 cudaError_t launch_blocks(Kern kern, const Arg &a, dim3 block, size_t smem, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
@@ -453,30 +443,23 @@ cudaError_t launch_blocks(Kern kern, const Arg &a, dim3 block, size_t smem, cuda
     return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
-template <typename Kern, typename Arg>
-cudaError_t launch(Kern kern, const Arg &a, int chunks, size_t smem, cudaStream_t st) {
-    int rows = kRowThreads / chunks;                 // a multiple of block_tokens
-    rows -= rows % a.block_tokens;
-    // no more lanes than there are rows (whole warps: the shuffles of a row)
-    const int need = (a.heads * a.block_tokens + 31) / 32 * 32;
-    rows = rows < need ? rows : need;
-    return launch_blocks(kern, a, dim3(chunks, rows), smem, st);
-}
-
 template <typename T, int FMT>
-cudaError_t launch_rows(const RowsArg &a, bool wide, cudaStream_t st) {
-    const size_t smem = a.positions ? (size_t)a.block_tokens * 4 * a.rot_chunks * sizeof(float4) : 0;
-    if (!wide) return launch(rows_kernel<T, FMT, NARROW>, a, a.chunks, smem, st);
-    return a.rope.interleaved ? launch(rows_kernel<T, FMT, WIDE_PAIRS>, a, a.chunks, smem, st)
-                              : launch(rows_kernel<T, FMT, WIDE_HALF>, a, a.chunks, smem, st);
+cudaError_t launch_rows(RowsArg &a, bool wide, int sms, cudaStream_t st) {
+    const RowBlock b = row_block(a.tokens, a.heads, a.chunks, sms);
+    a.block_tokens = b.tokens;
+    const dim3 block(a.chunks, b.rows);
+    const size_t smem = a.positions ? (size_t)b.tokens * 4 * a.rot_chunks * sizeof(float4) : 0;
+    if (!wide) return launch_blocks(rows_kernel<T, FMT, NARROW>, a, block, smem, st);
+    return a.rope.interleaved ? launch_blocks(rows_kernel<T, FMT, WIDE_PAIRS>, a, block, smem, st)
+                              : launch_blocks(rows_kernel<T, FMT, WIDE_HALF>, a, block, smem, st);
 }
 
 template <int FMT>
-cudaError_t launch_rows(int dtype, const RowsArg &a, bool wide, cudaStream_t st) {
+cudaError_t launch_rows(int dtype, RowsArg &a, bool wide, int sms, cudaStream_t st) {
     switch (dtype) {
-        case WICI_BF16: return launch_rows<__nv_bfloat16, FMT>(a, wide, st);
-        case WICI_F16: return launch_rows<__half, FMT>(a, wide, st);
-        default: return launch_rows<float, FMT>(a, wide, st);
+        case WICI_BF16: return launch_rows<__nv_bfloat16, FMT>(a, wide, sms, st);
+        case WICI_F16: return launch_rows<__half, FMT>(a, wide, sms, st);
+        default: return launch_rows<float, FMT>(a, wide, sms, st);
     }
 }
 
@@ -494,20 +477,23 @@ void set_rope(RowsArg *a, const wici_rope_plan *plan, bool inverse) {
 constexpr int64_t kMaxTokens = (int64_t)1 << 31;   // exclusive
 
 template <typename T, int FMT>
-cudaError_t launch_read(int d, const ReadArg &a, bool wide, cudaStream_t st) {
+cudaError_t launch_read(int d, ReadArg &a, bool wide, int sms, cudaStream_t st) {
+    const RowBlock b = row_block(a.tokens, a.heads, d / 16, sms);
+    a.block_tokens = b.tokens;
+    const dim3 block(d / 16, b.rows);
     if (d == 64)
-        return wide ? launch(read_kernel<T, FMT, 64, true>, a, 4, 0, st)
-                    : launch(read_kernel<T, FMT, 64, false>, a, 4, 0, st);
-    return wide ? launch(read_kernel<T, FMT, 128, true>, a, 8, 0, st)
-                : launch(read_kernel<T, FMT, 128, false>, a, 8, 0, st);
+        return wide ? launch_blocks(read_kernel<T, FMT, 64, true>, a, block, 0, st)
+                    : launch_blocks(read_kernel<T, FMT, 64, false>, a, block, 0, st);
+    return wide ? launch_blocks(read_kernel<T, FMT, 128, true>, a, block, 0, st)
+                : launch_blocks(read_kernel<T, FMT, 128, false>, a, block, 0, st);
 }
 
 template <typename T>
-cudaError_t launch_read(int fmt, int d, const ReadArg &a, bool wide, cudaStream_t st) {
+cudaError_t launch_read(int fmt, int d, ReadArg &a, bool wide, int sms, cudaStream_t st) {
     switch (fmt) {
-        case WICI_KV_BF16: return launch_read<T, WICI_KV_BF16>(d, a, wide, st);
-        case WICI_KV_INT8: return launch_read<T, WICI_KV_INT8>(d, a, wide, st);
-        default: return launch_read<T, WICI_KV_E4M3>(d, a, wide, st);
+        case WICI_KV_BF16: return launch_read<T, WICI_KV_BF16>(d, a, wide, sms, st);
+        case WICI_KV_INT8: return launch_read<T, WICI_KV_INT8>(d, a, wide, sms, st);
+        default: return launch_read<T, WICI_KV_E4M3>(d, a, wide, sms, st);
     }
 }
 
@@ -596,9 +582,8 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
             default: e = launch_blocks(ragged_kernel<float>, a, dim3(kRowThreads), 0, st); break;
         }
     } else {
-        a.block_tokens = tokens_of_block(tokens, kBlockTokens, sms);
         const bool wide = aligned && plan->head_dim % 8 == 0 && (plan->interleaved || plan->rot_dim % 16 == 0);
-        e = launch_rows<kRopeOnly>(x->dtype, a, wide, st);
+        e = launch_rows<kRopeOnly>(x->dtype, a, wide, sms, st);
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "rope: %s", cudaGetErrorString(e));
 }
@@ -655,14 +640,13 @@ int wici_kv_append(void *cuda_stream, const wici_kv_cache *cache, const int32_t 
     a.q_heads = q ? q->heads : 0;
     a.heads = a.q_heads + 2 * cache->n_kv_heads;
     a.tokens = tokens;
-    a.block_tokens = tokens_of_block(tokens, kBlockTokens, sms);
     const bool wide = wide_heads(k) && wide_heads(v) && (!q || (wide_heads(q) && wide_heads(q_out)));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
     switch (cache->format) {
-        case WICI_KV_BF16: e = launch_rows<WICI_KV_BF16>(k->dtype, a, wide, st); break;
-        case WICI_KV_INT8: e = launch_rows<WICI_KV_INT8>(k->dtype, a, wide, st); break;
-        default: e = launch_rows<WICI_KV_E4M3>(k->dtype, a, wide, st); break;
+        case WICI_KV_BF16: e = launch_rows<WICI_KV_BF16>(k->dtype, a, wide, sms, st); break;
+        case WICI_KV_INT8: e = launch_rows<WICI_KV_INT8>(k->dtype, a, wide, sms, st); break;
+        default: e = launch_rows<WICI_KV_E4M3>(k->dtype, a, wide, sms, st); break;
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "append: %s", cudaGetErrorString(e));
 }
@@ -691,15 +675,14 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
     a.status = status;
     a.heads = cache->n_kv_heads * ((k ? 1 : 0) + (v ? 1 : 0));
     a.tokens = tokens;
-    a.block_tokens = tokens_of_block(tokens, kBlockTokens, sms);
     a.has_k = k != nullptr;
     const bool wide = (!k || wide_heads(k)) && (!v || wide_heads(v));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e;
     switch ((k ? k : v)->dtype) {
-        case WICI_BF16: e = launch_read<__nv_bfloat16>(cache->format, d, a, wide, st); break;
-        case WICI_F16: e = launch_read<__half>(cache->format, d, a, wide, st); break;
-        default: e = launch_read<float>(cache->format, d, a, wide, st); break;
+        case WICI_BF16: e = launch_read<__nv_bfloat16>(cache->format, d, a, wide, sms, st); break;
+        case WICI_F16: e = launch_read<__half>(cache->format, d, a, wide, sms, st); break;
+        default: e = launch_read<float>(cache->format, d, a, wide, sms, st); break;
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "read: %s", cudaGetErrorString(e));
 }

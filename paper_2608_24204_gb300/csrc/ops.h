@@ -58,6 +58,34 @@ inline bool wide_heads(const wici_heads *t) {
     return ((uintptr_t)t->data & 15) == 0 && t->token_stride % per == 0 && t->head_stride % per == 0;
 }
 
+// ---- shape of the row-wise kernels' launches ----
+constexpr int kRowThreads = 128;
+constexpr int kRowBlocks = 8;         // blocks on an SM: 64 registers a thread
+constexpr int kBlockTokens = 8;       // tokens of a block at most
+
+// Tokens of a block, a power of two: as many as leave two waves of blocks and more.
+inline int tokens_of_block(int64_t tokens, int most, int sms) {
+    int n = 1;
+    while (2 * n <= most && tokens / (2 * n) >= 2 * kRowBlocks * sms) n *= 2;
+    return n;
+}
+
+struct RowBlock {
+    int tokens;                       // of a block: a power of two
+    int rows;                         // of `chunks` lanes each, a multiple of `tokens`
+};
+// A block for rows of `chunks` lanes, `heads` of them a token: every token has a row of the block at least (rotated
+// halves of 242 to 256 elements may take 17 lanes, which leaves 7 rows: 4 tokens), and no lanes are left without
+// a row but those that fill the last warp (the shuffles of a row).
+inline RowBlock row_block(int64_t tokens, int heads, int chunks, int sms) {
+    const int most = kRowThreads / chunks;
+    RowBlock b = {tokens_of_block(tokens, most < kBlockTokens ? most : kBlockTokens, sms), 0};
+    const int need = (heads * b.tokens + 31) / 32 * 32;
+    b.rows = most - most % b.tokens;
+    b.rows = b.rows < need ? b.rows : need;
+    return b;
+}
+
 inline bool words(const void *p) { return ((uintptr_t)p & 3) == 0; }   // of 32 bits; NULL among them
 
 inline const char *check_rope(const wici_rope_plan *p) {

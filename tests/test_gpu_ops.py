@@ -833,3 +833,77 @@ def test_batches_of_more_sequences_than_a_launch_takes(fmt, group, batch):
     cache.check()
     check_attention(cache, q, pages, lengths, vals, 0.125, 0, out, lse, "bf16")
     assert bool((out[batch:] == 7.0).all())
+
+
+# token counts on both sides of what changes the tokens of a block (1, 2, 4 and 8 of them with 152 SMs), most of them ragged
+LONG = [4863, 4864, 9729, 19457]
+
+
+@pytest.mark.parametrize("tokens", LONG)
+@pytest.mark.parametrize("dtype,d,rot,interleaved,odd", [
+    ("bf16", 128, 128, False, False), ("f32", 64, 32, False, False), ("f16", 96, 64, True, False), ("bf16", 128, 126, False, False),
+    ("bf16", 256, 100, False, True), ("f32", 256, 254, False, True), ("f16", 244, 18, False, False),
+])
+def test_rope_of_many_tokens(tokens, dtype, d, rot, interleaved, odd):
+    # wide, ragged and element-wise paths; heads of up to 17 lanes
+    rng = np.random.default_rng(tokens + d)
+    pos = rng.integers(-3, 1 << 20, tokens)
+    x = randn(rng, tokens * 3 * d + 1, dtype=dtype)[1 if odd else 0:][:tokens * 3 * d].view(tokens, 3, d)
+    y = torch.full((tokens + 1, 3, d), 7.0, dtype=DT[dtype], device="cuda")
+    Rope(d, 5e5, rot_dim=rot, interleaved=interleaved).apply(x, ints(pos), out=y[:tokens])
+    check_rope(x, y[:tokens], pos, rot, 5e5, interleaved, "none", False, dtype)
+    assert bool((y[tokens] == 7.0).all())
+
+
+def check_stored(codes, scales, slots, which, x, fmt, turned):
+    """K (which 0) or V of a cache at slots against x, in 64 bits.  A rotated element is off by up to 2^-21 (|x_a| + |x_b|),
+    and |x_a| + |x_b| <= 2 amax of the rotated head: 2^-20 amax, however small the element itself has become.  So a
+    quotient is off by top 2^-20, top the largest code, by as much of the scale's own error, and by 2^-22 of itself:
+    below top 2^-18; one of given values by top 2^-22."""
+    live = slots >= 0
+    x, got = x[live], codes[slots[live], which]
+    amax = np.abs(x).max(-1, keepdims=True)
+    if fmt == "bf16":
+        val = (got.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+        return within(val, x, half_step(x, "bf16") + (2.0 ** -20 * amax if turned else 0), "bf16 cache")
+    top = 127.0 if fmt == "int8" else 448.0
+    grid = np.arange(128.0) if fmt == "int8" else paged.E4M3[:127]
+    s = scales[slots[live], which]
+    within(s, amax[..., 0] / top, amax[..., 0] / top * (2.0 ** -19 if turned else 2.0 ** -23), "scale")
+    gv, q, near = np.abs(paged.code_values(got, fmt)), np.abs(x) * top / amax, top * 2.0 ** (-18 if turned else -22)
+    at = np.searchsorted(grid, gv)                             # the quotients that may round to this code, and `near` of them
+    lo = np.where(at > 0, (grid[np.maximum(at - 1, 0)] + gv) / 2, 0.0)
+    hi = np.where(at < grid.size - 1, (grid[np.minimum(at + 1, grid.size - 1)] + gv) / 2, top)
+    assert np.all(grid[at] == gv) and np.all((q >= lo - near) & (q <= hi + near)), f"{fmt} codes"
+    assert np.all((paged.code_values(got, fmt) * x >= 0) | (q <= near)), f"{fmt} signs"
+
+
+@pytest.mark.parametrize("tokens", LONG)
+@pytest.mark.parametrize("fmt,dtype,d", [("bf16", "bf16", 64), ("int8", "f32", 128), ("e4m3", "f16", 64), ("e4m3", "bf16", 128)])
+def test_append_and_read_of_many_tokens(fmt, dtype, d, tokens):
+    rng = np.random.default_rng(tokens + d)
+    pages, kv, q_heads = tokens // 16 + 3, 2, 3
+    before = torch.tensor(rng.integers(0, 256, pages * ops.wici_kv_page_bytes(ops.FORMATS[fmt], kv, d)), dtype=torch.uint8,
+                          device="cuda")
+    cache = PagedKV(kv, d, fmt, data=before.clone())
+    k, v, q = (randn(rng, tokens, n, d, dtype=dtype) for n in (kv, kv, q_heads))
+    slots, pos = slots_for(rng, tokens, pages), rng.integers(0, 100000, tokens)
+    slots[[3, tokens - 1]] = [-1, -7]
+    r, (f, g) = Rope(d, 5e5), paged.rope_frequencies(d, 5e5)
+    q_out = cache.append(k, v, ints(slots), rope=r, positions=ints(pos), q=q)
+    cache.check()
+    check_rope(q, q_out, pos, d, 5e5, False, "none", False, dtype)
+    codes, scales = paged.unpack(cache.data.cpu().numpy(), kv, d, fmt)
+    others = np.ones(pages * 16, bool)
+    others[slots[slots >= 0]] = False
+    for now, was in zip((codes, scales), paged.unpack(before.cpu().numpy(), kv, d, fmt)):
+        assert now is None or np.array_equal(now[others].view(np.uint8), was[others].view(np.uint8))
+    check_stored(codes, scales, slots, 0, paged.rope(f64(k), pos, d, f, g), fmt, True)
+    check_stored(codes, scales, slots, 1, f64(v), fmt, False)
+    got = cache.read(ints(slots), dtype=DT[dtype])
+    for which in (0, 1):
+        c = codes[slots, which]
+        want = (c.astype(np.uint32) << 16).view(np.float32).astype(np.float64) if fmt == "bf16" else \
+            paged.code_values(c, fmt) * scales[slots, which][..., None].astype(np.float64)
+        want[slots < 0] = 0
+        within(f64(got[which]), want, half_step(want, dtype) + 2.0 ** -24 * np.abs(want), "read")

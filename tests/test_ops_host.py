@@ -245,3 +245,40 @@ def test_the_header_is_c(tmp_path):
     subprocess.run([cc, "-std=c11", "-Wall", "-Werror", "-fsyntax-only", str(src)], check=True)
     assert [ctypes.sizeof(t) for t in (ops.wici_heads, ops.wici_rope_plan, ops.wici_kv_cache, ops.wici_attn_shape,
                                        ops.wici_rope_spec)] == [32, 1040, 32, 16, 64]
+
+
+def test_every_rows_block_holds_its_tokens(tmp_path):
+    # the shape of a row-wise launch (csrc/ops.h) for every rotation, head and token count: a row for each token of a
+    # block, whole warps for the shuffles of a cache row, and no more threads than the kernels are compiled for
+    import shutil
+    import subprocess
+    cxx = shutil.which("g++")
+    if not cxx:
+        pytest.skip("needs g++")
+    src, exe = tmp_path / "t.cc", tmp_path / "t"
+    src.write_text(f'#include "{ROOT}/paper_2608_24204_gb300/csrc/ops.h"\n' + r"""
+#include <cstdio>
+#include <initializer_list>
+using namespace wici;
+int main() {
+    int most = 0;
+    for (int64_t tokens : {1, 100, 4863, 4864, 9727, 9728, 19455, 19456, 1000000})
+        for (int heads : {1, 2, 3, 7, 40, 1000})
+            for (int sms : {1, 20, 152, 200})
+                for (int chunks = 1; chunks <= 17; ++chunks) {
+                    const RowBlock b = row_block(tokens, heads, chunks, sms);
+                    const bool power = b.tokens > 0 && (b.tokens & (b.tokens - 1)) == 0;
+                    const bool cache = chunks == 4 || chunks == 8;      // of 64 and 128 elements
+                    if (!power || b.tokens > kBlockTokens || b.rows < b.tokens || b.rows % b.tokens || b.rows * chunks > kRowThreads ||
+                        (cache && b.rows * chunks % 32)) {
+                        std::printf("%d tokens, %d heads, %d chunks, %d SMs: %d x %d\n", (int)tokens, heads, chunks, sms, b.tokens, b.rows);
+                        return 1;
+                    }
+                    most = b.tokens > most ? b.tokens : most;
+                }
+    return most == kBlockTokens ? 0 : 2;
+}
+""")
+    subprocess.run([cxx, "-std=c++17", "-O1", str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, f"exit {r.returncode}: {r.stdout}{r.stderr}"
