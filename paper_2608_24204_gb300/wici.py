@@ -348,19 +348,22 @@ class WiciModel:
 
     def read_kv(self, layer: int, first: int = 0, count: int | None = None, dtype=None):
         """(k, v) [count, kv heads, head_dim] of the cached positions first.. (k after RoPE), on the device; the
-        stream has been synchronised."""
+        context's stream has been synchronised.  They may be used, and dropped, on the stream that is current here."""
         import torch
 
         from . import ops
         count = self.kv_len - first if count is None else count
         if first < 0 or count < 0 or first + count > self.kv_len:
             raise ValueError(f"positions {first}..{first + count - 1} of {self.kv_len} cached ones")
+        caller = torch.cuda.current_stream(self.stream.device)
         with torch.cuda.stream(self.stream):
             cache, table = self.kv_cache(layer)
             pos = torch.arange(first, first + count, device=table.device, dtype=torch.int32)
             slots = table[pos // ops.PAGE_TOKENS] * ops.PAGE_TOKENS + pos % ops.PAGE_TOKENS
             out = cache.read(slots, dtype or torch.bfloat16)
             cache.check()
+        for t in out:                                          # memory of the context's stream: its next use waits for the caller's
+            t.record_stream(caller)
         return out
 
     def reset(self):

@@ -907,3 +907,31 @@ def test_append_and_read_of_many_tokens(fmt, dtype, d, tokens):
             paged.code_values(c, fmt) * scales[slots, which][..., None].astype(np.float64)
         want[slots < 0] = 0
         within(f64(got[which]), want, half_step(want, dtype) + 2.0 ** -24 * np.abs(want), "read")
+
+
+def model_on_a_stream_of_its_own():
+    cfg = gen.TINY
+    model = WiciModel(cfg, max_tokens=64, stream=torch.cuda.Stream()).load(gen.make_weights(cfg))
+    model.prefill(gen.make_prompt(cfg, 45, seed=3))
+    return model
+
+
+def test_what_read_kv_gives_outlives_the_next_read_on_the_callers_stream():
+    # a caller on another stream than the context's drops a layer's K and V with its own work on them still queued
+    model = model_on_a_stream_of_its_own()
+    layers = range(model.cfg.n_layers)
+    want = [[t.clone() for t in model.read_kv(i)] for i in layers]
+    torch.cuda.synchronize()
+    small = [PagedKV(model.cfg.n_kv_heads, model.cfg.head_dim, "bf16", n_pages=3) for _ in layers]
+    slots = ints(range(45))
+    for _ in range(3):
+        torch.cuda._sleep(20_000_000)                         # about 10 ms: the reads below run ahead of this stream
+        for i in layers:
+            k, v = model.read_kv(i)
+            small[i].append(k, v, slots)
+            del k, v
+        torch.cuda.synchronize()
+        for i in layers:
+            assert all(torch.equal(a, b) for a, b in zip(small[i].read(slots), want[i])), i
+            small[i].data.zero_()
+    model.close()
