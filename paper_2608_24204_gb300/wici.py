@@ -343,8 +343,11 @@ class WiciModel:
         first = cache.data - self._kv.data_ptr()
         data = self._kv[first:first + cache.n_pages * cache.page_stride]
         at = pages - self._ws.data_ptr()
-        return (ops.PagedKV(cache.n_kv_heads, cache.head_dim, "bf16", data=data),
-                self._ws[at:at + 4 * n].view(torch.int32))
+        caller = torch.cuda.current_stream(self.stream.device)
+        with torch.cuda.stream(self.stream):                   # the status word is cleared before any call that may set it
+            kv = ops.PagedKV(cache.n_kv_heads, cache.head_dim, "bf16", data=data)
+        kv.status.record_stream(caller)
+        return kv, self._ws[at:at + 4 * n].view(torch.int32)
 
     def read_kv(self, layer: int, first: int = 0, count: int | None = None, dtype=None):
         """(k, v) [count, kv heads, head_dim] of the cached positions first.. (k after RoPE), on the device; the

@@ -935,3 +935,17 @@ def test_what_read_kv_gives_outlives_the_next_read_on_the_callers_stream():
             assert all(torch.equal(a, b) for a, b in zip(small[i].read(slots), want[i])), i
             small[i].data.zero_()
     model.close()
+
+
+def test_a_contexts_cache_reports_calls_on_its_stream_whatever_the_callers_does():
+    model = model_on_a_stream_of_its_own()
+    bad = ints([1 << 20])
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)                             # the caller's stream is behind the context's
+    cache, _ = model.kv_cache(0)
+    with torch.cuda.stream(model.stream):
+        cache.read(bad)
+    torch.cuda.synchronize()
+    with pytest.raises(wici.WiciError, match="slot"):
+        cache.check()
+    model.close()
