@@ -157,13 +157,6 @@ __device__ __forceinline__ uint32_t split2(float &lo, float &hi) {
     return w;
 }
 
-// int8 codes c as the fp16 numbers (c + 128) 2^-24, exactly: two operations fewer a pair
-__device__ __forceinline__ void decode4_raised(uint32_t w, uint32_t &lo, uint32_t &hi) {
-    const uint32_t x = w ^ 0x80808080u;
-    lo = __byte_perm(x, 0, 0x4140);
-    hi = __byte_perm(x, 0, 0x4342);
-}
-
 // Where 16-byte chunk c of key row r stands in a ring slot.  The chunks of a row are permuted so
 // that the 8 lanes of a shared-memory phase, which take rows i and i + 4 (K), or rows 0..3 and
 // neighbouring chunks (V), meet 8 different bank groups.  Rows of 64 bytes share a line of 128 in pairs.
@@ -271,8 +264,6 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     constexpr int SETS = P == 1 ? 2 : 1;                  // accumulators of a score: four chains of products at least
     constexpr int KS = S::kKSlots, VS = S::kVSlots;
     constexpr int PER = BF16 || D == 64 ? 8 : 16;         // adjacent elements of O that a lane holds per column
-    // K's int8 codes raised by 128: q times 128 is taken off the score again, which costs it 2 bits.  fp32 in: not so.
-    constexpr bool RAISED = FMT == WICI_KV_INT8 && !EXACT;
     // The reference of a row's exponents moves when a score passes it by more than kLag (base 2): moving it
     // rescales all of O, which a new maximum would ask for in about 24 of a run's first 60 units (random scores, 16
     // rows of which any may rise), one that far above the last hardly ever.
@@ -561,7 +552,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 
         // ---- Q fragments ----
         uint32_t qf[QPASS][STEPS][4];
-        float cq[R], q128[R];             // products to base-2 logits; what RAISED takes off them first
+        float cq[R];                      // products to base-2 logits
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             cq[r] = a.scale * 1.44269504088896340736f;
@@ -585,17 +576,6 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 for (int s = 0; s < STEPS; ++s)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) x[s][j] *= down;
-            }
-            if (RAISED) {
-                float sum = 0.f;
-#pragma unroll
-                for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sum += x[s][j];
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                q128[r] = sum * (128.f * 0x1p-24f);
-                cq[r] *= 0x1p24f;
             }
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
@@ -649,8 +629,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
                         for (int s = 0; s < 4; ++s) {
                             uint32_t b0, b1;
-                            if (RAISED) decode4_raised(word[s], b0, b1);
-                            else decode4<FMT>(word[s], b0, b1);
+                            decode4<FMT>(word[s], b0, b1);
 #pragma unroll
                             for (int k = 0; k < QPASS; ++k) mma16816<false>(c[n][0], qf[k][4 * i + s], b0, b1);
                         }
@@ -686,7 +665,6 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                         dot += c[n][0][col + 2];
                         if (SETS == 2) dot += c[n][SETS - 1][col + 2];
                     }
-                    if (RAISED) dot -= q128[r];
                     x[r][j] = dot * (BF16 ? cq[r] : ksc * cq[r]);
                 }
             }

@@ -949,3 +949,33 @@ def test_a_contexts_cache_reports_calls_on_its_stream_whatever_the_callers_does(
     with pytest.raises(wici.WiciError, match="slot"):
         cache.check()
     model.close()
+
+
+@pytest.mark.parametrize("group", [4, 12])
+def test_scores_of_small_int8_codes_keep_their_bits(group):
+    # one channel sets the scales of the keys, and the queries do not look at it: the codes that they meet are 0 to 4; a
+    # second one is large in the queries and zero in the keys.
+    # A score's products are exact in fp32, and each of its d sums drops at most 2^-23 of sum |q k| (tensor cores may
+    # truncate): d 2^-23 sum |q k|, not of what the codes' whole range would allow.
+    rng = np.random.default_rng(31)
+    n, d = 40, 64
+    x = 10 * rng.normal(size=(n, 1, d))
+    x[:, :, 5], x[:, :, 7] = 1000.0, 0.0
+    cache = PagedKV(1, d, "int8", n_pages=3)
+    cache.append(torch.tensor(x, device="cuda").float(), randn(rng, n, 1, d), ints(range(n)))
+    kk, vv = (f64(t)[:, 0] for t in cache.read(ints(range(n)), dtype=torch.float32))
+    q = 1 + 0.1 * randn(rng, 1, group, d)
+    q[:, :, 5], q[:, :, 7] = 0.0, 3000.0
+    q = q.to(torch.bfloat16)
+    lse, out = torch.empty(1, group, device="cuda"), torch.empty(1, group, d, device="cuda")
+    cache.attend(q, ints([[0, 1, 2]]), ints([n]), lse=lse, out=out)
+    s = f64(q)[0] @ kk.T * d ** -0.5
+    top = s.max(-1, keepdims=True)
+    p = np.exp(s - top)
+    want_lse = (top + np.log(p.sum(-1, keepdims=True)))[:, 0]
+    p /= p.sum(-1, keepdims=True)
+    ds = d * 2.0 ** -23 * (np.abs(f64(q)[0]) @ np.abs(kk).T).max(-1) * d ** -0.5 + 2.0 ** -23 * np.abs(s).max(-1)
+    # the exponential to 2^-21, a sum of n to n 2^-23, the logarithm and lse's own rounding
+    rest = 2.0 ** -21 + n * 2.0 ** -23
+    within(f64(lse)[0], want_lse, ds + rest + 2.0 ** -22 * np.abs(want_lse), "lse")
+    within(f64(out)[0], p @ vv, (2 * ds + 2 * rest + 2.0 ** -21)[:, None] * (p @ np.abs(vv)) + 2.0 ** -24 * np.abs(p @ vv), "out")
