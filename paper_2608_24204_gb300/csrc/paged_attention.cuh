@@ -35,8 +35,9 @@
 //   bf16 cache: q that is not bf16 as three terms; p as two (16 bits), or three where q is not
 //   bf16 or the result is fp32 (EXACT).
 //   8-bit cache: q as one fp16 term (bf16 and fp16 fit exactly) or, from fp32, as two (EXACT),
-//   scaled by a power of two per head; p as two (22 bits), scaled by the value's scale relative
-//   to the largest one so far, so that neither leaves fp16's range.
+//   scaled by a power of two per head; p times its value's scale as two (22 bits), multiplied by a
+//   power of two per query that follows the largest such weight so far: a weight is off by 2^-22 of
+//   itself or 2^-32 of the largest one, however large the scale of a value is that hardly counts.
 #pragma once
 #include "ops.cuh"
 
@@ -268,7 +269,9 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     // rescales all of O, which a new maximum would ask for in about 24 of a run's first 60 units (random scores, 16
     // rows of which any may rise), one that far above the last hardly ever.
     constexpr float kLag = 6.f;
-    constexpr float kPUnit = BF16 ? 1.f : 128.f;          // what weights are scaled up by: fp16 holds 2^kLag 4 of them
+    // 8-bit: a row's weights are multiplied by a power of two that takes the largest so far to at most 2^8 when it is
+    // chosen, and is chosen again when one passes 2^15: fp16 holds 2^16, and 2^-25 as the second term's last half bit.
+    constexpr float kPRoom = 256.f, kPMost = 0x1p15f;
 
     extern __shared__ __align__(128) uint8_t smem[];
     struct Rec {                          // a segment
@@ -601,7 +604,16 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[n][j] = 0.f;
-        float vref = 0x1p-125f, vinv = 0x1p125f;      // 8-bit: a power of two, at least a quarter of the largest V scale
+        float heaviest[R], per[R];                    // 8-bit: the largest weight so far, what weights are multiplied by
+#pragma unroll
+        for (int r = 0; r < R; ++r) heaviest[r] = 0.f, per[r] = kPRoom * 0x1p118f;
+        // O so far is multiplied by f for `per` to follow `heaviest`
+        auto follow = [&](int r, float f) {
+            const float was = __uint_as_float(0x7F000000u - __float_as_uint(per[r])) * f;      // f / per
+            const uint32_t e = min(max((__float_as_uint(heaviest[r]) + 0x7FFFFFu) & 0x7F800000u, 0x04800000u), 0x7E800000u);
+            per[r] = kPRoom * __uint_as_float(0x7F000000u - e);      // heaviest to its power of two, in [2^-118, 2^126]
+            return was * per[r];
+        };
 
         // ---- scores of one unit (unscaled) ----
         float c[2 * P][SETS][4];                             // [8 keys][sets of steps]
@@ -688,38 +700,17 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 up[r] = fmaxf(m[r], top);
                 grew |= up[r] > m[r] + kLag;
             }
-            float ratio = 1.f, vscale[J];
-            if (!BF16) {
-                float vtop = 0.f;
-#pragma unroll
-                for (int j = 0; j < J; ++j) vscale[j] = lds32(vs + j / 4 * S::kBlock + kKvPage * D + (t + 4 * (j & 3)) * 4);
-                if (part) {
-#pragma unroll
-                    for (int j = 0; j < J; ++j) {
-                        const int key = key0 + t + 4 * j;
-                        if (key < keys.lo || key >= keys.n) vscale[j] = 0.f;
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < J; ++j) vtop = fmaxf(vtop, vscale[j]);
-                vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, 1));
-                vtop = fmaxf(vtop, __shfl_xor_sync(0xffffffffu, vtop, 2));
-                if (vtop > vref) {                           // the same in every lane
-                    const uint32_t e = min((__float_as_uint(vtop) + 0x7FFFFFu) & 0x7F800000u, 0x7E800000u);
-                    ratio = vref * __uint_as_float(0x7F000000u - e);
-                    vref = __uint_as_float(e);
-                    vinv = __uint_as_float(0x7F000000u - e);
-                    grew = true;
-                }
-            }
             if (__any_sync(0xffffffffu, grew)) {
                 float f[R];
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     f[r] = m[r] == -INFINITY ? 0.f : ex2(m[r] - up[r]);   // nothing yet: zeros
                     l[r] *= f[r];
-                    f[r] *= ratio;
                     m[r] = up[r];
+                    if (!BF16) {
+                        heaviest[r] *= f[r];
+                        f[r] = follow(r, f[r]);
+                    }
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
@@ -730,18 +721,70 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 }
             }
             scores(ks_next);                                 // c has been read
+            float ref[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) ref[r] = m[r] == -INFINITY ? 0.f : m[r];
+            if (!BF16) {
+                // the weights in the place of the scores
+                float top[R];
+                bool heavy = false;
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const float vscale = lds32(vs + j / 4 * S::kBlock + kKvPage * D + (t + 4 * (j & 3)) * 4);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const float p = ex2(x[r][j] - ref[r]);
+                        l[r] += p;
+                        x[r][j] = p * vscale;
+                    }
+                }
+                if (part) {                                  // scales of other keys may be anything
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const int key = key0 + t + 4 * j;
+#pragma unroll
+                        for (int r = 0; r < R; ++r) x[r][j] = key >= keys.lo && key < keys.n ? x[r][j] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    top[r] = x[r][0];
+#pragma unroll
+                    for (int j = 1; j < J; ++j) top[r] = fmaxf(top[r], x[r][j]);
+                    heavy |= top[r] * per[r] > kPMost;
+                }
+                if (__any_sync(0xffffffffu, heavy)) {
+                    float f[R];
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        heaviest[r] = fmaxf(heaviest[r], top[r]);
+                        heaviest[r] = fmaxf(heaviest[r], __shfl_xor_sync(0xffffffffu, heaviest[r], 1));
+                        heaviest[r] = fmaxf(heaviest[r], __shfl_xor_sync(0xffffffffu, heaviest[r], 2));
+                        f[r] = follow(r, 1.f);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        o[n][0] *= f[0];
+                        o[n][1] *= f[0];
+                        o[n][2] *= f[R - 1];
+                        o[n][3] *= f[R - 1];
+                    }
+                }
+            }
             uint32_t pf[P][PPASS][4];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float ref = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
                 for (int pg = 0; pg < P; ++pg) {
                     float p[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        p[j] = ex2(x[r][4 * pg + j] - ref);
-                        l[r] += p[j];
-                        if (!BF16) p[j] *= vscale[4 * pg + j] * (vinv * kPUnit);
+                        if (BF16) {
+                            p[j] = ex2(x[r][4 * pg + j] - ref[r]);
+                            l[r] += p[j];
+                        } else {
+                            p[j] = x[r][4 * pg + j] * per[r];
+                        }
                     }
 #pragma unroll
                     for (int k = 0; k < PPASS; ++k) {
@@ -826,7 +869,6 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             if (lane == 0) sh.leaving[warp] = seg;
         }
         __syncwarp();
-        const float unit_of_o = BF16 ? 1.f : vref / kPUnit;
         // what ends in the block's first run is the block's whole part of its segment
         const bool to_piece = !left && r0 == u0;
         float *part_at = to_piece ? a.pieces + (int64_t)blockIdx.x * 2 * attn_piece_floats(D) : part_of(warp, left);
@@ -838,7 +880,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
             const int row = g + 8 * r;
             const bool alone = !entered && !left;
-            const float f = alone ? unit_of_o / l[r] : unit_of_o;
+            const float unit_of_o = BF16 ? 1.f : 1.f / per[r], f = alone ? unit_of_o / l[r] : unit_of_o;
             if (row >= rows) continue;
 #pragma unroll
             for (int n = 0; n < NT; n += 4) {

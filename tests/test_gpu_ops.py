@@ -979,3 +979,28 @@ def test_scores_of_small_int8_codes_keep_their_bits(group):
     rest = 2.0 ** -21 + n * 2.0 ** -23
     within(f64(lse)[0], want_lse, ds + rest + 2.0 ** -22 * np.abs(want_lse), "lse")
     within(f64(out)[0], p @ vv, (2 * ds + 2 * rest + 2.0 ** -21)[:, None] * (p @ np.abs(vv)) + 2.0 ** -24 * np.abs(p @ vv), "out")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,group,n", [("bf16", 4, 300), ("f32", 3, 300), ("bf16", 12, 300), ("bf16", 2, 5000)])
+@pytest.mark.parametrize("shift,score", [(20, -70.0), (34, -70.0), (60, -80.0), (-40, 20.0), (-40, 45.0), (100, -75.0)])
+def test_one_key_whose_v_is_of_another_size_than_the_others(fmt, dtype, group, n, shift, score):
+    # one key's V is 2^shift times the others', its score `score` above theirs: large values that hardly count, or a key
+    # that takes most of the weight with next to no value.  The result is held to sum p |v|, wherever the key stands.
+    rng = np.random.default_rng(32)
+    d = 64
+    k, v = 0.05 * rng.normal(size=(n, 1, d)), rng.normal(size=(n, 1, d)) + 0.5
+    q = 0.2 * rng.normal(size=(1, group, d))
+    q[..., 9], k[..., 9] = 4.0, 0.0
+    for at in (0, 16 * 7 + 3, n - 1):
+        kk, vv = k.copy(), v.copy()
+        kk[at, 0, 9], vv[at] = score / 4.0, v[at] * 2.0 ** shift
+        cache = PagedKV(1, d, fmt, n_pages=(n + 15) // 16)
+        cache.append(torch.tensor(kk, device="cuda").float(), torch.tensor(vv, device="cuda").float(), ints(range(n)))
+        stored = [f64(t) for t in cache.read(ints(range(n)), dtype=torch.float32)]
+        qq = torch.tensor(q, device="cuda").to(DT[dtype])
+        pages, vals = np.arange(cache.n_pages)[None], np.zeros((cache.n_pages * 16, 2, 1, d))
+        vals[:n, 0], vals[:n, 1] = stored
+        lse, out = torch.empty(1, group, device="cuda"), torch.empty(1, group, d, device="cuda")
+        cache.attend(qq, ints(pages), ints([n]), scale=1.0, lse=lse, out=out)
+        check_attention(cache, qq, pages, [n], vals, 1.0, 0, out, lse, dtype, "f32")
