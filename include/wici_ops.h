@@ -146,7 +146,9 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
  * over its keys t in [max(0, n - window), n) (window 0: all), n = lengths[b]; key t
  * is place t % 16 of page pages[b * max_pages + t / 16].  Pages of other keys are
  * not read and may hold anything.  A sequence without keys (n <= 0) has out 0 and
- * lse -infinity.  Several sequences may share pages. */
+ * lse -infinity.  Infinities and NaNs in a sequence's own keys act as in the
+ * formula, in its own result alone (e^(s_t - max s) below 2^-126 counts as 0).
+ * Several sequences may share pages. */
 typedef struct wici_attn_shape {
     int32_t batch;            /* 0 .. 65535 */
     int32_t max_pages;        /* columns of `pages`, 1 .. 2^27 - 1; (max_pages + 2) * heads < 2^31 */

@@ -139,23 +139,54 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// two fp32 values to 16 bits each (lo in the low half), and what the rounding left
-template <bool BF16>
-__device__ __forceinline__ uint32_t split2(float &lo, float &hi) {
-    uint32_t w;
-    if (BF16) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-        w = *(const uint32_t *)&h;
-        lo -= __uint_as_float(w << 16);
-        hi -= __uint_as_float(w & 0xFFFF0000u);
-    } else {
-        const __half2 h = __floats2half2_rn(lo, hi);
-        w = *(const uint32_t *)&h;
-        const float2 f = __half22float2(h);
-        lo -= f.x;
-        hi -= f.y;
+// Two fp32 values (POSITIVE: or 0) as sums of N 16-bit terms each, lo in a term's low half; the last one is the nearest
+// to what the others leave, times `last`.
+// bf16: the others are cut off, not rounded, and what they leave counts as 2^-30 of the value at least: all terms have
+// the value's sign and none is 0 beside it.  Their products with an infinite key or value are then the infinity that
+// the value's own product is.  fp16 meets codes alone, which are finite: every term is the nearest.
+template <bool BF16, bool POSITIVE, int N>
+__device__ __forceinline__ void split(float lo, float hi, uint32_t *w, float last) {
+    const float lo_least = fabsf(lo) * 0x1p-30f, hi_least = fabsf(hi) * 0x1p-30f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i + 1 == N) lo *= last, hi *= last;
+        if (!BF16) {
+            const __half2 h = __floats2half2_rn(lo, hi);
+            const float2 f = __half22float2(h);
+            w[i] = *(const uint32_t *)&h;
+            lo -= f.x;
+            hi -= f.y;
+        } else if (i + 1 == N) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+            w[i] = *(const uint32_t *)&h;
+        } else {
+            w[i] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+            const float lo_rest = lo - __uint_as_float(w[i] << 16), hi_rest = hi - __uint_as_float(w[i] & 0xFFFF0000u);
+            lo = POSITIVE ? fmaxf(lo_rest, lo_least) : copysignf(fmaxf(fabsf(lo_rest), lo_least), lo);
+            hi = POSITIVE ? fmaxf(hi_rest, hi_least) : copysignf(fmaxf(fabsf(hi_rest), hi_least), hi);
+        }
     }
-    return w;
+}
+// The A fragments of one lane's 4 values of a row (two pairs) in N terms, over the passes of a tile.  STACK: a pass has
+// a term in the lane's row and the next in the row 8 below, and half of the last one in both where they do not pair up;
+// a single term leaves the lower row 0.  Otherwise a pass has a term in row r of the lane's two.
+template <bool BF16, bool POSITIVE, bool STACK, int N, int STRIDE>
+__device__ __forceinline__ void split_row(const float *x, int r, uint32_t (*a)[4]) {
+    uint32_t w[2][N];
+    const float last = STACK && N > 1 && N % 2 ? 0.5f : 1.f;
+    split<BF16, POSITIVE, N>(x[0], x[1], w[0], last);
+    split<BF16, POSITIVE, N>(x[2], x[3], w[1], last);
+#pragma unroll
+    for (int k = 0; k < (STACK ? (N + 1) / 2 : N); ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (STACK) {
+                a[k * STRIDE][2 * h] = w[h][2 * k];
+                a[k * STRIDE][2 * h + 1] = N == 1 ? 0u : w[h][2 * k + 1 < N ? 2 * k + 1 : N - 1];
+            } else {
+                a[k * STRIDE][2 * h + r] = w[h][k];
+            }
+        }
 }
 
 // Where 16-byte chunk c of key row r stands in a ring slot.  The chunks of a row are permuted so
@@ -581,20 +612,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     for (int j = 0; j < 4; ++j) x[s][j] *= down;
             }
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-#pragma unroll
-                for (int k = 0; k < QPASS; ++k) {
-                    if (STACK) {
-                        qf[k][s][0] = split2<BF16>(x[s][0], x[s][1]);
-                        qf[k][s][2] = split2<BF16>(x[s][2], x[s][3]);
-                        qf[k][s][1] = 2 * k + 1 < TQ ? split2<BF16>(x[s][0], x[s][1]) : 0u;
-                        qf[k][s][3] = 2 * k + 1 < TQ ? split2<BF16>(x[s][2], x[s][3]) : 0u;
-                    } else {
-                        qf[k][s][r] = split2<BF16>(x[s][0], x[s][1]);
-                        qf[k][s][2 + r] = split2<BF16>(x[s][2], x[s][3]);
-                    }
-                }
-            }
+            for (int s = 0; s < STEPS; ++s) split_row<BF16, false, STACK, TQ, STEPS>(x[s], r, &qf[0][s]);
         }
 
         float m[R], l[R], o[NT][4];
@@ -786,18 +804,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                             p[j] = x[r][4 * pg + j] * per[r];
                         }
                     }
-#pragma unroll
-                    for (int k = 0; k < PPASS; ++k) {
-                        if (STACK) {
-                            pf[pg][k][0] = split2<BF16>(p[0], p[1]);
-                            pf[pg][k][2] = split2<BF16>(p[2], p[3]);
-                            pf[pg][k][1] = 2 * k + 1 < TP ? split2<BF16>(p[0], p[1]) : 0u;
-                            pf[pg][k][3] = 2 * k + 1 < TP ? split2<BF16>(p[2], p[3]) : 0u;
-                        } else {
-                            pf[pg][k][r] = split2<BF16>(p[0], p[1]);
-                            pf[pg][k][2 + r] = split2<BF16>(p[2], p[3]);
-                        }
-                    }
+                    split_row<BF16, true, STACK, TP, 1>(p, r, pf[pg]);
                 }
             }
             // V: rows t + 4 i of a page; column g of tile n is element PER (g + 8 (n / PER)) + n % PER of the head

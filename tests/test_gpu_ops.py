@@ -1004,3 +1004,50 @@ def test_one_key_whose_v_is_of_another_size_than_the_others(fmt, dtype, group, n
         lse, out = torch.empty(1, group, device="cuda"), torch.empty(1, group, d, device="cuda")
         cache.attend(qq, ints(pages), ints([n]), scale=1.0, lse=lse, out=out)
         check_attention(cache, qq, pages, [n], vals, 1.0, 0, out, lse, dtype, "f32")
+
+
+@pytest.mark.parametrize("dtype,group", [("bf16", 4), ("f32", 4), ("f16", 12), ("bf16", 12)])
+def test_infinite_keys_and_values_follow_the_formula(dtype, group):
+    # a weight times an infinite value is that infinity, two of them NaN; a key whose score is -infinity has no weight,
+    # one of +infinity makes NaN; the rest of the sequence's result, and the other sequences', as if nothing were there
+    rng = np.random.default_rng(33)
+    d, kv, lengths = 64, 2, [20, 40, 40, 600]
+    cache, q, pages, vals = attention_case(rng, 4, kv, group, d, "bf16", dtype, lengths)
+    q[:, :, 10] = q[:, :, 10].abs() + 0.25
+    q[3, 1, 10] *= -1
+    blocks, inf = cache.data.view(torch.bfloat16).view(-1, 2, kv, 16, d), float("inf")
+
+    def put(b, t, which, head, i, x):
+        page = int(pages[b][t // 16])
+        blocks[page, which, head, t % 16, i] = x
+        vals[page * 16 + t % 16, which, head, i] = x
+
+    put(1, 3, 1, 0, 10, inf)
+    put(1, 33, 1, 0, 11, -inf)
+    put(1, 4, 1, 1, 12, inf), put(1, 37, 1, 1, 12, -inf)
+    put(2, 5, 0, 0, 10, -inf)                                 # no weight
+    put(2, 17, 0, 1, 10, inf)                                 # NaN
+    put(3, 500, 0, 0, 10, -inf)                               # no weight; for the query of the other sign NaN
+    put(3, 599, 1, 1, 63, inf), put(3, 0, 1, 1, 63, inf)
+    lse, out = torch.empty(4, kv * group, device="cuda"), torch.empty(4, kv * group, d, device="cuda")
+    cache.attend(q, ints(pages), ints(lengths), lse=lse, out=out)
+    for b, n in enumerate(lengths):
+        slots = [int(pages[b][t // 16]) * 16 + t % 16 for t in range(n)]
+        for h in range(kv * group):
+            k, v, q64 = vals[slots, 0, h // group], vals[slots, 1, h // group], f64(q)[b, h]
+            with np.errstate(invalid="ignore"):
+                s = k @ q64 * d ** -0.5
+                p = np.exp(s - s.max())
+                want, got = p @ v / p.sum(), f64(out)[b, h]
+                want_lse = s.max() + np.log(p.sum())
+            if np.isnan(want_lse):
+                assert np.isnan(got).all() and np.isnan(float(lse[b, h]))
+                continue
+            assert np.array_equal(np.isnan(want), np.isnan(got)) and np.array_equal(want[np.isinf(want)], got[np.isinf(want)])
+            there = np.isfinite(s)                            # of the keys that count
+            size = (np.abs(k[there]) @ np.abs(q64)).max() * d ** -0.5
+            ds = size * (2 * d * 2.0 ** -23 + (2.0 ** -16 if dtype == "f32" else 0.0))
+            weight = p[there] @ np.where(np.isfinite(v[there]), np.abs(v[there]), 0) / p.sum()
+            fine = np.isfinite(want)
+            within(got[fine], want[fine], ((2 * ds + 2.0 ** -16 + 2.0 ** -21 + n * 2.0 ** -23) * weight)[fine] + 1e-30, f"sequence {b}, head {h}")
+            within(float(lse[b, h]), want_lse, ds + 2.0 ** -20 + n * 2.0 ** -23 + 2.0 ** -23 * abs(want_lse), "lse")
