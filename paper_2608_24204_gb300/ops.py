@@ -235,7 +235,7 @@ class PagedKV:
         self.cache = wici_kv_cache(data.data_ptr(), page, self.n_pages, n_kv_heads, head_dim, FORMATS[fmt])
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._cache, self._status = ctypes.addressof(self.cache), self.status.data_ptr()
-        self._workspaces = {}
+        self._workspaces, self._served = {}, {}   # per stream; the largest batch that its workspace is known to take, per heads
         if self._device >= 0 and self._device == torch.cuda.current_device():
             self.workspace_bytes(n_kv_heads, 1)   # sets the attention kernels up, before a capture may need them
 
@@ -323,11 +323,12 @@ class PagedKV:
     def _workspace_for(self, stream: int, n_q_heads: int, batch: int) -> torch.Tensor:
         if torch.cuda.is_current_stream_capturing():
             return self.workspace(n_q_heads, batch)   # zeroed by every replay, in the graph's own memory
-        key = (stream, n_q_heads)
-        kept = self._workspaces.get(key)
-        if kept is None or kept[0] < batch:
-            kept = self._workspaces[key] = (batch, self.workspace(n_q_heads, batch))
-        return kept[1]
+        if self._served.get((stream, n_q_heads), -1) < batch:
+            kept = self._workspaces.get(stream)
+            if kept is None or kept.numel() < self.workspace_bytes(n_q_heads, batch):
+                self._workspaces[stream] = self.workspace(n_q_heads, batch)
+            self._served[stream, n_q_heads] = batch
+        return self._workspaces[stream]
 
     def check(self) -> None:
         """Waits for the current stream and raises if a call on it met a slot, page or length outside the cache

@@ -1051,3 +1051,20 @@ def test_infinite_keys_and_values_follow_the_formula(dtype, group):
             fine = np.isfinite(want)
             within(got[fine], want[fine], ((2 * ds + 2.0 ** -16 + 2.0 ** -21 + n * 2.0 ** -23) * weight)[fine] + 1e-30, f"sequence {b}, head {h}")
             within(float(lse[b, h]), want_lse, ds + 2.0 ** -20 + n * 2.0 ** -23 + 2.0 ** -23 * abs(want_lse), "lse")
+
+
+def test_a_stream_keeps_one_workspace_for_every_batch_and_head_count(monkeypatch):
+    rng = np.random.default_rng(34)
+    cache, _, pages, vals = attention_case(rng, 6, 2, 1, 64, "bf16", "bf16", [40, 1, 0, 700, 33, 16])
+    lengths, made, make = [40, 1, 0, 700, 33, 16], [], cache.workspace
+    monkeypatch.setattr(cache, "workspace", lambda *a: made.append(a) or make(*a))
+    other = torch.cuda.Stream()
+    for stream in (torch.cuda.current_stream(), other):
+        for batch, group in ((1, 1), (2, 1), (6, 1), (3, 5), (6, 16), (1, 16), (6, 1)):
+            q = randn(rng, batch, 2 * group, 64, dtype="bf16")
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                out = cache.attend(q, ints(pages[:batch]), ints(lengths[:batch]))
+            torch.cuda.synchronize()
+            check_attention(cache, q, pages[:batch], lengths[:batch], vals, 0.125, 0, out, None, "bf16")
+    assert len(made) == 2

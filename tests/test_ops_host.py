@@ -282,3 +282,13 @@ int main() {
     subprocess.run([cxx, "-std=c++17", "-O1", str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, f"exit {r.returncode}: {r.stdout}{r.stderr}"
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_workspace_serves_every_batch_and_head_count(d):
+    # the tickets, then for each of two blocks an SM two pieces of 16 rows of d + 2 floats
+    sizes = {ops.wici_paged_attention_workspace_bytes(cache(kv=kv, d=d), kv * group, b)
+             for kv in (1, 8) for group in (1, 4, 16, 71) for b in (0, 1, 64, 65535)}
+    size, = sizes
+    blocks, rest = divmod(size - ops.WICI_ATTN_ZEROED, 2 * 16 * (d + 2) * 4)
+    assert rest == 0 and blocks >= 2 and blocks % 2 == 0 and blocks * 4 <= ops.WICI_ATTN_ZEROED
