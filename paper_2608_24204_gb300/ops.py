@@ -181,6 +181,21 @@ def _stream(device: int) -> int:
     return _raw_stream(device) if _raw_stream else torch.cuda.current_stream(device).cuda_stream
 
 
+class _Rotation(torch.autograd.Function):
+    """A rotation that autograd sees: its gradient is the rotation back, with the same gain."""
+
+    @staticmethod
+    def forward(ctx, x, positions, rope, inverse):
+        ctx.rope, ctx.inverse = rope, inverse
+        ctx.save_for_backward(positions)
+        return rope.apply(x, positions, inverse=inverse)
+
+    @staticmethod
+    def backward(ctx, dy):
+        positions, = ctx.saved_tensors
+        return ctx.rope.apply(dy if dy.stride(2) == 1 else dy.contiguous(), positions, inverse=not ctx.inverse), None, None, None
+
+
 class Rope:
     """Rotary positions of heads of `head_dim`: see wici_rope_spec for the scaling rules."""
 
@@ -198,7 +213,10 @@ class Rope:
     def apply(self, x: torch.Tensor, positions: torch.Tensor, out: torch.Tensor | None = None,
               inverse: bool = False) -> torch.Tensor:
         """x [tokens, heads, head_dim] rotated by `positions` (int32 [tokens]); with `inverse` the gradient of
-        that with respect to x, from the gradient of its result.  `out` may be x."""
+        that with respect to x, from the gradient of its result.  `out` may be x.  Autograd sees the call where `out`
+        is not given."""
+        if out is None and x.requires_grad and torch.is_grad_enabled():
+            return _Rotation.apply(x, positions, self, inverse)
         device, d = x.get_device(), self.head_dim
         stream = _stream(device)
         hx = _heads(x, d, device, "x")

@@ -1068,3 +1068,46 @@ def test_a_stream_keeps_one_workspace_for_every_batch_and_head_count(monkeypatch
             torch.cuda.synchronize()
             check_attention(cache, q, pages[:batch], lengths[:batch], vals, 0.125, 0, out, None, "bf16")
     assert len(made) == 2
+
+
+@pytest.mark.parametrize("dtype,rot,interleaved,scaling", [("f32", 24, True, "yarn"), ("bf16", 32, False, "none"), ("f32", 32, False, "bands")])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_autograd_sees_a_rotation(dtype, rot, interleaved, scaling, inverse):
+    rng = np.random.default_rng(35)
+    T, H, d = 5, 3, 32
+    r = Rope(d, 1e4, rot_dim=rot, interleaved=interleaved, scaling=scaling, **SCALED[scaling])
+    f, g = paged.rope_frequencies(rot, 1e4, scaling, **SCALED[scaling])
+    pos = rng.integers(0, 3000, T)
+    x, w = randn(rng, T, H, d, dtype=dtype).requires_grad_(), randn(rng, T, H, d, dtype=dtype)
+    y = r.apply(x, ints(pos), inverse=inverse)
+    with torch.no_grad():
+        assert torch.equal(y, r.apply(x, ints(pos), inverse=inverse)) and not r.apply(x, ints(pos)).requires_grad
+    dx, = torch.autograd.grad(y, x, w)
+    check_rope(w, dx, pos, rot, 1e4, interleaved, scaling, not inverse, dtype)           # the formula's gradient
+    if dtype == "f32":                                        # and that of differences: the map is linear, the step is 1
+        for i in range(0, d, 5):
+            e = np.zeros((1, 1, d))
+            e[..., i] = 0.5
+            up, down = (paged.rope(f64(x) + s * e, pos, rot, f, g, interleaved, inverse) for s in (1, -1))
+            # off by 2^-21 (|w_a| + |w_b|) g, at most 2^-20 g max |w|, and half a step
+            within(f64(dx)[..., i], (f64(w) * (up - down)).sum(-1), 2.0 ** -19 * g * float(w.abs().max()), "differences")
+
+
+def test_gradients_of_rotations_of_broadcast_heads_and_of_gradients():
+    rng = np.random.default_rng(36)
+    T, H, d = 4, 6, 64
+    r, pos = Rope(d, 1e4), ints(rng.integers(0, 999, T))
+    one = randn(rng, T, 1, d).requires_grad_()
+    w = randn(rng, T, H, d)
+    dx, = torch.autograd.grad(r.apply(one.expand(T, H, d), pos), one, w)
+    back = r.apply(w, pos, inverse=True)
+    within(f64(dx), f64(back).sum(1, keepdims=True), H * 2.0 ** -23 * np.abs(f64(back)).sum(1, keepdims=True), "shared heads")
+    x = randn(rng, T, H, d).requires_grad_()
+    r.apply(x, pos).sum().backward()                          # a gradient whose elements share one place
+    assert torch.equal(x.grad, r.apply(torch.ones_like(w), pos, inverse=True))
+    v = randn(rng, T, H, d).requires_grad_()
+    dx, = torch.autograd.grad(r.apply(x, pos), x, v, create_graph=True)
+    dv, = torch.autograd.grad(dx, v, w)                       # the gradient's own gradient: forward again
+    assert torch.equal(dv, r.apply(w, pos))
+    with pytest.raises(ValueError):
+        r.apply(x, pos[:3])
