@@ -105,7 +105,8 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
  *   WICI_KV_INT8  int8 [16][head_dim], then fp32 scale[16]
  *   WICI_KV_E4M3  e4m3 [16][head_dim], then fp32 scale[16]
  * A token's head stands for code * scale; it is written with scale = max|x| / 127
- * (int8) or / 448 (e4m3) in fp32 and code = x / scale rounded to nearest even.  A
+ * (int8) or / 448 (e4m3) in fp32 and code = x / scale, an fp32 quotient that is
+ * right to its last bit, rounded to nearest even.  A
  * head whose scale would be below 2^-126, one of zeros among them, has scale 0, and
  * one that holds an infinity or NaN has scale NaN (it reads as NaN throughout).
  * Slot s is place s % 16 of page s / 16.  The paper names no cache precision; 8-bit
@@ -135,8 +136,9 @@ int wici_kv_append(void *cuda_stream, const wici_kv_cache *cache, const int32_t 
                    const wici_heads *k, const wici_heads *v, const wici_rope_plan *rope, const int32_t *positions,
                    const wici_heads *q, const wici_heads *q_out, int32_t *status);
 
-/* k[i], v[i] (outputs; either may be NULL) = the values at slots[i], rounded once
- * to the output's type; zeros where slots[i] < 0.  Slots may repeat. */
+/* k[i], v[i] (outputs; either may be NULL) = the values at slots[i], code * scale in
+ * fp32 and that rounded to the output's type; zeros where slots[i] < 0.  Slots may
+ * repeat. */
 int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *slots, int64_t tokens,
                  const wici_heads *k, const wici_heads *v, int32_t *status);
 
@@ -148,6 +150,8 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
  * not read and may hold anything.  A sequence without keys (n <= 0) has out 0 and
  * lse -infinity.  Infinities and NaNs in a sequence's own keys act as in the
  * formula, in its own result alone (e^(s_t - max s) below 2^-126 counts as 0).
+ * Over an 8-bit cache a key's weight times its scale of V is held to 2^-22 of itself
+ * or 2^-32 of the sequence's largest, far less than what codes cost that key's values.
  * Several sequences may share pages. */
 typedef struct wici_attn_shape {
     int32_t batch;            /* 0 .. 65535 */

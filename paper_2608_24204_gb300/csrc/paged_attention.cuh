@@ -13,8 +13,8 @@
 // joined by the block at its end, and by the block that finishes last where blocks share one:
 // short segments (kAttnWhole) they never share.
 // Measured (device time; 8 KV heads of 128): 32 sequences of up to 4000 tokens in bf16 47 us, 5.6 TB/s
-// of keys; two of 100001 to 131072 145 us, 6.5 TB/s; 64 of up to 8192 in int8, five queries a KV head,
-// 109 us, 5.6 TB/s; 256 of 20 to 300 35 us, 1000 of them 107 us; one of 200 tokens 7.9 us.  Of each
+// of keys; two of 100001 to 131072 141 us, 6.7 TB/s; 64 of up to 8192 in int8, five queries a KV head,
+// 108 us, 5.6 TB/s; 256 of 20 to 300 35 us, 1000 of them 108 us; one of 200 tokens 8.0 us.  Of each
 // about 4 us pass before the first keys are there (lengths, then pages, then keys), and 4 to 8 after the
 // first warp is done.
 //
@@ -47,10 +47,10 @@ constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = 32 * kAttnWarps;
 constexpr uint32_t kAttnSegment = 3;       // units that a segment weighs beside its own
 constexpr uint32_t kAttnMinUnits = 2;      // weight of a warp's run at least: shorter ones would not pay for joining more parts
-                                           // (8 heads of 1000 tokens 9.7 us, with 3 10.3; of 140, 16 sequences: 9.0 and 11.4)
+                                           // (8 heads of 1000 tokens 10.1 us; with 3 instead, before, 10.3 for 9.7; of 140, 16 sequences: 9.0 and 11.4)
 // Weight of a segment at most that blocks do not share.  Block edges moved by up to half of it cost the longest warp 3
 // units, a joining of pieces 3 us and more: 16 sequences of 70 tokens, 4 KV heads of 8 queries, 10.2 us (13.1 where
-// blocks share), 16 queries of an e4m3 cache 11.6 (23.3); 1000 of 20 to 300 tokens 107.6 (112.4).  16 and 40 in its
+// blocks share), 16 queries of an e4m3 cache 12.2 (23.3); 1000 of 20 to 300 tokens 108.5 (112.4).  16 and 40 in its
 // place: 111.5 and 106.9 for the 1000, the same for the others.
 constexpr uint32_t kAttnWhole = 24;
 constexpr int kAttnPieceRows = 16;    // rows of a piece in the workspace (a head tile has 8 or 16)
@@ -1050,7 +1050,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 // The kernels of a format.  A group of more than 8 queries takes 16 a tile where its terms are few, and tiles of 8
 // (each with its own pass over the keys) where they are many: with 16 a tile the terms of fp32 do not fit the
 // registers.  16 sequences of 1000 to 4000 tokens, 16 queries a group, head_dim 128, fp32: 51 us in tiles of 8, 64 in
-// tiles of 16; 12 queries, bf16, 32 sequences: 93 and 64 (an earlier form of the loop).
+// tiles of 16; 12 queries, bf16, 32 sequences: 93 and 64 (an earlier form of the loop; 59 now).  16 queries, 32
+// sequences of 1000 to 4000, head_dim 64: bf16 36 us, int8 37, e4m3 34.
 enum AttnKind { ATTN_STACK, ATTN_STACK_EXACT, ATTN_PLAIN };
 inline AttnKind attn_kind(int group, bool exact) {
     return exact ? ATTN_STACK_EXACT : group <= 8 ? ATTN_STACK : ATTN_PLAIN;

@@ -232,7 +232,10 @@ class Rope:
 
 class PagedKV:
     """A paged key-value cache of one layer: `n_pages` pages of 16 tokens in a torch buffer (or in `data`, a uint8
-    tensor of whole pages).  Slot s is place s % 16 of page s // 16."""
+    tensor of whole pages).  Slot s is place s % 16 of page s // 16.
+
+    A buffer made here and the word that `check` reads are cleared on the stream that is current here: calls on another
+    stream come after that, as with any tensor.  Autograd does not see the calls."""
 
     def __init__(self, n_kv_heads: int, head_dim: int, fmt: str = "bf16", n_pages: int | None = None,
                  data: torch.Tensor | None = None, device=None):

@@ -1111,3 +1111,28 @@ def test_gradients_of_rotations_of_broadcast_heads_and_of_gradients():
     assert torch.equal(dv, r.apply(w, pos))
     with pytest.raises(ValueError):
         r.apply(x, pos[:3])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,group", [("bf16", 4), ("f32", 5), ("f16", 12)])
+def test_weights_far_below_the_heaviest(fmt, dtype, group):
+    # scores tens apart: where the heaviest key's code is 0, what is left of an element are weights of 2^-20 and less.  A
+    # weight times its scale is in fp16 terms whose last half bit, 2^-25, is 2^-32 of the heaviest (at least 2^7 of those
+    # units): each code adds that much of its own size to the tolerance on sum p |v|.
+    rng = np.random.default_rng(37)
+    lengths, d, kv = [12, 90, 333, 3], 64, 2
+    cache, q, pages, vals = attention_case(rng, 4, kv, group, d, fmt, dtype, lengths)
+    out = torch.empty(q.shape, device="cuda")
+    cache.attend(q, ints(pages), ints(lengths), scale=1.0, out=out)
+    q64 = f64(q)
+    want, _, weight = paged.paged_attention(q64, vals[:, 0], vals[:, 1], pages, lengths, 1.0, 0)
+    for b, n in enumerate(lengths):
+        slots = [int(pages[b][t // 16]) * 16 + t % 16 for t in range(n)]
+        for h in range(q.shape[1]):
+            k, v = vals[slots, 0, h // group], vals[slots, 1, h // group]
+            p = np.exp(k @ q64[b, h] - (k @ q64[b, h]).max())
+            scale = np.abs(v).max(-1, keepdims=True) / (127 if fmt == "int8" else 448)    # every head's largest code is the top one
+            floor = 2.0 ** -32 * (p * scale[:, 0]).max() / p.sum() * np.abs(v / scale).sum(0)
+            ds = float(np.max(np.abs(k) @ np.abs(q64[b, h]))) * (2 * d * 2.0 ** -23 + (2.0 ** -16 if dtype == "f32" else 0.0))
+            within(f64(out)[b, h], want[b, h], (2 * ds + 2.0 ** -16 + 2.0 ** -21 + n * 2.0 ** -23) * weight[b, h] + floor,
+                   f"sequence {b}, head {h}")
