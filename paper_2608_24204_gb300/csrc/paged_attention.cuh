@@ -32,8 +32,8 @@
 // to the scores and to the weights in fp32.  Q and P are carried as sums of 16-bit terms.  With
 // at most 8 queries a group the second term's rows fill the upper half of the 16 (STACK), so two
 // terms cost what one does; larger groups take 16 queries a tile and a pass per term.
-//   bf16 cache: q that is not bf16 as three terms; p as two (16 bits), or three where q is not
-//   bf16 or the result is fp32 (EXACT).
+//   bf16 cache: q that is not bf16 as three terms; p as two (17 bits, in tiles of 16 queries 16),
+//   or three where q is not bf16 or the result is fp32 (EXACT).
 //   8-bit cache: q as one fp16 term (bf16 and fp16 fit exactly) or, from fp32, as two (EXACT),
 //   scaled by a power of two per head; p times its value's scale as two (22 bits), multiplied by a
 //   power of two per query that follows the largest such weight so far: a weight is off by 2^-22 of
@@ -141,10 +141,11 @@ __device__ __forceinline__ float ex2(float x) {
 }
 // Two fp32 values (POSITIVE: or 0) as sums of N 16-bit terms each, lo in a term's low half; the last one is the nearest
 // to what the others leave, times `last`.
-// bf16: the others are cut off, not rounded, and what they leave counts as 2^-30 of the value at least: all terms have
-// the value's sign and none is 0 beside it.  Their products with an infinite key or value are then the infinity that
-// the value's own product is.  fp16 meets codes alone, which are finite: every term is the nearest.
-template <bool BF16, bool POSITIVE, int N>
+// CUT (bf16): the others are cut off, not rounded, and what they leave counts as 2^-30 of the value at least: all terms
+// have the value's sign and none is 0 beside it.  Their products with an infinite key or value are then the infinity
+// that the value's own product is.  Otherwise every term is the nearest, which is worth a bit: fp16 terms meet codes
+// alone, which are finite, and of two bf16 terms in rows of their own the first one's sum tells (rows_sum).
+template <bool BF16, bool CUT, bool POSITIVE, int N>
 __device__ __forceinline__ void split(float lo, float hi, uint32_t *w, float last) {
     const float lo_least = fabsf(lo) * 0x1p-30f, hi_least = fabsf(hi) * 0x1p-30f;
 #pragma unroll
@@ -156,9 +157,11 @@ __device__ __forceinline__ void split(float lo, float hi, uint32_t *w, float las
             w[i] = *(const uint32_t *)&h;
             lo -= f.x;
             hi -= f.y;
-        } else if (i + 1 == N) {
+        } else if (i + 1 == N || !CUT) {
             const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
             w[i] = *(const uint32_t *)&h;
+            lo -= __uint_as_float(w[i] << 16);
+            hi -= __uint_as_float(w[i] & 0xFFFF0000u);
         } else {
             w[i] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
             const float lo_rest = lo - __uint_as_float(w[i] << 16), hi_rest = hi - __uint_as_float(w[i] & 0xFFFF0000u);
@@ -167,15 +170,20 @@ __device__ __forceinline__ void split(float lo, float hi, uint32_t *w, float las
         }
     }
 }
+// The sum of a stacked tile's two rows: where the first term has met an infinity, the second may have met it with any sign
+__device__ __forceinline__ float rows_sum(float first, float second) {
+    return fabsf(first) < INFINITY ? first + second : first;
+}
 // The A fragments of one lane's 4 values of a row (two pairs) in N terms, over the passes of a tile.  STACK: a pass has
 // a term in the lane's row and the next in the row 8 below, and half of the last one in both where they do not pair up;
 // a single term leaves the lower row 0.  Otherwise a pass has a term in row r of the lane's two.
 template <bool BF16, bool POSITIVE, bool STACK, int N, int STRIDE>
 __device__ __forceinline__ void split_row(const float *x, int r, uint32_t (*a)[4]) {
     uint32_t w[2][N];
+    constexpr bool CUT = BF16 && !(STACK && N == 2);
     const float last = STACK && N > 1 && N % 2 ? 0.5f : 1.f;
-    split<BF16, POSITIVE, N>(x[0], x[1], w[0], last);
-    split<BF16, POSITIVE, N>(x[2], x[3], w[1], last);
+    split<BF16, CUT, POSITIVE, N>(x[0], x[1], w[0], last);
+    split<BF16, CUT, POSITIVE, N>(x[2], x[3], w[1], last);
 #pragma unroll
     for (int k = 0; k < (STACK ? (N + 1) / 2 : N); ++k)
 #pragma unroll
@@ -896,7 +904,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) v[c][i] = (STACK ? o[n + i][c] + o[n + i][c + 2] : o[n + i][2 * r + c]) * f;
+                    for (int c = 0; c < 2; ++c) v[c][i] = (STACK ? rows_sum(o[n + i][c], o[n + i][c + 2]) : o[n + i][2 * r + c]) * f;
                 const int d0 = PER * (2 * t + 8 * (n / PER)) + n % PER;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
