@@ -105,8 +105,8 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
  *   WICI_KV_INT8  int8 [16][head_dim], then fp32 scale[16]
  *   WICI_KV_E4M3  e4m3 [16][head_dim], then fp32 scale[16]
  * A token's head stands for code * scale; it is written with scale = max|x| / 127
- * (int8) or / 448 (e4m3) in fp32 and code = x / scale, an fp32 quotient that is
- * right to its last bit, rounded to nearest even.  A
+ * (int8) or / 448 (e4m3) in fp32 and code = x / scale rounded to nearest even (for
+ * e4m3 from the fp32 quotient, which is right to its last bit).  A
  * head whose scale would be below 2^-126, one of zeros among them, has scale 0, and
  * one that holds an infinity or NaN has scale NaN (it reads as NaN throughout).
  * Slot s is place s % 16 of page s / 16.  The paper names no cache precision; 8-bit

@@ -1136,3 +1136,26 @@ def test_weights_far_below_the_heaviest(fmt, dtype, group):
             ds = float(np.max(np.abs(k) @ np.abs(q64[b, h]))) * (2 * d * 2.0 ** -23 + (2.0 ** -16 if dtype == "f32" else 0.0))
             within(f64(out)[b, h], want[b, h], (2 * ds + 2.0 ** -16 + 2.0 ** -21 + n * 2.0 ** -23) * weight[b, h] + floor,
                    f"sequence {b}, head {h}")
+
+
+@pytest.mark.parametrize("dtype,d,tokens", [("bf16", 128, 700), ("f16", 64, 700), ("f32", 64, 300), ("bf16", 64, 5000)])
+def test_int8_codes_are_the_nearest_to_the_quotient_itself(dtype, d, tokens):
+    # many quotients of 16-bit values are ties of x 127 / max; of x / scale, whose scale is rounded to fp32, they lie up to
+    # 2^-25 beside the border, and nearer than that never, so 64 bits tell the side: codes are compared exactly
+    rng = np.random.default_rng(38)
+    pages = tokens // 16 + 1
+    cache = PagedKV(2, d, "int8", n_pages=pages)
+    k, v = randn(rng, tokens, 2, d, dtype=dtype), randn(rng, tokens, 2, d, dtype=dtype)
+    v[:, 0] = (127 * v[:, 0].float()).round().to(DT[dtype]) * 0.5
+    v[:, 0, 0] = 127.0 if dtype != "bf16" else 254.0           # a scale of 1 or 2: true ties, to the even code
+    v[:, 0].clamp_(-127.0 if dtype != "bf16" else -254.0, float(v[0, 0, 0]))
+    v[5] *= 2.0 ** (-12 if dtype == "f16" else -116)           # scales near the end of the normal range
+    slots = slots_for(rng, tokens, pages)
+    cache.append(k, v, ints(slots))
+    codes, scales = paged.unpack(cache.data.cpu().numpy(), 2, d, "int8")
+    for which, x in ((0, f64(k)), (1, f64(v))):
+        s = scales[slots, which]
+        np.testing.assert_array_equal(s, (np.abs(x).max(-1).astype(np.float32) / np.float32(127)))
+        keep = s >= 2.0 ** -126
+        q = x / np.where(keep, s, 1).astype(np.float64)[..., None]
+        np.testing.assert_array_equal(codes[slots, which].view(np.int8)[keep], np.rint(q)[keep])
