@@ -1,7 +1,7 @@
 /*
  * wici_ops.h - operators of a batched decode step, for engines that own their
  * device memory: rotary positions, writing and reading a paged key-value cache
- * (bf16, or quantised to 8 bits), and attention of one new token per sequence
+ * (bf16, or quantised to 8 or 4 bits), and attention of one new token per sequence
  * over that cache.  They stand beside wici_lm_head_argmax_noalloc (wici.h) and
  * need no context; wici_kv_view hands them the cache of one.
  *
@@ -104,14 +104,20 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
  *   WICI_KV_BF16  bf16 [16][head_dim]           (a context's own layout, wici_get_sizes)
  *   WICI_KV_INT8  int8 [16][head_dim], then fp32 scale[16]
  *   WICI_KV_E4M3  e4m3 [16][head_dim], then fp32 scale[16]
+ *   WICI_KV_E2M1  e2m1 [16][head_dim / 2] bytes of two codes, the even element's in the lower
+ *                 half, then e4m3 block scale[16][head_dim / 16], then fp32 scale[16]
  * A token's head stands for code * scale; it is written with scale = max|x| / 127
  * (int8) or / 448 (e4m3) in fp32 and code = x / scale rounded to nearest even (for
  * e4m3 from the fp32 quotient, which is right to its last bit).  A
  * head whose scale would be below 2^-126, one of zeros among them, has scale 0, and
  * one that holds an infinity or NaN has scale NaN (it reads as NaN throughout).
+ * An e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4 or 6, with a sign) stands for code * block scale *
+ * scale: scale = max|x| / 2688 in fp32, block scale = max|x| of 16 neighbours / (6 scale) to the
+ * nearest e4m3, code = x / (block scale * scale) to the nearest e2m1, both as real numbers and
+ * half way to the even one.  Scale 0 is below 2^-100 here; NaN as above.
  * Slot s is place s % 16 of page s / 16.  The paper names no cache precision; 8-bit
- * codes halve the bytes that bound decoding. */
-enum { WICI_KV_BF16 = 0, WICI_KV_INT8 = 1, WICI_KV_E4M3 = 2 };
+ * codes halve the bytes that bound decoding, 4-bit codes take 0.3 of them. */
+enum { WICI_KV_BF16 = 0, WICI_KV_INT8 = 1, WICI_KV_E4M3 = 2, WICI_KV_E2M1 = 4 };
 
 typedef struct wici_kv_cache {
     void *data;               /* 16-byte aligned */
@@ -150,7 +156,7 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
  * not read and may hold anything.  A sequence without keys (n <= 0) has out 0 and
  * lse -infinity.  Infinities and NaNs in a sequence's own keys act as in the
  * formula, in its own result alone (e^(s_t - max s) below 2^-126 counts as 0).
- * Over an 8-bit cache a key's weight times its scale of V is held to 2^-22 of itself
+ * Over an 8- or 4-bit cache a key's weight times its scale of V is held to 2^-22 of itself
  * or 2^-32 of the sequence's largest, far less than what codes cost that key's values.
  * Several sequences may share pages. */
 typedef struct wici_attn_shape {

@@ -1,5 +1,5 @@
 """Oracle of the batched decode step's operators (test infrastructure only): rotary
-positions with their scaling rules, the paged cache's 8-bit formats, and attention of one
+positions with their scaling rules, the paged cache's 8- and 4-bit formats, and attention of one
 token over a paged cache, each written from its definition in fp64.
 
 A cache is held here as one entry per slot, not as bytes: `codes` [slots, 2, heads, d]
@@ -120,6 +120,66 @@ def unpack(data, heads, d, fmt):
     c = blocks[..., :PAGE * d].reshape(pages, 2, heads, PAGE, d)
     s = np.ascontiguousarray(blocks[..., PAGE * d:]).view(np.float32)
     return by_slot(c.view(np.int8) if fmt == "int8" else c), by_slot(s)
+
+
+# ------------------------------------------------------------ 4-bit format --
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0])
+E2M1_TOP, E2M1_LEAST = 2688.0, 2.0 ** -100          # 6 * 448; smaller scales are 0
+
+
+def _nearest_code(a, unit, grid):
+    """The place of the value of `grid` nearest to a / unit, the even one of two as near, by exact comparisons: a has 24
+    significant bits, unit and grid's middles together at most 39."""
+    middles = (grid[1:] + grid[:-1]) / 2
+    code = np.zeros(np.broadcast(a, unit).shape, np.int64)
+    for i, m in enumerate(middles):
+        code += (a > m * unit) | ((a == m * unit) & (i % 2 == 1))
+    return code
+
+
+def quantise_e2m1(x):
+    """(codes [..., d] in 0..15, e4m3 codes of blocks [..., d / 16], scales fp32) of heads x [..., d] that fp32 holds."""
+    x = np.asarray(x, np.float64)
+    bad = ~np.isfinite(x).all(-1)
+    x = np.where(bad[..., None], 0, x)
+    scale = (np.abs(x).max(-1) / E2M1_TOP).astype(np.float32)
+    scale = np.where(scale < E2M1_LEAST, np.float32(0), scale)
+    s = scale.astype(np.float64)[..., None]
+    a = np.abs(x).reshape(*x.shape[:-1], -1, 16)
+    each = np.where(s > 0, _nearest_code(a.max(-1), 6.0 * s, _POSITIVE), 0)
+    unit = (E4M3[each] * s)[..., None]
+    code = np.where(unit > 0, _nearest_code(a, unit, E2M1[:8]), 0)
+    sign = np.where(np.signbit(x).reshape(a.shape) & (s > 0)[..., None], 8, 0)
+    return (code | sign).reshape(x.shape).astype(np.uint8), each.astype(np.uint8), np.where(bad, np.float32(np.nan), scale)
+
+
+def e2m1_values(codes, each, scales):
+    v = E2M1[codes].reshape(*each.shape, 16) * E4M3[each][..., None]
+    return v.reshape(codes.shape) * np.asarray(scales, np.float64)[..., None]
+
+
+def pack_e2m1(codes, each, scales):
+    """uint8 pages from per-slot codes [slots, 2, heads, d], block codes and scales."""
+    def by_page(a):
+        a = a.reshape(a.shape[0] // PAGE, PAGE, *a.shape[1:])
+        return np.ascontiguousarray(np.moveaxis(a, 1, 3)).view(np.uint8).reshape(a.shape[0], 2, a.shape[3], -1)
+
+    return np.concatenate([by_page(codes[..., 0::2] | codes[..., 1::2] << 4), by_page(each),
+                           by_page(np.asarray(scales, np.float32))], axis=-1).reshape(-1)
+
+
+def unpack_e2m1(data, heads, d):
+    """The inverse of pack_e2m1."""
+    row, each = d // 2, d // 16
+    blocks = np.asarray(data).reshape(-1, 2, heads, PAGE * (row + each + 4))
+
+    def by_slot(a, kind):
+        a = np.ascontiguousarray(a).view(kind).reshape(*blocks.shape[:3], PAGE, -1)
+        return np.moveaxis(a, 3, 1).reshape(blocks.shape[0] * PAGE, 2, heads, -1)
+
+    c = by_slot(blocks[..., :PAGE * row], np.uint8)
+    return (np.stack((c & 15, c >> 4), -1).reshape(*c.shape[:3], d), by_slot(blocks[..., PAGE * row:PAGE * (row + each)], np.uint8),
+            by_slot(blocks[..., PAGE * (row + each):], np.float32)[..., 0])
 
 
 # --------------------------------------------------------------- attention --

@@ -79,6 +79,33 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
+// The largest magnitudes of the two blocks of 16 elements that a lane's two groups of 8 lie in.  Where halves of a row
+// are rotated, the other 8 of a block are another lane's: group c of the row's rotated part is lane c's first one, group
+// rot_chunks + c its second.
+__device__ __forceinline__ void blocks_of_16(const float *x, bool halves, const RowsArg &a, float *most) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        most[i] = fabsf(x[8 * i]);
+#pragma unroll
+        for (int j = 1; j < 7; j += 2) most[i] = max3(most[i], fabsf(x[8 * i + j]), fabsf(x[8 * i + j + 1]));
+        most[i] = max3(most[i], fabsf(x[8 * i + 7]), 0.f);
+    }
+    const float own[2] = {most[0], most[1]};
+    if (!a.rotate_k || a.rope.interleaved) {       // the same for every lane
+        most[0] = most[1] = max3(own[0], own[1], 0.f);
+        return;
+    }
+    const int c = threadIdx.x, first = (threadIdx.y * blockDim.x & 31);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int other = (c + i * a.rot_chunks) ^ 1;
+        const bool second = other >= a.rot_chunks;
+        const int from = halves ? first + other - (second ? a.rot_chunks : 0) : first + c;
+        const float u = __shfl_sync(0xffffffffu, own[0], from), v = __shfl_sync(0xffffffffu, own[1], from);
+        most[i] = max3(own[i], halves ? second ? v : u : own[1 - i], 0.f);
+    }
+}
+
 // One launch rotates q rows (FMT = kRopeOnly: all rows) and writes k and v rows into the cache.
 // A block takes block_tokens tokens.  It computes their cosines and sines once, one pair a thread
 // and turn, through shared memory; then a thread keeps its token, with its chunk's cosines and
@@ -167,7 +194,7 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
         slot = -1;
     }
     const int d = FMT == kRopeOnly ? 0 : 16 * a.chunks, where = slot & (kKvPage - 1);
-    const int kv_block = FMT == WICI_KV_BF16 ? kKvPage * d * 2 : kKvPage * (d + 4);
+    const int kv_block = FMT == kRopeOnly ? 0 : kv_block_bytes(FMT, d);
     uint8_t *page = FMT == kRopeOnly || slot < 0 ? nullptr : a.cache.data + (int64_t)(slot / kKvPage) * a.cache.page_stride;
     // every lane of a warp stays: rows are reduced by shuffles
     for (int base = 0; base < a.heads; base += step) {
@@ -222,7 +249,25 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
                 for (int j = 1; j < 15; j += 2) top = max3(top, fabsf(x[j]), fabsf(x[j + 1]));
                 top = max3(top, fabsf(x[15]), 0.f);
                 for (int o = a.chunks / 2; o > 0; o >>= 1) top = max3(top, __shfl_xor_sync(0xffffffffu, top, o), 0.f);
-                if (store) {
+                if (FMT == WICI_KV_E2M1) {
+                    float most[2];
+                    blocks_of_16(x, rotate && turns && !pairs, a, most);
+                    if (store) {
+                        const float s = top / kE2m1Top;
+                        const bool finite = top < __uint_as_float(kInfBits), some = finite && s >= kE2m1Least;
+                        const float per6 = some ? 1.f / (6.f * s) : 0.f;
+                        uint8_t *row = block + where * (d / 2), *each = block + kKvPage * (d / 2) + where * (d / 16);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int p = i ? p1 : p0;
+                            const uint32_t b = some ? block_scale(most[i], s, per6) : 0u;
+                            *(uint32_t *)(row + p / 2) = some ? quantise_e2m1(x + 8 * i, e4m3_value(b), s) : 0u;
+                            if ((p & 8) == 0) each[p / 16] = (uint8_t)b;
+                        }
+                        if (c == 0)
+                            ((float *)(block + kv_scales_at(FMT, d)))[where] = finite ? some ? s : 0.f : __uint_as_float(0x7FC00000u);
+                    }
+                } else if (store) {
                     uint32_t code[4];
                     const float scale = quantise16<FMT>(x, top, code);
                     uint8_t *dst = block + where * d;
@@ -354,7 +399,7 @@ constexpr int kReadRows = 4;
 template <typename T, int FMT, int D, bool WIDE>
 __global__ void __launch_bounds__(kRowThreads, kRowBlocks) read_kernel(const __grid_constant__ ReadArg a) {
     constexpr int W = FMT == WICI_KV_BF16 ? 2 : 1;               // 16-byte words of a lane's 16 values
-    constexpr int kBlock = FMT == WICI_KV_BF16 ? kKvPage * D * 2 : kKvPage * (D + 4);
+    constexpr int kBlock = kv_block_bytes(FMT, D);
     griddep_launch_dependents();
     griddep_wait();
     const int64_t t = (int64_t)blockIdx.x * a.block_tokens + (threadIdx.y & (a.block_tokens - 1));
@@ -382,6 +427,10 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) read_kernel(const __g
                 if (FMT == WICI_KV_BF16) {
 #pragma unroll
                     for (int w = 0; w < W; ++w) word[i][w] = *(const uint4 *)(block + (where * D + 16 * c) * 2 + 16 * w);
+                } else if (FMT == WICI_KV_E2M1) {
+                    const uint2 codes = *(const uint2 *)(block + where * (D / 2) + 8 * c);
+                    word[i][0] = make_uint4(codes.x, codes.y, block[kKvPage * (D / 2) + where * (D / 16) + c], 0);
+                    scale[i] = ((const float *)(block + kv_scales_at(FMT, D)))[where];
                 } else {
                     word[i][0] = *(const uint4 *)(block + where * D + 16 * c);
                     scale[i] = ((const float *)(block + kKvPage * D))[where];
@@ -399,6 +448,18 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) read_kernel(const __g
                 for (int j = 0; j < 8; ++j) {
                     x[2 * j] = good ? bf16lo(w[j]) : fill;
                     x[2 * j + 1] = good ? bf16hi(w[j]) : fill;
+                }
+            } else if (FMT == WICI_KV_E2M1) {
+                const float b = e4m3_value(w[2]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t h[4];
+                    decode_e2m1(w[j], h);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {                // code * b is exact
+                        const float2 f = __half22float2(*(const __half2 *)&h[k]);
+                        x[8 * j + 2 * k] = f.x * b * scale[i], x[8 * j + 2 * k + 1] = f.y * b * scale[i];
+                    }
                 }
             } else {
 #pragma unroll
@@ -493,6 +554,7 @@ cudaError_t launch_read(int fmt, int d, ReadArg &a, bool wide, int sms, cudaStre
     switch (fmt) {
         case WICI_KV_BF16: return launch_read<T, WICI_KV_BF16>(d, a, wide, sms, st);
         case WICI_KV_INT8: return launch_read<T, WICI_KV_INT8>(d, a, wide, sms, st);
+        case WICI_KV_E2M1: return launch_read<T, WICI_KV_E2M1>(d, a, wide, sms, st);
         default: return launch_read<T, WICI_KV_E4M3>(d, a, wide, sms, st);
     }
 }
@@ -589,9 +651,7 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
 }
 
 int64_t wici_kv_page_bytes(int32_t format, int32_t n_kv_heads, int32_t head_dim) {
-    if ((format != WICI_KV_BF16 && format != WICI_KV_INT8 && format != WICI_KV_E4M3) ||
-        (head_dim != 64 && head_dim != 128) || n_kv_heads < 1)
-        return 0;
+    if (!known_format(format) || (head_dim != 64 && head_dim != 128) || n_kv_heads < 1) return 0;
     return 2 * (int64_t)n_kv_heads * kv_block_bytes(format, head_dim);
 }
 
@@ -646,6 +706,7 @@ int wici_kv_append(void *cuda_stream, const wici_kv_cache *cache, const int32_t 
     switch (cache->format) {
         case WICI_KV_BF16: e = launch_rows<WICI_KV_BF16>(k->dtype, a, wide, sms, st); break;
         case WICI_KV_INT8: e = launch_rows<WICI_KV_INT8>(k->dtype, a, wide, sms, st); break;
+        case WICI_KV_E2M1: e = launch_rows<WICI_KV_E2M1>(k->dtype, a, wide, sms, st); break;
         default: e = launch_rows<WICI_KV_E4M3>(k->dtype, a, wide, sms, st); break;
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "append: %s", cudaGetErrorString(e));

@@ -1,7 +1,8 @@
-// Device helpers of the stand-alone operators: element types, the 8-bit cache formats.
+// Device helpers of the stand-alone operators: element types, the 8- and 4-bit cache formats.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <cuda_fp4.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -143,5 +144,57 @@ __device__ __forceinline__ void decode4(uint32_t w, uint32_t &lo, uint32_t &hi) 
     }
 }
 
+// ------------------------------------------------------------ 4-bit cache format
+// e2m1 codes c of 16 elements share an e4m3 scale b, and a head's elements an fp32 scale s: c b s.  c b has at most 6
+// significant bits between 2^-10 and 2688: fp16 holds it exactly.
+//
+// Which code a value gets is decided on the real numbers, not on rounded quotients, for bf16 values often lie half way
+// between two codes: x goes to the upper of two neighbours where x > m b s with m their middle, and fmaf(-m b, s, x) has
+// that difference's sign, for m b is exact (7 bits).  Nearly always a quotient within 2^-19 tells without it.
+constexpr float kE2m1Top = 2688.f;               // 6 * 448
+constexpr float kE2m1Least = 0x1p-100f;          // smaller scales are 0: with block scales, reciprocals and products stay normal
+constexpr float kNearLo = 1.f - 0x1p-19f, kNearHi = 1.f + 0x1p-19f;
+
+// the e4m3 nearest to most / (6 scale), the even one of two that are as near; per6 is about 1 / (6 scale)
+__device__ __forceinline__ uint32_t block_scale(float most, float scale, float per6) {
+    const float y = most * per6;
+    const uint32_t w = __nv_cvt_float2_to_fp8x2(make_float2(y * kNearLo, y * kNearHi), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t lo = w & 0xFF, hi = w >> 8;
+    if (lo == hi) return lo;
+    const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3)));
+    const float over = fmaf(-3.f * (v.x + v.y), scale, most);
+    return over > 0.f || (over == 0.f && (hi & 1) == 0) ? hi : lo;
+}
+__device__ __forceinline__ float e4m3_value(uint32_t code) {
+    return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+}
+// the codes of 8 values under the block scale b (its value) and the head's scale, the first in the lowest bits
+__device__ __forceinline__ uint32_t quantise_e2m1(const float *x, float b, float scale) {
+    const float r = b > 0.f ? 1.f / (b * scale) : 0.f, r_lo = r * kNearLo, r_hi = r * kNearHi;
+    uint32_t lo = 0, hi = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        lo |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(x[2 * j] * r_lo, x[2 * j + 1] * r_lo), __NV_E2M1, cudaRoundNearest) << 8 * j;
+        hi |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(x[2 * j] * r_hi, x[2 * j + 1] * r_hi), __NV_E2M1, cudaRoundNearest) << 8 * j;
+    }
+    if (lo != hi) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t c = lo >> 4 * j & 7;  // the lower neighbour, where they differ
+            if (((lo ^ hi) >> 4 * j & 15) == 0) continue;
+            const float middle = c < 4 ? 0.25f + 0.5f * (float)c : c == 4 ? 2.5f : c == 5 ? 3.5f : 5.f;
+            const float over = fmaf(-middle * b, scale, fabsf(x[j]));
+            if (over > 0.f || (over == 0.f && (c & 1))) lo += 1u << 4 * j;
+        }
+    }
+    return lo;
+}
+// 8 codes as fp16 pairs, exactly
+__device__ __forceinline__ void decode_e2m1(uint32_t w, uint32_t *h) {
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+}
 
 }  // namespace wici

@@ -14,19 +14,29 @@ constexpr int kMaxHeads = 1 << 16;
 
 inline int dtype_bytes(int dtype) { return dtype == WICI_F32 ? 4 : 2; }
 
-// bytes of one [K or V][kv head] block of a page: values, or codes and 16 fp32 scales
-inline int64_t kv_block_bytes(int format, int head_dim) {
-    return format == WICI_KV_BF16 ? (int64_t)kKvPage * head_dim * 2 : (int64_t)kKvPage * (head_dim + 4);
+// bytes of a token's elements in a [K or V][kv head] block of a page, and of the block: values, or codes (then e2m1's
+// scales of 16 elements) and 16 fp32 scales
+constexpr int kv_row_bytes(int format, int head_dim) {
+    return format == WICI_KV_BF16 ? head_dim * 2 : format == WICI_KV_E2M1 ? head_dim / 2 : head_dim;
+}
+constexpr int kv_scales_at(int format, int head_dim) {    // of the fp32 scales in a block
+    return kKvPage * (kv_row_bytes(format, head_dim) + (format == WICI_KV_E2M1 ? head_dim / 16 : 0));
+}
+constexpr int kv_block_bytes(int format, int head_dim) {
+    return kv_scales_at(format, head_dim) + (format == WICI_KV_BF16 ? 0 : kKvPage * 4);
+}
+inline bool known_format(int f) {
+    return f == WICI_KV_BF16 || f == WICI_KV_INT8 || f == WICI_KV_E4M3 || f == WICI_KV_E2M1;
 }
 
 inline const char *check_cache(const wici_kv_cache *c) {
     if (!c) return "null cache";
-    if (c->format != WICI_KV_BF16 && c->format != WICI_KV_INT8 && c->format != WICI_KV_E4M3) return "cache format";
+    if (!known_format(c->format)) return "cache format";
     if (c->head_dim != 64 && c->head_dim != 128) return "cache head_dim must be 64 or 128";
     if (c->n_kv_heads < 1 || c->n_kv_heads > 1024) return "cache n_kv_heads must be in [1, 1024]";
     if (c->n_pages < 1 || c->n_pages > kMaxPages) return "cache n_pages must be in [1, 2^27)";
     if (!c->data || ((uintptr_t)c->data & 15)) return "cache data null or not 16-byte aligned";
-    if (c->page_stride % 16 || c->page_stride < 2 * c->n_kv_heads * kv_block_bytes(c->format, c->head_dim))
+    if (c->page_stride % 16 || c->page_stride < 2 * (int64_t)c->n_kv_heads * kv_block_bytes(c->format, c->head_dim))
         return "cache page_stride must be a multiple of 16 and at least a page";
     if (c->page_stride > INT64_MAX / kMaxPages) return "cache page_stride";
     return nullptr;

@@ -32,6 +32,7 @@ int device_sms(int *n) {
         cudaError_t e1 = setup_attention_bf16();
         if (e1 == cudaSuccess) e1 = setup_attention_int8();
         if (e1 == cudaSuccess) e1 = setup_attention_e4m3();
+        if (e1 == cudaSuccess) e1 = setup_attention_e2m1();
         if (e1 != cudaSuccess) return e1;
         return cudaDeviceGetAttribute(d, cudaDevAttrMultiProcessorCount, dev);
     });
@@ -132,6 +133,7 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
         switch (cache->format) {
             case WICI_KV_BF16: e = launch_attention_bf16(cache->head_dim, a, kind, used_sms(sms), st); break;
             case WICI_KV_INT8: e = launch_attention_int8(cache->head_dim, a, kind, used_sms(sms), st); break;
+            case WICI_KV_E2M1: e = launch_attention_e2m1(cache->head_dim, a, kind, used_sms(sms), st); break;
             default: e = launch_attention_e4m3(cache->head_dim, a, kind, used_sms(sms), st); break;
         }
     }

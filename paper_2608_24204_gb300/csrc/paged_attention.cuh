@@ -70,7 +70,6 @@ struct AttnArg {
     float scale;
 };
 
-constexpr int attn_block(int fmt, int d) { return fmt == WICI_KV_BF16 ? kKvPage * d * 2 : kKvPage * (d + 4); }
 constexpr size_t attn_piece_floats(int d) { return (size_t)kAttnPieceRows * (d + 2); }
 
 template <int FMT, int D, bool STACK>
@@ -80,11 +79,11 @@ struct AttnShape {
     // Pages of a unit: 4 to 8 KB of K and V for the work that a unit costs beside its products (bf16, 128: one page
     // already; 8-bit: one page more a unit took the batch of 64 from 136 to 116 us with 128, from 76 to 74 with 64).
     static constexpr int kPages = FMT == WICI_KV_BF16 ? (D == 128 ? 1 : 2) : (D == 128 ? 2 : 4);
-    static constexpr int kBlock = attn_block(FMT, D);
+    static constexpr int kBlock = kv_block_bytes(FMT, D);
     static constexpr int kSlot = kPages * kBlock;
     // Two blocks on an SM, 8 warps with 250 registers each: three of 168 spill (131 us in place of then 116).
     static constexpr int kBlocks = 2;
-    static constexpr int kKSlots = 3, kVSlots = kKSlots - 1;       // of the ring: about 100 KB on their way per SM
+    static constexpr int kKSlots = FMT != WICI_KV_E2M1 ? 3 : D == 128 && !STACK ? 4 : 5, kVSlots = kKSlots - 1;   // of the ring: about 100 KB on their way per SM
     static constexpr int kRing = (kKSlots + kVSlots) * kSlot;
     static constexpr int kPartRow = D + 4;                         // floats: neighbouring rows in other banks
     static constexpr int kPart = kRows * (kPartRow + 2) * 4;       // a part of a segment: O, then m and l of each row
@@ -118,6 +117,20 @@ __device__ __forceinline__ float lds32(uint32_t a) {
     float v;
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
     return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+// an e4m3 code twice as fp16, and a product of fp16 pairs
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t code) {
+    const __half2 v = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(code | code << 8), __NV_E4M3));
+    return *(const uint32_t *)&v;
+}
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+    const __half2 v = __hmul2(*(const __half2 *)&a, *(const __half2 *)&b);
+    return *(const uint32_t *)&v;
 }
 template <bool BF16>
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
@@ -200,8 +213,18 @@ __device__ __forceinline__ void split_row(const float *x, int r, uint32_t (*a)[4
 // Where 16-byte chunk c of key row r stands in a ring slot.  The chunks of a row are permuted so
 // that the 8 lanes of a shared-memory phase, which take rows i and i + 4 (K), or rows 0..3 and
 // neighbouring chunks (V), meet 8 different bank groups.  Rows of 64 bytes share a line of 128 in pairs.
-template <int ROW>
+// Of rows of e2m1 a lane takes 8 bytes at a time (K: a row's chunks in order, V: those of rows 0..3): halves of a warp,
+// whose rows are {0, 4, 1, 5}, {2, 6, 3, 7} or 0..3, meet 16 different pairs of banks.
+template <int ROW, bool E2M1>
 __device__ __forceinline__ int chunk_at(int r, int c) {
+    if (E2M1 && ROW == 64) {
+        const int line = r >> 1;
+        return line * 128 + ((((r & 1) << 2 | c) ^ (((line ^ line >> 1) & 1) << 1)) << 4);
+    }
+    if (ROW == 32) {
+        const int line = r >> 2;
+        return line * 128 + ((((r & 3) << 1 | c) ^ ((line & 1) << 2)) << 4);
+    }
     if (ROW == 64) {
         const int line = r >> 1;
         return line * 128 + ((((r & 1) << 2 | c) ^ ((line & 1) << 1 ^ (line & 2) << 1)) << 4);
@@ -292,8 +315,12 @@ template <int FMT, int D, bool STACK, bool EXACT>
 __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlocks) paged_attention_kernel(const __grid_constant__ AttnArg a) {
     using S = AttnShape<FMT, D, STACK>;
     constexpr bool BF16 = FMT == WICI_KV_BF16;
-    constexpr int ROW = BF16 ? 2 * D : D;                 // bytes of a key row
+    constexpr bool E2M1 = FMT == WICI_KV_E2M1;
+    constexpr int ROW = kv_row_bytes(FMT, D);             // bytes of a key row
     constexpr int CHUNKS = ROW / 16;
+    constexpr int GROUPS = BF16 ? CHUNKS / 4 : D / 64;    // steps' elements that a lane loads at once: 8 of bf16, 16 codes
+    constexpr int EACH_AT = kKvPage * ROW, SCALES_AT = kv_scales_at(FMT, D);   // e2m1's block scales, the tokens' scales
+    constexpr int TAIL = (S::kBlock - EACH_AT) / 16;      // 16-byte words of a block behind its rows
     constexpr int P = S::kPages, UNIT = P * kKvPage;      // keys of a unit
     constexpr int HT = S::kRows;
     constexpr int R = STACK ? 1 : 2;                      // queries whose rows a lane holds
@@ -484,7 +511,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     int last_first = 0, last_end = 0;     // (end 0: no unit)
 
     const uint64_t policy = l2_evict_first();   // read once: code, queries and parts stay in L2 instead
-    const uint32_t lane_dst = chunk_at<ROW>(lane / CHUNKS, lane % CHUNKS);
+    const uint32_t lane_dst = chunk_at<ROW, E2M1>(lane / CHUNKS, lane % CHUNKS);
     const int64_t lane_v = (int64_t)a.cache.kv_heads * S::kBlock;   // from K to V of a head in a page
     constexpr int N = kKvPage * CHUNKS / 32, ROWS = 32 / CHUNKS;    // a page's block in N rounds of the warp, rows of a round
     // a unit's K or V: rows without a key of the sequence are zeroed, what the cache holds there is anything
@@ -495,8 +522,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 const uint8_t *from = src[p] + off + lane * 16;
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    cp_async16(dst + p * S::kBlock + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), from + i * 512, 16, policy);
-                if (!BF16 && lane < 4) cp_async16(dst + p * S::kBlock + kKvPage * D + lane * 16, from + kKvPage * D, 16, policy);
+                    cp_async16(dst + p * S::kBlock + (chunk_at<ROW, E2M1>(i * ROWS, 0) ^ lane_dst), from + i * 512, 16, policy);
+                if (lane < TAIL) cp_async16(dst + p * S::kBlock + EACH_AT + lane * 16, from + EACH_AT, 16, policy);
             }
         } else {
 #pragma unroll
@@ -505,12 +532,11 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const int r = p * kKvPage + i * ROWS + lane / CHUNKS;
-                    cp_async16(dst + p * S::kBlock + (chunk_at<ROW>(i * ROWS, 0) ^ lane_dst), src[p] ? from + i * 512 : from,
+                    cp_async16(dst + p * S::kBlock + (chunk_at<ROW, E2M1>(i * ROWS, 0) ^ lane_dst), src[p] ? from + i * 512 : from,
                                src[p] && r >= first && r < end ? 16 : 0, policy);
                 }
-                if (!BF16 && lane < 4)
-                    cp_async16(dst + p * S::kBlock + kKvPage * D + lane * 16, src[p] ? from + kKvPage * D : from,
-                               src[p] ? 16 : 0, policy);
+                if (lane < TAIL)
+                    cp_async16(dst + p * S::kBlock + EACH_AT + lane * 16, src[p] ? from + EACH_AT : from, src[p] ? 16 : 0, policy);
             }
         }
     };
@@ -651,11 +677,26 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
                     for (int j = 0; j < 4; ++j) c[n][e][j] = 0.f;
 #pragma unroll
-            for (int i = 0; i < CHUNKS / 4; ++i) {
+            for (int i = 0; i < GROUPS; ++i) {
 #pragma unroll
                 for (int n = 0; n < 2 * P; ++n) {
                     const int r = (g >> 1) + (g & 1) * 4 + 8 * (n & 1);   // the key of column g
-                    const uint4 w = lds128(ks + n / 2 * S::kBlock + chunk_at<ROW>(r, 4 * i + t));
+                    if (E2M1) {
+                        const int c16 = 4 * i + t;                       // 16 elements of the row: 8 bytes and a scale
+                        const uint32_t kp = ks + n / 2 * S::kBlock;
+                        const uint2 w = lds64(kp + chunk_at<ROW, E2M1>(r, c16 >> 1) + (c16 & 1) * 8);
+                        const uint32_t b2 = e4m3_pair(lds8(kp + EACH_AT + r * (D / 16) + c16));
+                        uint32_t h[8];
+                        decode_e2m1(w.x, h);
+                        decode_e2m1(w.y, h + 4);
+#pragma unroll
+                        for (int s = 0; s < 4; ++s)
+#pragma unroll
+                            for (int k = 0; k < QPASS; ++k)
+                                mma16816<false>(c[n][0], qf[k][4 * i + s], times(h[2 * s], b2), times(h[2 * s + 1], b2));
+                        continue;
+                    }
+                    const uint4 w = lds128(ks + n / 2 * S::kBlock + chunk_at<ROW, E2M1>(r, 4 * i + t));
                     if (BF16) {
 #pragma unroll
                         for (int k = 0; k < QPASS; ++k) {
@@ -694,7 +735,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const int n = j >> 1, col = j & 1;
-                const float ksc = BF16 ? 1.f : lds32(ks + j / 4 * S::kBlock + kKvPage * D + (t + 4 * (j & 3)) * 4);
+                const float ksc = BF16 ? 1.f : lds32(ks + j / 4 * S::kBlock + SCALES_AT + (t + 4 * (j & 3)) * 4);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     float dot = c[n][0][col + 2 * r];
@@ -756,7 +797,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 bool heavy = false;
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    const float vscale = lds32(vs + j / 4 * S::kBlock + kKvPage * D + (t + 4 * (j & 3)) * 4);
+                    const float vscale = lds32(vs + j / 4 * S::kBlock + SCALES_AT + (t + 4 * (j & 3)) * 4);
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         const float p = ex2(x[r][j] - ref[r]);
@@ -825,7 +866,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                         uint32_t w[4][4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const uint4 q = lds128(vp + chunk_at<ROW>(t + 4 * i, g + 8 * jj));
+                            const uint4 q = lds128(vp + chunk_at<ROW, E2M1>(t + 4 * i, g + 8 * jj));
                             w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
                         }
 #pragma unroll
@@ -837,16 +878,55 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                             for (int k = 0; k < PPASS; ++k) mma16816<true>(o[8 * jj + e], pf[pg][k], b0, b1);
                         }
                     }
+                } else if (E2M1) {
+                    constexpr int WORDS = D / 64;          // 4-byte words of a row that a lane takes
+                    uint32_t w[4][WORDS], b[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = t + 4 * i, key = key0 + pg * kKvPage + r;
+                        if (D == 128) {
+                            const uint2 q = lds64(vp + chunk_at<ROW, E2M1>(r, g >> 1) + (g & 1) * 8);
+                            w[i][0] = q.x, w[i][WORDS - 1] = q.y;
+                        } else {
+                            w[i][0] = __float_as_uint(lds32(vp + chunk_at<ROW, E2M1>(r, g >> 2) + (g & 3) * 4));
+                        }
+                        b[i] = lds8(vp + EACH_AT + r * (D / 16) + (D == 128 ? g : g >> 1));
+                        if (part && (key < keys.lo || key >= keys.n)) b[i] = 0;   // of another key: may be NaN
+                    }
+                    uint32_t b2[2];                        // of the rows of a fragment's half
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const __half2 v = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(b[2 * i] | b[2 * i + 1] << 8), __NV_E4M3));
+                        b2[i] = *(const uint32_t *)&v;
+                    }
+#pragma unroll
+                    for (int x8 = 0; x8 < WORDS; ++x8) {
+                        // halves of bytes of two rows interleaved first: columns 2 e in even[..][e], 2 e + 1 in odd[..][e]
+                        uint32_t even[2][4], odd[2][4];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t u = w[2 * i][x8], v = w[2 * i + 1][x8];
+                            decode_e2m1((u & 0x0F0F0F0Fu) | (v << 4 & 0xF0F0F0F0u), even[i]);
+                            decode_e2m1((u >> 4 & 0x0F0F0F0Fu) | (v & 0xF0F0F0F0u), odd[i]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int k = 0; k < PPASS; ++k) {
+                                mma16816<false>(o[8 * x8 + 2 * e], pf[pg][k], times(even[0][e], b2[0]), times(even[1][e], b2[1]));
+                                mma16816<false>(o[8 * x8 + 2 * e + 1], pf[pg][k], times(odd[0][e], b2[0]), times(odd[1][e], b2[1]));
+                            }
+                    }
                 } else {
                     constexpr int WORDS = D / 32;          // 4-byte words of a row that a lane takes
                     uint32_t w[4][WORDS];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if (D == 128) {
-                            const uint4 q = lds128(vp + chunk_at<ROW>(t + 4 * i, g));
+                            const uint4 q = lds128(vp + chunk_at<ROW, E2M1>(t + 4 * i, g));
                             w[i][0] = q.x, w[i][1] = q.y, w[i][WORDS - 2] = q.z, w[i][WORDS - 1] = q.w;
                         } else {
-                            const uint2 q = lds64(vp + chunk_at<ROW>(t + 4 * i, g >> 1) + (g & 1) * 8);
+                            const uint2 q = lds64(vp + chunk_at<ROW, E2M1>(t + 4 * i, g >> 1) + (g & 1) * 8);
                             w[i][0] = q.x, w[i][1] = q.y;
                         }
                     }
@@ -1069,9 +1149,11 @@ inline AttnKind attn_kind(int group, bool exact) {
 cudaError_t launch_attention_bf16(int d, const AttnArg &a, AttnKind kind, int sms, cudaStream_t st);
 cudaError_t launch_attention_int8(int d, const AttnArg &a, AttnKind kind, int sms, cudaStream_t st);
 cudaError_t launch_attention_e4m3(int d, const AttnArg &a, AttnKind kind, int sms, cudaStream_t st);
+cudaError_t launch_attention_e2m1(int d, const AttnArg &a, AttnKind kind, int sms, cudaStream_t st);
 cudaError_t setup_attention_bf16();
 cudaError_t setup_attention_int8();
 cudaError_t setup_attention_e4m3();
+cudaError_t setup_attention_e2m1();
 
 template <int FMT, int D, bool STACK, bool EXACT>
 cudaError_t launch_attention(const AttnArg &a, int sms, cudaStream_t st) {

@@ -18,12 +18,12 @@ from .wici import WiciError, _check  # noqa: F401
 WICI_BF16, WICI_F16, WICI_F32 = 0, 1, 2
 WICI_BAD_SLOT, WICI_BAD_PAGE, WICI_BAD_LENGTH = 1, 2, 4
 WICI_ROPE_NONE, WICI_ROPE_LINEAR, WICI_ROPE_BANDS, WICI_ROPE_YARN = 0, 1, 2, 3
-WICI_KV_BF16, WICI_KV_INT8, WICI_KV_E4M3 = 0, 1, 2
+WICI_KV_BF16, WICI_KV_INT8, WICI_KV_E4M3, WICI_KV_E2M1 = 0, 1, 2, 4
 
 PAGE_TOKENS = 16
 WICI_ATTN_ZEROED = 16384     # bytes at the start of an attention workspace that are zero before its first use
 SCALINGS = {"none": WICI_ROPE_NONE, "linear": WICI_ROPE_LINEAR, "bands": WICI_ROPE_BANDS, "yarn": WICI_ROPE_YARN}
-FORMATS = {"bf16": WICI_KV_BF16, "int8": WICI_KV_INT8, "e4m3": WICI_KV_E4M3}
+FORMATS = {"bf16": WICI_KV_BF16, "int8": WICI_KV_INT8, "e4m3": WICI_KV_E4M3, "e2m1": WICI_KV_E2M1}
 _DTYPES = {torch.bfloat16: WICI_BF16, torch.float16: WICI_F16, torch.float32: WICI_F32}
 
 # the entry points declared in include/wici_ops.h
