@@ -182,6 +182,54 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
                          const int32_t *pages, const int32_t *lengths, const wici_heads *q, const wici_heads *out,
                          float *lse, void *workspace, int32_t *status);
 
+/* The same where every KV head has pages of its own: pages int32[batch][n_kv_heads][max_pages], those of a
+ * sequence in the order of their tokens, 16 of each but the last (what wici_kv_select gives).  window is 0. */
+int wici_selected_attention(void *cuda_stream, const wici_kv_cache *cache, const wici_attn_shape *shape,
+                            const int32_t *pages, const int32_t *lengths, const wici_heads *q, const wici_heads *out,
+                            float *lse, void *workspace, int32_t *status);
+
+/* ------------------------------------------------------------- selection of pages
+ * Attention over part of a long cache: the pages whose keys may score highest.  Bounds of a
+ * page: for each KV head the largest and the smallest key element by element, as int8 codes
+ * hi, lo[head_dim] under one scale = max|k| times 1 / 127 in fp32 (codes are fp32's k / scale, to the
+ * nearest even).  A record per page, page_stride bytes apart, holds [kv head][hi|lo][head_dim], then
+ * scale[kv head].  A scale below 2^-126 is 0, and NaN where a key is infinite or NaN.
+ * The paper has no counterpart: its longest context is read whole. */
+typedef struct wici_kv_bounds {
+    void *data;               /* 16-byte aligned, a record for each page of the cache */
+    int64_t page_stride;      /* bytes, a multiple of 16, at least wici_kv_bounds_bytes */
+} wici_kv_bounds;
+
+/* Bytes of one record (0 for a head_dim that is not 64 or 128). */
+int64_t wici_kv_bounds_bytes(int32_t n_kv_heads, int32_t head_dim);
+
+/* Bounds of the pages of `count` slots: of the page of last[i] over its places up to that slot.  For tokens
+ * just appended, last[i] is the last one in its page: after a step's wici_kv_append of one token a sequence,
+ * its `slots`.  A negative entry is skipped; a page stands at most once in a call. */
+int wici_kv_bounds_update(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_bounds *bounds, const int32_t *last,
+                          int64_t count, int32_t *status);
+
+typedef struct wici_select_shape {
+    int32_t batch;            /* 0 .. 65535 */
+    int32_t max_pages;        /* columns of `pages`, 1 .. 32768 */
+    int32_t keep;             /* pages to select, 1 .. 32768 */
+    int32_t first, recent;    /* selected in any case: so many from the start (>= 0), from the end (>= 1); their sum <= keep */
+} wici_select_shape;
+
+/* The `keep` pages of sequence b for each KV head, all where it has no more.  With m = max|q| of a query head and
+ * w_d = q_d times (1 / m times 1023) in fp32, rounded to whole numbers, page p has for KV head h the score
+ *   max over the group's heads of (m sum_d w_d (w_d > 0 ? hi_d : lo_d)) times scale,
+ * sums exact and each product rounded to fp32: to rounding the largest q.k that keys within the page's bounds can
+ * have, for the attention of a positive scale.  Of equal scores the first page is selected.  A page of NaN scale scores
+ * +infinity; a head whose m is below 2^-100 or not finite scores 0.
+ *   out_pages   int32[batch][n_kv_heads][keep]: entries of `pages`, in the order of their tokens, -1 after the last
+ *   out_lengths int32[batch]: the tokens they hold (a length that is bad stays bad)
+ *   out_blocks  the same as out_pages with their columns in `pages`, or NULL
+ * q: `batch` tokens of up to 64 heads a KV head.  Outputs overlap nothing else. */
+int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_bounds *bounds, const wici_select_shape *shape,
+                   const int32_t *pages, const int32_t *lengths, const wici_heads *q, int32_t *out_pages,
+                   int32_t *out_lengths, int32_t *out_blocks, int32_t *status);
+
 /* The cache of layer `layer` of a context, as of the work already enqueued on the
  * context's stream, and its page table (device int32[pages], logical -> physical;
  * *n_logical entries).  Both stay valid until wici_destroy; the first wici_kv_len

@@ -205,3 +205,46 @@ def paged_attention(q, k, v, pages, lengths, scale, window=0):
             out[b, h] = p @ v[slots, h // group]
             weight[b, h] = p @ np.abs(v[slots, h // group])
     return out, lse, weight
+
+
+# -------------------------------------------------------- selection of pages --
+def key_bounds(k):
+    """(int8 codes [2, d], fp32 scale) of a page's keys [tokens, d], which fp32 holds: the largest and the smallest element
+    by element over max |k| (1 / 127), whole numbers of fp32 quotients."""
+    k = np.asarray(k, np.float32)
+    if not np.isfinite(k).all():
+        return np.zeros((2, k.shape[1]), np.int8), np.float32(np.nan)
+    ends = np.stack((k.max(0), k.min(0)))
+    scale = np.abs(ends).max() * (np.float32(1) / np.float32(127))
+    if scale < np.float32(2.0 ** -126):
+        return np.zeros_like(ends, np.int8), np.float32(0)
+    return np.rint(ends / scale).astype(np.int8), scale
+
+
+def page_scores(q, codes, scales):
+    """fp32 scores [pages] of one KV head's query heads q [group, d] against codes [pages, 2, d] and scales [pages]."""
+    q, best = np.asarray(q, np.float32), np.full(len(scales), -np.inf, np.float32)
+    for x in q:
+        m = np.abs(x).max()                                    # NaN where one is
+        ok = np.isfinite(m) and m >= 2.0 ** -100
+        w = [int(np.rint(v * (np.float32(1) / m * np.float32(1023)))) if ok else 0 for v in x]
+        m = m if ok else np.float32(0)
+        for p in range(len(scales)):
+            dot = sum(w[d] * int(codes[p, 0 if w[d] > 0 else 1, d]) for d in range(len(w)))
+            with np.errstate(over="ignore"):
+                best[p] = max(best[p], np.float32(dot) * m)
+    out = np.empty(len(scales), np.float32)
+    for p, s in enumerate(scales):
+        with np.errstate(over="ignore"):
+            out[p] = np.inf if not np.isfinite(s) else np.float32(0) if s == 0 else best[p] * s
+    return out
+
+
+def selected_pages(scores, keep, first, recent):
+    """The columns of the selected pages, ascending."""
+    n = len(scores)
+    if n <= keep:
+        return list(range(n))
+    forced = [p for p in range(n) if p < first or p >= n - recent]
+    rest = sorted((p for p in range(n) if p not in set(forced)), key=lambda p: (-float(scores[p]), p))
+    return sorted(forced + rest[:keep - len(forced)])

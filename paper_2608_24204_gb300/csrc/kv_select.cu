@@ -1,0 +1,526 @@
+// Bounds of a cache's pages and the pages that a query's cheap score selects (include/wici_ops.h).
+//
+// Bounds.  bounds_kernel keeps, of each page and KV head, the largest and the smallest key element by element, as int8
+// codes under one fp32 scale: (2 d + 4) bytes where the page's keys have 32 d (bf16).
+//
+// Scores.  sum_d max(q_d hi_d, q_d lo_d) is the largest q.k that keys between lo and hi can have.  q enters as whole
+// numbers of at most 1023 (11 bits: fp16 holds them), the positive ones against hi and the negative ones against lo, so a
+// score is a dot product of 2 d whole numbers below 2^24: mma.m16n8k16 gives it exactly, in any order, and the selection
+// does not depend on how sums are split.  16 pages are the rows, 8 queries of the group the columns.
+// Select.  A cluster of blocks takes one sequence and KV head.  Its blocks score the pages and leave the scores, as
+// integers that order as they do, in the first block's shared memory; that one finds the keep-th largest bit by bit and
+// writes the pages above it in order, of equal ones the first.
+#include <stdarg.h>
+#include <stdio.h>
+
+#include "device_table.h"
+#include "kernels.h"
+#include "ops.cuh"
+
+using namespace wici;
+
+namespace {
+
+int fail(int code, const char *fmt, ...) {
+    char buf[256];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    set_thread_error(buf);
+    return code;
+}
+
+// ------------------------------------------------------------------ bounds ----
+struct BoundsArg {
+    CacheArg cache;
+    uint8_t *bounds;
+    int64_t bounds_stride;
+    const int32_t *last;
+    int32_t *status;
+    int64_t items;                    // entries of `last` times KV heads
+};
+
+constexpr int kBoundsThreads = 128;
+
+// E values of a key row at element e0 in fp32, the token's scale left out
+template <int FMT, int D, int E>
+__device__ __forceinline__ void load_key(const uint8_t *block, int row, int e0, float *x) {
+    if (FMT == WICI_KV_BF16) {
+        uint32_t w[E / 2];
+        const uint8_t *p = block + (row * D + e0) * 2;
+        if (E == 4) *(uint2 *)w = *(const uint2 *)p;
+        else w[0] = *(const uint32_t *)p;
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) x[2 * i] = bf16lo(w[i]), x[2 * i + 1] = bf16hi(w[i]);
+    } else if (FMT == WICI_KV_E2M1) {
+        const uint8_t *p = block + row * (D / 2) + e0 / 2;
+        const uint32_t w = E == 4 ? *(const uint16_t *)p : *p;
+        const float b = e4m3_value(block[kKvPage * (D / 2) + row * (D / 16) + e0 / 16]);
+        uint32_t h[4];
+        decode_e2m1(w, h);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            const float2 f = __half22float2(*(const __half2 *)&h[i]);
+            x[2 * i] = f.x * b, x[2 * i + 1] = f.y * b;
+        }
+    } else {
+        const uint8_t *p = block + row * D + e0;
+        const uint32_t w = E == 4 ? *(const uint32_t *)p : *(const uint16_t *)p;
+        uint32_t h[2];
+        decode4<FMT>(w, h[0], h[1]);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            const float2 f = __half22float2(*(const __half2 *)&h[i]);
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        }
+    }
+}
+
+// A warp takes one page of one KV head, a lane E elements of all its rows.
+template <int FMT, int D>
+__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsArg a) {
+    constexpr int E = D / 32;
+    griddep_launch_dependents();
+    griddep_wait();
+    const int64_t item = (int64_t)blockIdx.x * (kBoundsThreads / 32) + threadIdx.x / 32;
+    if (item >= a.items) return;
+    const int lane = threadIdx.x & 31, kv = a.cache.kv_heads, head = (int)(item % kv);
+    const int last = a.last[item / kv];
+    if (last < 0) return;
+    const int page = last / kKvPage, rows = last % kKvPage + 1;
+    if (page >= a.cache.n_pages) {
+        if (lane == 0 && a.status) atomicOr(a.status, WICI_BAD_SLOT);
+        return;
+    }
+    const uint8_t *block = a.cache.data + page * a.cache.page_stride + (int64_t)head * kv_block_bytes(FMT, D);
+    float scale = 1.f;
+    if (FMT != WICI_KV_BF16 && lane < rows) scale = ((const float *)(block + kv_scales_at(FMT, D)))[lane];
+    float x[kKvPage][E];
+#pragma unroll
+    for (int r = 0; r < kKvPage; ++r)
+        if (r < rows) load_key<FMT, D, E>(block, r, lane * E, x[r]);
+    float hi[E], lo[E];
+    uint32_t most = 0;                // of the magnitudes' bits: an infinity or NaN is the largest
+#pragma unroll
+    for (int j = 0; j < E; ++j) hi[j] = -INFINITY, lo[j] = INFINITY;
+#pragma unroll
+    for (int r = 0; r < kKvPage; ++r) {
+        const float s = FMT == WICI_KV_BF16 ? 1.f : __shfl_sync(0xffffffffu, scale, r);
+        if (r >= rows) continue;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float v = FMT == WICI_KV_BF16 ? x[r][j] : x[r][j] * s;
+            hi[j] = fmaxf(hi[j], v);
+            lo[j] = fminf(lo[j], v);
+            most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
+        }
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    const bool finite = most < kInfBits;
+    const float s = finite ? __fmul_rn(__uint_as_float(most), 1.f / 127.f) : __uint_as_float(0x7FC00000u);
+    const bool some = finite && s >= 0x1p-126f;
+    int8_t code[2][E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        code[0][j] = some ? (int8_t)__float2int_rn(__fdiv_rn(hi[j], s)) : (int8_t)0;
+        code[1][j] = some ? (int8_t)__float2int_rn(__fdiv_rn(lo[j], s)) : (int8_t)0;
+    }
+    uint8_t *record = a.bounds + page * a.bounds_stride;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint8_t *to = record + (head * 2 + i) * D + lane * E;
+        if (E == 4) *(uint32_t *)to = *(const uint32_t *)code[i];
+        else *(uint16_t *)to = *(const uint16_t *)code[i];
+    }
+    if (lane == 0) ((float *)(record + kv * 2 * D))[head] = finite ? some ? s : 0.f : s;
+}
+
+// ------------------------------------------------------------------ select ----
+struct SelectArg {
+    HeadsArg q;
+    const uint8_t *bounds;
+    int64_t bounds_stride;
+    const int32_t *pages, *lengths;
+    int32_t *out_pages, *out_lengths, *out_blocks, *status;
+    int kv_heads, group, n_pages, max_pages, keep, first, recent, q_dtype;
+    int cluster;
+};
+
+constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
+constexpr int kMaxSelectPages = 1 << 15;   // of a sequence: their scores stand in shared memory
+constexpr int kMaxSelectGroup = 64;        // query heads of a KV head: so do they
+constexpr float kLevels = 1023.f;          // of a query's whole numbers: 128 * 127 * 1023 < 2^24
+constexpr uint32_t kForced = 0xFFFFFFFFu;  // in the place of a score: above every one
+constexpr uint32_t kFirst = 0xFF800000u;   // +infinity's
+
+constexpr size_t select_smem(int d, int group, int max_pages) {
+    return (size_t)(group + 7) / 8 * (2 * d / 16 * 256 + 8 * 4) + ((size_t)max_pages + 31) / 32 * 128;
+}
+
+// Scores in the order of unsigned integers; NaN, which no page should have, stands with +infinity
+__device__ __forceinline__ uint32_t order_of(float s) {
+    const uint32_t u = __float_as_uint(s + 0.f);
+    if (s != s) return kFirst;
+    return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ void mma_f16(float *c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
+}
+__device__ __forceinline__ void store_to_first(uint32_t addr, uint32_t v) {
+    asm volatile("{\n\t.reg .u32 ra;\n\tmapa.shared::cluster.u32 ra, %0, 0;\n\tst.shared::cluster.u32 [ra], %1;\n\t}" ::"r"(addr), "r"(v)
+                 : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_constant__ SelectArg a) {
+    constexpr int STEPS = 2 * D / 16, LOADS = 2 * D / 64;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ uint32_t part[2][2][kSelectWarps];
+    const int tiles = (a.group + 7) / 8;
+    __half *qs = (__half *)smem;                                  // [tile][step][lane][4]: B fragments
+    float *most = (float *)(smem + tiles * STEPS * 256);          // [tile * 8]: each query's largest magnitude
+    uint32_t *keys = (uint32_t *)(most + tiles * 8);              // [page], of the first block
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rank = blockIdx.x % a.cluster, h = blockIdx.x / a.cluster, b = blockIdx.y;
+    // Every block of a cluster comes to each barrier, whatever it reads
+    if (a.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    griddep_launch_dependents();
+    griddep_wait();
+    const int n = a.lengths[b];
+    const bool bad = n > (int64_t)a.max_pages * kKvPage;
+    const int count = bad || n <= 0 ? 0 : (n + kKvPage - 1) / kKvPage;
+    const bool choose = count > a.keep;
+
+    if (choose) {
+        for (int i = warp; i < tiles * 8; i += kSelectWarps) {    // one query a warp
+            float x[D / 32];
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                x[j] = 0.f;
+                if (i < a.group) {
+                    const int64_t e = lane + 32 * j;
+                    const int head = h * a.group + i;
+                    x[j] = a.q_dtype == WICI_F32 ? a.q.row<float>(b, head)[e]
+                           : a.q_dtype == WICI_F16 ? __half2float(a.q.row<__half>(b, head)[e])
+                                                   : __bfloat162float(a.q.row<__nv_bfloat16>(b, head)[e]);
+                }
+                top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+            }
+            top = __reduce_max_sync(0xffffffffu, top);
+            const bool some = top < kInfBits && __uint_as_float(top) >= 0x1p-100f;
+            const float per = some ? __fmul_rn(__frcp_rn(__uint_as_float(top)), kLevels) : 0.f;
+            if (lane == 0) most[i] = some ? __uint_as_float(top) : 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                const float w = some ? rintf(__fmul_rn(x[j], per)) : 0.f;
+#pragma unroll
+                for (int end = 0; end < 2; ++end) {               // against the largest keys, the smallest
+                    const int e = end * D + lane + 32 * j;        // byte of a record's row: chunk e / 16 is lane t's
+                    const int step = e / 64 * 4 + e % 16 / 4, to = i % 8 * 4 + e / 16 % 4;
+                    qs[((i / 8 * STEPS + step) * 32 + to) * 4 + e % 4] = __float2half_rn(end ? fminf(w, 0.f) : fmaxf(w, 0.f));
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (a.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // the first block runs
+
+    if (choose) {
+        const int32_t *table = a.pages + (int64_t)b * a.max_pages;
+        const uint32_t keys_at = smem_u32(keys);
+        const int step = kSelectWarps * a.cluster;
+        for (int tile = rank * kSelectWarps + warp; tile * 16 < count; tile += step) {
+            const int at = tile * 16 + (lane & 15);
+            const int page = at < count ? table[at] : 0;
+            if (lane < 16 && at < count && (uint32_t)page >= (uint32_t)a.n_pages && a.status) atomicOr(a.status, WICI_BAD_PAGE);
+            int row_page[2];
+            uint4 raw[2][LOADS];
+            float scale[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                row_page[r] = __shfl_sync(0xffffffffu, page, g + 8 * r);
+                const bool there = (uint32_t)row_page[r] < (uint32_t)a.n_pages;
+                const uint8_t *record = a.bounds + (int64_t)(there ? row_page[r] : 0) * a.bounds_stride;
+                const uint4 *src = (const uint4 *)(record + h * 2 * D) + t;
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) raw[r][i] = there ? src[4 * i] : make_uint4(0, 0, 0, 0);
+                scale[r] = there ? ((const float *)(record + a.kv_heads * 2 * D))[h] : INFINITY;
+            }
+            float best[2] = {-INFINITY, -INFINITY};
+            for (int q = 0; q < tiles; ++q) {
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint2 *frag = (const uint2 *)qs + q * STEPS * 32 + lane;
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) {
+                    const uint32_t *u = (const uint32_t *)&raw[0][i], *v = (const uint32_t *)&raw[1][i];
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        uint32_t a0, a1, a2, a3;
+                        decode4<WICI_KV_INT8>(u[s], a0, a2);
+                        decode4<WICI_KV_INT8>(v[s], a1, a3);
+                        mma_f16(c, a0, a1, a2, a3, frag[(4 * i + s) * 32]);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int head = q * 8 + 2 * t + j;
+                    if (head >= a.group) continue;
+                    best[0] = fmaxf(best[0], __fmul_rn(c[j], most[head]));
+                    best[1] = fmaxf(best[1], __fmul_rn(c[2 + j], most[head]));
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                best[r] = fmaxf(best[r], __shfl_xor_sync(0xffffffffu, best[r], 1));
+                best[r] = fmaxf(best[r], __shfl_xor_sync(0xffffffffu, best[r], 2));
+                const int i = tile * 16 + g + 8 * r;
+                uint32_t key = kFirst;                            // a key that is not finite, a page that is not there
+                if (scale[r] == 0.f) key = order_of(0.f);
+                else if (fabsf(scale[r]) < INFINITY) key = order_of(__fmul_rn(best[r], scale[r]));
+                if (i < a.first || i >= count - a.recent) key = kForced;
+                if (t == r && i < count) {
+                    if (a.cluster > 1) store_to_first(keys_at + 4 * i, key);
+                    else keys[i] = key;
+                }
+            }
+        }
+    }
+    if (a.cluster > 1) {
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (rank != 0) return;
+    } else {
+        __syncthreads();
+    }
+
+    // ---- the first block: the keep-th largest key, and the pages from it on ----
+    const int32_t *table = a.pages + (int64_t)b * a.max_pages;
+    int32_t *pages = a.out_pages + ((int64_t)b * a.kv_heads + h) * a.keep;
+    int32_t *blocks = a.out_blocks ? a.out_blocks + ((int64_t)b * a.kv_heads + h) * a.keep : nullptr;
+    if (h == 0 && threadIdx.x == 0) {
+        // what is bad stays bad: a length past the selected pages
+        a.out_lengths[b] = bad ? a.keep * kKvPage + 1 : choose ? (a.keep - 1) * kKvPage + (n - 1) % kKvPage + 1 : max(n, 0);
+        if (bad && a.status) atomicOr(a.status, WICI_BAD_LENGTH);
+    }
+    if (!choose) {
+        for (int i = threadIdx.x; i < a.keep; i += kSelectThreads) {
+            const int page = i < count ? table[i] : -1;
+            pages[i] = page;
+            if (blocks) blocks[i] = i < count ? i : -1;
+            if (h == 0 && i < count && (uint32_t)page >= (uint32_t)a.n_pages && a.status) atomicOr(a.status, WICI_BAD_PAGE);
+        }
+        return;
+    }
+    // over the block: sums of u (two halves of 16 bits) and v
+    int turn = 0;
+    auto sums = [&](uint32_t &u, uint32_t &v) {
+        u = __reduce_add_sync(0xffffffffu, u);
+        v = __reduce_add_sync(0xffffffffu, v);
+        if (lane == 0) part[turn][0][warp] = u, part[turn][1][warp] = v;
+        __syncthreads();
+        u = v = 0;
+#pragma unroll
+        for (int w = 0; w < kSelectWarps; ++w) u += part[turn][0][w], v += part[turn][1][w];
+        turn ^= 1;                                                // a turn's words are read before the next but one barrier
+    };
+    uint32_t limit = kForced;
+    if (a.first + a.recent < a.keep) {
+        // the keys that are not forced: their leading bits in common need no search
+        uint32_t hi = 0, lo = 0xFFFFFFFFu;
+        for (int i = threadIdx.x; i < count; i += kSelectThreads) {
+            const uint32_t k = keys[i];
+            if (k != kForced) hi = max(hi, k), lo = min(lo, k);
+        }
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        if (lane == 0) part[1][0][warp] = hi, part[1][1][warp] = lo;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kSelectWarps; ++w) hi = max(hi, part[1][0][w]), lo = min(lo, part[1][1][w]);
+        int bit = hi == lo ? 0 : 32 - __clz(hi ^ lo);             // bits that are open
+        bit = (bit + 1) & ~1;
+        limit = bit >= 32 ? 0u : hi >> bit << bit;
+        while (bit > 0) {
+            bit -= 2;
+            const uint32_t one = 1u << bit, x1 = limit | one, x2 = limit | 2 * one, x3 = limit | 3 * one;
+            uint32_t u = 0, v = 0;
+            for (int i = threadIdx.x; i < count; i += kSelectThreads) {
+                const uint32_t k = keys[i];
+                u += (k >= x1 ? 1u : 0u) + (k >= x2 ? 0x10000u : 0u);
+                v += k >= x3 ? 1u : 0u;
+            }
+            sums(u, v);
+            const uint32_t keep = (uint32_t)a.keep;
+            limit = v >= keep ? x3 : u >> 16 >= keep ? x2 : (u & 0xFFFF) >= keep ? x1 : limit;
+        }
+    }
+    // a warp's share of the pages, in order: those above the limit, and as many of those at it as there is room for
+    const int share = ((count + kSelectWarps - 1) / kSelectWarps + 31) & ~31, from = warp * share, to = min(count, from + share);
+    uint32_t over = 0, at = 0;
+    for (int i = from + lane; i < to; i += 32) over += keys[i] > limit, at += keys[i] == limit;
+    over = __reduce_add_sync(0xffffffffu, over);
+    at = __reduce_add_sync(0xffffffffu, at);
+    __syncthreads();                                              // the last turn's words have been read
+    if (lane == 0) part[0][0][warp] = over, part[0][1][warp] = at;
+    __syncthreads();
+    uint32_t all_over = 0;
+#pragma unroll
+    for (int w = 0; w < kSelectWarps; ++w) all_over += part[0][0][w];
+    uint32_t room = a.keep > (int)all_over ? a.keep - all_over : 0, place = 0;
+    for (int w = 0; w < warp; ++w) {
+        const uint32_t taken = min(room, part[0][1][w]);
+        place += part[0][0][w] + taken;
+        room -= taken;
+    }
+    const uint32_t below = (1u << lane) - 1;
+    for (int i0 = from; i0 < to; i0 += 32) {
+        const int i = i0 + lane;
+        const uint32_t k = i < to ? keys[i] : 0u;
+        const bool is_over = i < to && k > limit, is_at = i < to && k == limit;
+        const uint32_t m_at = __ballot_sync(0xffffffffu, is_at);
+        const bool taken = is_over || (is_at && (uint32_t)__popc(m_at & below) < room);
+        const uint32_t m = __ballot_sync(0xffffffffu, taken);
+        const uint32_t p = place + __popc(m & below);
+        if (taken && p < (uint32_t)a.keep) {
+            pages[p] = table[i];
+            if (blocks) blocks[p] = i;
+        }
+        place += __popc(m);
+        room -= min(room, (uint32_t)__popc(m_at));
+    }
+}
+
+struct Device {
+    int sms;
+};
+DeviceTable<Device> g_devices;
+
+int device_of(Device *d) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess)
+        e = g_devices.get(dev, d, [dev](Device *x) {
+            constexpr int kMost = (int)select_smem(128, kMaxSelectGroup, kMaxSelectPages);
+            cudaError_t e1 = cudaFuncSetAttribute(select_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+            if (e1 == cudaSuccess) e1 = cudaFuncSetAttribute(select_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+            return e1 == cudaSuccess ? cudaDeviceGetAttribute(&x->sms, cudaDevAttrMultiProcessorCount, dev) : e1;
+        });
+    return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "select setup: %s", cudaGetErrorString(e));
+}
+
+const char *check_bounds(const wici_kv_bounds *b, const wici_kv_cache *c) {
+    if (!b) return "null bounds";
+    if (!b->data || ((uintptr_t)b->data & 15)) return "bounds data null or not 16-byte aligned";
+    if (b->page_stride % 16 || b->page_stride < wici_kv_bounds_bytes(c->n_kv_heads, c->head_dim))
+        return "bounds page_stride must be a multiple of 16 and at least a record";
+    if (b->page_stride > INT64_MAX / kMaxPages) return "bounds page_stride";
+    return nullptr;
+}
+
+bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
+    return a && b && (uintptr_t)a < (uintptr_t)b + (size_t)nb && (uintptr_t)b < (uintptr_t)a + (size_t)na;
+}
+
+template <int FMT>
+cudaError_t launch_bounds(int d, const BoundsArg &a, cudaStream_t st) {
+    const dim3 grid((unsigned)((a.items + kBoundsThreads / 32 - 1) / (kBoundsThreads / 32)));
+    return d == 64 ? launch_kernel(bounds_kernel<FMT, 64>, grid, kBoundsThreads, 0, st, 1, true, a)
+                   : launch_kernel(bounds_kernel<FMT, 128>, grid, kBoundsThreads, 0, st, 1, true, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t wici_kv_bounds_bytes(int32_t n_kv_heads, int32_t head_dim) {
+    if ((head_dim != 64 && head_dim != 128) || n_kv_heads < 1) return 0;
+    return ((int64_t)n_kv_heads * (2 * head_dim + 4) + 15) / 16 * 16;
+}
+
+int wici_kv_bounds_update(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_bounds *bounds, const int32_t *last,
+                          int64_t count, int32_t *status) {
+    if (const char *m = check_cache(cache)) return fail(WICI_E_ARG, "bounds: %s", m);
+    if (const char *m = check_bounds(bounds, cache)) return fail(WICI_E_ARG, "bounds: %s", m);
+    if (count < 0 || count > kMaxPages) return fail(WICI_E_ARG, "bounds: count must be in [0, 2^27)");
+    if (count == 0) return WICI_OK;
+    if (!last || !words(last) || !words(status)) return fail(WICI_E_ARG, "bounds: last null, or last or status unaligned");
+    BoundsArg a = {};
+    a.cache = cache_arg(cache);
+    a.bounds = (uint8_t *)bounds->data;
+    a.bounds_stride = bounds->page_stride;
+    a.status = status;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t e = cudaSuccess;
+    const int64_t most = ((int64_t)1 << 31) / cache->n_kv_heads;    // of a launch: its blocks are below 2^30
+    for (int64_t i = 0; i < count && e == cudaSuccess; i += most) {
+        a.last = last + i;
+        a.items = (count - i < most ? count - i : most) * cache->n_kv_heads;
+        switch (cache->format) {
+            case WICI_KV_BF16: e = launch_bounds<WICI_KV_BF16>(cache->head_dim, a, st); break;
+            case WICI_KV_INT8: e = launch_bounds<WICI_KV_INT8>(cache->head_dim, a, st); break;
+            case WICI_KV_E2M1: e = launch_bounds<WICI_KV_E2M1>(cache->head_dim, a, st); break;
+            default: e = launch_bounds<WICI_KV_E4M3>(cache->head_dim, a, st); break;
+        }
+    }
+    return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "bounds: %s", cudaGetErrorString(e));
+}
+
+int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_bounds *bounds, const wici_select_shape *shape,
+                   const int32_t *pages, const int32_t *lengths, const wici_heads *q, int32_t *out_pages,
+                   int32_t *out_lengths, int32_t *out_blocks, int32_t *status) {
+    if (const char *m = check_cache(cache)) return fail(WICI_E_ARG, "select: %s", m);
+    if (const char *m = check_bounds(bounds, cache)) return fail(WICI_E_ARG, "select: %s", m);
+    if (!shape) return fail(WICI_E_ARG, "select: null shape");
+    if (shape->batch < 0 || shape->batch > 65535) return fail(WICI_E_ARG, "select: batch must be in [0, 65535]");
+    if (shape->max_pages < 1 || shape->max_pages > kMaxSelectPages) return fail(WICI_E_ARG, "select: max_pages must be in [1, 32768]");
+    if (shape->first < 0 || shape->recent < 1 || shape->keep < 1 || shape->keep > kMaxSelectPages ||
+        shape->first > shape->keep || shape->recent > shape->keep - shape->first)
+        return fail(WICI_E_ARG, "select: first >= 0, recent >= 1 and first + recent <= keep <= 32768 required");
+    if (const char *m = check_heads(q, shape->batch, cache->head_dim, false)) return fail(WICI_E_ARG, "select q: %s", m);
+    if (q->heads % cache->n_kv_heads || q->heads / cache->n_kv_heads > kMaxSelectGroup)
+        return fail(WICI_E_ARG, "select: query heads must be a multiple of the cache's heads, at most 64 times as many");
+    if (shape->batch == 0) return WICI_OK;
+    if (!pages || !lengths || !out_pages || !out_lengths) return fail(WICI_E_ARG, "select: null pages or lengths");
+    if (!words(pages) || !words(lengths) || !words(out_pages) || !words(out_lengths) || !words(out_blocks) || !words(status))
+        return fail(WICI_E_ARG, "select: pages, lengths, blocks or status unaligned");
+    const int64_t in = (int64_t)shape->batch * shape->max_pages * 4, list = (int64_t)shape->batch * cache->n_kv_heads * shape->keep * 4;
+    const int64_t len = (int64_t)shape->batch * 4;
+    const struct { const void *p; int64_t n; } outs[3] = {{out_pages, list}, {out_lengths, len}, {out_blocks, list}};
+    for (int i = 0; i < 3; ++i) {
+        bool shared = overlap(outs[i].p, outs[i].n, pages, in) || overlap(outs[i].p, outs[i].n, lengths, len);
+        for (int j = 0; j < i; ++j) shared |= overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n);
+        if (shared) return fail(WICI_E_ARG, "select: an output overlaps another tensor");
+    }
+    Device dev;
+    if (int rc = device_of(&dev)) return rc;
+    SelectArg a = {};
+    a.q = heads_arg(q);
+    a.bounds = (const uint8_t *)bounds->data;
+    a.bounds_stride = bounds->page_stride;
+    a.pages = pages;
+    a.lengths = lengths;
+    a.out_pages = out_pages;
+    a.out_lengths = out_lengths;
+    a.out_blocks = out_blocks;
+    a.status = status;
+    a.kv_heads = cache->n_kv_heads;
+    a.group = q->heads / cache->n_kv_heads;
+    a.n_pages = cache->n_pages;
+    a.max_pages = shape->max_pages;
+    a.keep = shape->keep;
+    a.first = shape->first;
+    a.recent = shape->recent;
+    a.q_dtype = q->dtype;
+    a.cluster = 1;
+    const dim3 grid((unsigned)(a.cluster * a.kv_heads), (unsigned)shape->batch);
+    const size_t smem = select_smem(cache->head_dim, a.group, a.max_pages);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const cudaError_t e = cache->head_dim == 64 ? launch_kernel(select_kernel<64>, grid, kSelectThreads, smem, st, a.cluster, true, a)
+                                                : launch_kernel(select_kernel<128>, grid, kSelectThreads, smem, st, a.cluster, true, a);
+    return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "select: %s", cudaGetErrorString(e));
+}
+
+}  // extern "C"

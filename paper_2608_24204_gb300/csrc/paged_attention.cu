@@ -53,35 +53,16 @@ const char *check_query_heads(const wici_kv_cache *c, int n_q_heads) {
                : nullptr;
 }
 
-}  // namespace
-
-extern "C" {
-
-int wici_paged_attention_workspace_bytes(const wici_kv_cache *cache, int32_t n_q_heads, int32_t batch, size_t *bytes) {
-    if (const char *m = check_cache(cache)) return fail(WICI_E_ARG, "attention: %s", m);
-    if (const char *m = check_query_heads(cache, n_q_heads)) return fail(WICI_E_ARG, "attention: %s", m);
-    if (batch < 0 || batch > 65535) return fail(WICI_E_ARG, "attention: batch must be in [0, 65535]");
-    if (!bytes) return fail(WICI_E_ARG, "attention: null output");
-    int sms = 152;   // without a device: a GB300's
-    int dev = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess) {
-        if (int rc = device_sms(&sms)) return rc;
-    } else {
-        cudaGetLastError();
-    }
-    *bytes = kTicketBytes + (size_t)used_sms(sms) * kBlocksPerSm * 2 * attn_piece_floats(cache->head_dim) * sizeof(float);
-    return WICI_OK;
-}
-
-int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wici_attn_shape *shape,
-                         const int32_t *pages, const int32_t *lengths, const wici_heads *q, const wici_heads *out,
-                         float *lse, void *workspace, int32_t *status) {
+int attend(void *cuda_stream, const wici_kv_cache *cache, const wici_attn_shape *shape, bool selected,
+           const int32_t *pages, const int32_t *lengths, const wici_heads *q, const wici_heads *out, float *lse,
+           void *workspace, int32_t *status) {
     if (const char *m = check_cache(cache)) return fail(WICI_E_ARG, "attention: %s", m);
     if (!shape) return fail(WICI_E_ARG, "attention: null shape");
     if (shape->batch < 0 || shape->batch > 65535) return fail(WICI_E_ARG, "attention: batch must be in [0, 65535]");
     if (shape->max_pages < 1 || shape->max_pages > kMaxPages)
         return fail(WICI_E_ARG, "attention: max_pages must be in [1, 2^27)");
     if (shape->window < 0) return fail(WICI_E_ARG, "attention: window must be >= 0");
+    if (selected && shape->window) return fail(WICI_E_ARG, "attention: a window over selected pages");
     if (!isfinite(shape->scale)) return fail(WICI_E_ARG, "attention: scale must be finite");
     if (const char *m = check_heads(q, shape->batch, cache->head_dim, false)) return fail(WICI_E_ARG, "attention q: %s", m);
     if (const char *m = check_heads(out, shape->batch, cache->head_dim, true))
@@ -111,6 +92,8 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     const AttnKind kind = attn_kind(a.group, exact);
     a.tiles = kind == ATTN_PLAIN ? (a.group + 15) / 16 : (a.group + 7) / 8;
     a.max_pages = shape->max_pages;
+    a.head_stride = selected ? shape->max_pages : 0;
+    a.table_stride = (int64_t)shape->max_pages * (selected ? cache->n_kv_heads : 1);
     a.window = shape->window;
     a.q_dtype = q->dtype;
     a.out_dtype = out->dtype;
@@ -125,7 +108,7 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
     cudaError_t e = cudaSuccess;
     for (int b = 0; b < shape->batch && e == cudaSuccess; b += most) {
         a.batch = shape->batch - b < most ? shape->batch - b : most;
-        a.pages = pages + (int64_t)b * shape->max_pages;
+        a.pages = pages + b * a.table_stride;
         a.lengths = lengths + b;
         a.lse = lse ? lse + (int64_t)b * q->heads : nullptr;
         a.q.data = (uint8_t *)q->data + (int64_t)b * q->token_stride * dtype_bytes(q->dtype);
@@ -138,6 +121,38 @@ int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wi
         }
     }
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "attention: %s", cudaGetErrorString(e));
+}
+
+}  // namespace
+
+extern "C" {
+
+int wici_paged_attention_workspace_bytes(const wici_kv_cache *cache, int32_t n_q_heads, int32_t batch, size_t *bytes) {
+    if (const char *m = check_cache(cache)) return fail(WICI_E_ARG, "attention: %s", m);
+    if (const char *m = check_query_heads(cache, n_q_heads)) return fail(WICI_E_ARG, "attention: %s", m);
+    if (batch < 0 || batch > 65535) return fail(WICI_E_ARG, "attention: batch must be in [0, 65535]");
+    if (!bytes) return fail(WICI_E_ARG, "attention: null output");
+    int sms = 152;   // without a device: a GB300's
+    int dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess) {
+        if (int rc = device_sms(&sms)) return rc;
+    } else {
+        cudaGetLastError();
+    }
+    *bytes = kTicketBytes + (size_t)used_sms(sms) * kBlocksPerSm * 2 * attn_piece_floats(cache->head_dim) * sizeof(float);
+    return WICI_OK;
+}
+
+int wici_paged_attention(void *cuda_stream, const wici_kv_cache *cache, const wici_attn_shape *shape,
+                         const int32_t *pages, const int32_t *lengths, const wici_heads *q, const wici_heads *out,
+                         float *lse, void *workspace, int32_t *status) {
+    return attend(cuda_stream, cache, shape, false, pages, lengths, q, out, lse, workspace, status);
+}
+
+int wici_selected_attention(void *cuda_stream, const wici_kv_cache *cache, const wici_attn_shape *shape,
+                            const int32_t *pages, const int32_t *lengths, const wici_heads *q, const wici_heads *out,
+                            float *lse, void *workspace, int32_t *status) {
+    return attend(cuda_stream, cache, shape, true, pages, lengths, q, out, lse, workspace, status);
 }
 
 }  // extern "C"

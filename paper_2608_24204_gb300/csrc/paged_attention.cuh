@@ -64,6 +64,8 @@ struct AttnArg {
     int *tickets;                     // [blocks]: arrivals at the segment that starts in a block and leaves it
     float *pieces;                    // [blocks][2][kAttnPieceRows][D + 2]: O, then m and l, of a block's part of a segment
     int batch, q_heads, group, tiles; // head tiles of a KV head
+    int64_t table_stride;             // of `pages`: entries from a sequence to the next
+    int head_stride;                  // and from a KV head to the next: 0 where all read the same pages
     int max_pages, window;
     int q_dtype, out_dtype;
     bool q_wide, out_wide;
@@ -494,7 +496,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
         const int b = s.b, head = s.head, at = (int)(r0 + i - s.start) * P;
         const Keys k = keys_of(length[b], a.window);
         const int first_page = k.lo / kKvPage + at;
-        const int32_t *row = a.pages + (int64_t)b * a.max_pages;
+        const int32_t *row = a.pages + b * a.table_stride + (int64_t)(head / a.tiles) * a.head_stride;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             if ((first_page + p) * (int64_t)kKvPage < k.n) d.page[p] = row[first_page + p];

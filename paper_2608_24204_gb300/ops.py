@@ -28,7 +28,8 @@ _DTYPES = {torch.bfloat16: WICI_BF16, torch.float16: WICI_F16, torch.float32: WI
 
 # the entry points declared in include/wici_ops.h
 EXPORTS = ("wici_rope_make_plan", "wici_rope", "wici_kv_page_bytes", "wici_kv_append", "wici_kv_read",
-           "wici_paged_attention_workspace_bytes", "wici_paged_attention", "wici_kv_view")
+           "wici_paged_attention_workspace_bytes", "wici_paged_attention", "wici_selected_attention",
+           "wici_kv_bounds_bytes", "wici_kv_bounds_update", "wici_kv_select", "wici_kv_view")
 
 
 class wici_heads(ctypes.Structure):
@@ -58,6 +59,15 @@ class wici_attn_shape(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+class wici_kv_bounds(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("page_stride", ctypes.c_int64)]
+
+
+class wici_select_shape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("keep", ctypes.c_int32),
+                ("first", ctypes.c_int32), ("recent", ctypes.c_int32)]
+
+
 _lib = None
 _fast = {}                   # the same entry points taking addresses and packed structures, for `Rope` and `PagedKV`
 
@@ -76,12 +86,18 @@ def lib():
         L.wici_kv_read.argtypes = [vp, cp, vp, i64, hp, hp, vp]
         L.wici_paged_attention_workspace_bytes.argtypes = [cp, i32, i32, P(ctypes.c_size_t)]
         L.wici_paged_attention.argtypes = [vp, cp, P(wici_attn_shape), vp, vp, hp, hp, vp, vp, vp]
+        L.wici_selected_attention.argtypes = L.wici_paged_attention.argtypes
+        L.wici_kv_bounds_bytes.argtypes = [i32, i32]
+        L.wici_kv_bounds_update.argtypes = [vp, cp, P(wici_kv_bounds), vp, i64, vp]
+        L.wici_kv_select.argtypes = [vp, cp, P(wici_kv_bounds), P(wici_select_shape), vp, vp, hp, vp, vp, vp, vp]
         L.wici_kv_view.argtypes = [vp, i32, cp, P(vp), P(i32)]
         for name in EXPORTS:
             getattr(L, name).restype = ctypes.c_int
-        L.wici_kv_page_bytes.restype = i64
+        L.wici_kv_page_bytes.restype = L.wici_kv_bounds_bytes.restype = i64
         for name, types in (("wici_rope", [vp, vp, i32, vp, i64, vp, vp]), ("wici_kv_append", [vp, vp, vp, i64] + [vp] * 7),
-                            ("wici_kv_read", [vp, vp, vp, i64, vp, vp, vp]), ("wici_paged_attention", [vp] * 10)):
+                            ("wici_kv_read", [vp, vp, vp, i64, vp, vp, vp]), ("wici_paged_attention", [vp] * 10),
+                            ("wici_selected_attention", [vp] * 10), ("wici_kv_bounds_update", [vp, vp, vp, vp, i64, vp]),
+                            ("wici_kv_select", [vp] * 11)):
             _fast[name] = L[name]          # a function object of its own
             _fast[name].argtypes, _fast[name].restype = types, ctypes.c_int
         _lib = L
@@ -127,6 +143,27 @@ def wici_paged_attention(stream: int, cache: wici_kv_cache, shape: wici_attn_sha
     _check(lib().wici_paged_attention(stream, cache, shape, pages, lengths, q, out, lse, workspace, status))
 
 
+def wici_selected_attention(stream: int, cache: wici_kv_cache, shape: wici_attn_shape, pages: int, lengths: int,
+                            q: wici_heads, out: wici_heads, lse: int | None, workspace: int,
+                            status: int | None = None) -> None:
+    _check(lib().wici_selected_attention(stream, cache, shape, pages, lengths, q, out, lse, workspace, status))
+
+
+def wici_kv_bounds_bytes(n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().wici_kv_bounds_bytes(n_kv_heads, head_dim))
+
+
+def wici_kv_bounds_update(stream: int, cache: wici_kv_cache, bounds: wici_kv_bounds, last: int, count: int,
+                          status: int | None = None) -> None:
+    _check(lib().wici_kv_bounds_update(stream, cache, bounds, last, count, status))
+
+
+def wici_kv_select(stream: int, cache: wici_kv_cache, bounds: wici_kv_bounds, shape: wici_select_shape, pages: int,
+                   lengths: int, q: wici_heads, out_pages: int, out_lengths: int, out_blocks: int | None = None,
+                   status: int | None = None) -> None:
+    _check(lib().wici_kv_select(stream, cache, bounds, shape, pages, lengths, q, out_pages, out_lengths, out_blocks, status))
+
+
 def wici_kv_view(ctx, layer: int):
     """(cache, device address of the page table, its entries) of a context's layer."""
     cache, pages, n = wici_kv_cache(), ctypes.c_void_p(), ctypes.c_int32()
@@ -137,6 +174,7 @@ def wici_kv_view(ctx, layer: int):
 # ------------------------------------------------------------- tensors
 _pack_heads = struct.Struct("@Pqqii").pack       # a wici_heads
 _pack_shape = struct.Struct("@iiif").pack        # a wici_attn_shape
+_pack_select = struct.Struct("@iiiii").pack      # a wici_select_shape
 # torch's own short cuts past Stream objects, where this torch has them (2 us of a call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
@@ -304,7 +342,8 @@ class PagedKV:
                window: int = 0, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
                workspace: torch.Tensor | None = None) -> torch.Tensor:
         """One token's attention per sequence: q [batch, heads, head_dim] over the first lengths[b] tokens (the last
-        `window` of them, 0: all) of the pages pages[b] (int32 [batch, max_pages]).  scale: head_dim ** -0.5 unless
+        `window` of them, 0: all) of the pages pages[b] (int32 [batch, max_pages], or [batch, n_kv_heads, max_pages]
+        where every KV head has pages of its own, as KeyBounds.select gives them; without a window).  scale: head_dim ** -0.5 unless
         given.  Fills lse (float32 [batch, heads]) when given.  The workspace, unless given (`workspace()`), is one
         per stream, or in a graph capture one of that call's own."""
         dev, d = self._device, self.head_dim
@@ -318,17 +357,19 @@ class PagedKV:
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != (batch, heads) or not lse.is_contiguous() or
                                 lse.get_device() != dev):
             raise ValueError(f"lse: expected contiguous float32 {[batch, heads]} on cuda:{dev}")
-        if pages.dim() != 2:
-            raise ValueError("pages: expected [batch, max_pages]")
+        selected = pages.dim() == 3
+        if not selected and pages.dim() != 2:
+            raise ValueError("pages: expected [batch, max_pages] or [batch, n_kv_heads, max_pages]")
         if workspace is None:
             workspace = self._workspace_for(stream, heads, batch)
         elif workspace.get_device() != dev or not workspace.is_contiguous() or \
                 workspace.numel() * workspace.element_size() < self.workspace_bytes(heads, batch):
             raise ValueError(f"workspace: expected {self.workspace_bytes(heads, batch)} bytes on cuda:{dev}")
-        columns = pages.shape[1]
+        columns = pages.shape[-1]
         shape = _pack_shape(batch, columns, window, d ** -0.5 if scale is None else scale)
-        _check(_fast["wici_paged_attention"](
-            stream, self._cache, shape, _ints(pages, (batch, columns), dev, "pages"), _ints(lengths, (batch,), dev, "lengths"),
+        table = _ints(pages, (batch, self.n_kv_heads, columns) if selected else (batch, columns), dev, "pages")
+        _check(_fast["wici_selected_attention" if selected else "wici_paged_attention"](
+            stream, self._cache, shape, table, _ints(lengths, (batch,), dev, "lengths"),
             hq, _heads(out, d, dev, "out"), None if lse is None else lse.data_ptr(), workspace.data_ptr(), self._status))
         return out
 
@@ -352,7 +393,7 @@ class PagedKV:
         return self._workspaces[stream]
 
     def check(self) -> None:
-        """Waits for the current stream and raises if a call on it met a slot, page or length outside the cache
+        """Waits for the current stream and raises if a call on it (a KeyBounds' among them) met a slot, page or length outside the cache
         (which clears the record)."""
         bits = int(self.status.item())
         if bits:
@@ -360,3 +401,60 @@ class PagedKV:
             what = [n for b, n in ((WICI_BAD_SLOT, "a slot"), (WICI_BAD_PAGE, "a page"), (WICI_BAD_LENGTH, "a length"))
                     if bits & b]
             raise WiciError(_w.WICI_E_ARG, f"paged cache: {' and '.join(what)} outside the cache or page table")
+
+
+class KeyBounds:
+    """Bounds of the keys in each page of a cache, by which `select` chooses the pages that a step attends to: the largest
+    and the smallest key element by element as int8 `codes` [page, kv head, 2, head_dim] under `scales` [page, kv head],
+    in a torch buffer (or in `data`, a uint8 tensor of a record for each page).
+
+    A step of a long context: PagedKV.append, `update` with its slots, `select`, PagedKV.attend over what that gives.
+    The cache's `check` reports slots, pages and lengths outside it.  Autograd does not see the calls."""
+
+    def __init__(self, cache: PagedKV, data: torch.Tensor | None = None):
+        kv, d = cache.n_kv_heads, cache.head_dim
+        record = wici_kv_bounds_bytes(kv, d)
+        if data is None:
+            data = torch.zeros(cache.n_pages * record, dtype=torch.uint8, device=cache.device)
+        if data.dtype != torch.uint8 or not data.is_contiguous() or data.numel() != cache.n_pages * record or data.device != cache.device:
+            raise ValueError(f"data: expected contiguous uint8 [{cache.n_pages * record}] on {cache.device}: records of {record} bytes")
+        self.cache, self.data = cache, data
+        rows = data.view(cache.n_pages, record)
+        self.codes = rows[:, :kv * 2 * d].view(torch.int8).unflatten(1, (kv, 2, d))
+        self.scales = rows[:, kv * 2 * d:kv * (2 * d + 4)].view(torch.float32)
+        self.bounds = wici_kv_bounds(data.data_ptr(), record)
+        self._bounds = ctypes.addressof(self.bounds)
+
+    def update(self, last: torch.Tensor) -> None:
+        """Bounds of the pages of slots `last` (int32 [n]; each the last token of its page, a page at most once; negative:
+        skipped), over a page's places up to that slot."""
+        c = self.cache
+        stream = _stream(c._device)
+        n = last.shape[0]
+        _check(_fast["wici_kv_bounds_update"](stream, c._cache, self._bounds, _ints(last, (n,), c._device, "last"), n, c._status))
+
+    def select(self, q: torch.Tensor, pages: torch.Tensor, lengths: torch.Tensor, keep: int, first: int = 1, recent: int = 1,
+               out: tuple[torch.Tensor, torch.Tensor] | None = None, blocks: torch.Tensor | None = None):
+        """(pages int32 [batch, n_kv_heads, keep], lengths int32 [batch]) for PagedKV.attend: of the pages pages[b] (int32
+        [batch, max_pages]) of a sequence of lengths[b] tokens the first `first`, the last `recent` and those that score
+        highest against q [batch, heads, head_dim], `keep` in all, for each KV head.  Into `out` when given; fills `blocks`
+        (as the pages) with their columns in `pages` when given."""
+        c = self.cache
+        dev, kv = c._device, c.n_kv_heads
+        stream = _stream(dev)
+        hq = _heads(q, c.head_dim, dev, "q")
+        batch = q.shape[0]
+        if pages.dim() != 2:
+            raise ValueError("pages: expected [batch, max_pages]")
+        if keep < 1:
+            raise ValueError(f"keep: expected at least 1, got {keep}")
+        if out is None:
+            out = (torch.empty((batch, kv, keep), dtype=torch.int32, device=c.device), torch.empty(batch, dtype=torch.int32, device=c.device))
+        chosen, held = out
+        shape = _pack_select(batch, pages.shape[1], keep, first, recent)
+        _check(_fast["wici_kv_select"](
+            stream, c._cache, self._bounds, shape, _ints(pages, (batch, pages.shape[1]), dev, "pages"),
+            _ints(lengths, (batch,), dev, "lengths"), hq, _ints(chosen, (batch, kv, keep), dev, "out pages"),
+            _ints(held, (batch,), dev, "out lengths"), None if blocks is None else _ints(blocks, (batch, kv, keep), dev, "blocks"),
+            c._status))
+        return chosen, held
