@@ -253,9 +253,10 @@ __global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __g
                     float most[2];
                     blocks_of_16(x, rotate && turns && !pairs, a, most);
                     if (store) {
-                        const float s = top / kE2m1Top;
+                        constexpr float kPer = 1.f / kE2m1Top;     // the quotient, right to its last bit
+                        const float near = top * kPer, s = fmaf(fmaf(-near, kE2m1Top, top), kPer, near);
                         const bool finite = top < __uint_as_float(kInfBits), some = finite && s >= kE2m1Least;
-                        const float per6 = some ? 1.f / (6.f * s) : 0.f;
+                        const float per6 = reciprocal(6.f * s);
                         uint8_t *row = block + where * (d / 2), *each = block + kKvPage * (d / 2) + where * (d / 16);
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {

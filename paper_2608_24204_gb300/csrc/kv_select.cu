@@ -8,8 +8,8 @@
 // score is a dot product of 2 d whole numbers below 2^24: mma.m16n8k16 gives it exactly, in any order, and the selection
 // does not depend on how sums are split.  16 pages are the rows, 8 queries of the group the columns.
 // Select.  A cluster of blocks takes one sequence and KV head.  Its blocks score the pages and leave the scores, as
-// integers that order as they do, in the first block's shared memory; that one finds the keep-th largest bit by bit and
-// writes the pages above it in order, of equal ones the first.
+// integers that order as they do, in the first block's shared memory; that one finds the keep-th largest, 11 bits at
+// a time by counting, and writes the pages from it on in order, of equal ones the first.
 #include <stdarg.h>
 #include <stdio.h>
 
@@ -77,6 +77,18 @@ __device__ __forceinline__ void load_key(const uint8_t *block, int row, int e0, 
     }
 }
 
+// the largest and the smallest of three, NaN where one is
+__device__ __forceinline__ float max_of(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float min_of(float a, float b, float c) {
+    float d;
+    asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // A warp takes one page of one KV head, a lane E elements of all its rows.
 template <int FMT, int D>
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsArg a) {
@@ -100,32 +112,43 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
 #pragma unroll
     for (int r = 0; r < kKvPage; ++r)
         if (r < rows) load_key<FMT, D, E>(block, r, lane * E, x[r]);
-    float hi[E], lo[E];
-    uint32_t most = 0;                // of the magnitudes' bits: an infinity or NaN is the largest
+    float hi[E], lo[E];               // NaN where one of the values is
+    {
+        const float s = FMT == WICI_KV_BF16 ? 1.f : __shfl_sync(0xffffffffu, scale, 0);
 #pragma unroll
-    for (int j = 0; j < E; ++j) hi[j] = -INFINITY, lo[j] = INFINITY;
+        for (int j = 0; j < E; ++j) hi[j] = lo[j] = FMT == WICI_KV_BF16 ? x[0][j] : x[0][j] * s;
+    }
 #pragma unroll
-    for (int r = 0; r < kKvPage; ++r) {
-        const float s = FMT == WICI_KV_BF16 ? 1.f : __shfl_sync(0xffffffffu, scale, r);
-        if (r >= rows) continue;
+    for (int r = 1; r < kKvPage; r += 3) {                    // past the last row: the largest so far, which changes neither
+        float v[3][E];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const float s = FMT == WICI_KV_BF16 ? 1.f : __shfl_sync(0xffffffffu, scale, r + i);
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[i][j] = r + i < rows ? FMT == WICI_KV_BF16 ? x[r + i][j] : x[r + i][j] * s : hi[j];
+        }
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            const float v = FMT == WICI_KV_BF16 ? x[r][j] : x[r][j] * s;
-            hi[j] = fmaxf(hi[j], v);
-            lo[j] = fminf(lo[j], v);
-            most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
+            hi[j] = max_of(max_of(hi[j], v[0][j], v[1][j]), v[2][j], v[2][j]);
+            lo[j] = min_of(min_of(lo[j], v[0][j], v[1][j]), v[2][j], v[2][j]);
         }
     }
+    uint32_t most = 0;                // of the magnitudes' bits: an infinity or NaN is the largest
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        most = max(most, max(__float_as_uint(hi[j]) & 0x7FFFFFFFu, __float_as_uint(lo[j]) & 0x7FFFFFFFu));
     most = __reduce_max_sync(0xffffffffu, most);
     const bool finite = most < kInfBits;
     const float s = finite ? __fmul_rn(__uint_as_float(most), 1.f / 127.f) : __uint_as_float(0x7FC00000u);
     const bool some = finite && s >= 0x1p-126f;
     int8_t code[2][E];
+    const float per = some ? 1.f / s : 0.f;
+    auto whole = [&](float v) {       // the quotient v / s, right to its last bit, to the nearest whole number
+        const float y = v * per;
+        return (int8_t)__float2int_rn(fmaf(fmaf(-y, s, v), per, y));
+    };
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-        code[0][j] = some ? (int8_t)__float2int_rn(__fdiv_rn(hi[j], s)) : (int8_t)0;
-        code[1][j] = some ? (int8_t)__float2int_rn(__fdiv_rn(lo[j], s)) : (int8_t)0;
-    }
+    for (int j = 0; j < E; ++j) code[0][j] = some ? whole(hi[j]) : (int8_t)0, code[1][j] = some ? whole(lo[j]) : (int8_t)0;
     uint8_t *record = a.bounds + page * a.bounds_stride;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -148,9 +171,11 @@ struct SelectArg {
 };
 
 constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectPerSm = 1;
 constexpr int kMaxSelectPages = 1 << 15;   // of a sequence: their scores stand in shared memory
 constexpr int kMaxSelectGroup = 64;        // query heads of a KV head: so do they
 constexpr float kLevels = 1023.f;          // of a query's whole numbers: 128 * 127 * 1023 < 2^24
+constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr uint32_t kForced = 0xFFFFFFFFu;  // in the place of a score: above every one
 constexpr uint32_t kFirst = 0xFF800000u;   // +infinity's
 
@@ -178,7 +203,7 @@ template <int D>
 __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_constant__ SelectArg a) {
     constexpr int STEPS = 2 * D / 16, LOADS = 2 * D / 64;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ uint32_t part[2][2][kSelectWarps];
+    __shared__ uint32_t part[2][kSelectWarps], bins[kBins];
     const int tiles = (a.group + 7) / 8;
     __half *qs = (__half *)smem;                                  // [tile][step][lane][4]: B fragments
     float *most = (float *)(smem + tiles * STEPS * 256);          // [tile * 8]: each query's largest magnitude
@@ -233,9 +258,14 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
         const int32_t *table = a.pages + (int64_t)b * a.max_pages;
         const uint32_t keys_at = smem_u32(keys);
         const int step = kSelectWarps * a.cluster;
-        for (int tile = rank * kSelectWarps + warp; tile * 16 < count; tile += step) {
+        auto page_of = [&](int tile) {
             const int at = tile * 16 + (lane & 15);
-            const int page = at < count ? table[at] : 0;
+            return at < count ? table[at] : 0;
+        };
+        int next_page = page_of(rank * kSelectWarps + warp);
+        for (int tile = rank * kSelectWarps + warp; tile * 16 < count; tile += step) {
+            const int at = tile * 16 + (lane & 15), page = next_page;
+            next_page = page_of(tile + step);
             if (lane < 16 && at < count && (uint32_t)page >= (uint32_t)a.n_pages && a.status) atomicOr(a.status, WICI_BAD_PAGE);
             int row_page[2];
             uint4 raw[2][LOADS];
@@ -314,18 +344,6 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
         }
         return;
     }
-    // over the block: sums of u (two halves of 16 bits) and v
-    int turn = 0;
-    auto sums = [&](uint32_t &u, uint32_t &v) {
-        u = __reduce_add_sync(0xffffffffu, u);
-        v = __reduce_add_sync(0xffffffffu, v);
-        if (lane == 0) part[turn][0][warp] = u, part[turn][1][warp] = v;
-        __syncthreads();
-        u = v = 0;
-#pragma unroll
-        for (int w = 0; w < kSelectWarps; ++w) u += part[turn][0][w], v += part[turn][1][w];
-        turn ^= 1;                                                // a turn's words are read before the next but one barrier
-    };
     uint32_t limit = kForced;
     if (a.first + a.recent < a.keep) {
         // the keys that are not forced: their leading bits in common need no search
@@ -336,25 +354,52 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
         }
         hi = __reduce_max_sync(0xffffffffu, hi);
         lo = __reduce_min_sync(0xffffffffu, lo);
-        if (lane == 0) part[1][0][warp] = hi, part[1][1][warp] = lo;
+        if (lane == 0) part[0][warp] = hi, part[1][warp] = lo;
+        for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kSelectWarps; ++w) hi = max(hi, part[1][0][w]), lo = min(lo, part[1][1][w]);
-        int bit = hi == lo ? 0 : 32 - __clz(hi ^ lo);             // bits that are open
-        bit = (bit + 1) & ~1;
-        limit = bit >= 32 ? 0u : hi >> bit << bit;
-        while (bit > 0) {
-            bit -= 2;
-            const uint32_t one = 1u << bit, x1 = limit | one, x2 = limit | 2 * one, x3 = limit | 3 * one;
-            uint32_t u = 0, v = 0;
+        for (int w = 0; w < kSelectWarps; ++w) hi = max(hi, part[0][w]), lo = min(lo, part[1][w]);
+        int open = hi == lo ? 0 : 32 - __clz(hi ^ lo);            // bits that may differ
+        // the keep-th largest of all is the rank-th largest of those that are not forced; kBinBits of its bits at a time
+        uint32_t above = a.first + a.recent;                      // keys known to be larger
+        limit = open == 32 ? 0u : hi >> open << open;
+        while (open > 0) {
+            const int low = open > kBinBits ? open - kBinBits : 0;
             for (int i = threadIdx.x; i < count; i += kSelectThreads) {
                 const uint32_t k = keys[i];
-                u += (k >= x1 ? 1u : 0u) + (k >= x2 ? 0x10000u : 0u);
-                v += k >= x3 ? 1u : 0u;
+                if (k != kForced && (open == 32 || (k ^ limit) >> open == 0)) atomicAdd(&bins[(k >> low) & (kBins - 1) & ((1u << (open - low)) - 1)], 1u);
             }
-            sums(u, v);
-            const uint32_t keep = (uint32_t)a.keep;
-            limit = v >= keep ? x3 : u >> 16 >= keep ? x2 : (u & 0xFFFF) >= keep ? x1 : limit;
+            __syncthreads();
+            // each thread has kEach bins, the highest first: the one where the count passes keep has the key
+            constexpr int kEach = kBins / kSelectThreads;
+            const int top = kBins - 1 - kEach * threadIdx.x;
+            uint32_t mine = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) mine += bins[top - i];
+            uint32_t upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            if (lane == 31) part[0][warp] = upto;
+            __syncthreads();
+            for (int w = 0; w < warp; ++w) upto += part[0][w];
+            uint32_t before = above + upto - mine;
+            if (before < (uint32_t)a.keep && before + mine >= (uint32_t)a.keep) {
+                int bin = top;
+                while (before + bins[bin] < (uint32_t)a.keep) before += bins[bin--];
+                part[1][0] = limit | (uint32_t)bin << low;
+                part[1][1] = before;
+            }
+            __syncthreads();
+            limit = part[1][0];
+            above = part[1][1];
+            open = low;
+            if (open > 0) {
+                for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
+                __syncthreads();
+            }
         }
     }
     // a warp's share of the pages, in order: those above the limit, and as many of those at it as there is room for
@@ -363,16 +408,16 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
     for (int i = from + lane; i < to; i += 32) over += keys[i] > limit, at += keys[i] == limit;
     over = __reduce_add_sync(0xffffffffu, over);
     at = __reduce_add_sync(0xffffffffu, at);
-    __syncthreads();                                              // the last turn's words have been read
-    if (lane == 0) part[0][0][warp] = over, part[0][1][warp] = at;
+    __syncthreads();                                              // what was left in `part` has been read
+    if (lane == 0) part[0][warp] = over, part[1][warp] = at;
     __syncthreads();
     uint32_t all_over = 0;
 #pragma unroll
-    for (int w = 0; w < kSelectWarps; ++w) all_over += part[0][0][w];
+    for (int w = 0; w < kSelectWarps; ++w) all_over += part[0][w];
     uint32_t room = a.keep > (int)all_over ? a.keep - all_over : 0, place = 0;
     for (int w = 0; w < warp; ++w) {
-        const uint32_t taken = min(room, part[0][1][w]);
-        place += part[0][0][w] + taken;
+        const uint32_t taken = min(room, part[1][w]);
+        place += part[0][w] + taken;
         room -= taken;
     }
     const uint32_t below = (1u << lane) - 1;
@@ -514,7 +559,11 @@ int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_
     a.first = shape->first;
     a.recent = shape->recent;
     a.q_dtype = q->dtype;
+    // Blocks of a cluster: as many as make kSelectPerSm blocks an SM of the launch, of 16 pages a warp at least
     a.cluster = 1;
+    while (a.cluster < 8 && (int64_t)a.cluster * a.kv_heads * shape->batch < kSelectPerSm * dev.sms &&
+           a.cluster * kSelectWarps * 16 < shape->max_pages)
+        a.cluster *= 2;
     const dim3 grid((unsigned)(a.cluster * a.kv_heads), (unsigned)shape->batch);
     const size_t smem = select_smem(cache->head_dim, a.group, a.max_pages);
     cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -168,15 +168,26 @@ __device__ __forceinline__ uint32_t block_scale(float most, float scale, float p
 __device__ __forceinline__ float e4m3_value(uint32_t code) {
     return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
 }
+// about 1 / x, of a normal x up to 2^126: within 2^-22 of it
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 8 values times r as the nearest codes, the first in the lowest bits
+__device__ __forceinline__ uint32_t encode_e2m1(const float *x, float r) {
+    uint32_t w;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(w)
+        : "f"(x[0] * r), "f"(x[1] * r), "f"(x[2] * r), "f"(x[3] * r), "f"(x[4] * r), "f"(x[5] * r), "f"(x[6] * r), "f"(x[7] * r));
+    return w;
+}
 // the codes of 8 values under the block scale b (its value) and the head's scale, the first in the lowest bits
 __device__ __forceinline__ uint32_t quantise_e2m1(const float *x, float b, float scale) {
-    const float r = b > 0.f ? 1.f / (b * scale) : 0.f, r_lo = r * kNearLo, r_hi = r * kNearHi;
-    uint32_t lo = 0, hi = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        lo |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(x[2 * j] * r_lo, x[2 * j + 1] * r_lo), __NV_E2M1, cudaRoundNearest) << 8 * j;
-        hi |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(x[2 * j] * r_hi, x[2 * j + 1] * r_hi), __NV_E2M1, cudaRoundNearest) << 8 * j;
-    }
+    const float r = b > 0.f ? reciprocal(b * scale) : 0.f;
+    uint32_t lo = encode_e2m1(x, r * kNearLo);
+    const uint32_t hi = encode_e2m1(x, r * kNearHi);
     if (lo != hi) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {

@@ -85,7 +85,7 @@ struct AttnShape {
     static constexpr int kSlot = kPages * kBlock;
     // Two blocks on an SM, 8 warps with 250 registers each: three of 168 spill (131 us in place of then 116).
     static constexpr int kBlocks = 2;
-    static constexpr int kKSlots = FMT != WICI_KV_E2M1 ? 3 : D == 128 && !STACK ? 4 : 5, kVSlots = kKSlots - 1;   // of the ring: about 100 KB on their way per SM
+    static constexpr int kKSlots = 3, kVSlots = kKSlots - 1;   // of the ring: about 100 KB on their way per SM
     static constexpr int kRing = (kKSlots + kVSlots) * kSlot;
     static constexpr int kPartRow = D + 4;                         // floats: neighbouring rows in other banks
     static constexpr int kPart = kRows * (kPartRow + 2) * 4;       // a part of a segment: O, then m and l of each row
@@ -120,20 +120,6 @@ __device__ __forceinline__ float lds32(uint32_t a) {
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
     return v;
 }
-__device__ __forceinline__ uint32_t lds8(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-// an e4m3 code twice as fp16, and a product of fp16 pairs
-__device__ __forceinline__ uint32_t e4m3_pair(uint32_t code) {
-    const __half2 v = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(code | code << 8), __NV_E4M3));
-    return *(const uint32_t *)&v;
-}
-__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
-    const __half2 v = __hmul2(*(const __half2 *)&a, *(const __half2 *)&b);
-    return *(const uint32_t *)&v;
-}
 template <bool BF16>
 __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
     if (BF16)
@@ -148,6 +134,39 @@ __device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b
             "{%0, %1, %2, %3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// a product in fp16 added to a sum, or to nothing
+__device__ __forceinline__ void mma_f16(float *c, bool first, const uint32_t *a, const uint32_t *b) {
+    if (first)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]), "f"(0.f));
+    else
+        mma16816<false>(c, a, b[0], b[1]);
+}
+// an 8 x 8 matrix of 16-bit values, two of a row in each lane, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+// an e4m3 code as fp16 in the lower half, products of fp16 pairs: with a pair, with a lower half
+__device__ __forceinline__ uint32_t e4m3_half(uint32_t code) {
+    const __half2 v = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)code, __NV_E4M3));
+    return *(const uint32_t *)&v;
+}
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+    const __half2 v = __hmul2(*(const __half2 *)&a, *(const __half2 *)&b);
+    return *(const uint32_t *)&v;
+}
+__device__ __forceinline__ uint32_t times_low(uint32_t a, uint32_t b) {
+    const __half2 v = __hmul2(*(const __half2 *)&a, __low2half2(*(const __half2 *)&b));
+    return *(const uint32_t *)&v;
 }
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -215,17 +234,17 @@ __device__ __forceinline__ void split_row(const float *x, int r, uint32_t (*a)[4
 // Where 16-byte chunk c of key row r stands in a ring slot.  The chunks of a row are permuted so
 // that the 8 lanes of a shared-memory phase, which take rows i and i + 4 (K), or rows 0..3 and
 // neighbouring chunks (V), meet 8 different bank groups.  Rows of 64 bytes share a line of 128 in pairs.
-// Of rows of e2m1 a lane takes 8 bytes at a time (K: a row's chunks in order, V: those of rows 0..3): halves of a warp,
-// whose rows are {0, 4, 1, 5}, {2, 6, 3, 7} or 0..3, meet 16 different pairs of banks.
+// Of rows of e2m1 a lane takes 8 bytes at a time (of V with head_dim 64: 4): the half of a warp that a phase serves, with
+// 4 neighbouring rows (K) or every other of 8 (V), meets all 32 banks.
 template <int ROW, bool E2M1>
 __device__ __forceinline__ int chunk_at(int r, int c) {
     if (E2M1 && ROW == 64) {
         const int line = r >> 1;
-        return line * 128 + ((((r & 1) << 2 | c) ^ (((line ^ line >> 1) & 1) << 1)) << 4);
+        return line * 128 + ((((r & 1) << 2 | c) ^ ((line & 3) << 1)) << 4);
     }
     if (ROW == 32) {
         const int line = r >> 2;
-        return line * 128 + ((((r & 3) << 1 | c) ^ ((line & 1) << 2)) << 4);
+        return line * 128 + ((((r & 3) << 1 | c) ^ ((line & 1) << 1)) << 4);
     }
     if (ROW == 64) {
         const int line = r >> 1;
@@ -320,9 +339,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     constexpr bool E2M1 = FMT == WICI_KV_E2M1;
     constexpr int ROW = kv_row_bytes(FMT, D);             // bytes of a key row
     constexpr int CHUNKS = ROW / 16;
-    constexpr int GROUPS = BF16 ? CHUNKS / 4 : D / 64;    // steps' elements that a lane loads at once: 8 of bf16, 16 codes
-    constexpr int EACH_AT = kKvPage * ROW, SCALES_AT = kv_scales_at(FMT, D);   // e2m1's block scales, the tokens' scales
-    constexpr int TAIL = (S::kBlock - EACH_AT) / 16;      // 16-byte words of a block behind its rows
+    constexpr int TAIL = (S::kBlock - kKvPage * ROW) / 16;   // 16-byte words of a block behind its rows: scales
     constexpr int P = S::kPages, UNIT = P * kKvPage;      // keys of a unit
     constexpr int HT = S::kRows;
     constexpr int R = STACK ? 1 : 2;                      // queries whose rows a lane holds
@@ -525,7 +542,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
                 for (int i = 0; i < N; ++i)
                     cp_async16(dst + p * S::kBlock + (chunk_at<ROW, E2M1>(i * ROWS, 0) ^ lane_dst), from + i * 512, 16, policy);
-                if (lane < TAIL) cp_async16(dst + p * S::kBlock + EACH_AT + lane * 16, from + EACH_AT, 16, policy);
+                if (lane < TAIL) cp_async16(dst + p * S::kBlock + kKvPage * ROW + lane * 16, from + kKvPage * ROW, 16, policy);
             }
         } else {
 #pragma unroll
@@ -538,8 +555,22 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                                src[p] && r >= first && r < end ? 16 : 0, policy);
                 }
                 if (lane < TAIL)
-                    cp_async16(dst + p * S::kBlock + EACH_AT + lane * 16, src[p] ? from + EACH_AT : from, src[p] ? 16 : 0, policy);
+                    cp_async16(dst + p * S::kBlock + kKvPage * ROW + lane * 16, src[p] ? from + kKvPage * ROW : from,
+                               src[p] ? 16 : 0, policy);
             }
+        }
+    };
+    // e2m1: a unit's K or V as it is; of rows without a key nothing is used (their codes are finite numbers whatever they are,
+    // their scales are left out).  A page that is not there gives zeros.
+    const uint32_t tail_dst = kKvPage * ROW + lane * 16;
+    auto copy_whole = [&](uint32_t dst, const uint8_t *const *src, int64_t off) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const uint8_t *from = (src[p] ? src[p] + off : a.cache.data) + lane * 16;
+            const int bytes = src[p] ? 16 : 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) cp_async16(dst + lane_dst + (p * S::kBlock + i * 512), from + i * 512, bytes, policy);
+            if (lane < TAIL) cp_async16(dst + tail_dst + p * S::kBlock, from + kKvPage * ROW, bytes, policy);
         }
     };
     // group j: K of unit j and V of the one before it (none past the last unit: the groups still count)
@@ -548,7 +579,10 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             cur = next;
             next = describe(issued + 32 + lane);
         }
-        if (last_end) copy_unit(v_to, last_src, lane_v, last_first, last_end);
+        if (last_end) {
+            if constexpr (E2M1) copy_whole(v_to, last_src, lane_v);
+            else copy_unit(v_to, last_src, lane_v, last_first, last_end);
+        }
         if (issued) v_to = v_to == ring + (KS + VS - 1) * S::kSlot ? ring + KS * S::kSlot : v_to + S::kSlot;
         last_end = 0;
         if (issued < mine) {
@@ -568,7 +602,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 if (lane == 0 && a.status) atomicOr(a.status, WICI_BAD_PAGE);
                 first = -1;                                  // not the way of whole units
             }
-            copy_unit(k_to, last_src, 0, first, end);
+            if constexpr (E2M1) copy_whole(k_to, last_src, 0);
+            else copy_unit(k_to, last_src, 0, first, end);
             last_first = first;
             last_end = end;
         }
@@ -620,17 +655,34 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
         const int row0 = seg.head % a.tiles * HT, rows = min(HT, a.group - row0);   // first query of the tile in the group
         const int head0 = seg.head / a.tiles * a.group + row0, seg_b = seg.b;
 
-        // ---- Q fragments ----
-        uint32_t qf[QPASS][STEPS][4];
-        float cq[R];                      // products to base-2 logits
+        // what ends in the block's first run is the block's whole part of its segment
+        const bool entered = seg.start < r0, left = seg.end > r1, to_piece = !left && r0 == u0;
+        float *part_at = to_piece ? a.pieces + (int64_t)blockIdx.x * 2 * attn_piece_floats(D) : part_of(warp, left);
+        const int part_row = to_piece ? D : S::kPartRow;
+        float2 *part_ml = (float2 *)(part_at + (to_piece ? kAttnPieceRows * D : HT * S::kPartRow));
+        auto ring_is_free = [&]() {                           // no unit follows
+            cp_wait<0>();
+            if (lane == 0) sh.leaving[warp] = seg;
+        };
+
+        if constexpr (E2M1) {
+            // ==== keys are the rows of S^T = K Q^T, elements of the head those of O^T = V^T P^T, queries the columns of
+            // both: a lane has keys g and g + 8 of a page for queries 2 t and 2 t + 1 of each tile of 8 (N8 of them).  Two
+            // terms of q or p are two products into the same sums, so O takes half of the registers that rows for each term
+            // would, and the codes, whose conversion costs most here, are converted once for both ====
+            constexpr int N8 = R, C = 2 * N8, TILES = D / 16;
+            constexpr int J = 2 * P;                          // keys of a query that a lane has
+            constexpr int EACH_AT = kKvPage * ROW, SCALES_AT = kv_scales_at(FMT, D);
+
+            // ---- Q fragments: query g of a tile, 4 elements a step ----
+            uint32_t qf[N8][TQ][STEPS][2];
+            float cq[C];                                      // products to base-2 logits, of queries 2 t, 2 t + 1
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            cq[r] = a.scale * 1.44269504088896340736f;
-            float x[STEPS][4];
-#pragma unroll
-            for (int i = 0; i < STEPS / 2; ++i) unpack_q8<QW>(a.q_dtype, qx[r][i], x[2 * i]);
-            if (!BF16) {
+            for (int n = 0; n < N8; ++n) {
+                float x[STEPS][4], of_g = a.scale * 1.44269504088896340736f;
                 uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < STEPS / 2; ++i) unpack_q8<QW>(a.q_dtype, qx[n][i], x[2 * i]);
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s)
 #pragma unroll
@@ -641,195 +693,415 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 int e = (int)(top >> 23) - 127 - 13;
                 e = top >= kInfBits || top == 0 ? 0 : max(-126, min(126, e));
                 const float down = __int_as_float((127 - e) << 23);
-                cq[r] *= __int_as_float((127 + e) << 23);
+                of_g *= __int_as_float((127 + e) << 23);
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s)
+                for (int s = 0; s < STEPS; ++s) {
+                    uint32_t w[2][TQ];
+                    split<false, false, false, TQ>(x[s][0] * down, x[s][1] * down, w[0], 1.f);
+                    split<false, false, false, TQ>(x[s][2] * down, x[s][3] * down, w[1], 1.f);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[s][j] *= down;
+                    for (int k = 0; k < TQ; ++k) qf[n][k][s][0] = w[0][k], qf[n][k][s][1] = w[1][k];
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) cq[2 * n + j] = __shfl_sync(0xffffffffu, of_g, 4 * (2 * t + j));
             }
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) split_row<BF16, false, STACK, TQ, STEPS>(x[s], r, &qf[0][s]);
-        }
 
-        float m[R], l[R], o[NT][4];
+            float m[C], l[C], o[TILES][N8][4], heaviest[C], per[C];   // the largest weight so far, what weights are multiplied by
 #pragma unroll
-        for (int r = 0; r < R; ++r) m[r] = -INFINITY, l[r] = 0.f;
+            for (int r = 0; r < C; ++r) m[r] = -INFINITY, l[r] = 0.f, heaviest[r] = 0.f, per[r] = kPRoom * 0x1p118f;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int x = 0; x < TILES; ++x)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[n][j] = 0.f;
-        float heaviest[R], per[R];                    // 8-bit: the largest weight so far, what weights are multiplied by
+                for (int n = 0; n < N8; ++n)
 #pragma unroll
-        for (int r = 0; r < R; ++r) heaviest[r] = 0.f, per[r] = kPRoom * 0x1p118f;
-        // O so far is multiplied by f for `per` to follow `heaviest`
-        auto follow = [&](int r, float f) {
-            const float was = __uint_as_float(0x7F000000u - __float_as_uint(per[r])) * f;      // f / per
-            const uint32_t e = min(max((__float_as_uint(heaviest[r]) + 0x7FFFFFu) & 0x7F800000u, 0x04800000u), 0x7E800000u);
-            per[r] = kPRoom * __uint_as_float(0x7F000000u - e);      // heaviest to its power of two, in [2^-118, 2^126]
-            return was * per[r];
-        };
+                    for (int j = 0; j < 4; ++j) o[x][n][j] = 0.f;
+            // O so far is multiplied by f for `per` to follow `heaviest`
+            auto follow = [&](int r, float f) {
+                const float was = __uint_as_float(0x7F000000u - __float_as_uint(per[r])) * f;      // f / per
+                const uint32_t e = min(max((__float_as_uint(heaviest[r]) + 0x7FFFFFu) & 0x7F800000u, 0x04800000u), 0x7E800000u);
+                per[r] = kPRoom * __uint_as_float(0x7F000000u - e);      // heaviest to its power of two, in [2^-118, 2^126]
+                return was * per[r];
+            };
+            auto rescale = [&](const float *f) {
+#pragma unroll
+                for (int x = 0; x < TILES; ++x)
+#pragma unroll
+                    for (int n = 0; n < N8; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[x][n][j] *= f[2 * n + (j & 1)];
+            };
+            auto largest = [&](float v) {                     // of the 8 lanes that share queries
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+                return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+            };
+            auto key_at = [&](int j) { return (j >> 1) * kKvPage + (j & 1) * 8 + g; };
 
-        // ---- scores of one unit (unscaled) ----
-        float c[2 * P][SETS][4];                             // [8 keys][sets of steps]
-        auto scores = [&](uint32_t ks) {
+            // where a lane's parts of a block are: of K the chunk t of key g (chunk 4 + t is 32 bytes across, key g + 8 as far
+            // on as rows are), of V the chunk g of key 2 t (key 2 t + 1 is ODD bytes across), and their block scales
+            constexpr uint32_t ODD = D == 128 ? 64 : 32, EIGHT = 8 * ROW;
+            const uint32_t k_lane = chunk_at<ROW, E2M1>(g, t >> 1) + (t & 1) * 8, each_k = EACH_AT + g * (D / 16) + t;
+            const uint32_t v_lane = D == 128 ? chunk_at<ROW, E2M1>(2 * t, g >> 1) + (g & 1) * 8 : chunk_at<ROW, E2M1>(2 * t, g >> 2) + (g & 3) * 4;
+            const uint32_t each_v = EACH_AT + 2 * t * (D / 16) + (D == 128 ? g : g >> 1);
+
+            // ---- scores of one unit (unscaled) ----
+            float c[P][N8][4];
+            auto scores = [&](uint32_t slot) {
 #pragma unroll
-            for (int n = 0; n < 2 * P; ++n)
+                for (int i = 0; i < D / 64; ++i) {
 #pragma unroll
-                for (int e = 0; e < SETS; ++e)
+                    for (int pg = 0; pg < P; ++pg) {
+                        uint32_t h[2][8], b[2];               // 16 elements of keys g, g + 8: 8 bytes and a scale
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) c[n][e][j] = 0.f;
-#pragma unroll
-            for (int i = 0; i < GROUPS; ++i) {
-#pragma unroll
-                for (int n = 0; n < 2 * P; ++n) {
-                    const int r = (g >> 1) + (g & 1) * 4 + 8 * (n & 1);   // the key of column g
-                    if (E2M1) {
-                        const int c16 = 4 * i + t;                       // 16 elements of the row: 8 bytes and a scale
-                        const uint32_t kp = ks + n / 2 * S::kBlock;
-                        const uint2 w = lds64(kp + chunk_at<ROW, E2M1>(r, c16 >> 1) + (c16 & 1) * 8);
-                        const uint32_t b2 = e4m3_pair(lds8(kp + EACH_AT + r * (D / 16) + c16));
-                        uint32_t h[8];
-                        decode_e2m1(w.x, h);
-                        decode_e2m1(w.y, h + 4);
-#pragma unroll
-                        for (int s = 0; s < 4; ++s)
-#pragma unroll
-                            for (int k = 0; k < QPASS; ++k)
-                                mma16816<false>(c[n][0], qf[k][4 * i + s], times(h[2 * s], b2), times(h[2 * s + 1], b2));
-                        continue;
-                    }
-                    const uint4 w = lds128(ks + n / 2 * S::kBlock + chunk_at<ROW, E2M1>(r, 4 * i + t));
-                    if (BF16) {
-#pragma unroll
-                        for (int k = 0; k < QPASS; ++k) {
-                            mma16816<true>(c[n][0], qf[k][2 * i], w.x, w.y);
-                            mma16816<true>(c[n][SETS - 1], qf[k][2 * i + 1], w.z, w.w);
+                        for (int k = 0; k < 2; ++k) {
+                            const uint2 w = lds64(slot + (i ? k_lane ^ 32 : k_lane) + pg * S::kBlock + k * EIGHT);
+                            b[k] = e4m3_half(lds8(slot + each_k + pg * S::kBlock + k * (D / 2) + 4 * i));
+                            decode_e2m1(w.x, h[k]);
+                            decode_e2m1(w.y, h[k] + 4);
                         }
-                    } else {
-                        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                         for (int s = 0; s < 4; ++s) {
-                            uint32_t b0, b1;
-                            decode4<FMT>(word[s], b0, b1);
+                            const uint32_t f[4] = {times_low(h[0][2 * s], b[0]), times_low(h[1][2 * s], b[1]),
+                                                   times_low(h[0][2 * s + 1], b[0]), times_low(h[1][2 * s + 1], b[1])};
 #pragma unroll
-                            for (int k = 0; k < QPASS; ++k) mma16816<false>(c[n][0], qf[k][4 * i + s], b0, b1);
+                            for (int n = 0; n < N8; ++n)
+#pragma unroll
+                                for (int k = 0; k < TQ; ++k) mma_f16(c[pg][n], i == 0 && s == 0 && k == 0, f, qf[n][k][4 * i + s]);
                         }
                     }
                 }
-            }
-        };
+            };
 
-        // ---- units of this segment: the scores of the next one run beside the softmax of this one (past the last
-        // one they are not used, whatever the slot holds) ----
-        int key0 = (keys.lo / kKvPage + (int)(r0 + done - seg.start) * P) * kKvPage;   // first key of the unit
-        cp_wait<KS - 1>();                                   // group `done` brings its K
-        __syncwarp();
-        scores(ks);
-        for (; done < stop; ++done, key0 += UNIT) {
-            // group done + 1: K of the next unit and V of this one
-            cp_wait<KS - 2>();
+            // ---- units of this segment: the scores of the next one run beside the softmax of this one (past the last
+            // one they are not used, whatever the slot holds) ----
+            int key0 = (keys.lo / kKvPage + (int)(r0 + done - seg.start) * P) * kKvPage;   // first key of the unit
+            cp_wait<KS - 1>();                                // group `done` brings its K
             __syncwarp();
-            const uint32_t ks_next = ks == ring + (KS - 1) * S::kSlot ? ring : ks + S::kSlot;
-            // x[r][j]: query g + 8 r, key t + 4 j of the unit
-            constexpr int J = 4 * P;
-            float x[R][J];
-            const bool part = key0 < keys.lo || key0 > keys.n - UNIT;   // not every key of the unit is the sequence's
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int n = j >> 1, col = j & 1;
-                const float ksc = BF16 ? 1.f : lds32(ks + j / 4 * S::kBlock + SCALES_AT + (t + 4 * (j & 3)) * 4);
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    float dot = c[n][0][col + 2 * r];
-                    if (SETS == 2) dot += c[n][SETS - 1][col + 2 * r];
-                    if (STACK && TQ > 1) {
-                        dot += c[n][0][col + 2];
-                        if (SETS == 2) dot += c[n][SETS - 1][col + 2];
-                    }
-                    x[r][j] = dot * (BF16 ? cq[r] : ksc * cq[r]);
-                }
-            }
-            if (part) {
+            scores(ks);
+            for (; done < stop; ++done, key0 += UNIT) {
+                // group done + 1: K of the next unit and V of this one
+                cp_wait<KS - 2>();
+                __syncwarp();
+                const uint32_t ks_next = ks == ring + (KS - 1) * S::kSlot ? ring : ks + S::kSlot;
+                float x[C][J];                                // queries 2 t + r % 2 of tile r / 2, keys key_at(j)
+                const bool part = key0 < keys.lo || key0 > keys.n - UNIT;   // not every key of the unit is the sequence's
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    const int key = key0 + t + 4 * j;
+                    const float ksc = lds32(ks + (j >> 1) * S::kBlock + SCALES_AT + (j & 1) * 32 + 4 * g);
 #pragma unroll
-                    for (int r = 0; r < R; ++r) x[r][j] = key >= keys.lo && key < keys.n ? x[r][j] : -INFINITY;
+                    for (int r = 0; r < C; ++r) x[r][j] = c[j >> 1][r >> 1][2 * (j & 1) + (r & 1)] * (ksc * cq[r]);
                 }
-            }
-            float up[R];
-            bool grew = false;
+                if (part) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float top = x[r][0];
+                    for (int j = 0; j < J; ++j) {
+                        const int key = key0 + key_at(j);
 #pragma unroll
-                for (int j = 1; j < J; ++j) top = fmaxf(top, x[r][j]);
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                up[r] = fmaxf(m[r], top);
-                grew |= up[r] > m[r] + kLag;
-            }
-            if (__any_sync(0xffffffffu, grew)) {
-                float f[R];
+                        for (int r = 0; r < C; ++r) x[r][j] = key >= keys.lo && key < keys.n ? x[r][j] : -INFINITY;
+                    }
+                }
+                float up[C];
+                bool grew = false;
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    f[r] = m[r] == -INFINITY ? 0.f : ex2(m[r] - up[r]);   // nothing yet: zeros
-                    l[r] *= f[r];
-                    m[r] = up[r];
-                    if (!BF16) {
+                for (int r = 0; r < C; ++r) {
+                    float top = x[r][0];
+#pragma unroll
+                    for (int j = 1; j < J; ++j) top = fmaxf(top, x[r][j]);
+                    up[r] = fmaxf(m[r], largest(top));
+                    grew |= up[r] > m[r] + kLag;
+                }
+                if (__any_sync(0xffffffffu, grew)) {
+                    float f[C];
+#pragma unroll
+                    for (int r = 0; r < C; ++r) {
+                        f[r] = m[r] == -INFINITY ? 0.f : ex2(m[r] - up[r]);   // nothing yet: zeros
+                        l[r] *= f[r];
+                        m[r] = up[r];
                         heaviest[r] *= f[r];
                         f[r] = follow(r, f[r]);
                     }
+                    rescale(f);
                 }
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    o[n][0] *= f[0];
-                    o[n][1] *= f[0];
-                    o[n][2] *= f[R - 1];
-                    o[n][3] *= f[R - 1];
-                }
-            }
-            scores(ks_next);                                 // c has been read
-            float ref[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) ref[r] = m[r] == -INFINITY ? 0.f : m[r];
-            if (!BF16) {
+                scores(ks_next);                              // c has been read
                 // the weights in the place of the scores
-                float top[R];
                 bool heavy = false;
+                float ref[C], top[C];
+#pragma unroll
+                for (int r = 0; r < C; ++r) ref[r] = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    const float vscale = lds32(vs + j / 4 * S::kBlock + SCALES_AT + (t + 4 * (j & 3)) * 4);
+                    const float vscale = lds32(vs + (j >> 1) * S::kBlock + SCALES_AT + (j & 1) * 32 + 4 * g);
 #pragma unroll
-                    for (int r = 0; r < R; ++r) {
+                    for (int r = 0; r < C; ++r) {
                         const float p = ex2(x[r][j] - ref[r]);
                         l[r] += p;
                         x[r][j] = p * vscale;
                     }
                 }
-                if (part) {                                  // scales of other keys may be anything
+                if (part) {                                   // scales of other keys may be anything
 #pragma unroll
                     for (int j = 0; j < J; ++j) {
-                        const int key = key0 + t + 4 * j;
+                        const int key = key0 + key_at(j);
 #pragma unroll
-                        for (int r = 0; r < R; ++r) x[r][j] = key >= keys.lo && key < keys.n ? x[r][j] : 0.f;
+                        for (int r = 0; r < C; ++r) x[r][j] = key >= keys.lo && key < keys.n ? x[r][j] : 0.f;
                     }
                 }
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
+                for (int r = 0; r < C; ++r) {
                     top[r] = x[r][0];
 #pragma unroll
                     for (int j = 1; j < J; ++j) top[r] = fmaxf(top[r], x[r][j]);
                     heavy |= top[r] * per[r] > kPMost;
                 }
                 if (__any_sync(0xffffffffu, heavy)) {
+                    float f[C];
+#pragma unroll
+                    for (int r = 0; r < C; ++r) {
+                        heaviest[r] = largest(fmaxf(heaviest[r], top[r]));
+                        f[r] = follow(r, 1.f);
+                    }
+                    rescale(f);
+                }
+#pragma unroll
+                for (int pg = 0; pg < P; ++pg) {
+                    uint32_t pf[N8][2][2];                    // [tile][term][keys 0..7, 8..15]
+#pragma unroll
+                    for (int n = 0; n < N8; ++n)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            uint32_t w[2];
+                            split<false, false, true, 2>(x[2 * n][2 * pg + k] * per[2 * n], x[2 * n + 1][2 * pg + k] * per[2 * n + 1], w, 1.f);
+                            pf[n][0][k] = transposed(w[0]);
+                            pf[n][1][k] = transposed(w[1]);
+                        }
+                    // V: keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9; element 2 x of the lane's PER is row g of tile x, the next row g + 8
+                    constexpr int WORDS = D / 64;             // 4-byte words of a row that a lane takes
+                    const uint32_t vp = vs + pg * S::kBlock;
+                    uint32_t w[4][WORDS], b[4], b2[2];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t at = vp + (i & 1 ? v_lane ^ ODD : v_lane) + (i >> 1) * EIGHT;
+                        if (D == 128) {
+                            const uint2 q = lds64(at);
+                            w[i][0] = q.x, w[i][WORDS - 1] = q.y;
+                        } else {
+                            w[i][0] = __float_as_uint(lds32(at));
+                        }
+                        b[i] = lds8(vp + each_v + ((i & 1) + (i >> 1) * 8) * (D / 16));
+                    }
+                    if (part) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {         // of another key: may be NaN
+                            const int key = key0 + pg * kKvPage + 2 * t + (i & 1) + (i >> 1) * 8;
+                            b[i] = key >= keys.lo && key < keys.n ? b[i] : 0u;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const __half2 v = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(b[2 * i] | b[2 * i + 1] << 8), __NV_E4M3));
+                        b2[i] = *(const uint32_t *)&v;
+                    }
+#pragma unroll
+                    for (int x8 = 0; x8 < WORDS; ++x8) {
+                        // halves of bytes of two rows interleaved first: elements 2 e in even[..][e], 2 e + 1 in odd[..][e]
+                        uint32_t even[2][4], odd[2][4];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t u = w[2 * i][x8], v = w[2 * i + 1][x8];
+                            decode_e2m1((u & 0x0F0F0F0Fu) | (v << 4 & 0xF0F0F0F0u), even[i]);
+                            decode_e2m1((u >> 4 & 0x0F0F0F0Fu) | (v & 0xF0F0F0F0u), odd[i]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t f[4] = {times(even[0][e], b2[0]), times(odd[0][e], b2[0]), times(even[1][e], b2[1]),
+                                                   times(odd[1][e], b2[1])};
+#pragma unroll
+                            for (int n = 0; n < N8; ++n)
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) mma16816<false>(o[4 * x8 + e][n], f, pf[n][k][0], pf[n][k][1]);
+                        }
+                    }
+                }
+                if (bad_units >> (done & 31) & 1) {
+                    bad_units &= ~(1u << (done & 31));
+#pragma unroll
+                    for (int r = 0; r < C; ++r) l[r] = __uint_as_float(0x7FC00000u);
+                }
+                __syncwarp();                                 // every lane has read the slots
+                issue();
+                ks = ks_next;
+                vs = vs == ring + (KS + VS - 1) * S::kSlot ? ring + KS * S::kSlot : vs + S::kSlot;
+            }
+
+            // ---- the segment's state, or this run's part of it: of queries 2 t, 2 t + 1 elements PER g .. PER g + PER - 1 ----
+            if (left) ring_is_free();
+            __syncwarp();
+#pragma unroll
+            for (int r = 0; r < C; ++r) {
+#pragma unroll
+                for (int s = 4; s < 32; s <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], s);
+                const int row = 8 * (r >> 1) + 2 * t + (r & 1);
+                const bool alone = !entered && !left;
+                const float f = alone ? 1.f / per[r] / l[r] : 1.f / per[r];
+                if (row >= rows) continue;
+#pragma unroll
+                for (int i = 0; i < PER; i += 4) {
+                    float v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = o[(i + j) / 2][r >> 1][2 * (j & 1) + (r & 1)] * f;
+                    if (alone) store_out4(a, seg_b, head0 + row, PER * g + i, v);
+                    else *(float4 *)(part_at + row * part_row + PER * g + i) = make_float4(v[0], v[1], v[2], v[3]);
+                }
+                if (g == 0) {
+                    if (!alone) part_ml[row] = make_float2(m[r], l[r]);
+                    else if (a.lse) a.lse[(int64_t)seg_b * a.q_heads + head0 + row] = (m[r] + log2f(l[r])) * 0.693147180559945309417f;
+                }
+            }
+        } else {
+            // ---- Q fragments ----
+            uint32_t qf[QPASS][STEPS][4];
+            float cq[R];                      // products to base-2 logits
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                cq[r] = a.scale * 1.44269504088896340736f;
+                float x[STEPS][4];
+#pragma unroll
+                for (int i = 0; i < STEPS / 2; ++i) unpack_q8<QW>(a.q_dtype, qx[r][i], x[2 * i]);
+                if (!BF16) {
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(x[s][j]) & 0x7FFFFFFFu);
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    // 2^(13 - exponent): the largest magnitude to [2^13, 2^14)
+                    int e = (int)(top >> 23) - 127 - 13;
+                    e = top >= kInfBits || top == 0 ? 0 : max(-126, min(126, e));
+                    const float down = __int_as_float((127 - e) << 23);
+                    cq[r] *= __int_as_float((127 + e) << 23);
+#pragma unroll
+                    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[s][j] *= down;
+                }
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) split_row<BF16, false, STACK, TQ, STEPS>(x[s], r, &qf[0][s]);
+            }
+
+            float m[R], l[R], o[NT][4];
+#pragma unroll
+            for (int r = 0; r < R; ++r) m[r] = -INFINITY, l[r] = 0.f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[n][j] = 0.f;
+            float heaviest[R], per[R];                    // 8-bit: the largest weight so far, what weights are multiplied by
+#pragma unroll
+            for (int r = 0; r < R; ++r) heaviest[r] = 0.f, per[r] = kPRoom * 0x1p118f;
+            // O so far is multiplied by f for `per` to follow `heaviest`
+            auto follow = [&](int r, float f) {
+                const float was = __uint_as_float(0x7F000000u - __float_as_uint(per[r])) * f;      // f / per
+                const uint32_t e = min(max((__float_as_uint(heaviest[r]) + 0x7FFFFFu) & 0x7F800000u, 0x04800000u), 0x7E800000u);
+                per[r] = kPRoom * __uint_as_float(0x7F000000u - e);      // heaviest to its power of two, in [2^-118, 2^126]
+                return was * per[r];
+            };
+
+            // ---- scores of one unit (unscaled) ----
+            float c[2 * P][SETS][4];                             // [8 keys][sets of steps]
+            auto scores = [&](uint32_t ks) {
+#pragma unroll
+                for (int n = 0; n < 2 * P; ++n)
+#pragma unroll
+                    for (int e = 0; e < SETS; ++e)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) c[n][e][j] = 0.f;
+#pragma unroll
+                for (int i = 0; i < CHUNKS / 4; ++i) {
+#pragma unroll
+                    for (int n = 0; n < 2 * P; ++n) {
+                        const int r = (g >> 1) + (g & 1) * 4 + 8 * (n & 1);   // the key of column g
+                        const uint4 w = lds128(ks + n / 2 * S::kBlock + chunk_at<ROW, E2M1>(r, 4 * i + t));
+                        if (BF16) {
+#pragma unroll
+                            for (int k = 0; k < QPASS; ++k) {
+                                mma16816<true>(c[n][0], qf[k][2 * i], w.x, w.y);
+                                mma16816<true>(c[n][SETS - 1], qf[k][2 * i + 1], w.z, w.w);
+                            }
+                        } else {
+                            const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                            for (int s = 0; s < 4; ++s) {
+                                uint32_t b0, b1;
+                                decode4<FMT>(word[s], b0, b1);
+#pragma unroll
+                                for (int k = 0; k < QPASS; ++k) mma16816<false>(c[n][0], qf[k][4 * i + s], b0, b1);
+                            }
+                        }
+                    }
+                }
+            };
+
+            // ---- units of this segment: the scores of the next one run beside the softmax of this one (past the last
+            // one they are not used, whatever the slot holds) ----
+            int key0 = (keys.lo / kKvPage + (int)(r0 + done - seg.start) * P) * kKvPage;   // first key of the unit
+            cp_wait<KS - 1>();                                   // group `done` brings its K
+            __syncwarp();
+            scores(ks);
+            for (; done < stop; ++done, key0 += UNIT) {
+                // group done + 1: K of the next unit and V of this one
+                cp_wait<KS - 2>();
+                __syncwarp();
+                const uint32_t ks_next = ks == ring + (KS - 1) * S::kSlot ? ring : ks + S::kSlot;
+                // x[r][j]: query g + 8 r, key t + 4 j of the unit
+                constexpr int J = 4 * P;
+                float x[R][J];
+                const bool part = key0 < keys.lo || key0 > keys.n - UNIT;   // not every key of the unit is the sequence's
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int n = j >> 1, col = j & 1;
+                    const float ksc = BF16 ? 1.f : lds32(ks + j / 4 * S::kBlock + kKvPage * D + (t + 4 * (j & 3)) * 4);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        float dot = c[n][0][col + 2 * r];
+                        if (SETS == 2) dot += c[n][SETS - 1][col + 2 * r];
+                        if (STACK && TQ > 1) {
+                            dot += c[n][0][col + 2];
+                            if (SETS == 2) dot += c[n][SETS - 1][col + 2];
+                        }
+                        x[r][j] = dot * (BF16 ? cq[r] : ksc * cq[r]);
+                    }
+                }
+                if (part) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const int key = key0 + t + 4 * j;
+#pragma unroll
+                        for (int r = 0; r < R; ++r) x[r][j] = key >= keys.lo && key < keys.n ? x[r][j] : -INFINITY;
+                    }
+                }
+                float up[R];
+                bool grew = false;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    float top = x[r][0];
+#pragma unroll
+                    for (int j = 1; j < J; ++j) top = fmaxf(top, x[r][j]);
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    up[r] = fmaxf(m[r], top);
+                    grew |= up[r] > m[r] + kLag;
+                }
+                if (__any_sync(0xffffffffu, grew)) {
                     float f[R];
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        heaviest[r] = fmaxf(heaviest[r], top[r]);
-                        heaviest[r] = fmaxf(heaviest[r], __shfl_xor_sync(0xffffffffu, heaviest[r], 1));
-                        heaviest[r] = fmaxf(heaviest[r], __shfl_xor_sync(0xffffffffu, heaviest[r], 2));
-                        f[r] = follow(r, 1.f);
+                        f[r] = m[r] == -INFINITY ? 0.f : ex2(m[r] - up[r]);   // nothing yet: zeros
+                        l[r] *= f[r];
+                        m[r] = up[r];
+                        if (!BF16) {
+                            heaviest[r] *= f[r];
+                            f[r] = follow(r, f[r]);
+                        }
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -839,164 +1111,167 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                         o[n][3] *= f[R - 1];
                     }
                 }
-            }
-            uint32_t pf[P][PPASS][4];
+                scores(ks_next);                                 // c has been read
+                float ref[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
+                for (int r = 0; r < R; ++r) ref[r] = m[r] == -INFINITY ? 0.f : m[r];
+                if (!BF16) {
+                    // the weights in the place of the scores
+                    float top[R];
+                    bool heavy = false;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const float vscale = lds32(vs + j / 4 * S::kBlock + kKvPage * D + (t + 4 * (j & 3)) * 4);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            const float p = ex2(x[r][j] - ref[r]);
+                            l[r] += p;
+                            x[r][j] = p * vscale;
+                        }
+                    }
+                    if (part) {                                  // scales of other keys may be anything
+#pragma unroll
+                        for (int j = 0; j < J; ++j) {
+                            const int key = key0 + t + 4 * j;
+#pragma unroll
+                            for (int r = 0; r < R; ++r) x[r][j] = key >= keys.lo && key < keys.n ? x[r][j] : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        top[r] = x[r][0];
+#pragma unroll
+                        for (int j = 1; j < J; ++j) top[r] = fmaxf(top[r], x[r][j]);
+                        heavy |= top[r] * per[r] > kPMost;
+                    }
+                    if (__any_sync(0xffffffffu, heavy)) {
+                        float f[R];
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            heaviest[r] = fmaxf(heaviest[r], top[r]);
+                            heaviest[r] = fmaxf(heaviest[r], __shfl_xor_sync(0xffffffffu, heaviest[r], 1));
+                            heaviest[r] = fmaxf(heaviest[r], __shfl_xor_sync(0xffffffffu, heaviest[r], 2));
+                            f[r] = follow(r, 1.f);
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            o[n][0] *= f[0];
+                            o[n][1] *= f[0];
+                            o[n][2] *= f[R - 1];
+                            o[n][3] *= f[R - 1];
+                        }
+                    }
+                }
+                uint32_t pf[P][PPASS][4];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+#pragma unroll
+                    for (int pg = 0; pg < P; ++pg) {
+                        float p[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (BF16) {
+                                p[j] = ex2(x[r][4 * pg + j] - ref[r]);
+                                l[r] += p[j];
+                            } else {
+                                p[j] = x[r][4 * pg + j] * per[r];
+                            }
+                        }
+                        split_row<BF16, true, STACK, TP, 1>(p, r, pf[pg]);
+                    }
+                }
+                // V: rows t + 4 i of a page; column g of tile n is element PER (g + 8 (n / PER)) + n % PER of the head
 #pragma unroll
                 for (int pg = 0; pg < P; ++pg) {
-                    float p[4];
+                    const uint32_t vp = vs + pg * S::kBlock;
+                    if (BF16) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (BF16) {
-                            p[j] = ex2(x[r][4 * pg + j] - ref[r]);
-                            l[r] += p[j];
-                        } else {
-                            p[j] = x[r][4 * pg + j] * per[r];
+                        for (int jj = 0; jj < CHUNKS / 8; ++jj) {
+                            uint32_t w[4][4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint4 q = lds128(vp + chunk_at<ROW, E2M1>(t + 4 * i, g + 8 * jj));
+                                w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const uint32_t sel = e & 1 ? 0x7632 : 0x5410;
+                                const uint32_t b0 = __byte_perm(w[0][e / 2], w[1][e / 2], sel);
+                                const uint32_t b1 = __byte_perm(w[2][e / 2], w[3][e / 2], sel);
+#pragma unroll
+                                for (int k = 0; k < PPASS; ++k) mma16816<true>(o[8 * jj + e], pf[pg][k], b0, b1);
+                            }
                         }
-                    }
-                    split_row<BF16, true, STACK, TP, 1>(p, r, pf[pg]);
-                }
-            }
-            // V: rows t + 4 i of a page; column g of tile n is element PER (g + 8 (n / PER)) + n % PER of the head
-#pragma unroll
-            for (int pg = 0; pg < P; ++pg) {
-                const uint32_t vp = vs + pg * S::kBlock;
-                if (BF16) {
-#pragma unroll
-                    for (int jj = 0; jj < CHUNKS / 8; ++jj) {
-                        uint32_t w[4][4];
+                    } else {
+                        constexpr int WORDS = D / 32;          // 4-byte words of a row that a lane takes
+                        uint32_t w[4][WORDS];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const uint4 q = lds128(vp + chunk_at<ROW, E2M1>(t + 4 * i, g + 8 * jj));
-                            w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const uint32_t sel = e & 1 ? 0x7632 : 0x5410;
-                            const uint32_t b0 = __byte_perm(w[0][e / 2], w[1][e / 2], sel);
-                            const uint32_t b1 = __byte_perm(w[2][e / 2], w[3][e / 2], sel);
-#pragma unroll
-                            for (int k = 0; k < PPASS; ++k) mma16816<true>(o[8 * jj + e], pf[pg][k], b0, b1);
-                        }
-                    }
-                } else if (E2M1) {
-                    constexpr int WORDS = D / 64;          // 4-byte words of a row that a lane takes
-                    uint32_t w[4][WORDS], b[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = t + 4 * i, key = key0 + pg * kKvPage + r;
-                        if (D == 128) {
-                            const uint2 q = lds64(vp + chunk_at<ROW, E2M1>(r, g >> 1) + (g & 1) * 8);
-                            w[i][0] = q.x, w[i][WORDS - 1] = q.y;
-                        } else {
-                            w[i][0] = __float_as_uint(lds32(vp + chunk_at<ROW, E2M1>(r, g >> 2) + (g & 3) * 4));
-                        }
-                        b[i] = lds8(vp + EACH_AT + r * (D / 16) + (D == 128 ? g : g >> 1));
-                        if (part && (key < keys.lo || key >= keys.n)) b[i] = 0;   // of another key: may be NaN
-                    }
-                    uint32_t b2[2];                        // of the rows of a fragment's half
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const __half2 v = __half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(b[2 * i] | b[2 * i + 1] << 8), __NV_E4M3));
-                        b2[i] = *(const uint32_t *)&v;
-                    }
-#pragma unroll
-                    for (int x8 = 0; x8 < WORDS; ++x8) {
-                        // halves of bytes of two rows interleaved first: columns 2 e in even[..][e], 2 e + 1 in odd[..][e]
-                        uint32_t even[2][4], odd[2][4];
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const uint32_t u = w[2 * i][x8], v = w[2 * i + 1][x8];
-                            decode_e2m1((u & 0x0F0F0F0Fu) | (v << 4 & 0xF0F0F0F0u), even[i]);
-                            decode_e2m1((u >> 4 & 0x0F0F0F0Fu) | (v & 0xF0F0F0F0u), odd[i]);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-#pragma unroll
-                            for (int k = 0; k < PPASS; ++k) {
-                                mma16816<false>(o[8 * x8 + 2 * e], pf[pg][k], times(even[0][e], b2[0]), times(even[1][e], b2[1]));
-                                mma16816<false>(o[8 * x8 + 2 * e + 1], pf[pg][k], times(odd[0][e], b2[0]), times(odd[1][e], b2[1]));
+                            if (D == 128) {
+                                const uint4 q = lds128(vp + chunk_at<ROW, E2M1>(t + 4 * i, g));
+                                w[i][0] = q.x, w[i][1] = q.y, w[i][WORDS - 2] = q.z, w[i][WORDS - 1] = q.w;
+                            } else {
+                                const uint2 q = lds64(vp + chunk_at<ROW, E2M1>(t + 4 * i, g >> 1) + (g & 1) * 8);
+                                w[i][0] = q.x, w[i][1] = q.y;
                             }
-                    }
-                } else {
-                    constexpr int WORDS = D / 32;          // 4-byte words of a row that a lane takes
-                    uint32_t w[4][WORDS];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (D == 128) {
-                            const uint4 q = lds128(vp + chunk_at<ROW, E2M1>(t + 4 * i, g));
-                            w[i][0] = q.x, w[i][1] = q.y, w[i][WORDS - 2] = q.z, w[i][WORDS - 1] = q.w;
-                        } else {
-                            const uint2 q = lds64(vp + chunk_at<ROW, E2M1>(t + 4 * i, g >> 1) + (g & 1) * 8);
-                            w[i][0] = q.x, w[i][1] = q.y;
-                        }
-                    }
-#pragma unroll
-                    for (int x4 = 0; x4 < WORDS; ++x4) {
-                        // the bytes of two rows interleaved first: a pair of them is a fragment's half
-                        uint32_t h[2][4];
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            decode4<FMT>(__byte_perm(w[2 * i][x4], w[2 * i + 1][x4], 0x5140), h[i][0], h[i][1]);
-                            decode4<FMT>(__byte_perm(w[2 * i][x4], w[2 * i + 1][x4], 0x7362), h[i][2], h[i][3]);
                         }
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
+                        for (int x4 = 0; x4 < WORDS; ++x4) {
+                            // the bytes of two rows interleaved first: a pair of them is a fragment's half
+                            uint32_t h[2][4];
 #pragma unroll
-                            for (int k = 0; k < PPASS; ++k) mma16816<false>(o[4 * x4 + e], pf[pg][k], h[0][e], h[1][e]);
+                            for (int i = 0; i < 2; ++i) {
+                                decode4<FMT>(__byte_perm(w[2 * i][x4], w[2 * i + 1][x4], 0x5140), h[i][0], h[i][1]);
+                                decode4<FMT>(__byte_perm(w[2 * i][x4], w[2 * i + 1][x4], 0x7362), h[i][2], h[i][3]);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                                for (int k = 0; k < PPASS; ++k) mma16816<false>(o[4 * x4 + e], pf[pg][k], h[0][e], h[1][e]);
+                        }
                     }
                 }
-            }
-            if (bad_units >> (done & 31) & 1) {
-                bad_units &= ~(1u << (done & 31));
+                if (bad_units >> (done & 31) & 1) {
+                    bad_units &= ~(1u << (done & 31));
 #pragma unroll
-                for (int r = 0; r < R; ++r) l[r] = __uint_as_float(0x7FC00000u);
+                    for (int r = 0; r < R; ++r) l[r] = __uint_as_float(0x7FC00000u);
+                }
+                __syncwarp();                                   // every lane has read the slots
+                issue();
+                ks = ks_next;
+                vs = vs == ring + (KS + VS - 1) * S::kSlot ? ring + KS * S::kSlot : vs + S::kSlot;
             }
-            __syncwarp();                                   // every lane has read the slots
-            issue();
-            ks = ks_next;
-            vs = vs == ring + (KS + VS - 1) * S::kSlot ? ring + KS * S::kSlot : vs + S::kSlot;
-        }
 
-        // ---- the segment's state, or this run's part of it ----
-        const bool entered = seg.start < r0, left = seg.end > r1;
-        if (left) {
-            cp_wait<0>();                                   // the ring is free: no unit follows
-            if (lane == 0) sh.leaving[warp] = seg;
-        }
-        __syncwarp();
-        // what ends in the block's first run is the block's whole part of its segment
-        const bool to_piece = !left && r0 == u0;
-        float *part_at = to_piece ? a.pieces + (int64_t)blockIdx.x * 2 * attn_piece_floats(D) : part_of(warp, left);
-        const int part_row = to_piece ? D : S::kPartRow;
-        float2 *part_ml = (float2 *)(part_at + (to_piece ? kAttnPieceRows * D : HT * S::kPartRow));
+            // ---- the segment's state, or this run's part of it ----
+            if (left) ring_is_free();
+            __syncwarp();
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-            const int row = g + 8 * r;
-            const bool alone = !entered && !left;
-            const float unit_of_o = BF16 ? 1.f : 1.f / per[r], f = alone ? unit_of_o / l[r] : unit_of_o;
-            if (row >= rows) continue;
+            for (int r = 0; r < R; ++r) {
+                l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+                l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+                const int row = g + 8 * r;
+                const bool alone = !entered && !left;
+                const float unit_of_o = BF16 ? 1.f : 1.f / per[r], f = alone ? unit_of_o / l[r] : unit_of_o;
+                if (row >= rows) continue;
 #pragma unroll
-            for (int n = 0; n < NT; n += 4) {
-                // columns 2 t and 2 t + 1 of tiles n .. n + 3: four adjacent elements each
-                float v[2][4];
+                for (int n = 0; n < NT; n += 4) {
+                    // columns 2 t and 2 t + 1 of tiles n .. n + 3: four adjacent elements each
+                    float v[2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) v[c][i] = (STACK ? rows_sum(o[n + i][c], o[n + i][c + 2]) : o[n + i][2 * r + c]) * f;
-                const int d0 = PER * (2 * t + 8 * (n / PER)) + n % PER;
+                        for (int c = 0; c < 2; ++c) v[c][i] = (STACK ? rows_sum(o[n + i][c], o[n + i][c + 2]) : o[n + i][2 * r + c]) * f;
+                    const int d0 = PER * (2 * t + 8 * (n / PER)) + n % PER;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if (alone) store_out4(a, seg_b, head0 + row, d0 + PER * c, v[c]);
-                    else *(float4 *)(part_at + row * part_row + d0 + PER * c) = make_float4(v[c][0], v[c][1], v[c][2], v[c][3]);
+                    for (int c = 0; c < 2; ++c) {
+                        if (alone) store_out4(a, seg_b, head0 + row, d0 + PER * c, v[c]);
+                        else *(float4 *)(part_at + row * part_row + d0 + PER * c) = make_float4(v[c][0], v[c][1], v[c][2], v[c][3]);
+                    }
                 }
-            }
-            if (t == 0) {
-                if (!alone) part_ml[row] = make_float2(m[r], l[r]);
-                else if (a.lse) a.lse[(int64_t)seg_b * a.q_heads + head0 + row] = (m[r] + log2f(l[r])) * 0.693147180559945309417f;
+                if (t == 0) {
+                    if (!alone) part_ml[row] = make_float2(m[r], l[r]);
+                    else if (a.lse) a.lse[(int64_t)seg_b * a.q_heads + head0 + row] = (m[r] + log2f(l[r])) * 0.693147180559945309417f;
+                }
             }
         }
         if (seg.end < r1) {
