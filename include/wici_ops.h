@@ -211,8 +211,8 @@ int wici_kv_bounds_update(void *cuda_stream, const wici_kv_cache *cache, const w
 
 typedef struct wici_select_shape {
     int32_t batch;            /* 0 .. 65535 */
-    int32_t max_pages;        /* columns of `pages`, 1 .. 32768 */
-    int32_t keep;             /* pages to select, 1 .. 32768 */
+    int32_t max_pages;        /* columns of `pages`, 1 .. 16384 (262144 tokens) */
+    int32_t keep;             /* pages to select, 1 .. 4096 */
     int32_t first, recent;    /* selected in any case: so many from the start (>= 0), from the end (>= 1); their sum <= keep */
 } wici_select_shape;
 

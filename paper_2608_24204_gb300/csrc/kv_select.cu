@@ -5,11 +5,11 @@
 //
 // Scores.  sum_d max(q_d hi_d, q_d lo_d) is the largest q.k that keys between lo and hi can have.  q enters as whole
 // numbers of at most 1023 (11 bits: fp16 holds them), the positive ones against hi and the negative ones against lo, so a
-// score is a dot product of 2 d whole numbers below 2^24: mma.m16n8k16 gives it exactly, in any order, and the selection
-// does not depend on how sums are split.  16 pages are the rows, 8 queries of the group the columns.
+// score is a dot product of whole numbers whose sums stay below 2^24: mma.m16n8k16 gives it exactly, in any order, and the
+// selection does not depend on how sums are split.  16 pages are the rows, 8 queries of the group the columns.
 // Select.  A cluster of blocks takes one sequence and KV head.  Its blocks score the pages and leave the scores, as
-// integers that order as they do, in the first block's shared memory; that one finds the keep-th largest, 11 bits at
-// a time by counting, and writes the pages from it on in order, of equal ones the first.
+// integers that order as they do, in the first block's shared memory; that one finds the keep-th largest by
+// counting into bins, and writes the pages from it on in order, of equal ones the first.
 #include <stdarg.h>
 #include <stdio.h>
 
@@ -167,20 +167,22 @@ struct SelectArg {
     const int32_t *pages, *lengths;
     int32_t *out_pages, *out_lengths, *out_blocks, *status;
     int kv_heads, group, n_pages, max_pages, keep, first, recent, q_dtype;
-    int cluster;
+    int cluster, stages;
 };
 
-constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
-constexpr int kSelectPerSm = 1;
-constexpr int kMaxSelectPages = 1 << 15;   // of a sequence: their scores stand in shared memory
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectWaves = 1;
+constexpr int kMaxSelectPages = 1 << 14;   // of a sequence: their scores stand in shared memory
+constexpr int kMaxKeep = 1 << 12;          // and the selected ones
+constexpr uint32_t kListed = 256;          // keys that are compared one with another, rather than counted
 constexpr int kMaxSelectGroup = 64;        // query heads of a KV head: so do they
 constexpr float kLevels = 1023.f;          // of a query's whole numbers: 128 * 127 * 1023 < 2^24
 constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr uint32_t kForced = 0xFFFFFFFFu;  // in the place of a score: above every one
 constexpr uint32_t kFirst = 0xFF800000u;   // +infinity's
 
-constexpr size_t select_smem(int d, int group, int max_pages) {
-    return (size_t)(group + 7) / 8 * (2 * d / 16 * 256 + 8 * 4) + ((size_t)max_pages + 31) / 32 * 128;
+constexpr size_t select_smem(int d, int group, int max_pages, int keep, int stages) {
+    return (size_t)kSelectWarps * stages * 16 * 2 * d + (size_t)(group + 7) / 8 * (2 * d / 16 * 256 + 8 * 12) + ((size_t)max_pages + 31) / 32 * 128 + (size_t)keep * 2;
 }
 
 // Scores in the order of unsigned integers; NaN, which no page should have, stands with +infinity
@@ -188,6 +190,19 @@ __device__ __forceinline__ uint32_t order_of(float s) {
     const uint32_t u = __float_as_uint(s + 0.f);
     if (s != s) return kFirst;
     return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+constexpr size_t kSelectSmem = 216 * 1024;   // at most, beside what the kernel has of its own
+static_assert(select_smem(128, kMaxSelectGroup, kMaxSelectPages, kMaxKeep, 1) <= kSelectSmem, "the largest call");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float score_of(uint32_t order) {
+    return __uint_as_float(order >> 31 ? order ^ 0x80000000u : ~order);
 }
 __device__ __forceinline__ void mma_f16(float *c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -200,14 +215,17 @@ __device__ __forceinline__ void store_to_first(uint32_t addr, uint32_t v) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_constant__ SelectArg a) {
-    constexpr int STEPS = 2 * D / 16, LOADS = 2 * D / 64;
+__global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_constant__ SelectArg a) {
+    constexpr int STEPS = 2 * D / 16, ROW = 2 * D;
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ uint32_t part[2][kSelectWarps], bins[kBins];
+    __shared__ uint32_t part[2][kSelectWarps], bins[kBins], ends[2][8 * kSelectWarps], listed;
     const int tiles = (a.group + 7) / 8;
-    __half *qs = (__half *)smem;                                  // [tile][step][lane][4]: B fragments
-    float *most = (float *)(smem + tiles * STEPS * 256);          // [tile * 8]: each query's largest magnitude
-    uint32_t *keys = (uint32_t *)(most + tiles * 8);              // [page], of the first block
+    const uint32_t rows_at = smem_u32(smem) + threadIdx.x / 32 * a.stages * 16 * ROW;   // this warp's: [stage][page of a tile]
+    __half *qs = (__half *)(smem + kSelectWarps * a.stages * 16 * ROW);                 // [tile][step][lane][4]: B fragments
+    float *most = (float *)((uint8_t *)qs + tiles * STEPS * 256); // [tile * 8]: each query's largest magnitude
+    float2 *bias = (float2 *)(most + tiles * 8);                  // [tile * 8]: 128 times the sums of its whole numbers
+    uint32_t *keys = (uint32_t *)(bias + tiles * 8);              // [page], of the first block
+    uint16_t *chosen = (uint16_t *)(keys + (a.max_pages + 31) / 32 * 32);   // [keep]
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int rank = blockIdx.x % a.cluster, h = blockIdx.x / a.cluster, b = blockIdx.y;
     // Every block of a cluster comes to each barrier, whatever it reads
@@ -218,6 +236,48 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
     const bool bad = n > (int64_t)a.max_pages * kKvPage;
     const int count = bad || n <= 0 ? 0 : (n + kKvPage - 1) / kKvPage;
     const bool choose = count > a.keep;
+    const int32_t *table = a.pages + (int64_t)b * a.max_pages;
+    // A tile is 16 pages; a warp's tiles come through cp.async, one under way while the one before is worked on.  (Loads to
+    // registers wait in L1, which the attention's shared memory leaves small: 46 in place of 30 us beside it.)
+    const int step = kSelectWarps * a.cluster, first_tile = rank * kSelectWarps + warp;
+    const uint64_t policy = l2_evict_first();
+    auto page_of = [&](int tile) {
+        const int at = tile * 16 + (lane & 15);
+        return choose && at < count ? table[at] : 0;
+    };
+    constexpr int CHUNKS = ROW / 16, ROUNDS = 16 * CHUNKS / 32;   // of a row; rounds of the warp for a tile
+    const uint8_t *const of_lane = a.bounds + h * ROW + lane % CHUNKS * 16;
+    const uint8_t *const of_scale = a.bounds + a.kv_heads * ROW + 4 * h;
+    // chunks of odd rows with their halves of 128 bytes exchanged: lanes that read 64 bytes of two rows meet all banks
+    const uint32_t lane_to = lane / CHUNKS * ROW + ((lane % CHUNKS ^ (lane / CHUNKS & 1) << 2) << 4);
+    struct Asked {                                                // of page lane % 16 of a tile
+        float scale;                                              // not looked at before it is needed: it is still on its way
+        bool there;
+    };
+    auto ask = [&](int tile, int page, int stage) {
+        if (tile * 16 < count) {
+            const bool there = (uint32_t)page < (uint32_t)a.n_pages;
+            if (!there && a.status) atomicOr(a.status, WICI_BAD_PAGE);
+            const int p = there ? page : 0;                       // (of page 0, not used)
+#pragma unroll
+            for (int i = 0; i < ROUNDS; ++i) {
+                const int of = __shfl_sync(0xffffffffu, p, i * (32 / CHUNKS) + lane / CHUNKS);
+                cp_async16(rows_at + stage * 16 * ROW + lane_to + i * 512, of_lane + of * a.bounds_stride, policy);
+            }
+            const float scale = *(const float *)(of_scale + p * a.bounds_stride);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            return Asked{scale, there};
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");      // none: the groups still count
+        return Asked{0.f, false};
+    };
+    int next_page = page_of(first_tile);
+    Asked asked = ask(first_tile, next_page, 0), next = {0.f, false};   // the tile to work on, the one after
+    next_page = page_of(first_tile + step);
+    if (a.stages == 2) {
+        next = ask(first_tile + step, next_page, 1);
+        next_page = page_of(first_tile + 2 * step);
+    }
 
     if (choose) {
         for (int i = warp; i < tiles * 8; i += kSelectWarps) {    // one query a warp
@@ -238,71 +298,72 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
             top = __reduce_max_sync(0xffffffffu, top);
             const bool some = top < kInfBits && __uint_as_float(top) >= 0x1p-100f;
             const float per = some ? __fmul_rn(__frcp_rn(__uint_as_float(top)), kLevels) : 0.f;
-            if (lane == 0) most[i] = some ? __uint_as_float(top) : 0.f;
+            float sums[2] = {0.f, 0.f};                           // over elements of even and of odd words
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 const float w = some ? rintf(__fmul_rn(x[j], per)) : 0.f;
 #pragma unroll
                 for (int end = 0; end < 2; ++end) {               // against the largest keys, the smallest
                     const int e = end * D + lane + 32 * j;        // byte of a record's row: chunk e / 16 is lane t's
-                    const int step = e / 64 * 4 + e % 16 / 4, to = i % 8 * 4 + e / 16 % 4;
-                    qs[((i / 8 * STEPS + step) * 32 + to) * 4 + e % 4] = __float2half_rn(end ? fminf(w, 0.f) : fmaxf(w, 0.f));
+                    const int at = e / 64 * 4 + e % 16 / 4, to = i % 8 * 4 + e / 16 % 4;
+                    qs[((i / 8 * STEPS + at) * 32 + to) * 4 + e % 4] = __float2half_rn(end ? fminf(w, 0.f) : fmaxf(w, 0.f));
                 }
+                sums[lane >> 2 & 1] += w;
             }
+            sums[0] = warp_sum(sums[0]), sums[1] = warp_sum(sums[1]);
+            if (lane == 0) most[i] = some ? __uint_as_float(top) : 0.f, bias[i] = make_float2(128.f * sums[0], 128.f * sums[1]);
         }
     }
     __syncthreads();
     if (a.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // the first block runs
 
+    uint32_t hi = 0, lo = 0xFFFFFFFFu;                            // of this lane's scores that are not forced
     if (choose) {
-        const int32_t *table = a.pages + (int64_t)b * a.max_pages;
         const uint32_t keys_at = smem_u32(keys);
-        const int step = kSelectWarps * a.cluster;
-        auto page_of = [&](int tile) {
-            const int at = tile * 16 + (lane & 15);
-            return at < count ? table[at] : 0;
-        };
-        int next_page = page_of(rank * kSelectWarps + warp);
-        for (int tile = rank * kSelectWarps + warp; tile * 16 < count; tile += step) {
-            const int at = tile * 16 + (lane & 15), page = next_page;
-            next_page = page_of(tile + step);
-            if (lane < 16 && at < count && (uint32_t)page >= (uint32_t)a.n_pages && a.status) atomicOr(a.status, WICI_BAD_PAGE);
-            int row_page[2];
-            uint4 raw[2][LOADS];
-            float scale[2];
+        int stage = 0;
+        const uint32_t row_at = rows_at + g * ROW + 16 * t, even = (g & 1) << 6;
+        for (int tile = first_tile; tile * 16 < count; tile += step) {
+            if (a.stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            float scale[2], best[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                row_page[r] = __shfl_sync(0xffffffffu, page, g + 8 * r);
-                const bool there = (uint32_t)row_page[r] < (uint32_t)a.n_pages;
-                const uint8_t *record = a.bounds + (int64_t)(there ? row_page[r] : 0) * a.bounds_stride;
-                const uint4 *src = (const uint4 *)(record + h * 2 * D) + t;
-#pragma unroll
-                for (int i = 0; i < LOADS; ++i) raw[r][i] = there ? src[4 * i] : make_uint4(0, 0, 0, 0);
-                scale[r] = there ? ((const float *)(record + a.kv_heads * 2 * D))[h] : INFINITY;
-            }
-            float best[2] = {-INFINITY, -INFINITY};
+            for (int r = 0; r < 2; ++r) scale[r] = __shfl_sync(0xffffffffu, asked.there ? asked.scale : INFINITY, g + 8 * r);
+            const uint32_t row = row_at + stage * 16 * ROW;
             for (int q = 0; q < tiles; ++q) {
-                float c[4] = {0.f, 0.f, 0.f, 0.f};
+                // codes + 128 as they are are fp16's smallest numbers, 2^-24 each: sums of 64 products with whole numbers up
+                // to 1023 stay below 2^24 of them, and 128 times the whole numbers' sum is taken off after
+                float c[2][4] = {};
                 const uint2 *frag = (const uint2 *)qs + q * STEPS * 32 + lane;
 #pragma unroll
-                for (int i = 0; i < LOADS; ++i) {
-                    const uint32_t *u = (const uint32_t *)&raw[0][i], *v = (const uint32_t *)&raw[1][i];
+                for (int i = 0; i < STEPS / 4; ++i) {
+                    const uint32_t at = row + (i & 1 ? even ^ 64 : even) + i / 2 * 128;
+                    const uint4 u4 = lds128(at), v4 = lds128(at + 8 * ROW);
+                    const uint32_t u[4] = {u4.x, u4.y, u4.z, u4.w}, v[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
-                        uint32_t a0, a1, a2, a3;
-                        decode4<WICI_KV_INT8>(u[s], a0, a2);
-                        decode4<WICI_KV_INT8>(v[s], a1, a3);
-                        mma_f16(c, a0, a1, a2, a3, frag[(4 * i + s) * 32]);
+                        const uint32_t x = u[s] ^ 0x80808080u, y = v[s] ^ 0x80808080u;
+                        mma_f16(c[s & 1], __byte_perm(x, 0, 0x4140), __byte_perm(y, 0, 0x4140), __byte_perm(x, 0, 0x4342),
+                                __byte_perm(y, 0, 0x4342), frag[(4 * i + s) * 32]);
                     }
                 }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int head = q * 8 + 2 * t + j;
-                    if (head >= a.group) continue;
-                    best[0] = fmaxf(best[0], __fmul_rn(c[j], most[head]));
-                    best[1] = fmaxf(best[1], __fmul_rn(c[2 + j], most[head]));
+                    const float m = most[head];
+                    const float2 off = bias[head];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float dot = fmaf(c[0][2 * r + j], 0x1p24f, -off.x) + fmaf(c[1][2 * r + j], 0x1p24f, -off.y);
+                        best[r] = fmaxf(best[r], head < a.group ? __fmul_rn(dot, m) : -INFINITY);
+                    }
                 }
             }
+            __syncwarp();                                         // the rows have been read
+            const Asked s = ask(tile + a.stages * step, next_page, stage);
+            next_page = page_of(tile + (a.stages + 1) * step);
+            if (a.stages == 2) asked = next, next = s, stage ^= 1;
+            else asked = s;
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 best[r] = fmaxf(best[r], __shfl_xor_sync(0xffffffffu, best[r], 1));
@@ -312,13 +373,25 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
                 if (scale[r] == 0.f) key = order_of(0.f);
                 else if (fabsf(scale[r]) < INFINITY) key = order_of(__fmul_rn(best[r], scale[r]));
                 if (i < a.first || i >= count - a.recent) key = kForced;
+                else hi = max(hi, key), lo = min(lo, key);
                 if (t == r && i < count) {
                     if (a.cluster > 1) store_to_first(keys_at + 4 * i, key);
                     else keys[i] = key;
                 }
             }
         }
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        if (lane == 0) {
+            const int at = rank * kSelectWarps + warp;
+            if (a.cluster > 1) store_to_first(smem_u32(&ends[0][at]), hi), store_to_first(smem_u32(&ends[1][at]), lo);
+            else ends[0][at] = hi, ends[1][at] = lo;
+        }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (rank == 0)
+        for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
+    if (threadIdx.x == 0) listed = 0;
     if (a.cluster > 1) {
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (rank != 0) return;
@@ -327,7 +400,6 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
     }
 
     // ---- the first block: the keep-th largest key, and the pages from it on ----
-    const int32_t *table = a.pages + (int64_t)b * a.max_pages;
     int32_t *pages = a.out_pages + ((int64_t)b * a.kv_heads + h) * a.keep;
     int32_t *blocks = a.out_blocks ? a.out_blocks + ((int64_t)b * a.kv_heads + h) * a.keep : nullptr;
     if (h == 0 && threadIdx.x == 0) {
@@ -346,32 +418,17 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
     }
     uint32_t limit = kForced;
     if (a.first + a.recent < a.keep) {
-        // the keys that are not forced: their leading bits in common need no search
-        uint32_t hi = 0, lo = 0xFFFFFFFFu;
-        for (int i = threadIdx.x; i < count; i += kSelectThreads) {
-            const uint32_t k = keys[i];
-            if (k != kForced) hi = max(hi, k), lo = min(lo, k);
-        }
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        if (lane == 0) part[0][warp] = hi, part[1][warp] = lo;
-        for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kSelectWarps; ++w) hi = max(hi, part[0][w]), lo = min(lo, part[1][w]);
-        int open = hi == lo ? 0 : 32 - __clz(hi ^ lo);            // bits that may differ
-        // the keep-th largest of all is the rank-th largest of those that are not forced; kBinBits of its bits at a time
-        uint32_t above = a.first + a.recent;                      // keys known to be larger
-        limit = open == 32 ? 0u : hi >> open << open;
-        while (open > 0) {
-            const int low = open > kBinBits ? open - kBinBits : 0;
+        // over the keys that are not forced and that `in` takes: a count for each value of `bin` (bins are 0 before), and
+        // then the bin that has the keep-th largest of all, where `above` keys are known to be larger
+        uint32_t above = a.first + a.recent;
+        auto narrow = [&](auto in, auto bin) {
+#pragma unroll 4
             for (int i = threadIdx.x; i < count; i += kSelectThreads) {
                 const uint32_t k = keys[i];
-                if (k != kForced && (open == 32 || (k ^ limit) >> open == 0)) atomicAdd(&bins[(k >> low) & (kBins - 1) & ((1u << (open - low)) - 1)], 1u);
+                if (k != kForced && in(k)) atomicAdd(&bins[bin(k)], 1u);
             }
             __syncthreads();
-            // each thread has kEach bins, the highest first: the one where the count passes keep has the key
-            constexpr int kEach = kBins / kSelectThreads;
+            constexpr int kEach = kBins / kSelectThreads;         // bins of a thread, the highest first
             const int top = kBins - 1 - kEach * threadIdx.x;
             uint32_t mine = 0;
 #pragma unroll
@@ -387,24 +444,80 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
             for (int w = 0; w < warp; ++w) upto += part[0][w];
             uint32_t before = above + upto - mine;
             if (before < (uint32_t)a.keep && before + mine >= (uint32_t)a.keep) {
-                int bin = top;
-                while (before + bins[bin] < (uint32_t)a.keep) before += bins[bin--];
-                part[1][0] = limit | (uint32_t)bin << low;
+                int at = top;
+                while (before + bins[at] < (uint32_t)a.keep) before += bins[at--];
+                part[1][0] = at;
                 part[1][1] = before;
+                part[1][2] = bins[at];
             }
             __syncthreads();
-            limit = part[1][0];
             above = part[1][1];
-            open = low;
-            if (open > 0) {
-                for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
+            return part[1][0];
+        };
+        hi = 0, lo = 0xFFFFFFFFu;                                 // the largest and the smallest of them
+        for (int w = lane; w < step; w += 32) hi = max(hi, ends[0][w]), lo = min(lo, ends[1][w]);
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        limit = hi;
+        if (hi != lo) {
+            // Bins of equal width first: bits of scores, of like size as they are, would fall into few bins, whose counting
+            // takes turns.  The bin of a score grows with it, whatever is rounded.  (Not where the width is no number.)
+            const float least = score_of(lo), per = (kBins - 1) / (score_of(hi) - least);
+            const bool even = per > 0.f && per < INFINITY;
+            auto bin = [=](uint32_t k) { return even ? min(kBins - 1, max(0, (int)((score_of(k) - least) * per))) : 0; };
+            const int found = even ? (int)narrow([](uint32_t) { return true; }, bin) : 0;
+            const uint32_t in_bin = even ? part[1][2] : 0xFFFFFFFFu;
+            __syncthreads();
+            if (in_bin <= kListed) {
+                // few keys: each is compared with the others
+                uint32_t *list = bins;
+#pragma unroll 4
+                for (int i = threadIdx.x; i < count; i += kSelectThreads) {
+                    const uint32_t k = keys[i];
+                    if (k != kForced && bin(k) == found) list[atomicAdd(&listed, 1u) & (kListed - 1)] = k;
+                }
                 __syncthreads();
+                for (uint32_t i = threadIdx.x; i < in_bin; i += kSelectThreads) {
+                    const uint32_t k = list[i];
+                    uint32_t larger = above, equal = 0;
+                    for (uint32_t j = 0; j < in_bin; ++j) larger += list[j] > k, equal += list[j] == k;
+                    if (larger < (uint32_t)a.keep && larger + equal >= (uint32_t)a.keep) part[0][0] = k;
+                }
+                __syncthreads();
+                limit = part[0][0];
+            } else {
+                // many: of the keys in the bin, kBinBits of their bits at a time from the first that differ
+                hi = 0, lo = 0xFFFFFFFFu;
+                for (int i = threadIdx.x; i < count; i += kSelectThreads) {
+                    const uint32_t k = keys[i];
+                    if (k != kForced && bin(k) == found) hi = max(hi, k), lo = min(lo, k);
+                }
+                hi = __reduce_max_sync(0xffffffffu, hi);
+                lo = __reduce_min_sync(0xffffffffu, lo);
+                if (lane == 0) part[0][warp] = hi, part[1][warp] = lo;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < kSelectWarps; ++w) hi = max(hi, part[0][w]), lo = min(lo, part[1][w]);
+                int open = hi == lo ? 0 : 32 - __clz(hi ^ lo);
+                const uint32_t most_key = hi, least_key = lo;
+                limit = open == 32 ? 0u : hi >> open << open;
+                while (open > 0) {
+                    __syncthreads();                              // `part` and `bins` have been read
+                    for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
+                    __syncthreads();
+                    const int low = open > kBinBits ? open - kBinBits : 0;
+                    const uint32_t mask = (1u << (open - low)) - 1, prefix = limit;
+                    limit |= narrow([=](uint32_t k) { return k >= least_key && k <= most_key && (open == 32 || (k ^ prefix) >> open == 0); },
+                                    [=](uint32_t k) { return (k >> low) & mask; }) << low;
+                    open = low;
+                }
             }
         }
     }
     // a warp's share of the pages, in order: those above the limit, and as many of those at it as there is room for
     const int share = ((count + kSelectWarps - 1) / kSelectWarps + 31) & ~31, from = warp * share, to = min(count, from + share);
     uint32_t over = 0, at = 0;
+#pragma unroll 4
     for (int i = from + lane; i < to; i += 32) over += keys[i] > limit, at += keys[i] == limit;
     over = __reduce_add_sync(0xffffffffu, over);
     at = __reduce_add_sync(0xffffffffu, at);
@@ -429,12 +542,15 @@ __global__ void __launch_bounds__(kSelectThreads, 2) select_kernel(const __grid_
         const bool taken = is_over || (is_at && (uint32_t)__popc(m_at & below) < room);
         const uint32_t m = __ballot_sync(0xffffffffu, taken);
         const uint32_t p = place + __popc(m & below);
-        if (taken && p < (uint32_t)a.keep) {
-            pages[p] = table[i];
-            if (blocks) blocks[p] = i;
-        }
+        if (taken && p < (uint32_t)a.keep) chosen[p] = (uint16_t)i;
         place += __popc(m);
         room -= min(room, (uint32_t)__popc(m_at));
+    }
+    __syncthreads();
+    for (int p = threadIdx.x; p < a.keep; p += kSelectThreads) {
+        const int i = min((int)chosen[p], count - 1);
+        pages[p] = table[i];
+        if (blocks) blocks[p] = i;
     }
 }
 
@@ -448,7 +564,7 @@ int device_of(Device *d) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess)
         e = g_devices.get(dev, d, [dev](Device *x) {
-            constexpr int kMost = (int)select_smem(128, kMaxSelectGroup, kMaxSelectPages);
+            constexpr int kMost = kSelectSmem;
             cudaError_t e1 = cudaFuncSetAttribute(select_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
             if (e1 == cudaSuccess) e1 = cudaFuncSetAttribute(select_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
             return e1 == cudaSuccess ? cudaDeviceGetAttribute(&x->sms, cudaDevAttrMultiProcessorCount, dev) : e1;
@@ -520,10 +636,10 @@ int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_
     if (const char *m = check_bounds(bounds, cache)) return fail(WICI_E_ARG, "select: %s", m);
     if (!shape) return fail(WICI_E_ARG, "select: null shape");
     if (shape->batch < 0 || shape->batch > 65535) return fail(WICI_E_ARG, "select: batch must be in [0, 65535]");
-    if (shape->max_pages < 1 || shape->max_pages > kMaxSelectPages) return fail(WICI_E_ARG, "select: max_pages must be in [1, 32768]");
-    if (shape->first < 0 || shape->recent < 1 || shape->keep < 1 || shape->keep > kMaxSelectPages ||
+    if (shape->max_pages < 1 || shape->max_pages > kMaxSelectPages) return fail(WICI_E_ARG, "select: max_pages must be in [1, 16384]");
+    if (shape->first < 0 || shape->recent < 1 || shape->keep < 1 || shape->keep > kMaxKeep ||
         shape->first > shape->keep || shape->recent > shape->keep - shape->first)
-        return fail(WICI_E_ARG, "select: first >= 0, recent >= 1 and first + recent <= keep <= 32768 required");
+        return fail(WICI_E_ARG, "select: first >= 0, recent >= 1 and first + recent <= keep <= 4096 required");
     if (const char *m = check_heads(q, shape->batch, cache->head_dim, false)) return fail(WICI_E_ARG, "select q: %s", m);
     if (q->heads % cache->n_kv_heads || q->heads / cache->n_kv_heads > kMaxSelectGroup)
         return fail(WICI_E_ARG, "select: query heads must be a multiple of the cache's heads, at most 64 times as many");
@@ -559,13 +675,14 @@ int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_
     a.first = shape->first;
     a.recent = shape->recent;
     a.q_dtype = q->dtype;
-    // Blocks of a cluster: as many as make kSelectPerSm blocks an SM of the launch, of 16 pages a warp at least
+    // Blocks of a cluster, one an SM: as many as there are SMs for, and pages for a tile a warp
     a.cluster = 1;
-    while (a.cluster < 8 && (int64_t)a.cluster * a.kv_heads * shape->batch < kSelectPerSm * dev.sms &&
+    while (a.cluster < 8 && (int64_t)2 * a.cluster * a.kv_heads * shape->batch <= kSelectWaves * dev.sms &&
            a.cluster * kSelectWarps * 16 < shape->max_pages)
         a.cluster *= 2;
     const dim3 grid((unsigned)(a.cluster * a.kv_heads), (unsigned)shape->batch);
-    const size_t smem = select_smem(cache->head_dim, a.group, a.max_pages);
+    a.stages = select_smem(cache->head_dim, a.group, a.max_pages, a.keep, 2) <= kSelectSmem ? 2 : 1;
+    const size_t smem = select_smem(cache->head_dim, a.group, a.max_pages, a.keep, a.stages);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const cudaError_t e = cache->head_dim == 64 ? launch_kernel(select_kernel<64>, grid, kSelectThreads, smem, st, a.cluster, true, a)
                                                 : launch_kernel(select_kernel<128>, grid, kSelectThreads, smem, st, a.cluster, true, a);

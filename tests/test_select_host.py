@@ -47,9 +47,9 @@ def test_bad_caches_are_refused():
 
 
 @pytest.mark.parametrize("shape,match", [
-    ((-1, 4, 2, 1, 1), "batch"), ((65536, 4, 2, 1, 1), "batch"), ((2, 0, 2, 1, 1), "max_pages"), ((2, 32769, 2, 1, 1), "max_pages"),
+    ((-1, 4, 2, 1, 1), "batch"), ((65536, 4, 2, 1, 1), "batch"), ((2, 0, 2, 1, 1), "max_pages"), ((2, 16385, 2, 1, 1), "max_pages"),
     ((2, 4, 0, 0, 1), "keep"), ((2, 4, 2, 2, 1), "keep"), ((2, 4, 2, -1, 1), "keep"), ((2, 4, 2, 1, 0), "keep"),
-    ((2, 4, 32769, 1, 1), "keep"), ((2, 4, 2, 2 ** 31 - 1, 2 ** 31 - 1), "keep")])
+    ((2, 4, 4097, 1, 1), "keep"), ((2, 4, 2, 2 ** 31 - 1, 2 ** 31 - 1), "keep")])
 def test_bad_shapes_are_refused(shape, match):
     select(shape=shape, match=match)
 
