@@ -197,7 +197,7 @@ int wici_selected_attention(void *cuda_stream, const wici_kv_cache *cache, const
  * The paper has no counterpart: its longest context is read whole. */
 typedef struct wici_kv_bounds {
     void *data;               /* 16-byte aligned, a record for each page of the cache */
-    int64_t page_stride;      /* bytes, a multiple of 16, at least wici_kv_bounds_bytes */
+    int64_t page_stride;      /* bytes, a multiple of 16, at least wici_kv_bounds_bytes, below 2^31 */
 } wici_kv_bounds;
 
 /* Bytes of one record (0 for a head_dim that is not 64 or 128). */

@@ -113,7 +113,7 @@ __device__ __forceinline__ void blocks_of_16(const float *x, bool halves, const 
 // before the row ahead of it is worked on), the arithmetic and its stores.  Lanes of a warp take
 // neighbouring heads of a token: a packed row's heads lie side by side.
 template <typename T, int FMT, int PATH>
-__global__ void __launch_bounds__(kRowThreads, kRowBlocks) rows_kernel(const __grid_constant__ RowsArg a) {
+__global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlocks) rows_kernel(const __grid_constant__ RowsArg a) {
     constexpr bool WIDE = PATH != NARROW;
     constexpr int W = sizeof(T) / 2;                             // 16-byte words of 8 elements
     extern __shared__ float4 cs[];    // [token][4][rot_chunks]: (cos, sin) of pairs 8 chunk + 2 j, + 2 j + 1

@@ -43,40 +43,39 @@ struct BoundsArg {
 
 constexpr int kBoundsThreads = 128;
 
-// E values of a key row at element e0 in fp32, the token's scale left out
+// E values of a key row from element e0 on, as they stand, and as fp32 (the token's scale left out)
 template <int FMT, int D, int E>
-__device__ __forceinline__ void load_key(const uint8_t *block, int row, int e0, float *x) {
-    if (FMT == WICI_KV_BF16) {
-        uint32_t w[E / 2];
-        const uint8_t *p = block + (row * D + e0) * 2;
-        if (E == 4) *(uint2 *)w = *(const uint2 *)p;
-        else w[0] = *(const uint32_t *)p;
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) x[2 * i] = bf16lo(w[i]), x[2 * i + 1] = bf16hi(w[i]);
-    } else if (FMT == WICI_KV_E2M1) {
-        const uint8_t *p = block + row * (D / 2) + e0 / 2;
-        const uint32_t w = E == 4 ? *(const uint16_t *)p : *p;
-        const float b = e4m3_value(block[kKvPage * (D / 2) + row * (D / 16) + e0 / 16]);
-        uint32_t h[4];
-        decode_e2m1(w, h);
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-            const float2 f = __half22float2(*(const __half2 *)&h[i]);
-            x[2 * i] = f.x * b, x[2 * i + 1] = f.y * b;
-        }
-    } else {
-        const uint8_t *p = block + row * D + e0;
-        const uint32_t w = E == 4 ? *(const uint32_t *)p : *(const uint16_t *)p;
-        uint32_t h[2];
-        decode4<FMT>(w, h[0], h[1]);
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-            const float2 f = __half22float2(*(const __half2 *)&h[i]);
-            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+struct KeyPart {
+    uint32_t w[FMT == WICI_KV_BF16 ? E / 2 : 1], each;
+    __device__ __forceinline__ void load(const uint8_t *block, int row, int e0) {
+        const uint8_t *p = block + row * kv_row_bytes(FMT, D) + (FMT == WICI_KV_BF16 ? 2 * e0 : FMT == WICI_KV_E2M1 ? e0 / 2 : e0);
+        if (FMT == WICI_KV_BF16 && E == 4) {
+            const uint2 v = *(const uint2 *)p;
+            w[0] = v.x, w[E / 2 - 1] = v.y;
+        } else if (FMT == WICI_KV_E2M1) {
+            w[0] = E == 4 ? *(const uint16_t *)p : *p;
+            each = block[kKvPage * (D / 2) + row * (D / 16) + e0 / 16];
+        } else {
+            w[0] = FMT == WICI_KV_BF16 || E == 4 ? *(const uint32_t *)p : *(const uint16_t *)p;
         }
     }
-}
-
+    __device__ __forceinline__ void values(float *x) const {
+        if (FMT == WICI_KV_BF16) {
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) x[2 * i] = bf16lo(w[i]), x[2 * i + 1] = bf16hi(w[i]);
+            return;
+        }
+        uint32_t h[4];
+        if (FMT == WICI_KV_E2M1) decode_e2m1(w[0], h);
+        else decode4<FMT>(w[0], h[0], h[1]);
+        const float b = FMT == WICI_KV_E2M1 ? e4m3_value(each) : 1.f;
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            const float2 f = __half22float2(*(const __half2 *)&h[i]);
+            x[2 * i] = FMT == WICI_KV_E2M1 ? f.x * b : f.x, x[2 * i + 1] = FMT == WICI_KV_E2M1 ? f.y * b : f.y;
+        }
+    }
+};
 // the largest and the smallest of three, NaN where one is
 __device__ __forceinline__ float max_of(float a, float b, float c) {
     float d;
@@ -89,7 +88,8 @@ __device__ __forceinline__ float min_of(float a, float b, float c) {
     return d;
 }
 
-// A warp takes one page of one KV head, a lane E elements of all its rows.
+// A warp takes one page of one KV head, a lane E elements of all its rows, which it asks for at once and keeps as they
+// stand: few registers, many warps.
 template <int FMT, int D>
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsArg a) {
     constexpr int E = D / 32;
@@ -97,8 +97,8 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
     griddep_wait();
     const int64_t item = (int64_t)blockIdx.x * (kBoundsThreads / 32) + threadIdx.x / 32;
     if (item >= a.items) return;
-    const int lane = threadIdx.x & 31, kv = a.cache.kv_heads, head = (int)(item % kv);
-    const int last = a.last[item / kv];
+    const int lane = threadIdx.x & 31, kv = a.cache.kv_heads, head = (int)((uint32_t)item % (uint32_t)kv);   // items <= 2^31
+    const int last = a.last[(uint32_t)item / (uint32_t)kv];
     if (last < 0) return;
     const int page = last / kKvPage, rows = last % kKvPage + 1;
     if (page >= a.cache.n_pages) {
@@ -106,32 +106,29 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
         return;
     }
     const uint8_t *block = a.cache.data + page * a.cache.page_stride + (int64_t)head * kv_block_bytes(FMT, D);
+    KeyPart<FMT, D, E> part[kKvPage];
+#pragma unroll
+    for (int r = 0; r < kKvPage; ++r) part[r].load(block, r < rows ? r : 0, lane * E);   // past the last row: row 0 again
     float scale = 1.f;
-    if (FMT != WICI_KV_BF16 && lane < rows) scale = ((const float *)(block + kv_scales_at(FMT, D)))[lane];
-    float x[kKvPage][E];
-#pragma unroll
-    for (int r = 0; r < kKvPage; ++r)
-        if (r < rows) load_key<FMT, D, E>(block, r, lane * E, x[r]);
+    if (FMT != WICI_KV_BF16) scale = ((const float *)(block + kv_scales_at(FMT, D)))[lane < rows ? lane : 0];
     float hi[E], lo[E];               // NaN where one of the values is
-    {
-        const float s = FMT == WICI_KV_BF16 ? 1.f : __shfl_sync(0xffffffffu, scale, 0);
+    auto row = [&](int r, float *v) {
+        part[r].values(v);
+        if (FMT == WICI_KV_BF16) return;
+        const float s = __shfl_sync(0xffffffffu, scale, r);
 #pragma unroll
-        for (int j = 0; j < E; ++j) hi[j] = lo[j] = FMT == WICI_KV_BF16 ? x[0][j] : x[0][j] * s;
-    }
+        for (int j = 0; j < E; ++j) v[j] *= s;
+    };
+    row(0, hi);
 #pragma unroll
-    for (int r = 1; r < kKvPage; r += 3) {                    // past the last row: the largest so far, which changes neither
-        float v[3][E];
+    for (int j = 0; j < E; ++j) lo[j] = hi[j];
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            const float s = FMT == WICI_KV_BF16 ? 1.f : __shfl_sync(0xffffffffu, scale, r + i);
+    for (int r = 1; r < kKvPage; r += 2) {
+        float u[E], v[E];
+        row(r, u);
+        row(r + 1 < kKvPage ? r + 1 : r, v);
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[i][j] = r + i < rows ? FMT == WICI_KV_BF16 ? x[r + i][j] : x[r + i][j] * s : hi[j];
-        }
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            hi[j] = max_of(max_of(hi[j], v[0][j], v[1][j]), v[2][j], v[2][j]);
-            lo[j] = min_of(min_of(lo[j], v[0][j], v[1][j]), v[2][j], v[2][j]);
-        }
+        for (int j = 0; j < E; ++j) hi[j] = max_of(hi[j], u[j], v[j]), lo[j] = min_of(lo[j], u[j], v[j]);
     }
     uint32_t most = 0;                // of the magnitudes' bits: an infinity or NaN is the largest
 #pragma unroll
@@ -241,6 +238,7 @@ __global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_
     // registers wait in L1, which the attention's shared memory leaves small: 46 in place of 30 us beside it.)
     const int step = kSelectWarps * a.cluster, first_tile = rank * kSelectWarps + warp;
     const uint64_t policy = l2_evict_first();
+    const uint32_t stride = (uint32_t)a.bounds_stride;            // below 2^31
     auto page_of = [&](int tile) {
         const int at = tile * 16 + (lane & 15);
         return choose && at < count ? table[at] : 0;
@@ -259,12 +257,13 @@ __global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_
             const bool there = (uint32_t)page < (uint32_t)a.n_pages;
             if (!there && a.status) atomicOr(a.status, WICI_BAD_PAGE);
             const int p = there ? page : 0;                       // (of page 0, not used)
+            const uint32_t to = rows_at + stage * 16 * ROW + lane_to;
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i) {
                 const int of = __shfl_sync(0xffffffffu, p, i * (32 / CHUNKS) + lane / CHUNKS);
-                cp_async16(rows_at + stage * 16 * ROW + lane_to + i * 512, of_lane + of * a.bounds_stride, policy);
+                cp_async16(to + i * 512, of_lane + (uint64_t)(uint32_t)of * stride, policy);
             }
-            const float scale = *(const float *)(of_scale + p * a.bounds_stride);
+            const float scale = *(const float *)(of_scale + (uint64_t)(uint32_t)p * stride);
             asm volatile("cp.async.commit_group;" ::: "memory");
             return Asked{scale, there};
         }
@@ -577,7 +576,7 @@ const char *check_bounds(const wici_kv_bounds *b, const wici_kv_cache *c) {
     if (!b->data || ((uintptr_t)b->data & 15)) return "bounds data null or not 16-byte aligned";
     if (b->page_stride % 16 || b->page_stride < wici_kv_bounds_bytes(c->n_kv_heads, c->head_dim))
         return "bounds page_stride must be a multiple of 16 and at least a record";
-    if (b->page_stride > INT64_MAX / kMaxPages) return "bounds page_stride";
+    if (b->page_stride > INT32_MAX) return "bounds page_stride must be below 2^31";
     return nullptr;
 }
 
