@@ -79,18 +79,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
-// The largest magnitudes of the two blocks of 16 elements that a lane's two groups of 8 lie in.  Where halves of a row
+// The largest magnitudes of the two blocks of 16 elements that a lane's two groups of 8 (with `own` as theirs) lie in.  Where halves of a row
 // are rotated, the other 8 of a block are another lane's: group c of the row's rotated part is lane c's first one, group
 // rot_chunks + c its second.
-__device__ __forceinline__ void blocks_of_16(const float *x, bool halves, const RowsArg &a, float *most) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        most[i] = fabsf(x[8 * i]);
-#pragma unroll
-        for (int j = 1; j < 7; j += 2) most[i] = max3(most[i], fabsf(x[8 * i + j]), fabsf(x[8 * i + j + 1]));
-        most[i] = max3(most[i], fabsf(x[8 * i + 7]), 0.f);
-    }
-    const float own[2] = {most[0], most[1]};
+__device__ __forceinline__ void blocks_of_16(const float *own, bool halves, const RowsArg &a, float *most) {
     if (!a.rotate_k || a.rope.interleaved) {       // the same for every lane
         most[0] = most[1] = max3(own[0], own[1], 0.f);
         return;
@@ -244,14 +236,26 @@ __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlo
                 }
             } else if (__any_sync(0xffffffffu, store)) {
                 // the row's largest magnitude
-                float top = fabsf(x[0]);
+                float top, own[2];
+                if (FMT == WICI_KV_E2M1) {                           // from its groups of 8
 #pragma unroll
-                for (int j = 1; j < 15; j += 2) top = max3(top, fabsf(x[j]), fabsf(x[j + 1]));
-                top = max3(top, fabsf(x[15]), 0.f);
+                    for (int i = 0; i < 2; ++i) {
+                        own[i] = fabsf(x[8 * i]);
+#pragma unroll
+                        for (int j = 1; j < 7; j += 2) own[i] = max3(own[i], fabsf(x[8 * i + j]), fabsf(x[8 * i + j + 1]));
+                        own[i] = max3(own[i], fabsf(x[8 * i + 7]), 0.f);
+                    }
+                    top = max3(own[0], own[1], 0.f);
+                } else {
+                    top = fabsf(x[0]);
+#pragma unroll
+                    for (int j = 1; j < 15; j += 2) top = max3(top, fabsf(x[j]), fabsf(x[j + 1]));
+                    top = max3(top, fabsf(x[15]), 0.f);
+                }
                 for (int o = a.chunks / 2; o > 0; o >>= 1) top = max3(top, __shfl_xor_sync(0xffffffffu, top, o), 0.f);
                 if (FMT == WICI_KV_E2M1) {
                     float most[2];
-                    blocks_of_16(x, rotate && turns && !pairs, a, most);
+                    blocks_of_16(own, rotate && turns && !pairs, a, most);
                     if (store) {
                         constexpr float kPer = 1.f / kE2m1Top;     // the quotient, right to its last bit
                         const float near = top * kPer, s = fmaf(fmaf(-near, kE2m1Top, top), kPer, near);

@@ -188,15 +188,17 @@ __device__ __forceinline__ uint32_t quantise_e2m1(const float *x, float b, float
     const float r = b > 0.f ? reciprocal(b * scale) : 0.f;
     uint32_t lo = encode_e2m1(x, r * kNearLo);
     const uint32_t hi = encode_e2m1(x, r * kNearHi);
-    if (lo != hi) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t c = lo >> 4 * j & 7;  // the lower neighbour, where they differ
-            if (((lo ^ hi) >> 4 * j & 15) == 0) continue;
-            const float middle = c < 4 ? 0.25f + 0.5f * (float)c : c == 4 ? 2.5f : c == 5 ? 3.5f : 5.f;
-            const float over = fmaf(-middle * b, scale, fabsf(x[j]));
-            if (over > 0.f || (over == 0.f && (c & 1))) lo += 1u << 4 * j;
-        }
+    // values of few bits are often on a middle: one lane or two of most warps have one, so it is one place at a time (all 8
+    // in turn: 34 in place of 32 us for 16384 tokens of 16 rows in bf16; 25 without the test)
+    for (uint32_t differ = lo ^ hi; differ;) {
+        const int at = (31 - __clz(differ)) & ~3, j = at >> 2;
+        differ &= (1u << at) - 1;
+        const float x0 = j & 1 ? x[1] : x[0], x2 = j & 1 ? x[3] : x[2], x4 = j & 1 ? x[5] : x[4], x6 = j & 1 ? x[7] : x[6];
+        const float x04 = j & 4 ? x4 : x0, x26 = j & 4 ? x6 : x2, xj = j & 2 ? x26 : x04;
+        const uint32_t c = lo >> at & 7;         // the lower neighbour
+        const float middle = c < 4 ? 0.25f + 0.5f * (float)c : c == 4 ? 2.5f : c == 5 ? 3.5f : 5.f;
+        const float over = fmaf(-middle * b, scale, fabsf(xj));
+        if (over > 0.f || (over == 0.f && (c & 1))) lo += 1u << at;
     }
     return lo;
 }
