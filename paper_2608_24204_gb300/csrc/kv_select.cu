@@ -167,8 +167,7 @@ struct SelectArg {
     int cluster, stages;
 };
 
-constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
-constexpr int kSelectWaves = 1;
+constexpr int kSelectWaves = 1, kSmallFrom = 4, kSmallPages = 1 << 14;
 constexpr int kMaxSelectPages = 1 << 14;   // of a sequence: their scores stand in shared memory
 constexpr int kMaxKeep = 1 << 12;          // and the selected ones
 constexpr uint32_t kListed = 256;          // keys that are compared one with another, rather than counted
@@ -178,8 +177,8 @@ constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr uint32_t kForced = 0xFFFFFFFFu;  // in the place of a score: above every one
 constexpr uint32_t kFirst = 0xFF800000u;   // +infinity's
 
-constexpr size_t select_smem(int d, int group, int max_pages, int keep, int stages) {
-    return (size_t)kSelectWarps * stages * 16 * 2 * d + (size_t)(group + 7) / 8 * (2 * d / 16 * 256 + 8 * 12) + ((size_t)max_pages + 31) / 32 * 128 + (size_t)keep * 2;
+constexpr size_t select_smem(int d, int warps, int group, int max_pages, int keep, int stages) {
+    return (size_t)warps * stages * 16 * 2 * d + (size_t)(group + 7) / 8 * (2 * d / 16 * 256 + 8 * 12) + ((size_t)max_pages + 31) / 32 * 128 + (size_t)keep * 2;
 }
 
 // Scores in the order of unsigned integers; NaN, which no page should have, stands with +infinity
@@ -189,7 +188,7 @@ __device__ __forceinline__ uint32_t order_of(float s) {
     return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
 constexpr size_t kSelectSmem = 216 * 1024;   // at most, beside what the kernel has of its own
-static_assert(select_smem(128, kMaxSelectGroup, kMaxSelectPages, kMaxKeep, 1) <= kSelectSmem, "the largest call");
+static_assert(select_smem(128, 16, kMaxSelectGroup, kMaxSelectPages, kMaxKeep, 1) <= kSelectSmem, "the largest call");
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint64_t policy) {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
@@ -211,8 +210,9 @@ __device__ __forceinline__ void store_to_first(uint32_t addr, uint32_t v) {
                  : "memory");
 }
 
-template <int D>
-__global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_constant__ SelectArg a) {
+template <int D, int kSelectThreads>
+__global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_kernel(const __grid_constant__ SelectArg a) {
+    constexpr int kSelectWarps = kSelectThreads / 32;
     constexpr int STEPS = 2 * D / 16, ROW = 2 * D;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ uint32_t part[2][kSelectWarps], bins[kBins], ends[2][8 * kSelectWarps], listed;
@@ -553,6 +553,17 @@ __global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_
     }
 }
 
+template <int D>
+cudaError_t limit_select(int most) {
+    const cudaError_t e = cudaFuncSetAttribute(select_kernel<D, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return e == cudaSuccess ? cudaFuncSetAttribute(select_kernel<D, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) : e;
+}
+template <int D>
+cudaError_t launch_select(int threads, dim3 grid, size_t smem, cudaStream_t st, const SelectArg &a) {
+    return threads == 128 ? launch_kernel(select_kernel<D, 128>, grid, 128, smem, st, a.cluster, true, a)
+                          : launch_kernel(select_kernel<D, 512>, grid, 512, smem, st, a.cluster, true, a);
+}
+
 struct Device {
     int sms;
 };
@@ -564,8 +575,8 @@ int device_of(Device *d) {
     if (e == cudaSuccess)
         e = g_devices.get(dev, d, [dev](Device *x) {
             constexpr int kMost = kSelectSmem;
-            cudaError_t e1 = cudaFuncSetAttribute(select_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-            if (e1 == cudaSuccess) e1 = cudaFuncSetAttribute(select_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+            cudaError_t e1 = limit_select<64>(kMost);
+            if (e1 == cudaSuccess) e1 = limit_select<128>(kMost);
             return e1 == cudaSuccess ? cudaDeviceGetAttribute(&x->sms, cudaDevAttrMultiProcessorCount, dev) : e1;
         });
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "select setup: %s", cudaGetErrorString(e));
@@ -674,17 +685,18 @@ int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_
     a.first = shape->first;
     a.recent = shape->recent;
     a.q_dtype = q->dtype;
-    // Blocks of a cluster, one an SM: as many as there are SMs for, and pages for a tile a warp
+    // Blocks of 16 warps where sequences and heads do not fill the SMs by themselves, of 4 where they do
+    const int64_t pairs = (int64_t)a.kv_heads * shape->batch;
+    const int threads = pairs > kSmallFrom * dev.sms / 4 && a.max_pages <= kSmallPages ? 128 : 512, warps = threads / 32;
+    // Blocks of a cluster: as many as there are SMs for, and pages for a tile a warp
     a.cluster = 1;
-    while (a.cluster < 8 && (int64_t)2 * a.cluster * a.kv_heads * shape->batch <= kSelectWaves * dev.sms &&
-           a.cluster * kSelectWarps * 16 < shape->max_pages)
+    while (a.cluster < 8 && 2 * a.cluster * pairs * threads <= (int64_t)512 * kSelectWaves * dev.sms && a.cluster * warps * 16 < a.max_pages)
         a.cluster *= 2;
     const dim3 grid((unsigned)(a.cluster * a.kv_heads), (unsigned)shape->batch);
-    a.stages = select_smem(cache->head_dim, a.group, a.max_pages, a.keep, 2) <= kSelectSmem ? 2 : 1;
-    const size_t smem = select_smem(cache->head_dim, a.group, a.max_pages, a.keep, a.stages);
+    a.stages = select_smem(cache->head_dim, warps, a.group, a.max_pages, a.keep, 2) <= kSelectSmem / (512 / threads) ? 2 : 1;
+    const size_t smem = select_smem(cache->head_dim, warps, a.group, a.max_pages, a.keep, a.stages);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const cudaError_t e = cache->head_dim == 64 ? launch_kernel(select_kernel<64>, grid, kSelectThreads, smem, st, a.cluster, true, a)
-                                                : launch_kernel(select_kernel<128>, grid, kSelectThreads, smem, st, a.cluster, true, a);
+    const cudaError_t e = cache->head_dim == 64 ? launch_select<64>(threads, grid, smem, st, a) : launch_select<128>(threads, grid, smem, st, a);
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "select: %s", cudaGetErrorString(e));
 }
 
