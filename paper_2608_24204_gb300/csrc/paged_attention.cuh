@@ -100,6 +100,13 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, int by
                  "l"(policy)
                  : "memory");
 }
+// the same where `there`, without a branch
+__device__ __forceinline__ void cp_async16_if(bool there, uint32_t dst, const void *src, int bytes, uint64_t policy) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "@p cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;\n\t}" ::"r"(dst), "l"(src), "r"(bytes), "l"(policy),
+                 "r"((uint32_t)there)
+                 : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() {
@@ -570,7 +577,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             const int bytes = src[p] ? 16 : 0;
 #pragma unroll
             for (int i = 0; i < N; ++i) cp_async16(dst + lane_dst + (p * S::kBlock + i * 512), from + i * 512, bytes, policy);
-            if (lane < TAIL) cp_async16(dst + tail_dst + p * S::kBlock, from + kKvPage * ROW, bytes, policy);
+            cp_async16_if(lane < TAIL, dst + tail_dst + p * S::kBlock, from + kKvPage * ROW, bytes, policy);
         }
     };
     // group j: K of unit j and V of the one before it (none past the last unit: the groups still count)

@@ -4,10 +4,16 @@
 Bounds and scores are defined by whole numbers and single fp32 roundings: codes, scales and selections have to be equal.
 Attention's tolerances are those of tests/test_gpu_ops.py.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
 from oracle import paged
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 pytestmark = pytest.mark.gpu
 
@@ -156,7 +162,8 @@ def test_selection_and_attention_over_it(dtype, fmt, kv, group, d, lengths, keep
     check_selected(cache, bounds, q, pages, lengths, vals, keep, first, recent, dtype)
 
 
-@pytest.mark.parametrize("n,keep,batch,kv,d", [(20000, 40, 1, 1, 64), (9000, 100, 3, 2, 128), (3000, 8, 40, 1, 64), (2000, 16, 24, 8, 64)])
+@pytest.mark.parametrize("n,keep,batch,kv,d", [(20000, 40, 1, 1, 64), (9000, 100, 3, 2, 128), (3000, 8, 40, 1, 64), (2000, 16, 24, 8, 64),
+                                                (6000, 30, 20, 8, 128), (9000, 50, 50, 8, 64), (100000, 900, 2, 1, 64)])
 def test_long_contexts_and_many_sequences(n, keep, batch, kv, d):
     # every number of blocks that share a sequence
     rng = np.random.default_rng(n)
@@ -212,6 +219,83 @@ def test_equal_scores_go_to_the_first_pages():
     bounds.scales.zero_()
     bounds.select(q, pages, ints([1600]), 20, first=0, recent=4, blocks=blocks)
     assert blocks[0, 0].tolist() == list(range(16)) + [96, 97, 98, 99]
+
+
+@pytest.mark.parametrize("kinds", [1, 2, 5])
+@pytest.mark.parametrize("huge", [False, True])
+def test_many_equal_scores_of_a_few_kinds(kinds, huge):
+    # more of them than are compared one by one, in one bin; scores whose differences fp32 does not hold
+    rng = np.random.default_rng(kinds)
+    n, d = 3000, 64
+    cache = PagedKV(1, d, "bf16", n_pages=n)
+    bounds = KeyBounds(cache)
+    bounds.codes.fill_(100)
+    size = (np.array([1.0, 1.0 + 2.0 ** -23, 1.0 + 2.0 ** -22, 0.999, 3.0]) * (1e30 if huge else 1.0)).astype(np.float32)
+    scales = size[rng.integers(0, kinds, n)]
+    if huge:
+        scales[::7] = np.nan
+    bounds.scales.copy_(torch.tensor(scales, device="cuda")[:, None])
+    q = torch.full((1, 1, d), 1e10, device="cuda") * torch.where(torch.arange(d, device="cuda") % 2 == 0, 1.0, -1.0)
+    q[..., :2] = 1e10
+    pages = ints(rng.permutation(n)[None])
+    for keep in (3, 500, 1400, 2999):
+        blocks = torch.empty(1, 1, keep, dtype=torch.int32, device="cuda")
+        chosen, held = bounds.select(q, pages, ints([16 * n - 5]), keep, first=1, recent=1, blocks=blocks)
+        scores = paged.page_scores(f64(q)[0], bounds.codes[:1, 0].cpu().numpy().repeat(n, 0), scales[pages[0].cpu().numpy()])
+        want = paged.selected_pages(scores, keep, 1, 1)
+        assert blocks[0, 0].tolist() == want
+        assert chosen[0, 0].tolist() == pages[0, want].tolist() and held.tolist() == [16 * keep - 5]
+
+
+def test_the_largest_call():
+    """The most pages, pages to select and query heads of a KV head."""
+    n, keep, d, group = 16384, 4096, 128, 64
+    cache = PagedKV(1, d, "e2m1", n_pages=n)
+    bounds = KeyBounds(cache)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    bounds.codes.copy_(torch.randint(-127, 128, bounds.codes.shape, generator=g, device="cuda", dtype=torch.int32))
+    bounds.scales.copy_(torch.rand(bounds.scales.shape, generator=g, device="cuda") + 0.5)
+    q = torch.randn((1, group, d), generator=g, device="cuda")
+    pages = torch.randperm(n, generator=g, device="cuda").int()[None]
+    blocks = torch.empty(1, 1, keep, dtype=torch.int32, device="cuda")
+    chosen, held = bounds.select(q, pages, ints([16 * n]), keep, first=3, recent=5, blocks=blocks)
+    m = q.abs().amax(-1, keepdim=True)
+    w = (q * (m.reciprocal() * 1023.0)).round().double()[0]
+    c = bounds.codes[pages[0].long(), 0].double()
+    score = ((w.clamp_min(0) @ c[:, 0].T + w.clamp_max(0) @ c[:, 1].T).float() * m[0]).amax(0) * bounds.scales[pages[0].long(), 0]
+    want = paged.selected_pages(score.cpu().numpy(), keep, 3, 5)
+    assert blocks[0, 0].tolist() == want and held.tolist() == [16 * keep]
+    assert torch.equal(chosen[0, 0], pages[0, torch.tensor(want, device="cuda")])
+
+
+def test_first_calls_of_a_process_inside_a_capture():
+    """Set-up that a first call makes must not need a call before the capture (attention's is made with the cache)."""
+    code = """
+import torch
+from paper_2608_24204_gb300 import KeyBounds, PagedKV
+cache = PagedKV(2, 64, "e2m1", n_pages=200)
+bounds = KeyBounds(cache)
+q = torch.randn(1, 4, 64, device="cuda")
+pages, n = torch.arange(200, device="cuda", dtype=torch.int32)[None], torch.tensor([3200], device="cuda", dtype=torch.int32)
+k = torch.randn(3200, 2, 64, device="cuda")
+slots = torch.arange(3200, device="cuda", dtype=torch.int32)
+last = torch.arange(15, 3200, 16, device="cuda", dtype=torch.int32)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    cache.append(k, k, slots)
+    bounds.update(last)
+    chosen, held = bounds.select(q, pages, n, 20)
+    out = cache.attend(q, chosen, held)
+graph.replay()
+torch.cuda.synchronize()
+cache.check()
+chosen2, held2 = bounds.select(q, pages, n, 20)
+assert torch.equal(chosen, chosen2) and held2.item() == 320 and torch.equal(out, cache.attend(q, chosen2, held2))
+print("fine")
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stdout + r.stderr
 
 
 def test_largest_products_stay_exact():
