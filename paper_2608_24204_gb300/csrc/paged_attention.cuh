@@ -662,14 +662,25 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
         const int row0 = seg.head % a.tiles * HT, rows = min(HT, a.group - row0);   // first query of the tile in the group
         const int head0 = seg.head / a.tiles * a.group + row0, seg_b = seg.b;
 
-        // what ends in the block's first run is the block's whole part of its segment
-        const bool entered = seg.start < r0, left = seg.end > r1, to_piece = !left && r0 == u0;
-        float *part_at = to_piece ? a.pieces + (int64_t)blockIdx.x * 2 * attn_piece_floats(D) : part_of(warp, left);
-        const int part_row = to_piece ? D : S::kPartRow;
-        float2 *part_ml = (float2 *)(part_at + (to_piece ? kAttnPieceRows * D : HT * S::kPartRow));
-        auto ring_is_free = [&]() {                           // no unit follows
-            cp_wait<0>();
-            if (lane == 0) sh.leaving[warp] = seg;
+        // where the part of a segment that this run shares goes, and its rows' m and l
+        struct Part {
+            float *at;
+            int row;
+            float2 *ml;
+        };
+        auto leave = [&](bool left) {
+            if (left) {
+                cp_wait<0>();                               // the ring is free: no unit follows
+                if (lane == 0) sh.leaving[warp] = seg;
+            }
+            __syncwarp();
+            // what ends in the block's first run is the block's whole part of its segment
+            const bool to_piece = !left && r0 == u0;
+            Part p;
+            p.at = to_piece ? a.pieces + (int64_t)blockIdx.x * 2 * attn_piece_floats(D) : part_of(warp, left);
+            p.row = to_piece ? D : S::kPartRow;
+            p.ml = (float2 *)(p.at + (to_piece ? kAttnPieceRows * D : HT * S::kPartRow));
+            return p;
         };
 
         if constexpr (E2M1) {
@@ -940,8 +951,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             }
 
             // ---- the segment's state, or this run's part of it: of queries 2 t, 2 t + 1 elements PER g .. PER g + PER - 1 ----
-            if (left) ring_is_free();
-            __syncwarp();
+            const bool entered = seg.start < r0, left = seg.end > r1;
+            const Part to = leave(left);
 #pragma unroll
             for (int r = 0; r < C; ++r) {
 #pragma unroll
@@ -956,10 +967,10 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[j] = o[(i + j) / 2][r >> 1][2 * (j & 1) + (r & 1)] * f;
                     if (alone) store_out4(a, seg_b, head0 + row, PER * g + i, v);
-                    else *(float4 *)(part_at + row * part_row + PER * g + i) = make_float4(v[0], v[1], v[2], v[3]);
+                    else *(float4 *)(to.at + row * to.row + PER * g + i) = make_float4(v[0], v[1], v[2], v[3]);
                 }
                 if (g == 0) {
-                    if (!alone) part_ml[row] = make_float2(m[r], l[r]);
+                    if (!alone) to.ml[row] = make_float2(m[r], l[r]);
                     else if (a.lse) a.lse[(int64_t)seg_b * a.q_heads + head0 + row] = (m[r] + log2f(l[r])) * 0.693147180559945309417f;
                 }
             }
@@ -1250,8 +1261,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             }
 
             // ---- the segment's state, or this run's part of it ----
-            if (left) ring_is_free();
-            __syncwarp();
+            const bool entered = seg.start < r0, left = seg.end > r1;
+            const Part to = leave(left);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
@@ -1272,11 +1283,11 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         if (alone) store_out4(a, seg_b, head0 + row, d0 + PER * c, v[c]);
-                        else *(float4 *)(part_at + row * part_row + d0 + PER * c) = make_float4(v[c][0], v[c][1], v[c][2], v[c][3]);
+                        else *(float4 *)(to.at + row * to.row + d0 + PER * c) = make_float4(v[c][0], v[c][1], v[c][2], v[c][3]);
                     }
                 }
                 if (t == 0) {
-                    if (!alone) part_ml[row] = make_float2(m[r], l[r]);
+                    if (!alone) to.ml[row] = make_float2(m[r], l[r]);
                     else if (a.lse) a.lse[(int64_t)seg_b * a.q_heads + head0 + row] = (m[r] + log2f(l[r])) * 0.693147180559945309417f;
                 }
             }
