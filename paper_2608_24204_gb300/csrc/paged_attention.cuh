@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
     int issued = 0;                       // K's of units issued; V's follow one behind
     uint32_t k_to = ring, v_to = ring + KS * S::kSlot;   // their slots
     uint32_t bad_units = 0;               // bit i % 32: unit i has a bad page
-    const uint8_t *last_src[P];           // of the unit before: K of its head in each page (null: no page), its rows
+    const uint8_t *last_src[P] = {};      // of the unit before: K of its head in each page (null: no page), its rows
     int last_first = 0, last_end = 0;     // (end 0: no unit)
 
     const uint64_t policy = l2_evict_first();   // read once: code, queries and parts stay in L2 instead
@@ -586,13 +586,13 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             cur = next;
             next = describe(issued + 32 + lane);
         }
-        if (last_end) {
-            if constexpr (E2M1) copy_whole(v_to, last_src, lane_v);
-            else copy_unit(v_to, last_src, lane_v, last_first, last_end);
-        }
+        // (e2m1: a unit past the last one has no pages; its zeros go where nothing is read)
+        if constexpr (E2M1) {
+            if (issued) copy_whole(v_to, last_src, lane_v);
+        } else if (last_end) copy_unit(v_to, last_src, lane_v, last_first, last_end);
         if (issued) v_to = v_to == ring + (KS + VS - 1) * S::kSlot ? ring + KS * S::kSlot : v_to + S::kSlot;
         last_end = 0;
-        if (issued < mine) {
+        if (E2M1 || issued < mine) {
             const int info = __shfl_sync(0xffffffffu, cur.info, issued & 31);
             int first = info >> 16 & 255, end = info >> 24;
             const uint8_t *head = a.cache.data + (int64_t)((info & 0xFFFF) * S::kBlock);
@@ -697,7 +697,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             float cq[C];                                      // products to base-2 logits, of queries 2 t, 2 t + 1
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
-                float x[STEPS][4], of_g = a.scale * 1.44269504088896340736f;
+                // a negative scale's sign goes to q, and so does a scale of 0: cq is positive
+                float x[STEPS][4], of_g = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896340736f;
                 uint32_t top = 0;
 #pragma unroll
                 for (int i = 0; i < STEPS / 2; ++i) unpack_q8<QW>(a.q_dtype, qx[n][i], x[2 * i]);
@@ -710,8 +711,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 // 2^(13 - exponent): the largest magnitude to [2^13, 2^14)
                 int e = (int)(top >> 23) - 127 - 13;
                 e = top >= kInfBits || top == 0 ? 0 : max(-126, min(126, e));
-                const float down = __int_as_float((127 - e) << 23);
-                of_g *= __int_as_float((127 + e) << 23);
+                const float down = a.scale == 0.f ? 0.f : copysignf(__int_as_float((127 - e) << 23), a.scale);
+                of_g = fmaxf(of_g * __int_as_float((127 + e) << 23), 0x1p-126f);
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
                     uint32_t w[2][TQ];
@@ -801,13 +802,13 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 cp_wait<KS - 2>();
                 __syncwarp();
                 const uint32_t ks_next = ks == ring + (KS - 1) * S::kSlot ? ring : ks + S::kSlot;
-                float x[C][J];                                // queries 2 t + r % 2 of tile r / 2, keys key_at(j)
+                float x[C][J];                                // queries 2 t + r % 2 of tile r / 2, keys key_at(j); cq is still to come
                 const bool part = key0 < keys.lo || key0 > keys.n - UNIT;   // not every key of the unit is the sequence's
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     const float ksc = lds32(ks + (j >> 1) * S::kBlock + SCALES_AT + (j & 1) * 32 + 4 * g);
 #pragma unroll
-                    for (int r = 0; r < C; ++r) x[r][j] = c[j >> 1][r >> 1][2 * (j & 1) + (r & 1)] * (ksc * cq[r]);
+                    for (int r = 0; r < C; ++r) x[r][j] = c[j >> 1][r >> 1][2 * (j & 1) + (r & 1)] * ksc;
                 }
                 if (part) {
 #pragma unroll
@@ -824,7 +825,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     float top = x[r][0];
 #pragma unroll
                     for (int j = 1; j < J; ++j) top = fmaxf(top, x[r][j]);
-                    up[r] = fmaxf(m[r], largest(top));
+                    up[r] = fmaxf(m[r], largest(top) * cq[r]);
                     grew |= up[r] > m[r] + kLag;
                 }
                 if (__any_sync(0xffffffffu, grew)) {
@@ -850,7 +851,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     const float vscale = lds32(vs + (j >> 1) * S::kBlock + SCALES_AT + (j & 1) * 32 + 4 * g);
 #pragma unroll
                     for (int r = 0; r < C; ++r) {
-                        const float p = ex2(x[r][j] - ref[r]);
+                        const float p = ex2(fmaf(x[r][j], cq[r], -ref[r]));
                         l[r] += p;
                         x[r][j] = p * vscale;
                     }

@@ -251,6 +251,68 @@ def test_attention_at_every_window_around_a_units_ends(d):
         check_attention(cache, q, pages, lengths, vals, d ** -0.5, window, out, None, "f32")
 
 
+@pytest.mark.parametrize("dtype,group,d", [("f32", 4, 64), ("bf16", 3, 128), ("f16", 12, 128)])
+def test_scales_of_either_sign_and_none(dtype, group, d):
+    # lengths that end inside a unit: keys that are left out, beside a scale of zero and very small ones
+    rng = np.random.default_rng(13)
+    cache, q, pages, vals = attention_case(rng, 2, 2, group, d, dtype, [100, 37], spread=8.0)
+    v_scales = paged.unpack_e2m1(cache.data.cpu().numpy(), 2, d)[2][:, 1].astype(np.float64)
+    q64 = f64(q)
+    for scale in (1.0, 0.0, -0.5, 1e-30, -1e-44, -0.0):
+        lse = torch.empty(q.shape[:2], device="cuda")
+        out = cache.attend(q, ints(pages), ints([100, 37]), scale=scale, lse=lse)
+        scale = float(np.float32(scale))
+        want, want_lse, weight = paged.paged_attention(q64, vals[:, 0], vals[:, 1], pages, [100, 37], scale)
+        for b, n in enumerate([100, 37]):
+            slots = pages[b][np.arange(n) // 16] * 16 + np.arange(n) % 16
+            for h in range(2 * group):
+                k, v, s = vals[slots, 0, h // group], vals[slots, 1, h // group], v_scales[slots, h // group]
+                x = k @ q64[b, h] * scale
+                p = np.exp(x - want_lse[b, h])
+                # the terms of check_attention, and what the scores far apart here bring out: a key's weight times its scale
+                # of V is held to 2^-32 of the largest such product, and what is lost of it counts v / scale times
+                ds = float(np.max(np.abs(k) @ np.abs(q64[b, h])) * abs(scale)) * (2 * d * 2.0 ** -23 + (2.0 ** -16 if dtype == "f32" else 0.0))
+                rel = 2 * ds + 2.0 ** -16 + 2.0 ** -21 + n * 2.0 ** -23
+                small = 2.0 ** -32 * (p * s).max() * (np.abs(v) / s[:, None]).sum(0)
+                within(f64(out[b, h]), want[b, h], rel * weight[b, h] + small * (1 + rel) + half_step(want[b, h], dtype), f"scale {scale}")
+                within(float(lse[b, h]), want_lse[b, h], ds + 2.0 ** -20 + n * 2.0 ** -23 + 2.0 ** -23 * abs(want_lse[b, h]), f"lse, scale {scale}")
+
+
+def test_queries_that_are_not_finite_stay_in_their_rows():
+    rng = np.random.default_rng(14)
+    cache, q, pages, vals = attention_case(rng, 2, 1, 12, 128, "bf16", [100, 37])
+    kept = q.clone()
+    q[0, 3, 5], q[1, 9, 0] = float("nan"), float("inf")
+    out = cache.attend(q, ints(pages), ints([100, 37]))
+    assert bool(torch.isnan(out[0, 3]).all()) and bool(torch.isnan(out[1, 9]).all())
+    out[0, 3], out[1, 9] = cache.attend(kept, ints(pages), ints([100, 37]))[[0, 1], [3, 9]]
+    check_attention(cache, kept, pages, [100, 37], vals, 128 ** -0.5, 0, out, None, "bf16")
+
+
+@pytest.mark.parametrize("shift,score", [(20, -70.0), (34, -70.0), (-40, 20.0)])
+@pytest.mark.parametrize("dtype,group,n", [("bf16", 4, 300), ("f32", 3, 300), ("bf16", 12, 300)])
+def test_one_key_whose_v_is_of_another_size_than_the_others(dtype, group, n, shift, score):
+    """Its weight is e^score of the others', its values 2^shift times theirs: what is lost is 2^-22 of a key's part or 2^-32 of the
+    largest one's."""
+    rng = np.random.default_rng(40)
+    d, odd = 64, 137
+    cache = PagedKV(1, d, "e2m1", n_pages=n // 16 + 1)
+    k, v = torch.zeros(n, 1, d, device="cuda"), randn(rng, n, 1, d)
+    k[odd, 0, 0] = score
+    v[odd] *= 2.0 ** shift
+    cache.append(k, v, ints(range(n)))
+    kk, vv = (f64(t)[:, 0] for t in cache.read(ints(range(n)), dtype=torch.float32))
+    q = torch.zeros(1, group, d, device="cuda")
+    q[..., 0] = 1.0
+    out = cache.attend(q.to(DT[dtype]), ints(np.arange(n // 16 + 1)[None]), ints([n]), scale=1.0, out=torch.empty(1, group, d, device="cuda"))
+    p = np.exp(kk[:, 0] - kk[:, 0].max())
+    p /= p.sum()
+    part = p[:, None] * np.abs(vv)
+    top = (p * np.abs(vv).max(1)).max()
+    # exponent, sums and their join: 2^-16 of each part as in the other tests; of the heaviest key's weight 2^-32 a key
+    within(f64(out[0]), np.broadcast_to(p @ vv, (group, d)), 2.0 ** -16 * part.sum(0) + n * 2.0 ** -32 * top + 1e-30, "out")
+
+
 def test_attention_of_many_ragged_sequences():
     rng = np.random.default_rng(12)
     lengths = rng.integers(0, 120, 300)
