@@ -6,7 +6,9 @@
 // of few tokens.  Measured (device time): rotation of 8192 tokens of 40 heads of 128 in bf16
 // 28.3 us, 5.9 TB/s (a copy of that size: 6.4); append of 16384 tokens, 32 q heads rotated, 8 k
 // and v heads to e4m3, 69.1 us, 5.4 TB/s, of which its arithmetic is 3 us; read of 30011 tokens from
-// e4m3 to bf16 32.1 us, 5.8 TB/s; one token of a step 2.3 to 3.4 us.
+// e4m3 to bf16 32.1 us, 5.8 TB/s; one token of a step 2.3 to 3.4 us.  From and to e2m1: append of 16384 tokens, 8 k and v
+// heads in bf16, 31.7 us, 2.7 TB/s, bound by its instructions (two conversions an element, and a look at those that lie on
+// a middle: 25 us without it); read of 30011 tokens to bf16 30.6 us, 5.2 TB/s.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -103,7 +105,8 @@ __device__ __forceinline__ void blocks_of_16(const float *own, bool halves, cons
 // and turn, through shared memory; then a thread keeps its token, with its chunk's cosines and
 // sines in registers, and walks over the token's heads: what is left for a row is its loads (issued
 // before the row ahead of it is worked on), the arithmetic and its stores.  Lanes of a warp take
-// neighbouring heads of a token: a packed row's heads lie side by side.
+// neighbouring heads of a token: a packed row's heads lie side by side.  (e2m1 has 80 registers in place of 64, where it
+// would spill: append of 1251 tokens, 8 k and v heads of 64, fp32 4.1 us, 5.3 with 64.)
 template <typename T, int FMT, int PATH>
 __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlocks) rows_kernel(const __grid_constant__ RowsArg a) {
     constexpr bool WIDE = PATH != NARROW;
@@ -261,12 +264,23 @@ __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlo
                         const float near = top * kPer, s = fmaf(fmaf(-near, kE2m1Top, top), kPer, near);
                         const bool finite = top < __uint_as_float(kInfBits), some = finite && s >= kE2m1Least;
                         const float per6 = reciprocal(6.f * s);
+                        // given 16-bit values, not rotated ones: one conversion each
+                        const float left = fmaf(-s, kE2m1Top, top), nudge = nudge_of(left);
+                        const bool sure = sizeof(T) == 2 && !rotate && left != 0.f;
                         uint8_t *row = block + where * (d / 2), *each = block + kKvPage * (d / 2) + where * (d / 16);
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const int p = i ? p1 : p0;
-                            const uint32_t b = some ? block_scale(most[i], s, per6) : 0u;
-                            *(uint32_t *)(row + p / 2) = some ? quantise_e2m1(x + 8 * i, e4m3_value(b), s) : 0u;
+                            uint32_t b = 0, codes = 0;
+                            if (some && sure) {
+                                b = __nv_cvt_float_to_fp8(most[i] * (per6 * nudge), __NV_SATFINITE, __NV_E4M3);
+                                const float unit = e4m3_value(b) * s;
+                                codes = encode_e2m1(x + 8 * i, unit > 0.f ? reciprocal(unit) * nudge : 0.f);
+                            } else if (some) {
+                                b = block_scale(most[i], s, per6);
+                                codes = quantise_e2m1(x + 8 * i, e4m3_value(b), s);
+                            }
+                            *(uint32_t *)(row + p / 2) = codes;
                             if ((p & 8) == 0) each[p / 16] = (uint8_t)b;
                         }
                         if (c == 0)

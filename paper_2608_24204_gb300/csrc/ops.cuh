@@ -183,13 +183,19 @@ __device__ __forceinline__ uint32_t encode_e2m1(const float *x, float r) {
         : "f"(x[0] * r), "f"(x[1] * r), "f"(x[2] * r), "f"(x[3] * r), "f"(x[4] * r), "f"(x[5] * r), "f"(x[6] * r), "f"(x[7] * r));
     return w;
 }
+// Quotients of values of 11 bits at most (16-bit types) with the row's largest such value need no second look.  x / (b s)
+// with s = top / 2688 unrounded is 21 X 2^k / (T B), with integers X, T < 2^11 and B < 2^4: it is a middle m / 2^j, m < 2^3,
+// or off by 2^-18 of it and more (2^-16 for a block scale's).  s being off by 2^-24, a quotient within 2^-19 of a middle is
+// that middle moved by s's own rounding, to the same side for a whole row: 2^-20 that way decides it, beside errors of 2^-21.
+// `left`: what top has over 2688 s; 0, where such quotients are middles exactly, is not for this.
+__device__ __forceinline__ float nudge_of(float left) { return left > 0.f ? 1.f + 0x1p-20f : 1.f - 0x1p-20f; }
 // the codes of 8 values under the block scale b (its value) and the head's scale, the first in the lowest bits
 __device__ __forceinline__ uint32_t quantise_e2m1(const float *x, float b, float scale) {
     const float r = b > 0.f ? reciprocal(b * scale) : 0.f;
     uint32_t lo = encode_e2m1(x, r * kNearLo);
     const uint32_t hi = encode_e2m1(x, r * kNearHi);
     // values of few bits are often on a middle: one lane or two of most warps have one, so it is one place at a time (all 8
-    // in turn: 34 in place of 32 us for 16384 tokens of 16 rows in bf16; 25 without the test)
+    // in turn: 34 in place of 32 us for 16384 tokens of 16 rows in bf16, before these had a way of their own)
     for (uint32_t differ = lo ^ hi; differ;) {
         const int at = (31 - __clz(differ)) & ~3, j = at >> 2;
         differ &= (1u << at) - 1;

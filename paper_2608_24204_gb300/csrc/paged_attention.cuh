@@ -38,6 +38,17 @@
 //   scaled by a power of two per head; p times its value's scale as two (22 bits), multiplied by a
 //   power of two per query that follows the largest such weight so far: a weight is off by 2^-22 of
 //   itself or 2^-32 of the largest one, however large the scale of a value is that hardly counts.
+//   4-bit cache: as 8-bit; a code times its block's scale is one fp16 number, exactly.
+//
+// 4-bit codes (E2M1).  Half of an 8-bit cache's bytes for the same arithmetic: this one is bound by the SMs (as fast from
+// L2), by conversions, products with block scales and what keeps them apart.  So the operands change places: S^T = K Q^T and
+// O^T = V^T P^T, with keys and elements of the head as the 16 rows and 8 queries as the columns.  A fragment of converted
+// codes then serves both terms of Q or P (and 16 queries a tile two tiles) at half the products of K, and O takes 32
+// registers in place of 64; P^T comes from the scores by movmatrix.  64 sequences of up to 8192 tokens, five queries a KV
+// head: 93 us (104 with queries as rows), two of 100001 to 131072: 72 us (80), 3.9 TB/s of codes, 750 instructions for 32
+// keys at 0.57 a cycle and scheduler.  Not kept: three blocks on an SM with 168 registers (74 us; beside an append 131 in
+// place of 103, for an append's blocks split the registers that a third block would need), four pages a unit (70.6, but
+// 95.6 for the 64 sequences), five ring slots (the same), two sums for a score or terms of P apart (the same).
 #pragma once
 #include "ops.cuh"
 
@@ -79,7 +90,8 @@ struct AttnShape {
     static constexpr int kRows = STACK ? 8 : 16;                   // queries of a head tile
     static constexpr int kMaxBatch = STACK ? 1024 : 256;           // sequences of a launch: their keys are in shared memory
     // Pages of a unit: 4 to 8 KB of K and V for the work that a unit costs beside its products (bf16, 128: one page
-    // already; 8-bit: one page more a unit took the batch of 64 from 136 to 116 us with 128, from 76 to 74 with 64).
+    // already; 8-bit: one page more a unit took the batch of 64 from 136 to 116 us with 128, from 76 to 74 with 64).  4-bit
+    // codes as 8-bit ones: the work a unit costs counts more than its bytes (half the pages: 48 in place of 42.5 us with 64).
     static constexpr int kPages = FMT == WICI_KV_BF16 ? (D == 128 ? 1 : 2) : (D == 128 ? 2 : 4);
     static constexpr int kBlock = kv_block_bytes(FMT, D);
     static constexpr int kSlot = kPages * kBlock;
