@@ -10,9 +10,11 @@
 // Select.  A cluster of blocks takes one sequence and KV head.  Its blocks score the pages and leave the scores, as
 // integers that order as they do, in the first block's shared memory; that one finds the keep-th largest by
 // counting into bins, and writes the pages from it on in order, of equal ones the first.
-// Measured (device time; 8 KV heads of 128, 4 queries each): 528 pages, 64 kept 8.0 us; 4 sequences of 6250 to 8192 pages,
-// 256 kept 26.7 us, 2.3 TB/s of bounds, of which the scores take 17 and the search and lists of 32 blocks 10; 32 sequences
-// of 125 to 2048 pages, 128 kept 36.8 us: the longest sequences' blocks end last.  Bounds of 4096 pages: e4m3 19.7 us,
+// Measured (device time; 8 KV heads of 128, 4 queries each): 528 pages, 64 kept 7.6 us; 4 sequences of 6250 to 8192 pages,
+// 256 kept 23.7 us, 2.5 TB/s of bounds; 32 sequences of 125 to 2048 pages, 128 kept 33.5 us.  What bounds it is latency: of
+// the 23.7 us 9 pass before scores and between them (lengths, page numbers, rows; a tile's chain from its rows to its
+// keys), 7 while copies are asked for, and 7 are the search and the lists of 32 blocks, in passes of one block each.  From
+// L2 it is as fast.  Bounds of 4096 pages: e4m3 19.7 us,
 // 3.9 TB/s, bf16 23.8 us, 6.5 TB/s, e2m1 24 us; of 64 pages 1.7 to 2.0 us.
 #include <stdarg.h>
 #include <stdio.h>
@@ -168,7 +170,7 @@ struct SelectArg {
     const int32_t *pages, *lengths;
     int32_t *out_pages, *out_lengths, *out_blocks, *status;
     int kv_heads, group, n_pages, max_pages, keep, first, recent, q_dtype;
-    int cluster, stages;
+    int cluster;
 };
 
 constexpr int kMaxSelectPages = 1 << 14;   // of a sequence: their scores stand in shared memory
@@ -180,8 +182,8 @@ constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr uint32_t kForced = 0xFFFFFFFFu;  // in the place of a score: above every one
 constexpr uint32_t kFirst = 0xFF800000u;   // +infinity's
 
-constexpr size_t select_smem(int d, int warps, int group, int max_pages, int keep, int stages) {
-    return (size_t)warps * stages * 16 * 2 * d + (size_t)(group + 7) / 8 * (2 * d / 16 * 256 + 8 * 12) + ((size_t)max_pages + 31) / 32 * 128 + (size_t)keep * 2;
+constexpr size_t select_smem(int d, int warps, int tile, int group, int max_pages, int keep) {
+    return (size_t)warps * tile * 2 * d + (size_t)(group + 7) / 8 * (2 * d / 16 * 256 + 8 * 12) + ((size_t)max_pages + 31) / 32 * 128 + (size_t)keep * 2;
 }
 
 // Scores in the order of unsigned integers; NaN, which no page should have, stands with +infinity
@@ -190,8 +192,8 @@ __device__ __forceinline__ uint32_t order_of(float s) {
     if (s != s) return kFirst;
     return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
-constexpr size_t kSelectSmem = 216 * 1024;   // at most, beside what the kernel has of its own
-static_assert(select_smem(128, 16, kMaxSelectGroup, kMaxSelectPages, kMaxKeep, 1) <= kSelectSmem, "the largest call");
+constexpr size_t kSelectSmem = 217 * 1024;   // at most, beside what the kernel has of its own
+static_assert(select_smem(128, 16, 16, kMaxSelectGroup, kMaxSelectPages, kMaxKeep) <= kSelectSmem, "the largest call");
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint64_t policy) {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
@@ -213,15 +215,15 @@ __device__ __forceinline__ void store_to_first(uint32_t addr, uint32_t v) {
                  : "memory");
 }
 
-template <int D, int kSelectThreads>
+template <int D, int kSelectThreads, int kTile>
 __global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_kernel(const __grid_constant__ SelectArg a) {
-    constexpr int kSelectWarps = kSelectThreads / 32;
+    constexpr int kSelectWarps = kSelectThreads / 32, GROUPS = kTile / 8;   // of 8 pages of a tile
     constexpr int STEPS = 2 * D / 16, ROW = 2 * D;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ uint32_t part[2][kSelectWarps], bins[kBins], ends[2][8 * kSelectWarps], listed;
     const int tiles = (a.group + 7) / 8;
-    const uint32_t rows_at = smem_u32(smem) + threadIdx.x / 32 * a.stages * 16 * ROW;   // this warp's: [stage][page of a tile]
-    __half *qs = (__half *)(smem + kSelectWarps * a.stages * 16 * ROW);                 // [tile][step][lane][4]: B fragments
+    const uint32_t rows_at = smem_u32(smem) + threadIdx.x / 32 * kTile * ROW;   // this warp's: [page of a tile]
+    __half *qs = (__half *)(smem + kSelectWarps * kTile * ROW);                 // [tile][step][lane][4]: B fragments
     float *most = (float *)((uint8_t *)qs + tiles * STEPS * 256); // [tile * 8]: each query's largest magnitude
     float2 *bias = (float2 *)(most + tiles * 8);                  // [tile * 8]: 128 times the sums of its whole numbers
     uint32_t *keys = (uint32_t *)(bias + tiles * 8);              // [page], of the first block
@@ -237,49 +239,40 @@ __global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_k
     const int count = bad || n <= 0 ? 0 : (n + kKvPage - 1) / kKvPage;
     const bool choose = count > a.keep;
     const int32_t *table = a.pages + (int64_t)b * a.max_pages;
-    // A tile is 16 pages; a warp's tiles come through cp.async, one under way while the one before is worked on.  (Loads to
-    // registers wait in L1, which the attention's shared memory leaves small: 46 in place of 30 us beside it.)
+    // A tile is kTile pages, lane l looks after page l (l % 16).  Tiles come through cp.async, the next one asked for when this one has been
+    // read: what waits for it is hidden by other warps, and a second one under way was no faster.  (Loads to registers wait
+    // in L1, which the attention's shared memory leaves small: 46 in place of 30 us beside it.)
     const int step = kSelectWarps * a.cluster, first_tile = rank * kSelectWarps + warp;
     const uint64_t policy = l2_evict_first();
     const uint32_t stride = (uint32_t)a.bounds_stride;            // below 2^31
     auto page_of = [&](int tile) {
-        const int at = tile * 16 + (lane & 15);
+        const int at = tile * kTile + lane % kTile;
         return choose && at < count ? table[at] : 0;
     };
-    constexpr int CHUNKS = ROW / 16, ROUNDS = 16 * CHUNKS / 32;   // of a row; rounds of the warp for a tile
+    constexpr int CHUNKS = ROW / 16, ROUNDS = kTile * CHUNKS / 32;   // of a row; rounds of the warp for a tile
     const uint8_t *const of_lane = a.bounds + h * ROW + lane % CHUNKS * 16;
     const uint8_t *const of_scale = a.bounds + a.kv_heads * ROW + 4 * h;
     // chunks of odd rows with their halves of 128 bytes exchanged: lanes that read 64 bytes of two rows meet all banks
-    const uint32_t lane_to = lane / CHUNKS * ROW + ((lane % CHUNKS ^ (lane / CHUNKS & 1) << 2) << 4);
-    struct Asked {                                                // of page lane % 16 of a tile
+    const uint32_t copy_to = rows_at + lane / CHUNKS * ROW + ((lane % CHUNKS ^ (lane / CHUNKS & 1) << 2) << 4);
+    struct Asked {                                                // of the lane's page
         float scale;                                              // not looked at before it is needed: it is still on its way
         bool there;
     };
-    auto ask = [&](int tile, int page, int stage) {
-        if (tile * 16 < count) {
-            const bool there = (uint32_t)page < (uint32_t)a.n_pages;
-            if (!there && a.status) atomicOr(a.status, WICI_BAD_PAGE);
-            const int p = there ? page : 0;                       // (of page 0, not used)
-            const uint32_t to = rows_at + stage * 16 * ROW + lane_to;
+    auto ask = [&](int tile, int page) {
+        if (tile * kTile >= count) return Asked{0.f, false};
+        const bool there = (uint32_t)page < (uint32_t)a.n_pages;
+        if (!there && a.status) atomicOr(a.status, WICI_BAD_PAGE);
+        const int p = there ? page : 0;                           // (of page 0, not used)
 #pragma unroll
-            for (int i = 0; i < ROUNDS; ++i) {
-                const int of = __shfl_sync(0xffffffffu, p, i * (32 / CHUNKS) + lane / CHUNKS);
-                cp_async16(to + i * 512, of_lane + (uint64_t)(uint32_t)of * stride, policy);
-            }
-            const float scale = *(const float *)(of_scale + (uint64_t)(uint32_t)p * stride);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            return Asked{scale, there};
+        for (int i = 0; i < ROUNDS; ++i) {
+            const int of = __shfl_sync(0xffffffffu, p, i * (32 / CHUNKS) + lane / CHUNKS);
+            cp_async16(copy_to + i * 512, of_lane + (uint64_t)(uint32_t)of * stride, policy);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");      // none: the groups still count
-        return Asked{0.f, false};
+        return Asked{*(const float *)(of_scale + (uint64_t)(uint32_t)p * stride), there};
     };
     int next_page = page_of(first_tile);
-    Asked asked = ask(first_tile, next_page, 0), next = {0.f, false};   // the tile to work on, the one after
+    Asked asked = ask(first_tile, next_page);
     next_page = page_of(first_tile + step);
-    if (a.stages == 2) {
-        next = ask(first_tile + step, next_page, 1);
-        next_page = page_of(first_tile + 2 * step);
-    }
 
     if (choose) {
         for (int i = warp; i < tiles * 8; i += kSelectWarps) {    // one query a warp
@@ -322,31 +315,34 @@ __global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_k
     uint32_t hi = 0, lo = 0xFFFFFFFFu;                            // of this lane's scores that are not forced
     if (choose) {
         const uint32_t keys_at = smem_u32(keys);
-        int stage = 0;
-        const uint32_t row_at = rows_at + g * ROW + 16 * t, even = (g & 1) << 6;
-        for (int tile = first_tile; tile * 16 < count; tile += step) {
-            if (a.stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        const uint32_t row = rows_at + g * ROW + 16 * t, even = (g & 1) << 6;
+        for (int tile = first_tile; tile * kTile < count; tile += step) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();
-            float scale[2], best[2] = {-INFINITY, -INFINITY};
+            float best[GROUPS];                                   // of pages g + 8 r
 #pragma unroll
-            for (int r = 0; r < 2; ++r) scale[r] = __shfl_sync(0xffffffffu, asked.there ? asked.scale : INFINITY, g + 8 * r);
-            const uint32_t row = row_at + stage * 16 * ROW;
+            for (int r = 0; r < GROUPS; ++r) best[r] = -INFINITY;
             for (int q = 0; q < tiles; ++q) {
                 // codes + 128 as they are are fp16's smallest numbers, 2^-24 each: sums of 64 products with whole numbers up
                 // to 1023 stay below 2^24 of them, and 128 times the whole numbers' sum is taken off after
-                float c[2][4] = {};
+                float c[GROUPS / 2][2][4] = {};                   // [16 pages][sums side by side]
                 const uint2 *frag = (const uint2 *)qs + q * STEPS * 32 + lane;
 #pragma unroll
                 for (int i = 0; i < STEPS / 4; ++i) {
                     const uint32_t at = row + (i & 1 ? even ^ 64 : even) + i / 2 * 128;
-                    const uint4 u4 = lds128(at), v4 = lds128(at + 8 * ROW);
-                    const uint32_t u[4] = {u4.x, u4.y, u4.z, u4.w}, v[4] = {v4.x, v4.y, v4.z, v4.w};
+                    uint32_t w[GROUPS][4];
+#pragma unroll
+                    for (int r = 0; r < GROUPS; ++r) {
+                        const uint4 v = lds128(at + 8 * r * ROW);
+                        w[r][0] = v.x ^ 0x80808080u, w[r][1] = v.y ^ 0x80808080u, w[r][2] = v.z ^ 0x80808080u, w[r][3] = v.w ^ 0x80808080u;
+                    }
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
-                        const uint32_t x = u[s] ^ 0x80808080u, y = v[s] ^ 0x80808080u;
-                        mma_f16(c[s & 1], __byte_perm(x, 0, 0x4140), __byte_perm(y, 0, 0x4140), __byte_perm(x, 0, 0x4342),
-                                __byte_perm(y, 0, 0x4342), frag[(4 * i + s) * 32]);
+                        const uint2 f = frag[(4 * i + s) * 32];
+#pragma unroll
+                        for (int k = 0; k < GROUPS / 2; ++k)
+                            mma_f16(c[k][s & 1], __byte_perm(w[2 * k][s], 0, 0x4140), __byte_perm(w[2 * k + 1][s], 0, 0x4140),
+                                    __byte_perm(w[2 * k][s], 0, 0x4342), __byte_perm(w[2 * k + 1][s], 0, 0x4342), f);
                     }
                 }
 #pragma unroll
@@ -355,31 +351,37 @@ __global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_k
                     const float m = most[head];
                     const float2 off = bias[head];
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float dot = fmaf(c[0][2 * r + j], 0x1p24f, -off.x) + fmaf(c[1][2 * r + j], 0x1p24f, -off.y);
+                    for (int r = 0; r < GROUPS; ++r) {
+                        const int x = 2 * (r & 1) + j;
+                        const float dot = fmaf(c[r >> 1][0][x], 0x1p24f, -off.x) + fmaf(c[r >> 1][1][x], 0x1p24f, -off.y);
                         best[r] = fmaxf(best[r], head < a.group ? __fmul_rn(dot, m) : -INFINITY);
                     }
                 }
             }
+            const float of_page = asked.there ? asked.scale : INFINITY;
             __syncwarp();                                         // the rows have been read
-            const Asked s = ask(tile + a.stages * step, next_page, stage);
-            next_page = page_of(tile + (a.stages + 1) * step);
-            if (a.stages == 2) asked = next, next = s, stage ^= 1;
-            else asked = s;
+            asked = ask(tile + step, next_page);
+            next_page = page_of(tile + 2 * step);
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
+            for (int r = 0; r < GROUPS; ++r) {
                 best[r] = fmaxf(best[r], __shfl_xor_sync(0xffffffffu, best[r], 1));
                 best[r] = fmaxf(best[r], __shfl_xor_sync(0xffffffffu, best[r], 2));
-                const int i = tile * 16 + g + 8 * r;
-                uint32_t key = kFirst;                            // a key that is not finite, a page that is not there
-                if (scale[r] == 0.f) key = order_of(0.f);
-                else if (fabsf(scale[r]) < INFINITY) key = order_of(__fmul_rn(best[r], scale[r]));
-                if (i < a.first || i >= count - a.recent) key = kForced;
-                else hi = max(hi, key), lo = min(lo, key);
-                if (t == r && i < count) {
-                    if (a.cluster > 1) store_to_first(keys_at + 4 * i, key);
-                    else keys[i] = key;
-                }
+            }
+            // lane (g, t) has page g + 8 t now (of 16 pages, half of the lanes)
+            const int of_t = t & (GROUPS - 1);
+            float mine = best[0];
+#pragma unroll
+            for (int r = 1; r < GROUPS; ++r) mine = of_t == r ? best[r] : mine;
+            const float scale = __shfl_sync(0xffffffffu, of_page, g + 8 * of_t);
+            const int i = tile * kTile + g + 8 * of_t;
+            uint32_t key = kFirst;                                // a key that is not finite, a page that is not there
+            if (scale == 0.f) key = order_of(0.f);
+            else if (fabsf(scale) < INFINITY) key = order_of(__fmul_rn(mine, scale));
+            if (i < a.first || i >= count - a.recent) key = kForced;
+            else hi = max(hi, key), lo = min(lo, key);
+            if (i < count) {
+                if (a.cluster > 1) store_to_first(keys_at + 4 * i, key);
+                else keys[i] = key;
             }
         }
         hi = __reduce_max_sync(0xffffffffu, hi);
@@ -390,7 +392,7 @@ __global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_k
             else ends[0][at] = hi, ends[1][at] = lo;
         }
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if (rank == 0)
         for (int i = threadIdx.x; i < kBins; i += kSelectThreads) bins[i] = 0;
     if (threadIdx.x == 0) listed = 0;
@@ -558,13 +560,16 @@ __global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_k
 
 template <int D>
 cudaError_t limit_select(int most) {
-    const cudaError_t e = cudaFuncSetAttribute(select_kernel<D, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    return e == cudaSuccess ? cudaFuncSetAttribute(select_kernel<D, 512>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) : e;
+    cudaError_t e = cudaFuncSetAttribute(select_kernel<D, 128, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(select_kernel<D, 512, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(select_kernel<D, 512, 32>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return e;
 }
 template <int D>
-cudaError_t launch_select(int threads, dim3 grid, size_t smem, cudaStream_t st, const SelectArg &a) {
-    return threads == 128 ? launch_kernel(select_kernel<D, 128>, grid, 128, smem, st, a.cluster, true, a)
-                          : launch_kernel(select_kernel<D, 512>, grid, 512, smem, st, a.cluster, true, a);
+cudaError_t launch_select(int threads, int tile, dim3 grid, size_t smem, cudaStream_t st, const SelectArg &a) {
+    if (threads == 128) return launch_kernel(select_kernel<D, 128, 32>, grid, 128, smem, st, a.cluster, true, a);
+    return tile == 32 ? launch_kernel(select_kernel<D, 512, 32>, grid, 512, smem, st, a.cluster, true, a)
+                      : launch_kernel(select_kernel<D, 512, 16>, grid, 512, smem, st, a.cluster, true, a);
 }
 
 struct Device {
@@ -689,19 +694,23 @@ int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_
     a.recent = shape->recent;
     a.q_dtype = q->dtype;
     // Blocks of 16 warps where sequences and heads do not fill the SMs by themselves, of 4 where they do: 96 x 8 heads of up
-    // to 250 pages 24 us (35 with 16), 32 x 8 of up to 2048 36.8 (38.6), but 4 x 8 of 8192 41 with 4 warps (26.7 with 16)
+    // to 250 pages 24 us (34 with 16), 32 x 8 of up to 2048 33.5 (34.5), but 4 x 8 of 8192 39 with 4 warps (24 with 16)
     const int64_t pairs = (int64_t)a.kv_heads * shape->batch;
     const int threads = pairs > dev.sms ? 128 : 512, warps = threads / 32;
-    // Blocks of a cluster: as many as there are SMs for (with twice as many 43 us in place of 26.7 for the 4 x 8 heads), and
-    // pages for a tile a warp
+    auto smem_of = [&](int tile) { return select_smem(cache->head_dim, warps, tile, a.group, a.max_pages, a.keep); };
+    // Tiles of 32 pages, which cost less a page (the 4 x 8 heads 23.7 us, 26.7 with 16), but of 16 where each warp has one of
+    // these at most (528 pages 7.6 us, 9.6 with 32), and where 32 take more shared memory than there is.  Blocks of a
+    // cluster: as many as there are SMs for (with twice as many 43 us in place of 26.7, in tiles of 16), and pages for a
+    // tile a warp.
     a.cluster = 1;
     while (a.cluster < 8 && 2 * a.cluster * pairs * threads <= (int64_t)512 * dev.sms && a.cluster * warps * 16 < a.max_pages)
         a.cluster *= 2;
+    const int tile = threads == 128 || (a.cluster * warps * 16 < a.max_pages && smem_of(32) <= kSelectSmem) ? 32 : 16;
     const dim3 grid((unsigned)(a.cluster * a.kv_heads), (unsigned)shape->batch);
-    a.stages = select_smem(cache->head_dim, warps, a.group, a.max_pages, a.keep, 2) <= kSelectSmem / (512 / threads) ? 2 : 1;
-    const size_t smem = select_smem(cache->head_dim, warps, a.group, a.max_pages, a.keep, a.stages);
+    const size_t smem = smem_of(tile);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const cudaError_t e = cache->head_dim == 64 ? launch_select<64>(threads, grid, smem, st, a) : launch_select<128>(threads, grid, smem, st, a);
+    const cudaError_t e = cache->head_dim == 64 ? launch_select<64>(threads, tile, grid, smem, st, a)
+                                                : launch_select<128>(threads, tile, grid, smem, st, a);
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "select: %s", cudaGetErrorString(e));
 }
 
