@@ -239,9 +239,9 @@ __global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_k
     const int count = bad || n <= 0 ? 0 : (n + kKvPage - 1) / kKvPage;
     const bool choose = count > a.keep;
     const int32_t *table = a.pages + (int64_t)b * a.max_pages;
-    // A tile is kTile pages, lane l looks after page l (l % 16).  Tiles come through cp.async, the next one asked for when this one has been
-    // read: what waits for it is hidden by other warps, and a second one under way was no faster.  (Loads to registers wait
-    // in L1, which the attention's shared memory leaves small: 46 in place of 30 us beside it.)
+    // A tile is kTile pages, lane l looks after page l (l % 16).  Tiles come through cp.async, the next one asked for when
+    // this one has been read: what waits for it is hidden by other warps, and a second one under way was no faster.  (Loads
+    // to registers wait in L1, which the attention's shared memory leaves small: 46 in place of 30 us beside it.)
     const int step = kSelectWarps * a.cluster, first_tile = rank * kSelectWarps + warp;
     const uint64_t policy = l2_evict_first();
     const uint32_t stride = (uint32_t)a.bounds_stride;            // below 2^31
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kSelectThreads, 512 / kSelectThreads) select_k
         bool there;
     };
     auto ask = [&](int tile, int page) {
-        if (tile * kTile >= count) return Asked{0.f, false};
+        if (!choose || tile * kTile >= count) return Asked{0.f, false};
         const bool there = (uint32_t)page < (uint32_t)a.n_pages;
         if (!there && a.status) atomicOr(a.status, WICI_BAD_PAGE);
         const int p = there ? page : 0;                           // (of page 0, not used)
