@@ -7,8 +7,7 @@
 // 28.3 us, 5.9 TB/s (a copy of that size: 6.4); append of 16384 tokens, 32 q heads rotated, 8 k
 // and v heads to e4m3, 69.1 us, 5.4 TB/s, of which its arithmetic is 3 us; read of 30011 tokens from
 // e4m3 to bf16 32.1 us, 5.8 TB/s; one token of a step 2.3 to 3.4 us.  From and to e2m1: append of 16384 tokens, 8 k and v
-// heads in bf16, 31.7 us, 2.7 TB/s, bound by its instructions (two conversions an element, and a look at those that lie on
-// a middle: 25 us without it); read of 30011 tokens to bf16 30.6 us, 5.2 TB/s.
+// heads in bf16, nothing rotated, 22.2 us, 3.9 TB/s, bound by its instructions; read of 30011 tokens to bf16 30.6 us, 5.2 TB/s.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -32,7 +31,7 @@ int fail(int code, const char *fmt, ...) {
 }
 
 constexpr int kRopeOnly = -1;         // FMT of a launch without a cache
-enum Path { WIDE_HALF, WIDE_PAIRS, NARROW };   // 16-byte accesses of either layout, or element by element
+enum Path { WIDE_HALF, WIDE_PAIRS, WIDE_PLAIN, NARROW };   // 16-byte accesses of either layout or without a rope, or element by element
 
 struct RopeArg {
     uint64_t turns[128];
@@ -109,7 +108,7 @@ __device__ __forceinline__ void blocks_of_16(const float *own, bool halves, cons
 // would spill: append of 1251 tokens, 8 k and v heads of 64, fp32 4.1 us, 5.3 with 64.)
 template <typename T, int FMT, int PATH>
 __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlocks) rows_kernel(const __grid_constant__ RowsArg a) {
-    constexpr bool WIDE = PATH != NARROW;
+    constexpr bool WIDE = PATH != NARROW, PLAIN = PATH == WIDE_PLAIN;
     constexpr int W = sizeof(T) / 2;                             // 16-byte words of 8 elements
     extern __shared__ float4 cs[];    // [token][4][rot_chunks]: (cos, sin) of pairs 8 chunk + 2 j, + 2 j + 1
     const bool pairs = PATH == NARROW ? a.rope.interleaved : PATH == WIDE_PAIRS;
@@ -118,15 +117,15 @@ __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlo
     // The chunk's two groups of 8 elements in a rotated row: where they start, how many they hold.  Interleaved
     // rows are cut as they lie, so a chunk may hold pairs that are not rotated; halves are cut apart.
     int o0, o1, n0, n1;
-    const bool turns = c < a.rot_chunks;
+    const bool turns = !PLAIN && c < a.rot_chunks;
     if (turns && !pairs) {
         o0 = 8 * c;
         o1 = half + 8 * c;
         n0 = n1 = half - 8 * c < 8 ? half - 8 * c : 8;
     } else {
-        o0 = pairs ? 16 * c : a.rope.rot + 16 * (c - a.rot_chunks);
+        o0 = pairs || PLAIN ? 16 * c : a.rope.rot + 16 * (c - a.rot_chunks);
         o1 = o0 + 8;
-        const int n = a.rope.head_dim - o0 < 16 ? a.rope.head_dim - o0 : 16;
+        const int n = PLAIN ? 16 : a.rope.head_dim - o0 < 16 ? a.rope.head_dim - o0 : 16;
         n0 = n < 8 ? n : 8;
         n1 = n - n0;
     }
@@ -142,7 +141,7 @@ __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlo
     const int k0 = a.q_heads, v0 = FMT == kRopeOnly ? a.heads : a.q_heads + a.cache.kv_heads;   // first k row, first v row
     // a row's two groups of elements as they stand
     auto fetch = [&](int h, uint4 *raw) {
-        const bool is_q = FMT == kRopeOnly || h < k0, is_v = !is_q && h >= v0, rotate = is_q || (!is_v && a.rotate_k);
+        const bool is_q = !PLAIN && (FMT == kRopeOnly || h < k0), is_v = !is_q && h >= v0, rotate = !PLAIN && (is_q || (!is_v && a.rotate_k));
         const T *src = is_q ? sq + h * a.q.hs : is_v ? sv + (h - v0) * a.v.hs : sk + (h - k0) * a.k.hs;
         const T *p0 = src + (rotate ? o0 : 16 * c), *p1 = src + (rotate ? o1 : 16 * c + 8);
         if (WIDE) {
@@ -163,7 +162,7 @@ __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlo
     const int h0 = threadIdx.y % step;
     if (h0 < a.heads) fetch(h0, raw);     // on its way while the angles are computed
     float2 w[8];                                                 // cosine and sine of the chunk's pairs
-    if (a.positions) {
+    if (!PLAIN && a.positions) {
         const int per = 8 * a.rot_chunks;
         for (int i = tid; i < a.block_tokens * per; i += nthreads) {
             const int tt = i / per, p = i - tt * per;
@@ -195,7 +194,7 @@ __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlo
     for (int base = 0; base < a.heads; base += step) {
         const int h = base + h0;
         const bool live = here && h < a.heads;
-        const bool is_q = FMT == kRopeOnly || h < k0, is_v = !is_q && h >= v0, rotate = is_q || (!is_v && a.rotate_k);
+        const bool is_q = !PLAIN && (FMT == kRopeOnly || h < k0), is_v = !is_q && h >= v0, rotate = !PLAIN && (is_q || (!is_v && a.rotate_k));
         float x[16];
         if (WIDE) {
             const T *e = (const T *)raw;
@@ -258,7 +257,8 @@ __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlo
                 for (int o = a.chunks / 2; o > 0; o >>= 1) top = max3(top, __shfl_xor_sync(0xffffffffu, top, o), 0.f);
                 if (FMT == WICI_KV_E2M1) {
                     float most[2];
-                    blocks_of_16(own, rotate && turns && !pairs, a, most);
+                    if (PLAIN) most[0] = most[1] = max3(own[0], own[1], 0.f);
+                    else blocks_of_16(own, rotate && turns && !pairs, a, most);
                     if (store) {
                         constexpr float kPer = 1.f / kE2m1Top;     // the quotient, right to its last bit
                         const float near = top * kPer, s = fmaf(fmaf(-near, kE2m1Top, top), kPer, near);
@@ -530,6 +530,10 @@ cudaError_t launch_rows(RowsArg &a, bool wide, int sms, cudaStream_t st) {
     const dim3 block(a.chunks, b.rows);
     const size_t smem = a.positions ? (size_t)b.tokens * 4 * a.rot_chunks * sizeof(float4) : 0;
     if (!wide) return launch_blocks(rows_kernel<T, FMT, NARROW>, a, block, smem, st);
+    // Without a rope e2m1, bound by its instructions, has a kernel of its own: append of 16384 tokens 22.2 us, 29.2 where rows
+    // that might turn are told apart.  The other formats are bound by HBM either way.
+    if constexpr (FMT == WICI_KV_E2M1)
+        if (!a.positions) return launch_blocks(rows_kernel<T, FMT, WIDE_PLAIN>, a, block, smem, st);
     return a.rope.interleaved ? launch_blocks(rows_kernel<T, FMT, WIDE_PAIRS>, a, block, smem, st)
                               : launch_blocks(rows_kernel<T, FMT, WIDE_HALF>, a, block, smem, st);
 }

@@ -195,7 +195,7 @@ __device__ __forceinline__ uint32_t quantise_e2m1(const float *x, float b, float
     uint32_t lo = encode_e2m1(x, r * kNearLo);
     const uint32_t hi = encode_e2m1(x, r * kNearHi);
     // values of few bits are often on a middle: one lane or two of most warps have one, so it is one place at a time (all 8
-    // in turn: 34 in place of 32 us for 16384 tokens of 16 rows in bf16, before these had a way of their own)
+    // in turn: 34 in place of 32 us for 16384 tokens of 16 rows in bf16, before 16-bit values had a way of their own)
     for (uint32_t differ = lo ^ hi; differ;) {
         const int at = (31 - __clz(differ)) & ~3, j = at >> 2;
         differ &= (1u << at) - 1;
