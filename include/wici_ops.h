@@ -2,11 +2,13 @@
  * wici_ops.h - operators of a batched decode step, for engines that own their
  * device memory: rotary positions, writing and reading a paged key-value cache
  * (bf16, or quantised to 8 or 4 bits), and attention of one new token per sequence
- * over that cache.  They stand beside wici_lm_head_argmax_noalloc (wici.h) and
- * need no context; wici_kv_view hands them the cache of one.
+ * over that cache, or over the pages of it that a cheap score selects.  They stand
+ * beside wici_lm_head_argmax_noalloc (wici.h) and need no context; wici_kv_view
+ * hands them the cache of one.
  *
  * A step of one layer for a batch of clients: the q|k|v projection, then
- * wici_kv_append (rotates q and k, writes k and v), then wici_paged_attention.
+ * wici_kv_append (rotates q and k, writes k and v), then wici_paged_attention; of a
+ * long context wici_kv_bounds_update, wici_kv_select and wici_selected_attention.
  *
  * Conventions for every entry point
  *   - Return value as in wici.h; messages are in wici_last_error(NULL).  On

@@ -572,8 +572,29 @@ cudaError_t launch_select(int threads, int tile, dim3 grid, size_t smem, cudaStr
                       : launch_kernel(select_kernel<D, 512, 16>, grid, 512, smem, st, a.cluster, true, a);
 }
 
+// the most blocks of a cluster that the current device has room for, with the most shared memory: 8 unless it is a part of one
+cudaError_t resident_cluster(int *most) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.blockDim = dim3(512);
+    cfg.dynamicSmemBytes = kSelectSmem;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    for (*most = 8; *most > 1; *most /= 2) {
+        attr.val.clusterDim.x = *most;
+        cfg.gridDim = dim3(*most);
+        int n = 0;
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, select_kernel<128, 512, 32>, &cfg);
+        if (e != cudaSuccess) return e;
+        if (n > 0) break;
+    }
+    return cudaSuccess;
+}
+
 struct Device {
-    int sms;
+    int sms, cluster;
 };
 DeviceTable<Device> g_devices;
 
@@ -585,6 +606,7 @@ int device_of(Device *d) {
             constexpr int kMost = kSelectSmem;
             cudaError_t e1 = limit_select<64>(kMost);
             if (e1 == cudaSuccess) e1 = limit_select<128>(kMost);
+            if (e1 == cudaSuccess) e1 = resident_cluster(&x->cluster);
             return e1 == cudaSuccess ? cudaDeviceGetAttribute(&x->sms, cudaDevAttrMultiProcessorCount, dev) : e1;
         });
     return e == cudaSuccess ? WICI_OK : fail(WICI_E_CUDA, "select setup: %s", cudaGetErrorString(e));
@@ -703,7 +725,7 @@ int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_
     // cluster: as many as there are SMs for (with twice as many 43 us in place of 26.7, in tiles of 16), and pages for a
     // tile a warp.
     a.cluster = 1;
-    while (a.cluster < 8 && 2 * a.cluster * pairs * threads <= (int64_t)512 * dev.sms && a.cluster * warps * 16 < a.max_pages)
+    while (a.cluster < dev.cluster && 2 * a.cluster * pairs * threads <= (int64_t)512 * dev.sms && a.cluster * warps * 16 < a.max_pages)
         a.cluster *= 2;
     const int tile = threads == 128 || (a.cluster * warps * 16 < a.max_pages && smem_of(32) <= kSelectSmem) ? 32 : 16;
     const dim3 grid((unsigned)(a.cluster * a.kv_heads), (unsigned)shape->batch);

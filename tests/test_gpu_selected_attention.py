@@ -476,6 +476,43 @@ def test_a_contexts_prompt_attended_in_part():
     model.close()
 
 
+@pytest.mark.parametrize("fmt,group,batch,kv", [("e2m1", 1, 1100, 2), ("bf16", 3, 1030, 1), ("e2m1", 12, 300, 1), ("int8", 9, 270, 2)])
+def test_batches_of_more_sequences_than_a_launch_takes(fmt, group, batch, kv):
+    rng = np.random.default_rng(batch)
+    lengths = rng.integers(0, 90, batch)
+    lengths[-1] = 85
+    cache, bounds, q, pages, vals = selection_case(rng, kv, group, 64, fmt, "bf16", lengths)
+    chosen, held, out = check_selected(cache, bounds, q, pages, lengths, vals, 3, 1, 1, "bf16")
+    lse = torch.empty(q.shape[:2], device="cuda")
+    check_attention(cache, q, pages, lengths, vals, 0.125, 0, cache.attend(q, ints(pages), ints(lengths), lse=lse), lse, "bf16")
+
+
+@pytest.mark.parametrize("fmt,n_pages", [("e2m1", 3_600_000), ("bf16", 1_200_000)])
+def test_a_cache_of_more_than_4_gb(fmt, n_pages):
+    """Tokens in the last pages, and the same tokens in the first ones of a small cache: the same bounds, lists and results."""
+    rng = np.random.default_rng(4)
+    n, d = 600, 64
+    k, v = randn(rng, n, 1, d), randn(rng, n, 1, d)
+    q = randn(rng, 1, 5, d)
+    results = []
+    for pages_of, first in ((n_pages, n_pages - 38), (38, 0)):
+        cache = PagedKV(1, d, fmt, n_pages=pages_of)
+        assert pages_of == 38 or cache.data.numel() > 1 << 32
+        bounds = KeyBounds(cache)
+        slots = first * 16 + np.arange(n)
+        cache.append(k, v, ints(slots))
+        bounds.update(ints(np.append(slots[15::16], slots[-1])))
+        pages = ints((first + np.arange(38))[None])
+        blocks = torch.empty(1, 1, 9, dtype=torch.int32, device="cuda")
+        chosen, held = bounds.select(q, pages, ints([n]), 9, blocks=blocks)
+        assert torch.equal(chosen, blocks + first)
+        results.append([bounds.data.view(pages_of, -1)[first:first + 38].clone(), blocks, held, cache.attend(q, chosen, held), cache.attend(q, pages, ints([n])),
+                        *cache.read(ints(slots), dtype=torch.float32)])
+        cache.check()
+        del cache, bounds
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
 def test_two_streams_at_once():
     rng = np.random.default_rng(30)
     cases = [selection_case(rng, 2, 4, 128, fmt, "bf16", [1500, 200, 900]) for fmt in ("bf16", "e2m1")]
