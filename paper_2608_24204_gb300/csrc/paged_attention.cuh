@@ -816,13 +816,15 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 cp_wait<KS - 2>();
                 __syncwarp();
                 const uint32_t ks_next = ks == ring + (KS - 1) * S::kSlot ? ring : ks + S::kSlot;
-                float x[C][J];                                // queries 2 t + r % 2 of tile r / 2, keys key_at(j); cq is still to come
+                float x[C][J];                                // queries 2 t + r % 2 of tile r / 2, keys key_at(j)
                 const bool part = key0 < keys.lo || key0 > keys.n - UNIT;   // not every key of the unit is the sequence's
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     const float ksc = lds32(ks + (j >> 1) * S::kBlock + SCALES_AT + (j & 1) * 32 + 4 * g);
+                    // Rounded here, once for the reference and for the exponent, which is 0 then for the largest logit: a product
+                    // taken into the exponent's own rounding is off from the reference by up to 2^-25 of a logit of any size.
 #pragma unroll
-                    for (int r = 0; r < C; ++r) x[r][j] = c[j >> 1][r >> 1][2 * (j & 1) + (r & 1)] * ksc;
+                    for (int r = 0; r < C; ++r) x[r][j] = __fmul_rn(c[j >> 1][r >> 1][2 * (j & 1) + (r & 1)] * ksc, cq[r]);
                 }
                 if (part) {
 #pragma unroll
@@ -839,7 +841,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     float top = x[r][0];
 #pragma unroll
                     for (int j = 1; j < J; ++j) top = fmaxf(top, x[r][j]);
-                    up[r] = fmaxf(m[r], largest(top) * cq[r]);
+                    up[r] = fmaxf(m[r], largest(top));
                     grew |= up[r] > m[r] + kLag;
                 }
                 if (__any_sync(0xffffffffu, grew)) {
@@ -865,7 +867,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     const float vscale = lds32(vs + (j >> 1) * S::kBlock + SCALES_AT + (j & 1) * 32 + 4 * g);
 #pragma unroll
                     for (int r = 0; r < C; ++r) {
-                        const float p = ex2(fmaf(x[r][j], cq[r], -ref[r]));
+                        const float p = ex2(x[r][j] - ref[r]);
                         l[r] += p;
                         x[r][j] = p * vscale;
                     }
