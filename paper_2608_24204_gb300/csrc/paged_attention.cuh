@@ -709,10 +709,12 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             // ---- Q fragments: query g of a tile, 4 elements a step ----
             uint32_t qf[N8][TQ][STEPS][2];
             float cq[C];                                      // products to base-2 logits, of queries 2 t, 2 t + 1
+            const float log2_scale = a.scale * 1.44269504088896340736f;
+            // the smallest power of two that takes the scale to no less than 2^-126, where it has its 24 bits
+            const int least = 1 - min((int)(__float_as_uint(log2_scale) >> 23 & 0xFF), 127);
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
-                // a negative scale's sign goes to q, and so does a scale of 0: cq is positive
-                float x[STEPS][4], of_g = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896340736f;
+                float x[STEPS][4];
                 uint32_t top = 0;
 #pragma unroll
                 for (int i = 0; i < STEPS / 2; ++i) unpack_q8<QW>(a.q_dtype, qx[n][i], x[2 * i]);
@@ -722,11 +724,10 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(x[s][j]) & 0x7FFFFFFFu);
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                // 2^(13 - exponent): the largest magnitude to [2^13, 2^14)
+                // 2^(13 - exponent): the largest magnitude to [2^13, 2^14), a smaller one where q and the scale are very small
                 int e = (int)(top >> 23) - 127 - 13;
-                e = top >= kInfBits || top == 0 ? 0 : max(-126, min(126, e));
-                const float down = a.scale == 0.f ? 0.f : copysignf(__int_as_float((127 - e) << 23), a.scale);
-                of_g = fmaxf(of_g * __int_as_float((127 + e) << 23), 0x1p-126f);
+                e = top >= kInfBits || top == 0 ? 0 : max(least, e);
+                const float down = __int_as_float((127 - e) << 23), of_g = log2_scale * __int_as_float((127 + e) << 23);
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
                     uint32_t w[2][TQ];
@@ -823,8 +824,9 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     const float ksc = lds32(ks + (j >> 1) * S::kBlock + SCALES_AT + (j & 1) * 32 + 4 * g);
                     // Rounded here, once for the reference and for the exponent, which is 0 then for the largest logit: a product
                     // taken into the exponent's own rounding is off from the reference by up to 2^-25 of a logit of any size.
+                    // (c is up to 2^32, of a query scaled to 2^13: cq's power of two goes to the key's scale, which may be 2^116, first.)
 #pragma unroll
-                    for (int r = 0; r < C; ++r) x[r][j] = __fmul_rn(c[j >> 1][r >> 1][2 * (j & 1) + (r & 1)] * ksc, cq[r]);
+                    for (int r = 0; r < C; ++r) x[r][j] = __fmul_rn(c[j >> 1][r >> 1][2 * (j & 1) + (r & 1)], ksc * cq[r]);
                 }
                 if (part) {
 #pragma unroll

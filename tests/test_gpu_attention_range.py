@@ -56,3 +56,54 @@ def test_large_logits(fmt, dtype, group, d, q_size, k_size, scale):
     within(f64(out[0]), want, 2.0 ** -16 * np.abs(want) + half_step(want, "f32"), "out")
     size = np.abs(f64(q)[0]) @ np.abs(vals[:n, 0, 0]).T * abs(scale)
     within(f64(lse[0]), logits.max(1), size.max(1) * (2 * d * 2.0 ** -23 + 2.0 ** -16) + 2.0 ** -20, "lse")
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("dtype,group,d", [("bf16", 4, 128), ("f32", 3, 64), ("bf16", 12, 64)])
+@pytest.mark.parametrize("q_size,k_size,scale", [(-110, 110, 1.0), (-100, 125, 2.0 ** -22), (0, 110, 2.0 ** -110), (-20, 118, -2.0 ** -98),
+                                                  (-115, 107, 1.0), (-120, 122, 0.088), (-125, 126, 0.088), (100, -80, 2.0 ** -15), (120, -85, 2.0 ** -30)])
+def test_keys_of_any_size(fmt, dtype, group, d, q_size, k_size, scale):
+    """Keys and queries near the ends of what fp32 holds, whose logits the other or the scale makes ordinary ones."""
+    check_moderate(fmt, dtype, group, d, q_size, k_size, scale)
+
+
+def check_moderate(fmt, dtype, group, d, q_size, k_size, scale):
+    rng = np.random.default_rng(abs(d + group + k_size))
+    n = 150
+    # below 4 2^k_size: finite numbers, of the products' sums as well
+    k = torch.tensor(np.clip(rng.normal(size=(n, 1, d)), -4, 4) * 2.0 ** k_size * d ** -0.5, device="cuda").to(DT[dtype])
+    q = torch.tensor(rng.normal(size=(2, group, d)) * 2.0 ** q_size, device="cuda").to(DT[dtype])
+    cache, vals, pages = stored(k, randn(rng, n, 1, d, dtype=dtype), fmt)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    pages, lengths = np.repeat(pages, 2, 0), [n, 77]
+    out = cache.attend(q, ints(pages), ints(lengths), scale=scale, out=torch.empty(q.shape, device="cuda"), lse=lse)
+    stored_as = (paged.unpack_e2m1 if fmt == "e2m1" else lambda *x: paged.unpack(*x, fmt))(cache.data.cpu().numpy(), 1, d)
+    v_scales = stored_as[-1][:n, 1, 0].astype(np.float64)
+    scale, q64 = float(np.float32(scale)), f64(q)
+    want, want_lse, weight = paged.paged_attention(q64, vals[:, 0], vals[:, 1], pages, lengths, scale)
+    for b, m in enumerate(lengths):
+        keys, v, s = vals[:m, 0, 0], vals[:m, 1, 0], v_scales[:m]
+        for h in range(group):
+            # the terms of check_attention, and one for logits far apart: a key's weight times its scale of V is held to 2^-32
+            # of the largest such product, and what is lost of it counts v / scale times
+            p = np.exp(keys @ q64[b, h] * scale - want_lse[b, h])
+            ds = float(np.max(np.abs(keys) @ np.abs(q64[b, h])) * abs(scale)) * (2 * d * 2.0 ** -23 + (2.0 ** -16 if dtype == "f32" else 0.0))
+            rel = 2 * ds + 2.0 ** -16 + 2.0 ** -21 + m * 2.0 ** -23
+            small = 2.0 ** -32 * (p * s).max() * (np.abs(v) / s[:, None]).sum(0)
+            within(f64(out[b, h]), want[b, h], rel * weight[b, h] + small * (1 + rel) + half_step(want[b, h], "f32"), "out")
+            within(float(lse[b, h]), want_lse[b, h], ds + 2.0 ** -20 + m * 2.0 ** -23 + 2.0 ** -23 * abs(want_lse[b, h]), "lse")
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("dtype,group,d", [("bf16", 4, 128), ("f32", 3, 64)])
+@pytest.mark.parametrize("q_size,k_size", [(1e-33, 1e33), (1e-35, 1e35), (3e-4, 3e35)])
+def test_every_element_of_a_key_is_large(fmt, dtype, group, d, q_size, k_size):
+    """Sums over the head of 2^20 and more times a key's scale, before the query's own size comes in."""
+    n = 40
+    k = torch.tensor(np.cos(np.arange(n))[:, None, None] * np.full((n, 1, d), k_size), device="cuda").to(DT[dtype])
+    q = torch.full((1, group, d), q_size, device="cuda").to(DT[dtype])
+    cache, vals, pages = stored(k, randn(np.random.default_rng(d), n, 1, d, dtype=dtype), fmt)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    scale = float(np.float32(1e-33 / (q_size * (k_size / 1e33)) * d ** -0.5))
+    out = cache.attend(q, ints(pages), ints([n]), scale=scale, out=torch.empty(q.shape, device="cuda"), lse=lse)
+    check_attention(cache, q, pages, [n], vals, scale, 0, out, lse, dtype, "f32")
