@@ -229,7 +229,7 @@ typedef struct wici_select_shape {
  *   out_pages   int32[batch][n_kv_heads][keep]: entries of `pages`, in the order of their tokens, -1 after the last
  *   out_lengths int32[batch]: the tokens they hold (a length that is bad stays bad)
  *   out_blocks  the same as out_pages with their columns in `pages`, or NULL
- * q: `batch` tokens of up to 64 heads a KV head.  Outputs overlap nothing else. */
+ * q: `batch` tokens of up to 64 heads a KV head.  Outputs overlap no other tensor, and no record or page. */
 int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_bounds *bounds, const wici_select_shape *shape,
                    const int32_t *pages, const int32_t *lengths, const wici_heads *q, int32_t *out_pages,
                    int32_t *out_lengths, int32_t *out_blocks, int32_t *status);

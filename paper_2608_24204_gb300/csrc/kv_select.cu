@@ -624,6 +624,20 @@ const char *check_bounds(const wici_kv_bounds *b, const wici_kv_cache *c) {
 bool overlap(const void *a, int64_t na, const void *b, int64_t nb) {
     return a && b && (uintptr_t)a < (uintptr_t)b + (size_t)nb && (uintptr_t)b < (uintptr_t)a + (size_t)na;
 }
+// whether n bytes at p meet one of `count` rows of `len` bytes, `stride` apart (what lies between them is not the rows')
+bool meets(const void *p, int64_t n, const void *rows, int64_t count, int64_t stride, int64_t len) {
+    if (!p || !overlap(p, n, rows, (count - 1) * stride + len)) return false;
+    const int64_t at = (int64_t)((uintptr_t)p - (uintptr_t)rows);
+    const int64_t i = at < len || stride == 0 ? 0 : (at - len) / stride + 1;   // the first row that ends behind p
+    return i < count && i * stride < at + n;
+}
+bool meets(const void *p, int64_t n, const wici_heads *t, int64_t tokens, int d) {
+    const int64_t e = dtype_bytes(t->dtype), token = t->token_stride * e, head = t->head_stride * e;
+    if (!overlap(p, n, t->data, (tokens - 1) * token + (t->heads - 1) * head + d * e)) return false;
+    for (int64_t i = 0; i < tokens; ++i)
+        if (meets(p, n, (const uint8_t *)t->data + i * token, t->heads, head, d * e)) return true;
+    return false;
+}
 
 template <int FMT>
 cudaError_t launch_bounds(int d, const BoundsArg &a, cudaStream_t st) {
@@ -691,7 +705,12 @@ int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_
     const int64_t len = (int64_t)shape->batch * 4;
     const struct { const void *p; int64_t n; } outs[3] = {{out_pages, list}, {out_lengths, len}, {out_blocks, list}};
     for (int i = 0; i < 3; ++i) {
-        bool shared = overlap(outs[i].p, outs[i].n, pages, in) || overlap(outs[i].p, outs[i].n, lengths, len);
+        bool shared = overlap(outs[i].p, outs[i].n, pages, in) || overlap(outs[i].p, outs[i].n, lengths, len) ||
+                      overlap(outs[i].p, outs[i].n, status, 4) || meets(outs[i].p, outs[i].n, q, shape->batch, cache->head_dim) ||
+                      meets(outs[i].p, outs[i].n, bounds->data, cache->n_pages, bounds->page_stride,
+                            wici_kv_bounds_bytes(cache->n_kv_heads, cache->head_dim)) ||
+                      meets(outs[i].p, outs[i].n, cache->data, cache->n_pages, cache->page_stride,
+                            wici_kv_page_bytes(cache->format, cache->n_kv_heads, cache->head_dim));
         for (int j = 0; j < i; ++j) shared |= overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n);
         if (shared) return fail(WICI_E_ARG, "select: an output overlaps another tensor");
     }

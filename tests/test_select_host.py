@@ -120,3 +120,22 @@ def test_oracle_selection():
     assert paged.selected_pages(s, 3, 1, 2) == [0, 6, 7]
     assert paged.selected_pages(s, 5, 0, 1) == [0, 2, 3, 4, 7]
     assert np.isnan(paged.key_bounds(np.array([[1.0, np.inf]]))[1]) and paged.key_bounds(np.zeros((2, 4)))[1] == 0
+
+
+@pytest.mark.parametrize("out", ["out", "held", "blocks"])
+def test_outputs_over_what_a_selection_reads_are_refused(out):
+    def places(q=FAR[5], b=FAR[6], c=FAR[7], status=None):
+        return dict(q=heads(n=32, data=q), b=bounds(data=b), c=cache(data=c), status=status)
+    n = 8 if out == "held" else 128                            # bytes of the output
+    q_bytes, record, page = 2 * 32 * 128 * 2, ops.wici_kv_bounds_bytes(8, 128), cache().page_stride
+    for at, size in ((FAR[5], q_bytes), (FAR[6], 4 * record), (FAR[7], 4 * page)):
+        for first in (at - n + 4, at, at + size - 4):
+            select(**{out: first}, **places(), match="overlap")
+    word = A + (1 << 36)
+    for first in (word - n + 4, word):
+        select(**{out: first}, **places(status=word), match="overlap")
+    # inside a record of records that lie apart, and a head of heads that do
+    select(**{out: FAR[6] + 3 * (1 << 16) + 64}, **dict(places(), b=bounds(data=FAR[6], stride=1 << 16)), match="overlap")
+    at = A + (1 << 37)
+    apart = heads(n=32, data=at, token=1 << 20, head=1 << 12)
+    select(**{out: at + 2 * ((1 << 20) + 31 * (1 << 12)) + 64}, **dict(places(), q=apart), match="overlap")
