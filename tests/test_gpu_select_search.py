@@ -47,3 +47,50 @@ def test_outputs_between_heads_and_records_are_as_good_as_any():
         with pytest.raises(wici.WiciError, match="overlap"):
             select(*bad)
     cache.check()
+
+
+def check_search(scales, codes, q, keeps):
+    """One sequence of a page for each scale, in any order; q and codes [pages, 2] meet in their first element."""
+    n, d = len(scales), q.shape[-1]
+    rng = np.random.default_rng(n)
+    cache = PagedKV(1, d, "bf16", n_pages=n)
+    bounds = KeyBounds(cache)
+    bounds.codes[:, 0, :, 0] = torch.tensor(codes, dtype=torch.int8, device="cuda")
+    bounds.scales.copy_(torch.tensor(scales, device="cuda")[:, None])
+    order = rng.permutation(n)
+    scores = paged.page_scores(f64(q)[0], bounds.codes[:, 0].cpu().numpy()[order], scales[order])
+    for keep in keeps:
+        blocks = torch.empty(1, 1, keep, dtype=torch.int32, device="cuda")
+        chosen, held = bounds.select(q, ints(order[None]), ints([16 * n - 5]), keep, first=1, recent=1, blocks=blocks)
+        want = paged.selected_pages(scores, keep, 1, 1)
+        assert blocks[0, 0].tolist() == want and chosen[0, 0].tolist() == order[want].tolist() and held.tolist() == [16 * keep - 5]
+    cache.check()
+    return scores
+
+
+@pytest.mark.parametrize("size", [1e-30, 1.0, 1e30])
+def test_negative_scores_beside_infinite_ones(size):
+    # pages of NaN scale score +infinity: the scores' width is no number, and their orders differ in the first bit
+    rng = np.random.default_rng(5)
+    n = 3000
+    scales = (rng.uniform(0.5, 2, n) * size).astype(np.float32)
+    scales[::7] = np.nan
+    q = torch.zeros(1, 1, 64, device="cuda")
+    q[..., 0] = -1.0
+    scores = check_search(scales, np.full((n, 2), 100), q, (3, 200, 428, 429, 431, 900, 2990))
+    assert np.isinf(scores).sum() == 429 and (scores < 0).sum() == n - 429
+
+
+@pytest.mark.parametrize("top", [1e3, 1e25])
+def test_small_scores_of_both_signs_beside_a_large_one(top):
+    # all but one score in one bin of equal width, more than are compared one with another
+    rng = np.random.default_rng(6)
+    n = 2500
+    scales = rng.uniform(0.5, 2, n).astype(np.float32) * np.float32(1e-8)
+    scales[rng.integers(0, n, 300)] = np.float32(0.75e-8)                      # equal ones among them
+    codes = rng.integers(-127, 128, n).repeat(2).reshape(n, 2)
+    scales[1234], codes[1234] = top, 127
+    q = torch.zeros(1, 2, 64, device="cuda")
+    q[0, :, 0] = torch.tensor([1.0, 0.25])
+    scores = check_search(scales, codes, q, (2, 3, 4, 600, 1249, 1251, 1400, 2400))
+    assert (scores > 0).sum() > 1000 and (scores < 0).sum() > 1000
