@@ -158,7 +158,7 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
  * not read and may hold anything.  A sequence without keys (n <= 0) has out 0 and
  * lse -infinity.  Infinities and NaNs in a sequence's own keys act as in the
  * formula, in its own result alone (e^(s_t - max s) below 2^-126 counts as 0).
- * Finite ones do where |scale| max|q| max|k_t| head_dim and 64 n max|v_t| are below 2^128:
+ * Finite ones do where max(1, |scale|) max|q| max|k_t| head_dim and 64 n max|v_t| are below 2^128:
  * scores and sums are fp32 numbers, weights up to 64 before they are divided.
  * Over an 8- or 4-bit cache a key's weight times its scale of V is held to 2^-22 of itself
  * or 2^-32 of the sequence's largest, far less than what codes cost that key's values.

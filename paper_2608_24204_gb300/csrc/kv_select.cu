@@ -193,6 +193,9 @@ __device__ __forceinline__ uint32_t order_of(float s) {
     return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
 constexpr size_t kSelectSmem = 217 * 1024;   // at most, beside what the kernel has of its own
+constexpr size_t kSelectOwn = kBins * 4 + 1536;   // that, and what every block of an SM has besides
+constexpr size_t kSmSmem = 228 * 1024;            // of an SM
+constexpr int kFewPages = 2048;                   // four blocks of 4 warps fit with these, and few heads a group
 static_assert(select_smem(128, 16, 16, kMaxSelectGroup, kMaxSelectPages, kMaxKeep) <= kSelectSmem, "the largest call");
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint64_t policy) {
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
@@ -735,20 +738,34 @@ int wici_kv_select(void *cuda_stream, const wici_kv_cache *cache, const wici_kv_
     a.recent = shape->recent;
     a.q_dtype = q->dtype;
     // Blocks of 16 warps where sequences and heads do not fill the SMs by themselves, of 4 where they do: 96 x 8 heads of up
-    // to 250 pages 24 us (34 with 16), 32 x 8 of up to 2048 33.5 (34.5), but 4 x 8 of 8192 39 with 4 warps (24 with 16)
+    // to 250 pages 24 us (34 with 16), 32 x 8 of up to 2048 33.5 (34.5), but 4 x 8 of 8192 39 with 4 warps (24 with 16).
+    // Blocks of a cluster: as many as there are SMs for (with twice as many 43 us in place of 26.7, in tiles of 16), and
+    // pages for a tile a warp.
     const int64_t pairs = (int64_t)a.kv_heads * shape->batch;
-    const int threads = pairs > dev.sms ? 128 : 512, warps = threads / 32;
-    auto smem_of = [&](int tile) { return select_smem(cache->head_dim, warps, tile, a.group, a.max_pages, a.keep); };
+    auto smem_of = [&](int warps, int tile) { return select_smem(cache->head_dim, warps, tile, a.group, a.max_pages, a.keep); };
+    auto cluster_of = [&](int threads) {
+        int c = 1;
+        while (c < dev.cluster && 2 * c * pairs * threads <= (int64_t)512 * dev.sms && c * (threads / 32) * 16 < a.max_pages) c *= 2;
+        return c;
+    };
+    int threads = pairs > dev.sms ? 128 : 512;
+    if (threads == 128 && a.max_pages > kFewPages) {
+        // Many pages: their scores leave an SM room for fewer blocks of 4 warps, and those take more waves.  A warp's share of
+        // the pages in all waves, of 4 warps and of 16 (whose waves cost 1.4 times that: nothing runs beside a block's ends):
+        // 20 x 8 heads of 8192 pages 110 us with 16 warps, 140 with 4; of 6000 84 and 74; 32 x 8 of 16384, 4096 kept, 237 and
+        // 498; 64 x 8 of 4096 129 and 148; 96 x 8 of these 191 and 176.
+        const int c = cluster_of(128), fit = (int)(kSmSmem / (smem_of(4, 32) + kSelectOwn));
+        const int64_t room = (int64_t)(fit < 4 ? fit : 4) * dev.sms;
+        const int64_t waves4 = (pairs * c + room - 1) / room, waves16 = (pairs + dev.sms - 1) / dev.sms;
+        if (20 * waves4 > 7 * c * waves16) threads = 512;
+    }
+    const int warps = threads / 32;
+    a.cluster = cluster_of(threads);
     // Tiles of 32 pages, which cost less a page (the 4 x 8 heads 23.7 us, 26.7 with 16), but of 16 where each warp has one of
-    // these at most (528 pages 7.6 us, 9.6 with 32), and where 32 take more shared memory than there is.  Blocks of a
-    // cluster: as many as there are SMs for (with twice as many 43 us in place of 26.7, in tiles of 16), and pages for a
-    // tile a warp.
-    a.cluster = 1;
-    while (a.cluster < dev.cluster && 2 * a.cluster * pairs * threads <= (int64_t)512 * dev.sms && a.cluster * warps * 16 < a.max_pages)
-        a.cluster *= 2;
-    const int tile = threads == 128 || (a.cluster * warps * 16 < a.max_pages && smem_of(32) <= kSelectSmem) ? 32 : 16;
+    // these at most (528 pages 7.6 us, 9.6 with 32), and where 32 take more shared memory than there is.
+    const int tile = threads == 128 || (a.cluster * warps * 16 < a.max_pages && smem_of(warps, 32) <= kSelectSmem) ? 32 : 16;
     const dim3 grid((unsigned)(a.cluster * a.kv_heads), (unsigned)shape->batch);
-    const size_t smem = smem_of(tile);
+    const size_t smem = smem_of(warps, tile);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     const cudaError_t e = cache->head_dim == 64 ? launch_select<64>(threads, tile, grid, smem, st, a)
                                                 : launch_select<128>(threads, tile, grid, smem, st, a);

@@ -94,3 +94,34 @@ def test_small_scores_of_both_signs_beside_a_large_one(top):
     q[0, :, 0] = torch.tensor([1.0, 0.25])
     scores = check_search(scales, codes, q, (2, 3, 4, 600, 1249, 1251, 1400, 2400))
     assert (scores > 0).sum() > 1000 and (scores < 0).sum() > 1000
+
+
+@pytest.mark.parametrize("batch,kv,most", [(32, 8, 3000), (40, 8, 2049), (20, 8, 8192), (160, 1, 6000)])
+def test_more_sequences_and_heads_than_sms_over_many_pages(batch, kv, most):
+    """Blocks of either size, in several waves: short sequences beside long ones, some with nothing to choose."""
+    d, group, keep, total = 128, 4, 60, 16384
+    g = torch.Generator(device="cuda").manual_seed(most)
+    cache = PagedKV(kv, d, "e2m1", n_pages=total)
+    bounds = KeyBounds(cache)
+    bounds.codes.copy_(torch.randint(-127, 128, bounds.codes.shape, generator=g, device="cuda", dtype=torch.int32))
+    bounds.scales.copy_(torch.rand(bounds.scales.shape, generator=g, device="cuda") + 0.5)
+    q = torch.randn((batch, kv * group, d), generator=g, device="cuda").bfloat16()
+    pages = torch.randint(0, total, (batch, most), generator=g, device="cuda", dtype=torch.int32)   # sequences may share pages
+    lengths = torch.randint(1, 16 * most + 1, (batch,), generator=g, device="cuda", dtype=torch.int32)
+    lengths[:6] = ints([0, 1, 16 * keep, 16 * keep + 1, 16 * most, 16 * most - 15])
+    blocks = torch.empty(batch, kv, keep, dtype=torch.int32, device="cuda")
+    chosen, held = bounds.select(q, pages, lengths, keep, first=1, recent=3, blocks=blocks)
+    cache.check()
+    m = q.float().abs().amax(-1, keepdim=True)
+    w = (q.float() * (m.reciprocal() * 1023.0)).round().double().view(batch, kv, group, d)
+    for b, n in enumerate(lengths.tolist()):
+        count = -(-n // 16)
+        at = pages[b, :count].long()
+        c = bounds.codes[at].double()                                          # [pages, kv, 2, d]
+        dot = torch.einsum("hgd,phd->hgp", w[b].clamp_min(0), c[:, :, 0]) + torch.einsum("hgd,phd->hgp", w[b].clamp_max(0), c[:, :, 1])
+        score = ((dot.float() * m[b].view(kv, group, 1)).amax(1) * bounds.scales[at].T).cpu().numpy()
+        for h in range(kv):
+            want = paged.selected_pages(score[h], keep, 1, 3) if count else []
+            assert blocks[b, h].tolist() == want + [-1] * (keep - len(want))
+            assert chosen[b, h, :len(want)].tolist() == at[want].tolist()
+        assert held[b].item() == (n if count <= keep else (keep - 1) * 16 + (n - 1) % 16 + 1)
