@@ -116,7 +116,8 @@ int wici_rope(void *cuda_stream, const wici_rope_plan *plan, int32_t inverse, co
  * An e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4 or 6, with a sign) stands for code * block scale *
  * scale: scale = max|x| / 2688 in fp32, block scale = max|x| of 16 neighbours / (6 scale) to the
  * nearest e4m3, code = x / (block scale * scale) to the nearest e2m1, both as real numbers and
- * half way to the even one.  Scale 0 is below 2^-100 here; NaN as above.
+ * half way to the even one.  Scale 0 is below 2^-100 here; NaN as above.  (Element and scale
+ * types: OCP Microscaling Formats 1.0, 2023; e4m3 scales of 16 under an fp32 one are vendors' use.)
  * Slot s is place s % 16 of page s / 16.  The paper names no cache precision; 8-bit
  * codes halve the bytes that bound decoding, 4-bit codes take 0.3 of them. */
 enum { WICI_KV_BF16 = 0, WICI_KV_INT8 = 1, WICI_KV_E4M3 = 2, WICI_KV_E2M1 = 4 };
@@ -161,7 +162,8 @@ int wici_kv_read(void *cuda_stream, const wici_kv_cache *cache, const int32_t *s
  * Finite ones do where max(1, |scale|) max|q| max|k_t| head_dim and 64 n max|v_t| are below 2^128:
  * scores and sums are fp32 numbers, weights up to 64 before they are divided.
  * Over an 8- or 4-bit cache a key's weight times its scale of V is held to 2^-22 of itself
- * or 2^-32 of the sequence's largest, far less than what codes cost that key's values.
+ * or 2^-32 of the sequence's largest, far less than what codes cost that key's values, and an
+ * element of an fp32 q to 2^-22 of itself or 2^-38 of its head's largest.
  * Several sequences may share pages. */
 typedef struct wici_attn_shape {
     int32_t batch;            /* 0 .. 65535 */
@@ -198,7 +200,8 @@ int wici_selected_attention(void *cuda_stream, const wici_kv_cache *cache, const
  * hi, lo[head_dim] under one scale = max|k| times 1 / 127 in fp32 (codes are fp32's k / scale, to the
  * nearest even).  A record per page, page_stride bytes apart, holds [kv head][hi|lo][head_dim], then
  * scale[kv head].  A scale below 2^-126 is 0, and NaN where a key is infinite or NaN.
- * The paper has no counterpart: its longest context is read whole. */
+ * The paper has no counterpart: its longest context is read whole.  (Pages chosen by such a bound:
+ * Tang et al. 2024, query-aware sparsity.) */
 typedef struct wici_kv_bounds {
     void *data;               /* 16-byte aligned, a record for each page of the cache */
     int64_t page_stride;      /* bytes, a multiple of 16, at least wici_kv_bounds_bytes, below 2^31 */

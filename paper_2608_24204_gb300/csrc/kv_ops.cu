@@ -7,7 +7,8 @@
 // 28.3 us, 5.9 TB/s (a copy of that size: 6.4); append of 16384 tokens, 32 q heads rotated, 8 k
 // and v heads to e4m3, 69.1 us, 5.4 TB/s, of which its arithmetic is 3 us; read of 30011 tokens from
 // e4m3 to bf16 32.1 us, 5.8 TB/s; one token of a step 2.3 to 3.4 us.  From and to e2m1: append of 16384 tokens, 8 k and v
-// heads in bf16, nothing rotated, 22.2 us, 3.9 TB/s, bound by its instructions; read of 30011 tokens to bf16 30.6 us, 5.2 TB/s.
+// heads in bf16, nothing rotated, 22.1 us, 3.9 TB/s: issue slots 68% busy, stalls of fixed latencies and of loads alike; with rotated keys
+// 38.2 us, with 32 q heads too 76; read of 30011 tokens to bf16 28.8 us, 5.6 TB/s.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -104,8 +105,9 @@ __device__ __forceinline__ void blocks_of_16(const float *own, bool halves, cons
 // and turn, through shared memory; then a thread keeps its token, with its chunk's cosines and
 // sines in registers, and walks over the token's heads: what is left for a row is its loads (issued
 // before the row ahead of it is worked on), the arithmetic and its stores.  Lanes of a warp take
-// neighbouring heads of a token: a packed row's heads lie side by side.  (e2m1 has 80 registers in place of 64, where it
-// would spill: append of 1251 tokens, 8 k and v heads of 64, fp32 4.1 us, 5.3 with 64.)
+// neighbouring heads of a token: a packed row's heads lie side by side.  (e2m1 has 80 registers in place of 64, where rotated
+// rows spill: 8 k and v heads in fp32 rotated, 1251 tokens of 64 5.6 us, 6.3 with 64, 16384 of 128 38.6 and 41.8; not
+// rotated, in bf16, 22.1 and 21.5.)
 template <typename T, int FMT, int PATH>
 __global__ void __launch_bounds__(kRowThreads, FMT == WICI_KV_E2M1 ? 6 : kRowBlocks) rows_kernel(const __grid_constant__ RowsArg a) {
     constexpr bool WIDE = PATH != NARROW, PLAIN = PATH == WIDE_PLAIN;
@@ -530,7 +532,7 @@ cudaError_t launch_rows(RowsArg &a, bool wide, int sms, cudaStream_t st) {
     const dim3 block(a.chunks, b.rows);
     const size_t smem = a.positions ? (size_t)b.tokens * 4 * a.rot_chunks * sizeof(float4) : 0;
     if (!wide) return launch_blocks(rows_kernel<T, FMT, NARROW>, a, block, smem, st);
-    // Without a rope e2m1, bound by its instructions, has a kernel of its own: append of 16384 tokens 22.2 us, 29.2 where rows
+    // Without a rope e2m1, where instructions count, has a kernel of its own: append of 16384 tokens 22.1 us, 29.2 where rows
     // that might turn are told apart.  The other formats are bound by HBM either way.
     if constexpr (FMT == WICI_KV_E2M1)
         if (!a.positions) return launch_blocks(rows_kernel<T, FMT, WIDE_PLAIN>, a, block, smem, st);

@@ -39,14 +39,19 @@
 //   power of two per query that follows the largest such weight so far: a weight is off by 2^-22 of
 //   itself or 2^-32 of the largest one, however large the scale of a value is that hardly counts.
 //   4-bit cache: as 8-bit; a code times its block's scale is one fp16 number, exactly.
+//   Tensor cores cut what an addition leaves over, always downwards in size: a long run's sums of P V come out too small by
+//   some 2^-24 an addition.  Rows of their own (8-bit and bf16, up to 8 queries) take one a page, the two terms of P over 4-bit codes two: 3000
+//   keys in fp32 are 1.9e-7 and 3.5e-7 off (e4m3, e2m1), 4096 of a sequence among 48 2.1e-6, nearly all of it that one factor.
 //
-// 4-bit codes (E2M1).  Half of an 8-bit cache's bytes for the same arithmetic: this one is bound by the SMs (as fast from
-// L2), by conversions, products with block scales and what keeps them apart.  So the operands change places: S^T = K Q^T and
+// 4-bit codes (E2M1).  Half of an 8-bit cache's bytes for the same arithmetic.  As fast from L2, and no pipe is full either
+// (of the active cycles issue slots 52%, ALU 42%, tensor cores 26%): two warps a scheduler wait for one another's chains of
+// loads from shared memory, conversions, products with block scales and matrix products, first of all for the fixed latency
+// of the instruction before.  So the operands change places: S^T = K Q^T and
 // O^T = V^T P^T, with keys and elements of the head as the 16 rows and 8 queries as the columns.  A fragment of converted
 // codes then serves both terms of Q or P (and 16 queries a tile two tiles) at half the products of K, and O takes 32
 // registers in place of 64; P^T comes from the scores by movmatrix.  64 sequences of up to 8192 tokens, five queries a KV
-// head: 93 us (104 with queries as rows), two of 100001 to 131072: 72 us (80), 3.9 TB/s of codes, 750 instructions for 32
-// keys at 0.57 a cycle and scheduler.  Not kept: three blocks on an SM with 168 registers (74 us; beside an append 131 in
+// head: 93 us (104 with queries as rows), two of 100001 to 131072: 72 us (80), 3.9 TB/s of codes, 730 instructions for 32
+// keys at 0.52 a cycle and scheduler.  16 queries a KV head: 106 us for the two.  Not kept: three blocks on an SM with 168 registers (74 us; beside an append 131 in
 // place of 103, for an append's blocks split the registers that a third block would need), four pages a unit (70.6, but
 // 95.6 for the 64 sequences), five ring slots (the same), two sums for a score or terms of P apart (the same).
 #pragma once
@@ -710,7 +715,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
             uint32_t qf[N8][TQ][STEPS][2];
             float cq[C];                                      // products to base-2 logits, of queries 2 t, 2 t + 1
             const float log2_scale = a.scale * 1.44269504088896340736f;
-            // the smallest power of two that takes the scale to no less than 2^-126, where it has its 24 bits
+            // the smallest power of two that takes the scale to no less than 2^-126, where it has its 24 bits (what smaller
+            // queries lose by it is below head_dim 2^-25 2^-126 max|k| < 2^-16 of a logit)
             const int least = 1 - min((int)(__float_as_uint(log2_scale) >> 23 & 0xFF), 127);
 #pragma unroll
             for (int n = 0; n < N8; ++n) {
