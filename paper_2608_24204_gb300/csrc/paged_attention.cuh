@@ -40,8 +40,8 @@
 //   itself or 2^-32 of the largest one, however large the scale of a value is that hardly counts.
 //   4-bit cache: as 8-bit; a code times its block's scale is one fp16 number, exactly.
 //   Tensor cores cut what an addition leaves over, always downwards in size: a long run's sums of P V come out too small by
-//   some 2^-24 an addition.  Rows of their own (8-bit and bf16, up to 8 queries) take one a page, the two terms of P over 4-bit codes two: 3000
-//   keys in fp32 are 1.9e-7 and 3.5e-7 off (e4m3, e2m1), 4096 of a sequence among 48 2.1e-6, nearly all of it that one factor.
+//   some 2^-24 an addition.  Rows of their own (8-bit and bf16, up to 8 queries) take one a page, the two terms of P over
+//   4-bit codes two; for fp32 queries these are summed a unit at a time.
 //
 // 4-bit codes (E2M1).  Half of an 8-bit cache's bytes for the same arithmetic.  As fast from L2, and no pipe is full either
 // (of the active cycles issue slots 52%, ALU 42%, tensor cores 26%): two warps a scheduler wait for one another's chains of
@@ -904,6 +904,9 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     }
                     rescale(f);
                 }
+                // EXACT (fp32): a unit's sums apart, added to O in fp32: in one sum the tensor cores' cut additions make 4096 keys
+                // 2.1e-6 too small (7e-7 off this way; head_dim 64 42.2 and 42.7 us, 128 61.7 and 65.7)
+                float sum[TILES][N8][4];
 #pragma unroll
                 for (int pg = 0; pg < P; ++pg) {
                     uint32_t pf[N8][2][2];                    // [tile][term][keys 0..7, 8..15]
@@ -958,11 +961,21 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                             const uint32_t f[4] = {times(even[0][e], b2[0]), times(odd[0][e], b2[0]), times(even[1][e], b2[1]),
                                                    times(odd[1][e], b2[1])};
 #pragma unroll
-                            for (int n = 0; n < N8; ++n)
+                            for (int n = 0; n < N8; ++n) {
+                                float *to = EXACT ? sum[4 * x8 + e][n] : o[4 * x8 + e][n];
 #pragma unroll
-                                for (int k = 0; k < 2; ++k) mma16816<false>(o[4 * x8 + e][n], f, pf[n][k][0], pf[n][k][1]);
+                                for (int k = 0; k < 2; ++k) mma_f16(to, EXACT && pg == 0 && k == 0, f, pf[n][k]);
+                            }
                         }
                     }
+                }
+                if (EXACT) {
+#pragma unroll
+                    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+                        for (int n = 0; n < N8; ++n)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[i][n][j] += sum[i][n][j];
                 }
                 if (bad_units >> (done & 31) & 1) {
                     bad_units &= ~(1u << (done & 31));

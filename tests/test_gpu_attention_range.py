@@ -107,3 +107,31 @@ def test_every_element_of_a_key_is_large(fmt, dtype, group, d, q_size, k_size):
     scale = float(np.float32(1e-33 / (q_size * (k_size / 1e33)) * d ** -0.5))
     out = cache.attend(q, ints(pages), ints([n]), scale=scale, out=torch.empty(q.shape, device="cuda"), lse=lse)
     check_attention(cache, q, pages, [n], vals, scale, 0, out, lse, dtype, "f32")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_fp32_sums_are_not_all_cut_the_same_way(d):
+    """The mean relative error of positive results over long runs of keys.  Additions on tensor cores are cut, by 2^-23 of the sum at
+    most: 8 of a unit's 64 keys (head_dim 64) make 2^-20 of it; what is rounded to the nearest averages out over the 4096
+    elements, of which each row's sum of weights is common to head_dim: some 400 additions of 2^-25 each in 8 x 20 lanes of 64
+    rows, 6e-9."""
+    n, kv, group, batch = 1 << 18, 8, 4, 2
+    g = torch.Generator(device="cuda").manual_seed(d)
+    cache = PagedKV(kv, d, "e2m1", n_pages=batch * n // 16)
+    slots = torch.arange(batch * n, device="cuda", dtype=torch.int32)
+    for i in range(0, batch * n, n // 4):
+        at = slots[i:i + n // 4]
+        k = torch.randn(len(at), kv, d, generator=g, device="cuda")
+        cache.append(k, torch.rand(len(at), kv, d, generator=g, device="cuda") + 0.5, at)
+    q = torch.randn(batch, kv * group, d, generator=g, device="cuda")
+    pages = torch.arange(batch * n // 16, device="cuda", dtype=torch.int32).view(batch, -1)
+    out = cache.attend(q, pages, ints([n, n]), scale=0.25 * d ** -0.5)
+    cache.check()
+    off = []
+    for b in range(batch):
+        k, v = cache.read(slots[b * n:(b + 1) * n], dtype=torch.float32)
+        for h in range(kv):
+            p = torch.softmax(q[b, h * group:(h + 1) * group].double() @ k[:, h].double().T * (0.25 * d ** -0.5), -1)
+            want = p @ v[:, h].double()
+            off.append((out[b, h * group:(h + 1) * group].double() / want - 1).mean())
+    assert abs(torch.stack(off).mean().item()) < 2.0 ** -20 + 2.0 ** -21
