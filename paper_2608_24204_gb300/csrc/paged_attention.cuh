@@ -732,7 +732,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 // 2^(13 - exponent): the largest magnitude to [2^13, 2^14), a smaller one where q and the scale are very small
                 int e = (int)(top >> 23) - 127 - 13;
-                e = top >= kInfBits || top == 0 ? 0 : max(least, e);
+                e = top >= kInfBits ? 0 : max(least, e);
                 const float down = __int_as_float((127 - e) << 23), of_g = log2_scale * __int_as_float((127 + e) << 23);
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
@@ -1032,7 +1032,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnShape<FMT, D, STACK>::kBlock
                     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
                     // 2^(13 - exponent): the largest magnitude to [2^13, 2^14)
                     int e = (int)(top >> 23) - 127 - 13;
-                    e = top >= kInfBits || top == 0 ? 0 : max(-126, min(126, e));
+                    e = top >= kInfBits ? 0 : max(-126, min(126, e));   // (of zeros the smallest: a factor that is finite)
                     const float down = __int_as_float((127 - e) << 23);
                     cq[r] *= __int_as_float((127 + e) << 23);
 #pragma unroll

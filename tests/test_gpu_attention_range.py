@@ -135,3 +135,17 @@ def test_long_fp32_sums_are_not_all_cut_the_same_way(d):
             want = p @ v[:, h].double()
             off.append((out[b, h * group:(h + 1) * group].double() / want - 1).mean())
     assert abs(torch.stack(off).mean().item()) < 2.0 ** -20 + 2.0 ** -21
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8", "e4m3", "e2m1"])
+@pytest.mark.parametrize("dtype,group,d", [("bf16", 4, 128), ("f32", 3, 64), ("bf16", 12, 64)])
+def test_queries_of_zeros_beside_a_large_scale(fmt, dtype, group, d):
+    # its logits are 0 whatever the scale and the keys are, as far as these are finite
+    n = 90
+    rng = np.random.default_rng(d)
+    k = torch.tensor(rng.normal(size=(n, 1, d)) * 2.0 ** 100, device="cuda").to(DT[dtype])
+    cache, vals, pages = stored(k, randn(rng, n, 1, d, dtype=dtype), fmt)
+    q = torch.zeros(1, group, d, dtype=DT[dtype], device="cuda")
+    lse = torch.empty(1, group, device="cuda")
+    out = cache.attend(q, ints(pages), ints([n]), scale=2.0 ** 60, out=torch.empty(1, group, d, device="cuda"), lse=lse)
+    check_attention(cache, q, pages, [n], vals, 2.0 ** 60, 0, out, lse, dtype, "f32")
