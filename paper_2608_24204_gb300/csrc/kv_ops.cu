@@ -7,8 +7,8 @@
 // 28.3 us, 5.9 TB/s (a copy of that size: 6.4); append of 16384 tokens, 32 q heads rotated, 8 k
 // and v heads to e4m3, 69.1 us, 5.4 TB/s, of which its arithmetic is 3 us; read of 30011 tokens from
 // e4m3 to bf16 32.1 us, 5.8 TB/s; one token of a step 2.3 to 3.4 us.  From and to e2m1: append of 16384 tokens, 8 k and v
-// heads in bf16, nothing rotated, 22.1 us, 3.9 TB/s: issue slots 68% busy, stalls of fixed latencies and of loads alike; with rotated keys
-// 38.2 us, with 32 q heads too 76; read of 30011 tokens to bf16 28.8 us, 5.6 TB/s.
+// heads in bf16, nothing rotated, 22.1 us, 3.9 TB/s: issue slots 68% busy, stalls of fixed latencies and of loads alike; with
+// rotated keys 38.2 us, with 32 q heads too 76; read of 30011 tokens to bf16 28.8 us, 5.6 TB/s.
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>

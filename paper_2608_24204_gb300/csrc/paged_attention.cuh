@@ -51,9 +51,10 @@
 // codes then serves both terms of Q or P (and 16 queries a tile two tiles) at half the products of K, and O takes 32
 // registers in place of 64; P^T comes from the scores by movmatrix.  64 sequences of up to 8192 tokens, five queries a KV
 // head: 93 us (104 with queries as rows), two of 100001 to 131072: 72 us (80), 3.9 TB/s of codes, 730 instructions for 32
-// keys at 0.52 a cycle and scheduler.  16 queries a KV head: 106 us for the two.  Not kept: three blocks on an SM with 168 registers (74 us; beside an append 131 in
-// place of 103, for an append's blocks split the registers that a third block would need), four pages a unit (70.6, but
-// 95.6 for the 64 sequences), five ring slots (the same), two sums for a score or terms of P apart (the same).
+// keys at 0.52 a cycle and scheduler; with 16 queries a KV head 106 us.  Not kept: three blocks on an SM with 168 registers
+// (74 us; beside an append 131 in place of 103, for an append's blocks split the registers that a third block would need),
+// four pages a unit (70.6, but 95.6 for the 64 sequences), five ring slots (the same), two sums for a score or terms of P
+// apart (the same).
 #pragma once
 #include "ops.cuh"
 
